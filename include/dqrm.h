@@ -15,6 +15,8 @@
  * and, between the forward and the backward of the tables, the dense part of the model:
  *   dqrm_dense_step      every step      MLPs, interaction, loss, their backward, dense SGD
  *   dqrm_dense_step_quant  the same with channel-wise INT4 weights and / or INT8 gradients + error compensation
+ * Apart from that step, for wider dense parts than it has: layer norm (dqrm_layernorm_fwd, _bwd) and linear layers whose
+ * operands are held in 4 bits with a scale to every 32 values (dqrm_mxfp4_quant, _dequant, _matmul, _linear).
  *
  * Conventions common to every entry point
  *   - Returns 0 (DQRM_OK) or a negative DQRM_ERR_* code.  Never throws, never aborts.
@@ -32,7 +34,7 @@
  *     the first problem in a per-device status word that dqrm_check_status()
  *     reads and clears.
  *   - All floating point is IEEE binary32, one rounding per operation (no fused
- *     multiply-add), true division.
+ *     multiply-add), true division; the layer norm and the MXFP4 calls state theirs.
  *
  * The quantiser (the paper states "uniform", "one scale per table"; the formula
  * is this library's reading): scale = max(absmax / (2^(b-1) - 1), 1e-8),
@@ -419,6 +421,84 @@ int64_t dqrm_dense_param_count(const dqrm_dense_model_t *model); /* P, or -1 for
 int32_t dqrm_dense_step_quant(const dqrm_dense_model_t *model, const dqrm_dense_quant_t *quant, int32_t batch,
                               const float *dense_x, const float *emb_out, const float *labels, float lr, float *loss,
                               float *grad_emb, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- layer norm and 4-bit microscaled (MXFP4) linear layers ------------------------------------------------------
+ * Layers y = relu(xhat W^T + b) whose operands the matrix cores multiply as 4-bit codes, and the norm that keeps a
+ * layer's inputs in the range of few bits.  Sums, statistics and scales are held in 32 bits.
+ *
+ * Element types of matrices that are not codes.  A matrix has a row stride in elements (ld >= cols; any value if there
+ * is one row) and starts at any multiple of its element's size; rows and cols are at most 2147482623. */
+#define DQRM_F32 0
+#define DQRM_BF16 1
+#define DQRM_F16 2
+
+/* A matrix in MXFP4.  32 consecutive values of a row share a scale 2^e, e = max(floor(log2(max |v|)) - 2, -127), held
+ * as the byte e + 127; each value is held as the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale, ties to the
+ * even code, magnitudes beyond 6 as 6: four bits, sign above magnitude index.  A block with an infinity or a NaN has
+ * scale byte 255 and zero codes: all its values are NaN, and so is every output of a product that reads it.
+ *   codes  [rows][64 * ceil(cols / 128)] bytes, 16-byte aligned: value 2k of a row in the low half of byte k
+ *   scales [rows][4 * ceil(cols / 128)] bytes, 4-byte aligned
+ * The padding behind a row's values is part of the format: zero codes; blocks without a value have scale byte 0.  The
+ * calls below write it; a caller who writes codes has to write it too.  The struct is read on the host during the call;
+ * the memory is the caller's DEVICE memory. */
+typedef struct {
+    int64_t rows, cols;
+    uint8_t *codes;
+    uint8_t *scales;
+} dqrm_mxfp4_t;
+
+/* x [rows][cols] to MXFP4 from one read of it.  At least one output is wanted:
+ *   by_rows   blocks along x's rows: [rows][cols], or NULL
+ *   by_cols   blocks along x's columns: the codes of the transposed matrix, [cols][rows], or NULL (a product of the
+ *             backward pass sums over the other axis, and blocks lie along the axis that is summed over)
+ *   col_sums  [cols] fp32: the sums of x's columns before quantisation (a bias's gradient), or NULL.  Needs the workspace
+ *             (256-byte aligned); their order of addition depends on the shape alone.
+ *   gate      [rows][cols] of the same type, or NULL: x counts as 0 where gate > 0 does not hold (a ReLU's backward,
+ *             gate being the layer's output) */
+size_t dqrm_mxfp4_quant_workspace_bytes(int64_t rows, int64_t cols);
+int32_t dqrm_mxfp4_quant(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *gate,
+                         int64_t ldgate, const dqrm_mxfp4_t *by_rows, const dqrm_mxfp4_t *by_cols, float *col_sums,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* The values that codes stand for, out [q->rows][q->cols], rounded to the element type. */
+int32_t dqrm_mxfp4_dequant(const dqrm_mxfp4_t *q, int32_t dtype, void *out, int64_t ldo, void *stream);
+
+/* out [m][n] = act(sum over k of a[m][k] b[n][k] + bias[n]), act = max(., 0) if relu (a NaN stays), rounded once to the
+ * element type.  a->cols = b->cols = k; k = 0 gives act(bias).  With A by rows and B = W by rows it is a linear layer's
+ * forward; with dY by rows and W by columns the input's gradient; with dY and X by columns the weights'.  bias: [n] fp32
+ * or NULL.  The order of the sums depends on the shape alone.  out must not overlap the operands. */
+size_t dqrm_mxfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int32_t dqrm_mxfp4_matmul(const dqrm_mxfp4_t *a, const dqrm_mxfp4_t *b, const float *bias, int32_t relu, int32_t dtype,
+                          void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A linear layer on activations as they are, for requests: x [m][k] of `dtype`, through a layer norm first if `norm`
+ * (gamma, beta: as in dqrm_layernorm_fwd), is quantised by rows and multiplied with w [n][k]; out [m][n] of the same
+ * type.  The result is that of dqrm_mxfp4_quant (or dqrm_layernorm_fwd with `q`) followed by dqrm_mxfp4_matmul up to the
+ * order of the 32-bit sums (the norm's among them: a value within their last bits of a boundary between two codes may
+ * take either). */
+size_t dqrm_mxfp4_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int32_t dqrm_mxfp4_linear(int32_t dtype, int64_t m, const void *x, int64_t ldx, int32_t norm, const float *gamma,
+                          const float *beta, float eps, const dqrm_mxfp4_t *w, const float *bias, int32_t relu,
+                          void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Layer norm of the rows of x [rows][cols], cols >= 1, eps >= 0:
+ *   mean = sum x / cols, rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps), y = (x - mean) rstd gamma + beta
+ * gamma, beta: [cols] fp32 or NULL (1 and 0).  At least one output is wanted: y [rows][cols] of x's type (may be x's own
+ * memory, with the same stride), mean [rows], rstd [rows] fp32 (what the backward needs), q: y in MXFP4, quantised from
+ * its 32-bit values. */
+int32_t dqrm_layernorm_fwd(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const float *gamma,
+                           const float *beta, float eps, void *y, int64_t ldy, float *mean, float *rstd,
+                           const dqrm_mxfp4_t *q, void *stream);
+
+/* Its backward: with xhat = (x - mean) rstd and g = dy gamma,
+ *   dx = rstd (g - mean over the row of g - xhat mean over the row of (g xhat))   or NULL; may be dy's or x's own memory
+ *   dgamma [cols] = sum over rows of dy xhat, dbeta [cols] = sum over rows of dy, fp32   both or neither (NULL)
+ * dy, x, dx of one type; mean and rstd from the forward.  The workspace (256-byte aligned) is needed for dgamma and dbeta;
+ * their order of addition depends on the shape alone.  rows = 0 gives zeros. */
+size_t dqrm_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void *dy, int64_t lddy, const void *x,
+                           int64_t ldx, const float *mean, const float *rstd, const float *gamma, void *dx, int64_t lddx,
+                           float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Synchronises `stream`, returns the first data-dependent problem recorded on
  * the current device since the last call (DQRM_OK if none) and clears it.

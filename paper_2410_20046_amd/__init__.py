@@ -13,5 +13,8 @@ from .binding import (  # noqa: F401
     dqrm_sparse_merge_workspace_bytes, dqrm_sparse_merge, dqrm_sparse_update_sums, dqrm_sparse_block_t,
     dqrm_fwd_bwd_step, dqrm_dense_workspace_bytes, dqrm_dense_step, dqrm_dense_param_count, dqrm_dense_step_quant,
     DenseQuant,
+    F32, BF16, F16, MxMatrix, dqrm_mxfp4_t, dqrm_mxfp4_quant_workspace_bytes, dqrm_mxfp4_quant, dqrm_mxfp4_dequant,
+    dqrm_mxfp4_matmul_workspace_bytes, dqrm_mxfp4_matmul, dqrm_mxfp4_linear_workspace_bytes, dqrm_mxfp4_linear,
+    dqrm_layernorm_fwd, dqrm_layernorm_bwd_workspace_bytes, dqrm_layernorm_bwd,
 )
 from .build import build_library  # noqa: F401

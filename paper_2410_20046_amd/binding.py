@@ -41,7 +41,9 @@ EXPORTS = ("dqrm_find_scale", "dqrm_pack_int4", "dqrm_embbag_fwd", "dqrm_embbag_
            "dqrm_grad_quant_int8", "dqrm_grad_quant_int8_multi",
            "dqrm_sparse_update", "dqrm_sparse_merge_workspace_bytes", "dqrm_sparse_merge", "dqrm_sparse_update_sums",
            "dqrm_quant_update", "dqrm_fwd_bwd_step", "dqrm_dense_workspace_bytes", "dqrm_dense_step",
-           "dqrm_dense_param_count", "dqrm_dense_step_quant", "dqrm_check_status", "dqrm_last_hip_error", "dqrm_version")
+           "dqrm_dense_param_count", "dqrm_dense_step_quant", "dqrm_mxfp4_quant_workspace_bytes", "dqrm_mxfp4_quant",
+           "dqrm_mxfp4_dequant", "dqrm_mxfp4_matmul_workspace_bytes", "dqrm_mxfp4_matmul", "dqrm_mxfp4_linear_workspace_bytes",
+           "dqrm_mxfp4_linear", "dqrm_layernorm_fwd", "dqrm_layernorm_bwd_workspace_bytes", "dqrm_layernorm_bwd", "dqrm_check_status", "dqrm_last_hip_error", "dqrm_version")
 
 
 class DqrmError(RuntimeError):
@@ -93,6 +95,13 @@ class dqrm_dense_quant_t(C.Structure):
                 ("grad_buffer", C.c_void_p), ("buffer_add", C.c_int32), ("buffer_update", C.c_int32)]
 
 
+class dqrm_mxfp4_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+F32, BF16, F16 = 0, 1, 2
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -143,6 +152,20 @@ def lib() -> C.CDLL:
         L.dqrm_dense_step_quant.argtypes = [dp, C.POINTER(dqrm_dense_quant_t), i32, vp, vp, vp, C.c_float, vp, vp, vp,
                                             sz, vp]
         L.dqrm_dense_step_quant.restype = i32
+        qp, f32 = C.POINTER(dqrm_mxfp4_t), C.c_float
+        L.dqrm_mxfp4_quant.argtypes = [i32, i64, i64, vp, i64, vp, i64, qp, qp, vp, vp, sz, vp]
+        L.dqrm_mxfp4_dequant.argtypes = [qp, i32, vp, i64, vp]
+        L.dqrm_mxfp4_matmul.argtypes = [qp, qp, vp, i32, i32, vp, i64, vp, sz, vp]
+        L.dqrm_mxfp4_linear.argtypes = [i32, i64, vp, i64, i32, vp, vp, f32, qp, vp, i32, vp, i64, vp, sz, vp]
+        L.dqrm_layernorm_fwd.argtypes = [i32, i64, i64, vp, i64, vp, vp, f32, vp, i64, vp, vp, qp, vp]
+        L.dqrm_layernorm_bwd.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.dqrm_mxfp4_quant_workspace_bytes.argtypes = L.dqrm_layernorm_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.dqrm_mxfp4_matmul_workspace_bytes.argtypes = L.dqrm_mxfp4_linear_workspace_bytes.argtypes = [i64, i64, i64]
+        for n in ("quant", "matmul", "linear"):
+            getattr(L, f"dqrm_mxfp4_{n}").restype = i32
+            getattr(L, f"dqrm_mxfp4_{n}_workspace_bytes").restype = sz
+        L.dqrm_mxfp4_dequant.restype = L.dqrm_layernorm_fwd.restype = L.dqrm_layernorm_bwd.restype = i32
+        L.dqrm_layernorm_bwd_workspace_bytes.restype = sz
         L.dqrm_check_status.argtypes = [vp, C.POINTER(i32), C.POINTER(i64)]
         for n in ("dqrm_find_scale", "dqrm_pack_int4", "dqrm_embbag_fwd", "dqrm_embbag_bwd", "dqrm_dedupe", "dqrm_segment_sum",
                   "dqrm_quant_update", "dqrm_grad_quant_int8", "dqrm_sparse_update", "dqrm_check_status"):
@@ -448,3 +471,131 @@ def dqrm_fwd_bwd_step(tables: Tables, bufs: StepBuffers, indices: torch.Tensor, 
                                    _ptr(b.table_uniq_offsets), _ptr(b.num_unique), _ptr(b.values), _ptr(b.g_absmax), _ptr(b.gq),
                                    _ptr(b.g_scale), _ptr(b.workspace), b.workspace.numel() * b.workspace.element_size(),
                                    _stream(stream)), "dqrm_fwd_bwd_step")
+
+
+# ---- layer norm and MXFP4 linear layers ---------------------------------------------------------------------------------
+
+
+def _matrix(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
+    """(dtype, address, row stride) of a matrix whose rows' elements lie one behind the other."""
+    assert t.dim() == 2 and t.dtype in _DTYPES, f"{what}: a matrix of float32, bfloat16 or float16"
+    ld, step = t.stride()
+    assert step == 1 or t.shape[1] <= 1, f"{what}: the elements of a row must be contiguous"
+    return _DTYPES[t.dtype], t.data_ptr(), ld
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    assert t.dtype == torch.float32 and t.shape == (n,) and t.is_contiguous(), f"{what}: {n} contiguous float32 values"
+    return t.data_ptr()
+
+
+def _like(t: torch.Tensor, shape, dtype, what: str) -> None:
+    assert tuple(t.shape) == tuple(shape) and t.dtype == dtype, f"{what}: {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}"
+
+
+def _space(ws: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+
+
+class MxMatrix:
+    """A matrix in MXFP4 (see ``dqrm_mxfp4_t``): the device buffers of its codes and scales and the C descriptor."""
+
+    def __init__(self, rows: int, cols: int, device=None, codes: Optional[torch.Tensor] = None,
+                 scales: Optional[torch.Tensor] = None):
+        self.rows, self.cols = int(rows), int(cols)
+        groups = -(-self.cols // 128)
+        byte = lambda n: torch.empty((self.rows, n), dtype=torch.uint8, device=device)  # noqa: E731
+        self.codes = codes if codes is not None else byte(64 * groups)
+        self.scales = scales if scales is not None else byte(4 * groups)
+        for t, n in ((self.codes, 64 * groups), (self.scales, 4 * groups)):
+            _like(t, (self.rows, n), torch.uint8, "MxMatrix")
+        self.c = dqrm_mxfp4_t(self.rows, self.cols, _ptr(self.codes), _ptr(self.scales))
+        self.ref = C.byref(self.c)
+
+
+def _mx(q: Optional[MxMatrix]):
+    return None if q is None else q.ref
+
+
+def dqrm_mxfp4_quant_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().dqrm_mxfp4_quant_workspace_bytes(rows, cols))
+
+
+def dqrm_mxfp4_quant(x: torch.Tensor, by_rows: Optional[MxMatrix] = None, by_cols: Optional[MxMatrix] = None,
+                     gate: Optional[torch.Tensor] = None, col_sums: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    dtype, p, ld = _matrix(x, "x")
+    pg, ldg = None, 0
+    if gate is not None:
+        _like(gate, x.shape, x.dtype, "gate")
+        _, pg, ldg = _matrix(gate, "gate")
+    _check(lib().dqrm_mxfp4_quant(dtype, x.shape[0], x.shape[1], p, ld, pg, ldg, _mx(by_rows), _mx(by_cols),
+                                  _vector(col_sums, x.shape[1], "col_sums"), *_space(workspace), _stream(stream)), "dqrm_mxfp4_quant")
+
+
+def dqrm_mxfp4_dequant(q: MxMatrix, out: torch.Tensor, stream=None) -> None:
+    _like(out, (q.rows, q.cols), out.dtype, "out")
+    _check(lib().dqrm_mxfp4_dequant(q.ref, *_matrix(out, "out"), _stream(stream)), "dqrm_mxfp4_dequant")
+
+
+def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(lib().dqrm_mxfp4_matmul_workspace_bytes(m, n, k))
+
+
+def dqrm_mxfp4_matmul(a: MxMatrix, b: MxMatrix, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    _like(out, (a.rows, b.rows), out.dtype, "out")
+    _check(lib().dqrm_mxfp4_matmul(a.ref, b.ref, _vector(bias, b.rows, "bias"), relu, *_matrix(out, "out"), *_space(workspace),
+                                   _stream(stream)), "dqrm_mxfp4_matmul")
+
+
+def dqrm_mxfp4_linear_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(lib().dqrm_mxfp4_linear_workspace_bytes(m, n, k))
+
+
+def dqrm_mxfp4_linear(x: torch.Tensor, w: MxMatrix, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
+                      gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: Optional[float] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``eps`` given: x goes through a layer norm (with ``gamma`` and ``beta`` if given) first."""
+    dtype, p, ld = _matrix(x, "x")
+    _like(x, (x.shape[0], w.cols), x.dtype, "x")
+    _like(out, (x.shape[0], w.rows), x.dtype, "out")
+    _, po, ldo = _matrix(out, "out")
+    _check(lib().dqrm_mxfp4_linear(dtype, x.shape[0], p, ld, eps is not None, _vector(gamma, w.cols, "gamma"),
+                                   _vector(beta, w.cols, "beta"), eps or 0.0, w.ref, _vector(bias, w.rows, "bias"), relu, po, ldo,
+                                   *_space(workspace), _stream(stream)), "dqrm_mxfp4_linear")
+
+
+def dqrm_layernorm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
+                       y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                       q: Optional[MxMatrix] = None, stream=None) -> None:
+    dtype, p, ld = _matrix(x, "x")
+    R, D = x.shape
+    py, ldy = None, 0
+    if y is not None:
+        _like(y, x.shape, x.dtype, "y")
+        _, py, ldy = _matrix(y, "y")
+    _check(lib().dqrm_layernorm_fwd(dtype, R, D, p, ld, _vector(gamma, D, "gamma"), _vector(beta, D, "beta"), eps, py, ldy,
+                                    _vector(mean, R, "mean"), _vector(rstd, R, "rstd"), _mx(q), _stream(stream)), "dqrm_layernorm_fwd")
+
+
+def dqrm_layernorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().dqrm_layernorm_bwd_workspace_bytes(rows, cols))
+
+
+def dqrm_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
+                       dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
+                       dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    dtype, p, ld = _matrix(x, "x")
+    R, D = x.shape
+    _like(dy, x.shape, x.dtype, "dy")
+    _, pdy, lddy = _matrix(dy, "dy")
+    pdx, lddx = None, 0
+    if dx is not None:
+        _like(dx, x.shape, x.dtype, "dx")
+        _, pdx, lddx = _matrix(dx, "dx")
+    _check(lib().dqrm_layernorm_bwd(dtype, R, D, pdy, lddy, p, ld, _vector(mean, R, "mean"), _vector(rstd, R, "rstd"),
+                                    _vector(gamma, D, "gamma"), pdx, lddx, _vector(dgamma, D, "dgamma"), _vector(dbeta, D, "dbeta"),
+                                    *_space(workspace), _stream(stream)), "dqrm_layernorm_bwd")

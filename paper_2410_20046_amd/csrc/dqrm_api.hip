@@ -11,6 +11,7 @@
 
 #include "dqrm.h"
 #include "dqrm_device.hpp"
+#include "dqrm_host.hpp"
 #include "dqrm_fwd.hpp"
 #include "dqrm_dedupe.hpp"
 #include "dqrm_bwd.hpp"
@@ -23,15 +24,17 @@
 // this name is only a handle for hipGetSymbolAddress; kernels receive the address that call returns.
 static __device__ __align__(256) unsigned char scratch[DQRM_NOALLOC_SCRATCH_BYTES];
 
-namespace {
+static thread_local char t_hip_error[256] = "";
 
-thread_local char t_hip_error[256] = "";
-
-int32_t hip_fail(hipError_t e, const char *what)
+int32_t dqrm_host::hip_fail(hipError_t e, const char *what)
 {
     std::snprintf(t_hip_error, sizeof(t_hip_error), "%s: %s", what, hipGetErrorString(e));
     return DQRM_ERR_HIP;
 }
+
+namespace {
+
+using dqrm_host::hip_fail;
 
 #define DQRM_HIP_CHECK(expr)                                 \
     do {                                                     \

@@ -1,0 +1,427 @@
+// C ABI of layer norm and of MXFP4 linear layers: host-side validation and kernel dispatch.
+// Every entry point validates on the host first and enqueues nothing on error.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "dqrm.h"
+#include "dqrm_host.hpp"
+#include "dqrm_mx.hpp"
+#include "dqrm_mx_gemm.hpp"
+#include "dqrm_norm.hpp"
+
+namespace {
+
+using namespace dqrm_mx;
+using dqrm_host::hip_fail;
+
+#define DQRM_HIP_CHECK(expr)                              \
+    do {                                                  \
+        hipError_t e_ = (expr);                           \
+        if (e_ != hipSuccess) return hip_fail(e_, #expr); \
+    } while (0)
+
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+int64_t ceil_div(int64_t x, int64_t d) { return (x + d - 1) / d; }
+
+constexpr int64_t kMaxDim = 2147483647LL - 1024; // rows, columns and row strides' limit
+constexpr int64_t kMaxBlocks = 1 << 22;          // of one launch (blocks times threads is below 2^32)
+
+size_t size_of(int32_t dtype) { return dtype == DQRM_F32 ? 4 : 2; }
+
+// f(Elem type) for a dtype that has been checked
+template <typename F>
+void with_type(int32_t dtype, F f)
+{
+    if (dtype == DQRM_F32)
+        f(std::integral_constant<int, DQRM_F32>{});
+    else if (dtype == DQRM_BF16)
+        f(std::integral_constant<int, DQRM_BF16>{});
+    else
+        f(std::integral_constant<int, DQRM_F16>{});
+}
+
+int32_t check_shape(int32_t dtype, int64_t rows, int64_t cols)
+{
+    if (dtype != DQRM_F32 && dtype != DQRM_BF16 && dtype != DQRM_F16) return DQRM_ERR_INVALID_ARG;
+    if (rows < 0 || cols < 0) return DQRM_ERR_INVALID_ARG;
+    if (rows > kMaxDim || cols > kMaxDim) return DQRM_ERR_UNSUPPORTED;
+    return DQRM_OK;
+}
+
+// a matrix of elements: there if it has any, at its elements' alignment, rows that do not overlap
+int32_t check_matrix(const void *p, int64_t ld, int32_t dtype, int64_t rows, int64_t cols)
+{
+    if (rows == 0 || cols == 0) return DQRM_OK;
+    if (!p || !aligned(p, size_of(dtype)) || (rows > 1 && ld < cols)) return DQRM_ERR_INVALID_ARG;
+    if (rows > 1 && ld > (int64_t)1 << 40) return DQRM_ERR_UNSUPPORTED;
+    return DQRM_OK;
+}
+
+int32_t check_mx(const dqrm_mxfp4_t *q, int64_t rows, int64_t cols)
+{
+    if (!q || q->rows != rows || q->cols != cols) return DQRM_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return DQRM_OK;
+    if (!q->codes || !q->scales || !aligned(q->codes, 16) || !aligned(q->scales, 4)) return DQRM_ERR_INVALID_ARG;
+    return DQRM_OK;
+}
+
+int32_t check_workspace(const void *ws, size_t have, size_t need)
+{
+    if (need == 0) return DQRM_OK;
+    if (!ws || !aligned(ws, 256)) return DQRM_ERR_INVALID_ARG;
+    return have < need ? DQRM_ERR_WORKSPACE_TOO_SMALL : DQRM_OK;
+}
+
+#define DQRM_CHECK(expr)                 \
+    do {                                 \
+        const int32_t rc_ = (expr);      \
+        if (rc_ != DQRM_OK) return rc_;  \
+    } while (0)
+
+int num_cus()
+{
+    static const int n = [] {
+        int dev = 0, v = 0;
+        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v < 1) return 256;
+        return v;
+    }();
+    return n;
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(float *p, int64_t n)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) p[i] = 0.0f;
+}
+
+void fill_zero(float *p, int64_t n, hipStream_t st)
+{
+    if (p && n > 0) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, p, n);
+}
+
+void join_columns(const float *partial, int64_t stride, int n, int64_t cols, float *out0, float *out1, hipStream_t st)
+{
+    hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(cols, 16), out1 ? 2 : 1), dim3(256), 0, st, partial, stride, n, cols, out0, out1);
+}
+
+// ---- quantisation ------------------------------------------------------------------------------------------------------
+size_t quant_workspace(int64_t rows, int64_t cols) { return align_up((size_t)(ceil_div(rows, kTile) * cols) * sizeof(float), 256); }
+
+void launch_quant_rows(int32_t dtype, QuantArgs a, hipStream_t st)
+{
+    const int64_t per_row = groups_of(a.cols) * (kRowPad / kChunk);
+    const int64_t step = std::max<int64_t>(1, kMaxBlocks * 256 / per_row), rows = a.rows;
+    const size_t es = size_of(dtype);
+    for (int64_t r0 = 0; r0 < rows; r0 += step) {
+        QuantArgs b = a;
+        b.rows = std::min(step, rows - r0);
+        b.x = static_cast<const char *>(a.x) + r0 * a.ldx * es;
+        if (a.gate) b.gate = static_cast<const char *>(a.gate) + r0 * a.ldgate * es;
+        b.codes += r0 * codes_pitch(a.cols), b.scales += r0 * scales_pitch(a.cols);
+        with_type(dtype, [&](auto t) {
+            hipLaunchKernelGGL(quant_rows_kernel<decltype(t)::value>, dim3((unsigned)ceil_div(b.rows * per_row, 256)), dim3(256), 0, st, b);
+        });
+    }
+}
+
+// ---- layer norm ----------------------------------------------------------------------------------------------------------
+constexpr int64_t kNormRegisterCols = 16384; // longer rows are read more than once
+
+// f(threads per row, chunks per thread) for rows of `cols` <= kNormRegisterCols
+template <typename F>
+void with_norm_shape(int64_t cols, F f)
+{
+#define DQRM_SHAPE(TPR, CH) \
+    if (cols <= (int64_t)TPR * CH * kChunk) return f(std::integral_constant<int, TPR>{}, std::integral_constant<int, CH>{})
+    DQRM_SHAPE(16, 1);
+    DQRM_SHAPE(64, 1);
+    DQRM_SHAPE(64, 2);
+    DQRM_SHAPE(256, 1);
+    DQRM_SHAPE(256, 2);
+    DQRM_SHAPE(256, 4);
+    DQRM_SHAPE(512, 4);
+#undef DQRM_SHAPE
+}
+
+int norm_rows_per_block(int64_t cols)
+{
+    int n = 1;
+    with_norm_shape(cols, [&](auto tpr, auto) { n = norm_block(decltype(tpr)::value) / decltype(tpr)::value; });
+    return n;
+}
+
+void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
+{
+    const bool in_registers = a.cols <= kNormRegisterCols;
+    const int per_block = in_registers ? norm_rows_per_block(a.cols) : 1;
+    const int64_t step = kMaxBlocks * per_block;
+    const size_t es = size_of(dtype);
+    for (int64_t r0 = 0; r0 < a.rows; r0 += step) {
+        NormArgs b = a;
+        b.rows = std::min(step, a.rows - r0);
+        b.x = static_cast<const char *>(a.x) + r0 * a.ldx * es;
+        if (a.y) b.y = static_cast<char *>(a.y) + r0 * a.ldy * es;
+        if (a.mean) b.mean += r0;
+        if (a.rstd) b.rstd += r0;
+        if (a.codes) b.codes += r0 * codes_pitch(a.cols), b.scales += r0 * scales_pitch(a.cols);
+        const dim3 grid((unsigned)ceil_div(b.rows, per_block));
+        with_type(dtype, [&](auto t) {
+            constexpr int DT = decltype(t)::value;
+            if (!in_registers) {
+                hipLaunchKernelGGL(norm_fwd_long_kernel<DT>, grid, dim3(256), 0, st, b);
+                return;
+            }
+            with_norm_shape(a.cols, [&](auto tpr, auto ch) {
+                constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+                hipLaunchKernelGGL((norm_fwd_kernel<DT, TPR, CH>), grid, dim3(norm_block(TPR)), 0, st, b);
+            });
+        });
+    }
+}
+
+// workgroups, each with a slice of the rows and a pair of partial sums of every column
+int norm_bwd_blocks(int64_t rows, int64_t cols)
+{
+    if (rows < 1 || cols < 1) return 0;
+    if (cols > kNormRegisterCols) return (int)std::min<int64_t>(ceil_div(rows, 32), 64);
+    return (int)std::min<int64_t>(ceil_div(rows, norm_rows_per_block(cols)), 512);
+}
+
+size_t norm_bwd_workspace(int64_t rows, int64_t cols) { return align_up((size_t)norm_bwd_blocks(rows, cols) * 2 * (size_t)cols * sizeof(float), 256); }
+
+// ---- products --------------------------------------------------------------------------------------------------------------
+size_t matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
+
+int32_t launch_matmul(int32_t dtype, const MatmulArgs &g, void *, hipStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(g.n, 32), (unsigned)ceil_div(g.m, 32));
+    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(matmul_simple_kernel<decltype(t)::value>, grid, dim3(64), 0, st, g); });
+    DQRM_HIP_CHECK(hipGetLastError());
+    return DQRM_OK;
+}
+
+struct LinearWs {
+    size_t scales, matmul, total;
+};
+
+LinearWs linear_ws(int64_t m, int64_t n, int64_t k)
+{
+    LinearWs w;
+    w.scales = align_up((size_t)(m * codes_pitch(k)), 256);
+    w.matmul = w.scales + align_up((size_t)(m * scales_pitch(k)), 256);
+    w.total = w.matmul + matmul_workspace(m, n, k);
+    return w;
+}
+
+} // namespace
+
+extern "C" {
+
+size_t dqrm_mxfp4_quant_workspace_bytes(int64_t rows, int64_t cols)
+{
+    return check_shape(DQRM_F32, rows, cols) == DQRM_OK ? quant_workspace(rows, cols) : 0;
+}
+
+int32_t dqrm_mxfp4_quant(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *gate, int64_t ldgate,
+                         const dqrm_mxfp4_t *by_rows, const dqrm_mxfp4_t *by_cols, float *col_sums, void *workspace,
+                         size_t workspace_bytes, void *stream)
+{
+    DQRM_CHECK(check_shape(dtype, rows, cols));
+    if (!by_rows && !by_cols && !col_sums && rows > 0 && cols > 0) return DQRM_ERR_INVALID_ARG; // (an empty output may be null)
+    DQRM_CHECK(check_matrix(x, ldx, dtype, rows, cols));
+    if (gate) DQRM_CHECK(check_matrix(gate, ldgate, dtype, rows, cols));
+    if (by_rows) DQRM_CHECK(check_mx(by_rows, rows, cols));
+    if (by_cols) DQRM_CHECK(check_mx(by_cols, cols, rows));
+    if (col_sums && !aligned(col_sums, 4)) return DQRM_ERR_INVALID_ARG;
+    if (col_sums) DQRM_CHECK(check_workspace(workspace, workspace_bytes, quant_workspace(rows, cols)));
+    const int64_t row_tiles = ceil_div(rows, kTile), col_tiles = ceil_div(cols, kTile);
+    const bool tiles = by_cols || col_sums;
+    if (tiles && row_tiles * col_tiles > kMaxBlocks * 4) return DQRM_ERR_UNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rows == 0 || cols == 0) {
+        fill_zero(col_sums, cols, st);
+        DQRM_HIP_CHECK(hipGetLastError());
+        return DQRM_OK;
+    }
+    QuantArgs a{};
+    a.x = x, a.gate = gate, a.ldx = ldx, a.ldgate = ldgate, a.rows = rows, a.cols = cols;
+    if (by_rows) a.codes = by_rows->codes, a.scales = by_rows->scales;
+    if (by_cols) a.codes_t = by_cols->codes, a.scales_t = by_cols->scales;
+    a.partial = col_sums ? static_cast<float *>(workspace) : nullptr;
+    a.col_tiles = (unsigned)col_tiles;
+    if (!tiles) {
+        launch_quant_rows(dtype, a, st);
+    } else {
+        with_type(dtype, [&](auto t) {
+            hipLaunchKernelGGL(quant_tile_kernel<decltype(t)::value>, dim3((unsigned)(row_tiles * col_tiles)), dim3(256), 0, st, a);
+        });
+        if (col_sums) join_columns(a.partial, cols, (int)row_tiles, cols, col_sums, nullptr, st);
+    }
+    DQRM_HIP_CHECK(hipGetLastError());
+    return DQRM_OK;
+}
+
+int32_t dqrm_mxfp4_dequant(const dqrm_mxfp4_t *q, int32_t dtype, void *out, int64_t ldo, void *stream)
+{
+    if (!q) return DQRM_ERR_INVALID_ARG;
+    DQRM_CHECK(check_shape(dtype, q->rows, q->cols));
+    DQRM_CHECK(check_mx(q, q->rows, q->cols));
+    DQRM_CHECK(check_matrix(out, ldo, dtype, q->rows, q->cols));
+    if (q->rows == 0 || q->cols == 0) return DQRM_OK;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t per_row = ceil_div(q->cols, kChunk), step = std::max<int64_t>(1, kMaxBlocks * 256 / per_row);
+    for (int64_t r0 = 0; r0 < q->rows; r0 += step) {
+        const int64_t rows = std::min(step, q->rows - r0);
+        with_type(dtype, [&](auto t) {
+            hipLaunchKernelGGL(dequant_kernel<decltype(t)::value>, dim3((unsigned)ceil_div(rows * per_row, 256)), dim3(256), 0, st,
+                               q->codes + r0 * codes_pitch(q->cols), q->scales + r0 * scales_pitch(q->cols), rows, q->cols,
+                               static_cast<char *>(out) + r0 * ldo * size_of(dtype), ldo);
+        });
+    }
+    DQRM_HIP_CHECK(hipGetLastError());
+    return DQRM_OK;
+}
+
+size_t dqrm_mxfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (check_shape(DQRM_F32, m, n) != DQRM_OK || check_shape(DQRM_F32, m, k) != DQRM_OK) return 0;
+    return matmul_workspace(m, n, k);
+}
+
+int32_t dqrm_mxfp4_matmul(const dqrm_mxfp4_t *a, const dqrm_mxfp4_t *b, const float *bias, int32_t relu, int32_t dtype, void *out,
+                          int64_t ldo, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!a || !b || a->cols != b->cols) return DQRM_ERR_INVALID_ARG;
+    const int64_t m = a->rows, n = b->rows, k = a->cols;
+    DQRM_CHECK(check_shape(dtype, m, n));
+    DQRM_CHECK(check_shape(dtype, m, k));
+    DQRM_CHECK(check_mx(a, m, k));
+    DQRM_CHECK(check_mx(b, n, k));
+    if (bias && !aligned(bias, 4)) return DQRM_ERR_INVALID_ARG;
+    DQRM_CHECK(check_matrix(out, ldo, dtype, m, n));
+    DQRM_CHECK(check_workspace(workspace, workspace_bytes, matmul_workspace(m, n, k)));
+    if (m == 0 || n == 0) return DQRM_OK;
+    const MatmulArgs g{a->codes, a->scales, b->codes, b->scales, m, n, k, bias, relu != 0, out, ldo};
+    return launch_matmul(dtype, g, workspace, static_cast<hipStream_t>(stream));
+}
+
+size_t dqrm_mxfp4_linear_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (check_shape(DQRM_F32, m, n) != DQRM_OK || check_shape(DQRM_F32, m, k) != DQRM_OK) return 0;
+    return linear_ws(m, n, k).total;
+}
+
+int32_t dqrm_mxfp4_linear(int32_t dtype, int64_t m, const void *x, int64_t ldx, int32_t norm, const float *gamma, const float *beta,
+                          float eps, const dqrm_mxfp4_t *w, const float *bias, int32_t relu, void *out, int64_t ldo, void *workspace,
+                          size_t workspace_bytes, void *stream)
+{
+    if (!w) return DQRM_ERR_INVALID_ARG;
+    const int64_t n = w->rows, k = w->cols;
+    DQRM_CHECK(check_shape(dtype, m, n));
+    DQRM_CHECK(check_shape(dtype, m, k));
+    DQRM_CHECK(check_matrix(x, ldx, dtype, m, k));
+    DQRM_CHECK(check_mx(w, n, k));
+    if ((gamma && !aligned(gamma, 4)) || (beta && !aligned(beta, 4)) || (bias && !aligned(bias, 4))) return DQRM_ERR_INVALID_ARG;
+    if (!norm && (gamma || beta)) return DQRM_ERR_INVALID_ARG;
+    if (norm && !(eps >= 0.0f)) return DQRM_ERR_INVALID_ARG;
+    DQRM_CHECK(check_matrix(out, ldo, dtype, m, n));
+    const LinearWs L = linear_ws(m, n, k);
+    DQRM_CHECK(check_workspace(workspace, workspace_bytes, L.total));
+    if (m == 0 || n == 0) return DQRM_OK;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    uint8_t *codes = ws, *scales = ws + L.scales;
+    if (k > 0) {
+        if (norm) {
+            NormArgs a{};
+            a.x = x, a.ldx = ldx, a.rows = m, a.cols = k, a.gamma = gamma, a.beta = beta, a.eps = eps, a.codes = codes, a.scales = scales;
+            launch_norm_fwd(dtype, a, st);
+        } else {
+            QuantArgs a{};
+            a.x = x, a.ldx = ldx, a.rows = m, a.cols = k, a.codes = codes, a.scales = scales;
+            launch_quant_rows(dtype, a, st);
+        }
+    }
+    const MatmulArgs g{codes, scales, w->codes, w->scales, m, n, k, bias, relu != 0, out, ldo};
+    return launch_matmul(dtype, g, ws + L.matmul, st);
+}
+
+int32_t dqrm_layernorm_fwd(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const float *gamma, const float *beta,
+                           float eps, void *y, int64_t ldy, float *mean, float *rstd, const dqrm_mxfp4_t *q, void *stream)
+{
+    DQRM_CHECK(check_shape(dtype, rows, cols));
+    if (cols < 1 || !(eps >= 0.0f)) return DQRM_ERR_INVALID_ARG;
+    if (!y && !mean && !rstd && !q && rows > 0) return DQRM_ERR_INVALID_ARG; // (an empty output may be null)
+    DQRM_CHECK(check_matrix(x, ldx, dtype, rows, cols));
+    if (y) DQRM_CHECK(check_matrix(y, ldy, dtype, rows, cols));
+    if (q) DQRM_CHECK(check_mx(q, rows, cols));
+    for (const float *p : {gamma, beta, (const float *)mean, (const float *)rstd})
+        if (p && !aligned(p, 4)) return DQRM_ERR_INVALID_ARG;
+    if (rows == 0) return DQRM_OK;
+    NormArgs a{};
+    a.x = x, a.ldx = ldx, a.rows = rows, a.cols = cols, a.gamma = gamma, a.beta = beta, a.eps = eps;
+    a.y = y, a.ldy = ldy, a.mean = mean, a.rstd = rstd;
+    if (q) a.codes = q->codes, a.scales = q->scales;
+    launch_norm_fwd(dtype, a, static_cast<hipStream_t>(stream));
+    DQRM_HIP_CHECK(hipGetLastError());
+    return DQRM_OK;
+}
+
+size_t dqrm_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols)
+{
+    return check_shape(DQRM_F32, rows, cols) == DQRM_OK ? norm_bwd_workspace(rows, cols) : 0;
+}
+
+int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                           const float *mean, const float *rstd, const float *gamma, void *dx, int64_t lddx, float *dgamma,
+                           float *dbeta, void *workspace, size_t workspace_bytes, void *stream)
+{
+    DQRM_CHECK(check_shape(dtype, rows, cols));
+    if (cols < 1 || (!dgamma) != (!dbeta) || (!dx && !dgamma && rows > 0)) return DQRM_ERR_INVALID_ARG;
+    DQRM_CHECK(check_matrix(dy, lddy, dtype, rows, cols));
+    DQRM_CHECK(check_matrix(x, ldx, dtype, rows, cols));
+    if (dx) DQRM_CHECK(check_matrix(dx, lddx, dtype, rows, cols));
+    if (rows > 0 && (!mean || !rstd)) return DQRM_ERR_INVALID_ARG;
+    for (const float *p : {mean, rstd, gamma, (const float *)dgamma, (const float *)dbeta})
+        if (p && !aligned(p, 4)) return DQRM_ERR_INVALID_ARG;
+    if (dgamma) DQRM_CHECK(check_workspace(workspace, workspace_bytes, norm_bwd_workspace(rows, cols)));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rows == 0) {
+        fill_zero(dgamma, cols, st);
+        fill_zero(dbeta, cols, st);
+        DQRM_HIP_CHECK(hipGetLastError());
+        return DQRM_OK;
+    }
+    NormBwdArgs a{dy, x, lddy, ldx, rows, cols, mean, rstd, gamma, dx, lddx, dgamma ? static_cast<float *>(workspace) : nullptr};
+    const int blocks = norm_bwd_blocks(rows, cols);
+    with_type(dtype, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        if (cols <= kNormRegisterCols) {
+            with_norm_shape(cols, [&](auto tpr, auto ch) {
+                constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+                hipLaunchKernelGGL((norm_bwd_kernel<DT, TPR, CH>), dim3((unsigned)blocks), dim3(norm_block(TPR)), 0, st, a);
+            });
+            return;
+        }
+        // (the columns' sums first: dx may be dy's or x's own memory)
+        if (dgamma)
+            hipLaunchKernelGGL(norm_bwd_columns_kernel<DT>, dim3((unsigned)ceil_div(cols, 256 * kChunk), (unsigned)blocks), dim3(256), 0, st, a,
+                               ceil_div(rows, blocks));
+        const size_t es = size_of(dtype);
+        for (int64_t r0 = 0; dx && r0 < rows; r0 += kMaxBlocks) {
+            NormBwdArgs b = a;
+            b.rows = std::min(kMaxBlocks, rows - r0);
+            b.dy = static_cast<const char *>(dy) + r0 * lddy * es, b.x = static_cast<const char *>(x) + r0 * ldx * es;
+            b.dx = static_cast<char *>(dx) + r0 * lddx * es, b.mean = mean + r0, b.rstd = rstd + r0;
+            hipLaunchKernelGGL(norm_bwd_long_kernel<DT>, dim3((unsigned)b.rows), dim3(256), 0, st, b);
+        }
+    });
+    if (dgamma) join_columns(a.partial, 2 * cols, blocks, cols, dgamma, dbeta, st);
+    DQRM_HIP_CHECK(hipGetLastError());
+    return DQRM_OK;
+}
+
+} // extern "C"

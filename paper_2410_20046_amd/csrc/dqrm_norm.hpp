@@ -1,0 +1,307 @@
+// Layer norm forward and backward (gfx950, wave64).
+//
+//   mean = sum x / n, var = sum (x - mean)^2 / n, rstd = 1 / sqrt(var + eps), xhat = (x - mean) rstd, y = xhat gamma + beta
+//   g = dy gamma, dx = rstd (g - mean(g) - xhat mean(g xhat)), dgamma = sum over rows of dy xhat, dbeta = sum over rows of dy
+//
+// All in 32 bits; the variance is taken about the mean, from values that are still in registers.
+#pragma once
+
+#include "dqrm_mx.hpp"
+
+namespace dqrm_mx {
+
+struct NormArgs {
+    const void *x;
+    int64_t ldx, rows, cols;
+    const float *gamma, *beta; // or null: 1 and 0
+    float eps;
+    void *y; // or null
+    int64_t ldy;
+    float *mean, *rstd;      // or null
+    uint8_t *codes, *scales; // MXFP4 of y (before its rounding to the element type), or null
+};
+
+// sum over the TPR threads of a row; every one of them gets it.  TPR > 64: over the waves of a workgroup by way of LDS.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*s_part)[N])
+{
+#pragma unroll
+    for (int d = (TPR < kWaveSize ? TPR : kWaveSize) / 2; d >= 1; d >>= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d, kWaveSize);
+    }
+    if constexpr (TPR > kWaveSize) {
+        constexpr int waves = TPR / kWaveSize;
+        const int wave = threadIdx.x / kWaveSize;
+        __syncthreads(); // the sums of before are read
+        if ((threadIdx.x & (kWaveSize - 1)) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) s_part[wave][i] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float t = s_part[0][i];
+#pragma unroll
+            for (int w = 1; w < waves; ++w) t += s_part[w][i];
+            v[i] = t;
+        }
+    }
+}
+
+__device__ __forceinline__ void load_gain(const float *p, int64_t c, int64_t cols, float without, float (&v)[kChunk])
+{
+    if (p) {
+        load_chunk(p, c, cols, false, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) v[i] = without;
+    }
+}
+
+constexpr int norm_block(int tpr) { return tpr > 256 ? tpr : 256; }
+
+// TPR threads to a row, CH chunks of 8 values to a thread: the row stays in registers (cols <= TPR * CH * 8).
+template <int DT, int TPR, int CH>
+__global__ __launch_bounds__(norm_block(TPR)) void norm_fwd_kernel(NormArgs a)
+{
+    using T = elem_t<DT>;
+    constexpr int rows_per_block = norm_block(TPR) / TPR;
+    __shared__ float s_part[TPR > kWaveSize ? TPR / kWaveSize : 1][1];
+    const int t = threadIdx.x % TPR;
+    const int64_t r_own = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
+    const bool own = r_own < a.rows;
+    const int64_t r = own ? r_own : a.rows - 1; // (a group past the last row works on that row and writes nothing)
+    const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+    float x[CH][kChunk];
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        load_chunk(row, (int64_t)(j * TPR + t) * kChunk, a.cols, r + 1 < a.rows, x[j]);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) sum[0] += x[j][i];
+    }
+    row_sums<TPR>(sum, s_part);
+    const float mean = sum[0] / (float)a.cols;
+    float sq[1] = {0.0f};
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int64_t c = (int64_t)(j * TPR + t) * kChunk;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            x[j][i] -= mean;
+            if (c + i < a.cols) sq[0] += x[j][i] * x[j][i];
+        }
+    }
+    row_sums<TPR>(sq, s_part);
+    const float rstd = 1.0f / sqrtf(sq[0] / (float)a.cols + a.eps);
+    if (own && t == 0) {
+        if (a.mean) a.mean[r] = mean;
+        if (a.rstd) a.rstd[r] = rstd;
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int64_t c = (int64_t)(j * TPR + t) * kChunk;
+        float g[kChunk], b[kChunk];
+        load_gain(a.gamma, c, a.cols, 1.0f, g);
+        load_gain(a.beta, c, a.cols, 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) x[j][i] = c + i < a.cols ? x[j][i] * rstd * g[i] + b[i] : 0.0f;
+        if (!own) continue;
+        if (a.y && c < a.cols) store_chunk(static_cast<T *>(a.y) + r * a.ldy, c, a.cols, x[j]);
+        if (a.codes && c < groups_of(a.cols) * kRowPad)
+            write_chunk(a.codes + r * codes_pitch(a.cols), a.scales + r * scales_pitch(a.cols), (unsigned)(c / kChunk), x[j]);
+    }
+}
+
+// Rows of any length, a workgroup to each: three passes over the row.
+template <int DT>
+__global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
+{
+    using T = elem_t<DT>;
+    __shared__ float s_part[4][1];
+    const int64_t r = blockIdx.x;
+    const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+    const int64_t step = 256 * kChunk, end = groups_of(a.cols) * kRowPad;
+    float sum[1] = {0.0f}, sq[1] = {0.0f};
+    float x[kChunk];
+    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += step) {
+        load_chunk(row, c, a.cols, false, x);
+        sum[0] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
+    row_sums<256>(sum, s_part);
+    const float mean = sum[0] / (float)a.cols;
+    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += step) {
+        load_chunk(row, c, a.cols, false, x);
+        float q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) q += c + i < a.cols ? (x[i] - mean) * (x[i] - mean) : 0.0f;
+        sq[0] += q;
+    }
+    row_sums<256>(sq, s_part);
+    const float rstd = 1.0f / sqrtf(sq[0] / (float)a.cols + a.eps);
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[r] = mean;
+        if (a.rstd) a.rstd[r] = rstd;
+    }
+    if (!a.y && !a.codes) return;
+    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < end; c += step) {
+        float g[kChunk], b[kChunk];
+        load_chunk(row, c, a.cols, false, x);
+        load_gain(a.gamma, c, a.cols, 1.0f, g);
+        load_gain(a.beta, c, a.cols, 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) x[i] = c + i < a.cols ? (x[i] - mean) * rstd * g[i] + b[i] : 0.0f;
+        if (a.y && c < a.cols) store_chunk(static_cast<T *>(a.y) + r * a.ldy, c, a.cols, x);
+        if (a.codes) write_chunk(a.codes + r * codes_pitch(a.cols), a.scales + r * scales_pitch(a.cols), (unsigned)(c / kChunk), x);
+    }
+}
+
+struct NormBwdArgs {
+    const void *dy, *x;
+    int64_t lddy, ldx, rows, cols;
+    const float *mean, *rstd, *gamma; // gamma or null: 1
+    void *dx;                         // or null
+    int64_t lddx;
+    float *partial; // [blocks][2][cols]: the workgroups' sums for dgamma and dbeta, or null
+};
+
+// The row of dy and of x in registers; a thread has the same columns in every row of its workgroup's slice, and keeps their sums.
+template <int DT, int TPR, int CH>
+__global__ __launch_bounds__(norm_block(TPR)) void norm_bwd_kernel(NormBwdArgs a)
+{
+    using T = elem_t<DT>;
+    constexpr int rows_per_block = norm_block(TPR) / TPR;
+    __shared__ float s_part[TPR > kWaveSize ? TPR / kWaveSize : 1][2];
+    const int t = threadIdx.x % TPR;
+    const float inv_n = 1.0f / (float)a.cols;
+    float dg[CH][kChunk] = {}, db[CH][kChunk] = {}, gamma[CH][kChunk];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) load_gain(a.gamma, (int64_t)(j * TPR + t) * kChunk, a.cols, 1.0f, gamma[j]);
+    for (int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR; r - threadIdx.x / TPR < a.rows; r += (int64_t)gridDim.x * rows_per_block) {
+        const bool own = r < a.rows;
+        float dy[CH][kChunk], xh[CH][kChunk];
+        float s[2] = {0.0f, 0.0f};
+        float rstd = 0.0f;
+        if (own) {
+            const float mean = a.mean[r];
+            rstd = a.rstd[r];
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int64_t c = (int64_t)(j * TPR + t) * kChunk;
+                load_chunk(static_cast<const T *>(a.dy) + r * a.lddy, c, a.cols, r + 1 < a.rows, dy[j]);
+                load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, r + 1 < a.rows, xh[j]);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) {
+                    xh[j][i] = c + i < a.cols ? (xh[j][i] - mean) * rstd : 0.0f;
+                    dg[j][i] += dy[j][i] * xh[j][i];
+                    db[j][i] += dy[j][i];
+                    dy[j][i] *= gamma[j][i];
+                    s[0] += dy[j][i];
+                    s[1] += dy[j][i] * xh[j][i];
+                }
+            }
+        }
+        if (!a.dx) continue;
+        row_sums<TPR>(s, s_part);
+        if (own) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int64_t c = (int64_t)(j * TPR + t) * kChunk;
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) dy[j][i] = rstd * (dy[j][i] - s[0] * inv_n - xh[j][i] * (s[1] * inv_n));
+                if (c < a.cols) store_chunk(static_cast<T *>(a.dx) + r * a.lddx, c, a.cols, dy[j]);
+            }
+        }
+    }
+    if (!a.partial) return;
+    float *out = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
+    if constexpr (rows_per_block == 1) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t c = (int64_t)(j * TPR + t) * kChunk;
+            if (c < a.cols) {
+                store_chunk(out, c, a.cols, dg[j]);
+                store_chunk(out + a.cols, c, a.cols, db[j]);
+            }
+        }
+    } else {
+        // the rows' groups of the workgroup are added in turn
+        __shared__ float s_acc[rows_per_block][TPR * kChunk];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) s_acc[threadIdx.x / TPR][t * kChunk + i] = k ? db[j][i] : dg[j][i];
+                __syncthreads();
+                for (int c = threadIdx.x; c < TPR * kChunk; c += norm_block(TPR)) {
+                    float v = s_acc[0][c];
+                    for (int w = 1; w < rows_per_block; ++w) v += s_acc[w][c];
+                    const int64_t col = (int64_t)j * TPR * kChunk + c;
+                    if (col < a.cols) out[k * a.cols + col] = v;
+                }
+            }
+        }
+    }
+}
+
+// Rows of any length: dx from two passes over the row, a workgroup to each.
+template <int DT>
+__global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
+{
+    using T = elem_t<DT>;
+    __shared__ float s_part[4][2];
+    const int64_t r = blockIdx.x;
+    const float mean = a.mean[r], rstd = a.rstd[r], inv_n = 1.0f / (float)a.cols;
+    const T *pdy = static_cast<const T *>(a.dy) + r * a.lddy, *px = static_cast<const T *>(a.x) + r * a.ldx;
+    float s[2] = {0.0f, 0.0f};
+    float dy[kChunk], x[kChunk], g[kChunk];
+    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += 256 * kChunk) {
+        load_chunk(pdy, c, a.cols, false, dy);
+        load_chunk(px, c, a.cols, false, x);
+        load_gain(a.gamma, c, a.cols, 1.0f, g);
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            const float gi = c + i < a.cols ? dy[i] * g[i] : 0.0f;
+            s0 += gi;
+            s1 += c + i < a.cols ? gi * ((x[i] - mean) * rstd) : 0.0f;
+        }
+        s[0] += s0, s[1] += s1;
+    }
+    row_sums<256>(s, s_part);
+    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += 256 * kChunk) {
+        load_chunk(pdy, c, a.cols, false, dy);
+        load_chunk(px, c, a.cols, false, x);
+        load_gain(a.gamma, c, a.cols, 1.0f, g);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) x[i] = rstd * (dy[i] * g[i] - s[0] * inv_n - (x[i] - mean) * rstd * (s[1] * inv_n));
+        store_chunk(static_cast<T *>(a.dx) + r * a.lddx, c, a.cols, x);
+    }
+}
+
+// ... and the sums over a slice of rows, eight columns to a thread.
+template <int DT>
+__global__ __launch_bounds__(256) void norm_bwd_columns_kernel(NormBwdArgs a, int64_t rows_per_slice)
+{
+    using T = elem_t<DT>;
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * kChunk;
+    if (c >= a.cols) return;
+    const int64_t r0 = (int64_t)blockIdx.y * rows_per_slice, r1 = min(r0 + rows_per_slice, a.rows);
+    float dg[kChunk] = {}, db[kChunk] = {};
+    for (int64_t r = r0; r < r1; ++r) {
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        float dy[kChunk], x[kChunk];
+        load_chunk(static_cast<const T *>(a.dy) + r * a.lddy, c, a.cols, false, dy);
+        load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, false, x);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) dg[i] += c + i < a.cols ? dy[i] * ((x[i] - mean) * rstd) : 0.0f, db[i] += dy[i];
+    }
+    float *out = a.partial + (int64_t)blockIdx.y * 2 * a.cols;
+    store_chunk(out, c, a.cols, dg);
+    store_chunk(out + a.cols, c, a.cols, db);
+}
+
+} // namespace dqrm_mx
