@@ -193,12 +193,69 @@ int norm_bwd_blocks(int64_t rows, int64_t cols)
 size_t norm_bwd_workspace(int64_t rows, int64_t cols) { return align_up((size_t)norm_bwd_blocks(rows, cols) * 2 * (size_t)cols * sizeof(float), 256); }
 
 // ---- products --------------------------------------------------------------------------------------------------------------
-size_t matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
+using Tile256 = TileShape<4, 4, 2, 2>;
+using Tile128 = TileShape<2, 2, 2, 2>;
+using Tile64 = TileShape<1, 1, 2, 2>;
 
-int32_t launch_matmul(int32_t dtype, const MatmulArgs &g, void *, hipStream_t st)
+struct MatmulPlan {
+    int tile;        // 256, 128 or 64
+    unsigned slices; // of k
+    unsigned stages_per_slice;
+};
+
+MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
-    const dim3 grid((unsigned)ceil_div(g.n, 32), (unsigned)ceil_div(g.m, 32));
-    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(matmul_simple_kernel<decltype(t)::value>, grid, dim3(64), 0, st, g); });
+    const auto tiles = [&](int64_t t) { return ceil_div(m, t) * ceil_div(n, t); };
+    MatmulPlan p{};
+    p.tile = tiles(256) >= num_cus() ? 256 : tiles(128) >= num_cus() / 2 || k >= 4096 ? 128 : 64;
+    const int64_t stages = std::max<int64_t>(1, ceil_div(groups_of(k), 2));
+    const int64_t want = std::max<int64_t>(1, num_cus() / std::max<int64_t>(1, tiles(p.tile)));
+    const int64_t most = std::max<int64_t>(1, stages / 4); // four stages to a slice at least
+    const int64_t slices = std::min(want, most);
+    p.stages_per_slice = (unsigned)ceil_div(stages, slices);
+    p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
+    return p;
+}
+
+size_t matmul_workspace(int64_t m, int64_t n, int64_t k)
+{
+    const MatmulPlan p = matmul_plan(m, n, k);
+    return p.slices > 1 ? align_up((size_t)p.slices * (size_t)m * (size_t)n * sizeof(float), 256) : 0;
+}
+
+template <typename T>
+void launch_tiles(const MatmulPlan &p, MatmulArgs g, hipStream_t st)
+{
+    const auto go = [&](auto shape) {
+        using S = decltype(shape);
+        g.tiles_m = (unsigned)ceil_div(g.m, S::BM), g.tiles_n = (unsigned)ceil_div(g.n, S::BN);
+        hipLaunchKernelGGL((matmul_kernel<T, S>), dim3(g.tiles_m * g.tiles_n * g.slices), dim3(S::waves * kWaveSize), 0, st, g);
+    };
+    if (p.tile == 256)
+        go(Tile256{});
+    else if (p.tile == 128)
+        go(Tile128{});
+    else
+        go(Tile64{});
+}
+
+constexpr int64_t kMaxInner = 1 << 24; // a tile's rows of codes are addressed with 32 bits
+
+int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t st)
+{
+    const MatmulPlan p = matmul_plan(g.m, g.n, g.k);
+    g.slices = p.slices, g.stages_per_slice = p.stages_per_slice;
+    if (p.slices > 1) {
+        MatmulArgs part = g;
+        part.c = workspace;
+        launch_tiles<float>(p, part, st);
+        const unsigned blocks = (unsigned)ceil_div(g.m * g.n, 1024);
+        with_type(dtype, [&](auto t) {
+            hipLaunchKernelGGL(matmul_join_kernel<decltype(t)::value>, dim3(blocks), dim3(256), 0, st, static_cast<const float *>(workspace), g);
+        });
+    } else {
+        with_type(dtype, [&](auto t) { launch_tiles<elem_t<decltype(t)::value>>(p, g, st); });
+    }
     DQRM_HIP_CHECK(hipGetLastError());
     return DQRM_OK;
 }
@@ -303,6 +360,7 @@ int32_t dqrm_mxfp4_matmul(const dqrm_mxfp4_t *a, const dqrm_mxfp4_t *b, const fl
     if (bias && !aligned(bias, 4)) return DQRM_ERR_INVALID_ARG;
     DQRM_CHECK(check_matrix(out, ldo, dtype, m, n));
     DQRM_CHECK(check_workspace(workspace, workspace_bytes, matmul_workspace(m, n, k)));
+    if (k > kMaxInner) return DQRM_ERR_UNSUPPORTED;
     if (m == 0 || n == 0) return DQRM_OK;
     const MatmulArgs g{a->codes, a->scales, b->codes, b->scales, m, n, k, bias, relu != 0, out, ldo};
     return launch_matmul(dtype, g, workspace, static_cast<hipStream_t>(stream));
@@ -330,6 +388,7 @@ int32_t dqrm_mxfp4_linear(int32_t dtype, int64_t m, const void *x, int64_t ldx, 
     DQRM_CHECK(check_matrix(out, ldo, dtype, m, n));
     const LinearWs L = linear_ws(m, n, k);
     DQRM_CHECK(check_workspace(workspace, workspace_bytes, L.total));
+    if (k > kMaxInner) return DQRM_ERR_UNSUPPORTED;
     if (m == 0 || n == 0) return DQRM_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
