@@ -13,7 +13,7 @@ _SHARED = ["dqrm_host.hpp", os.path.join(ROOT, "include", "dqrm.h")]
 UNITS = {
     "dqrm_api.hip": ["dqrm_device.hpp", "dqrm_fwd.hpp", "dqrm_dedupe.hpp", "dqrm_bwd.hpp", "dqrm_update.hpp", "dqrm_merge.hpp",
                      "dqrm_dense.hpp", "dqrm_step.hpp"] + _SHARED,
-    "dqrm_mx_api.hip": ["dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_norm.hpp"] + _SHARED,
+    "dqrm_mx_api.hip": ["dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_mx_few.hpp", "dqrm_norm.hpp"] + _SHARED,
 }
 SOURCES = [os.path.join(CSRC, f) for f in UNITS]
 HEADERS = sorted({os.path.join(CSRC, f) for headers in UNITS.values() for f in headers})

@@ -10,6 +10,7 @@
 #include "dqrm_mx.hpp"
 #include "dqrm_mx_gemm.hpp"
 #include "dqrm_norm.hpp"
+#include "dqrm_mx_few.hpp"
 
 namespace {
 
@@ -198,13 +199,17 @@ using Tile128 = TileShape<2, 2, 2, 2>;
 using Tile64 = TileShape<1, 1, 2, 2>;
 
 struct MatmulPlan {
-    int tile;        // 256, 128 or 64
+    int tile;        // 256, 128 or 64; 0: few_kernel
     unsigned slices; // of k
     unsigned stages_per_slice;
 };
 
+// Few rows of A, and W's strips enough to keep the chip's memory busy or k short.
+bool is_few(int64_t m, int64_t n, int64_t k) { return m <= 64 && (n >= 512 || k <= 16384); }
+
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
+    if (is_few(m, n, k)) return MatmulPlan{0, 1, 0};
     const auto tiles = [&](int64_t t) { return ceil_div(m, t) * ceil_div(n, t); };
     MatmulPlan p{};
     p.tile = tiles(256) >= num_cus() ? 256 : tiles(128) >= num_cus() / 2 || k >= 4096 ? 128 : 64;
@@ -241,9 +246,35 @@ void launch_tiles(const MatmulPlan &p, MatmulArgs g, hipStream_t st)
 
 constexpr int64_t kMaxInner = 1 << 24; // a tile's rows of codes are addressed with 32 bits
 
+template <int DT, FewSource SRC, int MT>
+void launch_few(const FewArgs &a, hipStream_t st)
+{
+    const int64_t strips = ceil_div(a.g.n, 16);
+    const size_t lds = SRC == kFewCodes ? 0 : (size_t)(a.g.m * (codes_pitch(a.g.k) + scales_pitch(a.g.k)));
+    if (strips > num_cus())
+        hipLaunchKernelGGL((few_kernel<DT, SRC, MT, 2>), dim3((unsigned)ceil_div(strips, 2)), dim3(kFewBlock), lds, st, a);
+    else
+        hipLaunchKernelGGL((few_kernel<DT, SRC, MT, 1>), dim3((unsigned)strips), dim3(kFewBlock), lds, st, a);
+}
+
 int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t st)
 {
     const MatmulPlan p = matmul_plan(g.m, g.n, g.k);
+    if (p.tile == 0) {
+        FewArgs a{};
+        a.g = g;
+        with_type(dtype, [&](auto t) {
+            constexpr int DT = decltype(t)::value;
+            if (g.m <= 16)
+                launch_few<DT, kFewCodes, 1>(a, st);
+            else if (g.m <= 32)
+                launch_few<DT, kFewCodes, 2>(a, st);
+            else
+                launch_few<DT, kFewCodes, 4>(a, st);
+        });
+        DQRM_HIP_CHECK(hipGetLastError());
+        return DQRM_OK;
+    }
     g.slices = p.slices, g.stages_per_slice = p.stages_per_slice;
     if (p.slices > 1) {
         MatmulArgs part = g;
@@ -258,6 +289,13 @@ int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t 
     }
     DQRM_HIP_CHECK(hipGetLastError());
     return DQRM_OK;
+}
+
+// Whether the product quantises the activations itself, every workgroup all of them: as far as quantise_few's registers go.
+bool linear_in_one(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t waves = m <= 1 ? 8 : m <= 2 ? 4 : m <= 4 ? 2 : 1;
+    return m <= 8 && k > 0 && k <= waves * kWaveSize * kFewChunks * kChunk && is_few(m, n, k);
 }
 
 struct LinearWs {
@@ -393,6 +431,20 @@ int32_t dqrm_mxfp4_linear(int32_t dtype, int64_t m, const void *x, int64_t ldx, 
     hipStream_t st = static_cast<hipStream_t>(stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     uint8_t *codes = ws, *scales = ws + L.scales;
+    if (linear_in_one(m, n, k)) {
+        FewArgs a{};
+        a.g = MatmulArgs{nullptr, nullptr, w->codes, w->scales, m, n, k, bias, relu != 0, out, ldo};
+        a.x.x = x, a.x.ldx = ldx, a.x.rows = m, a.x.cols = k, a.x.gamma = gamma, a.x.beta = beta, a.x.eps = eps;
+        with_type(dtype, [&](auto t) {
+            constexpr int DT = decltype(t)::value;
+            if (norm)
+                launch_few<DT, kFewNorm, 1>(a, st);
+            else
+                launch_few<DT, kFewPlain, 1>(a, st);
+        });
+        DQRM_HIP_CHECK(hipGetLastError());
+        return DQRM_OK;
+    }
     if (k > 0) {
         if (norm) {
             NormArgs a{};

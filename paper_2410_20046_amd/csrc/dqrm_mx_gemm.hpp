@@ -43,27 +43,35 @@ constexpr int kStageCodes = kStage / 2, kStageScales = kStage / 32;
 // such load before any read of LDS.  They have no output registers; lds_barrier() is what waits for them.
 typedef unsigned rsrc_t __attribute__((ext_vector_type(4)));
 
+// a value that all lanes hold, in a scalar register
+__device__ __forceinline__ unsigned uniform(unsigned v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // `bytes` of memory from p on; what lies past them reads as zeros
 __device__ __forceinline__ rsrc_t buffer_of(const uint8_t *p, int64_t bytes)
 {
     const uint64_t at = reinterpret_cast<uint64_t>(p);
     rsrc_t r;
-    r.x = __builtin_amdgcn_readfirstlane((unsigned)at), r.y = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32) & 0xFFFFu);
-    r.z = __builtin_amdgcn_readfirstlane((unsigned)min(bytes, (int64_t)0xFFFFFFFF)), r.w = 0x00027000u;
+    r.x = uniform((unsigned)at), r.y = uniform((unsigned)(at >> 32) & 0xFFFFu);
+    r.z = uniform((unsigned)min(bytes, (int64_t)0xFFFFFFFF)), r.w = 0x00027000u;
     return r;
 }
 
 // lane l's 16 (4) bytes at offset + base come to LDS address lds + 16 l (4 l); lds and base are the wave's
 __device__ __forceinline__ void load16_to_lds(rsrc_t r, unsigned offset, unsigned base, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(r), "s"(__builtin_amdgcn_readfirstlane(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(uniform(lds)), "v"(offset), "s"(r), "s"(uniform(base)) : "memory");
 }
 __device__ __forceinline__ void load4_to_lds(rsrc_t r, unsigned offset, unsigned base, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(r), "s"(__builtin_amdgcn_readfirstlane(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(uniform(lds)), "v"(offset), "s"(r), "s"(uniform(base)) : "memory");
 }
 // every load of this wave is in LDS and every read of LDS has its data; then every wave's
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// every wave has what it has read from LDS
+__device__ __forceinline__ void read_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// every wave's loads are in LDS but for its last N
+template <int N>
+__device__ __forceinline__ void loaded_barrier() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ unsigned lds_address(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
@@ -73,6 +81,21 @@ struct TileShape {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, waves = WM * WN, BM = TM * WM * 32, BN = TN * WN * 32;
     static constexpr int rows = BM + BN;
     static constexpr int code_bytes = rows * kStageCodes, stage_bytes = code_bytes + rows * kStageScales;
+    // loads of a wave in a stage: vectors of A's and of B's codes, scales
+    static constexpr int a_loads = BM / 8 / waves, b_loads = BN / 8 / waves, loads = a_loads + b_loads + (rows / 32 + waves - 1) / waves;
+    // Order of a stage's instructions, in places behind each of a step's products: reads for the next step in the first half; in the
+    // last step but one, behind place `freed`, every wave has read the stage and the loads of the stage after the next go into its
+    // memory, spread evenly; in the last step, behind place `arrived`, the next stage is there.
+    static constexpr int products = TM * TN, freed = products * 3 / 4 - (products > 1), arrived = products / 2 - (products > 1);
+    static constexpr int load_places = 2 * products - freed;
+    static constexpr int load_place(int q) { return q * load_places / loads; }
+    static constexpr int read_place(int r) { return r * products / (TM + TN) / 2; }
+    static constexpr int loads_before_arrival()
+    {
+        int n = 0;
+        for (int q = 0; q < loads; ++q) n += load_place(q) <= products - freed + arrived;
+        return n;
+    }
 };
 
 // Rows m by columns n of a wave's accumulators through LDS to memory: the lane has four neighbouring columns of one row in
@@ -128,16 +151,16 @@ __global__ __launch_bounds__(S::waves *kWaveSize, 1) void matmul_kernel(MatmulAr
     constexpr int lds_bytes = 2 * S::stage_bytes > S::waves * 32 * pitch_out ? 2 * S::stage_bytes : S::waves * 32 * pitch_out;
     __shared__ __align__(1024) char lds[lds_bytes];
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = (int)uniform(threadIdx.x >> 6);
     const unsigned tiles = g.tiles_m * g.tiles_n;
     // Workgroups are dealt to the chip's parts in turn: each part gets a run of tiles, in columns of up to 8 rows of tiles, so
     // that the operands its second-level cache holds are read by several.
     const unsigned part = blockIdx.x % kParts, per_part = gridDim.x / kParts, more = gridDim.x % kParts;
     const unsigned place = part * per_part + min(part, more) + blockIdx.x / kParts;
-    const unsigned slice = place / tiles, at = place - slice * tiles;
-    const unsigned column = at / (kTileRows * g.tiles_n), in_column = at - column * kTileRows * g.tiles_n;
+    const unsigned slice = uniform(place / tiles), at = place - slice * tiles;
+    const unsigned column = uniform(at / (kTileRows * g.tiles_n)), in_column = at - column * kTileRows * g.tiles_n;
     const unsigned high = min((unsigned)kTileRows, g.tiles_m - column * kTileRows);
-    const unsigned tn = in_column / high, tm = column * kTileRows + in_column - tn * high;
+    const unsigned tn = uniform(in_column / high), tm = column * kTileRows + in_column - tn * high;
     const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
     const int64_t groups = groups_of(g.k), cp = groups * 64, sp = groups * 4;
     const int all = (int)((groups + 1) / 2);
@@ -149,58 +172,52 @@ __global__ __launch_bounds__(S::waves *kWaveSize, 1) void matmul_kernel(MatmulAr
     // codes in LDS: 8 vectors of 16 bytes to a row, vector v of row r in place v ^ (r & 7)
     const unsigned code_at = (unsigned)(lane >> 3) * (unsigned)cp + (unsigned)(((lane & 7) ^ (lane >> 3)) * 16);
     const unsigned scale_at = (unsigned)(lane >> 1) * (unsigned)sp + (unsigned)(lane & 1) * 4;
-    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds));
+    const unsigned lds0 = uniform(lds_address(lds));
 
-    auto request = [&](int s) {
-        constexpr int a_loads = S::BM / 8, b_loads = S::BN / 8, sa_loads = S::BM / 32, s_loads = S::rows / 32;
+    // Load q of the S::loads that a wave has in stage s.  A stage past the last one is requested from a buffer without bytes.
+    auto request = [&](int s, int q) {
         const unsigned to = lds0 + (unsigned)((s - first) & 1) * S::stage_bytes;
-#pragma unroll
-        for (int i = 0; i < a_loads / S::waves; ++i) {
-            const unsigned j = (unsigned)(i * S::waves + wave);
-            load16_to_lds(ra, code_at, (unsigned)s * kStageCodes + j * 8 * (unsigned)cp, to + j * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < b_loads / S::waves; ++i) {
-            const unsigned j = (unsigned)(i * S::waves + wave);
-            load16_to_lds(rb, code_at, (unsigned)s * kStageCodes + j * 8 * (unsigned)cp, to + (a_loads + j) * 1024);
-        }
-if constexpr (sa_loads % S::waves == 0) {
-#pragma unroll
-            for (int i = 0; i < sa_loads / S::waves; ++i) {
-                const unsigned j = (unsigned)(i * S::waves + wave);
-                load4_to_lds(rsa, scale_at, (unsigned)s * kStageScales + j * 32 * (unsigned)sp, to + S::code_bytes + j * 256);
-            }
-#pragma unroll
-            for (int i = 0; i < (s_loads - sa_loads) / S::waves; ++i) {
-                const unsigned j = (unsigned)(i * S::waves + wave);
-                load4_to_lds(rsb, scale_at, (unsigned)s * kStageScales + j * 32 * (unsigned)sp, to + S::code_bytes + (sa_loads + j) * 256);
-            }
+        auto here = [&](rsrc_t r) {
+            r.z = uniform(s < last ? r.z : 0u);
+            return r;
+        };
+        if (q < S::a_loads + S::b_loads) {
+            const bool of_a = q < S::a_loads;
+            const unsigned j = (unsigned)((of_a ? q : q - S::a_loads) * S::waves + wave);
+            load16_to_lds(here(of_a ? ra : rb), code_at, (unsigned)s * kStageCodes + j * 8 * (unsigned)cp, to + (of_a ? 0 : S::BM * kStageCodes) + j * 1024);
+        } else if constexpr (S::BM / 32 % S::waves == 0) {
+            constexpr int each = S::BM / 32 / S::waves;
+            const int k = q - S::a_loads - S::b_loads;
+            const bool of_a = k < each;
+            const unsigned j = (unsigned)((of_a ? k : k - each) * S::waves + wave);
+            load4_to_lds(here(of_a ? rsa : rsb), scale_at, (unsigned)s * kStageScales + j * 32 * (unsigned)sp, to + S::code_bytes + (of_a ? 0 : S::BM * kStageScales) + j * 256);
         } else {
-            static_assert(s_loads == S::waves, "one load of scales to a wave");
-            const bool of_a = wave < sa_loads;
-            const unsigned j = (unsigned)(of_a ? wave : wave - sa_loads);
-            load4_to_lds(of_a ? rsa : rsb, scale_at, (unsigned)s * kStageScales + j * 32 * (unsigned)sp, to + S::code_bytes + wave * 256);
+            static_assert(S::BM / 32 % S::waves == 0 || S::rows / 32 == S::waves, "one load of scales to a wave");
+            const bool of_a = wave < S::BM / 32;
+            const unsigned j = (unsigned)(of_a ? wave : wave - S::BM / 32);
+            load4_to_lds(here(of_a ? rsa : rsb), scale_at, (unsigned)s * kStageScales + j * 32 * (unsigned)sp, to + S::code_bytes + wave * 256);
         }
     };
 
     const int wm = wave / S::WN, wn = wave % S::WN;
     const int row_a = wm * S::TM * 32 + (lane & 31), row_b = S::BM + wn * S::TN * 32 + (lane & 31);
     uint4 a[2][S::TM], b[2][S::TN];
-    auto read_codes = [&](int s, int t, int to) {
+    // operand r of a step: A's rows, then B's
+    auto read_codes = [&](int s, int t, int r) {
         const char *now = lds + ((s - first) & 1) * S::stage_bytes;
         const int at = ((2 * t + half) ^ (lane & 7)) * 16;
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i) a[to][i] = *reinterpret_cast<const uint4 *>(now + (row_a + i * 32) * kStageCodes + at);
-#pragma unroll
-        for (int i = 0; i < S::TN; ++i) b[to][i] = *reinterpret_cast<const uint4 *>(now + (row_b + i * 32) * kStageCodes + at);
+        if (r < S::TM)
+            a[t & 1][r] = *reinterpret_cast<const uint4 *>(now + (row_a + r * 32) * kStageCodes + at);
+        else
+            b[t & 1][r - S::TM] = *reinterpret_cast<const uint4 *>(now + (row_b + (r - S::TM) * 32) * kStageCodes + at);
     };
     uint2 sa[S::TM], sb[S::TN];
-    auto read_scales = [&](int s) {
+    auto read_scales = [&](int s, int r) {
         const char *now = lds + ((s - first) & 1) * S::stage_bytes + S::code_bytes;
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i) sa[i] = *reinterpret_cast<const uint2 *>(now + (row_a + i * 32) * kStageScales);
-#pragma unroll
-        for (int i = 0; i < S::TN; ++i) sb[i] = *reinterpret_cast<const uint2 *>(now + (row_b + i * 32) * kStageScales);
+        if (r < S::TM)
+            sa[r] = *reinterpret_cast<const uint2 *>(now + (row_a + r * 32) * kStageScales);
+        else
+            sb[r - S::TM] = *reinterpret_cast<const uint2 *>(now + (row_b + (r - S::TM) * 32) * kStageScales);
     };
     // the sums begin with the bias
     const bool finish = g.slices <= 1;
@@ -225,37 +242,54 @@ if constexpr (sa_loads % S::waves == 0) {
         for (int i = 0; i < S::TM; ++i) ua[0][i] = sa[i].x >> (8 * half), ua[1][i] = odd_end ? 0u : sa[i].y >> (8 * half);
 #pragma unroll
         for (int i = 0; i < S::TN; ++i) ub[0][i] = sb[i].x >> (8 * half), ub[1][i] = odd_end ? 0u : sb[i].y >> (8 * half);
+constexpr int steps = kStage / 64, reads = S::TM + S::TN;
+        constexpr bool more = !decltype(is_last)::value;
 #pragma unroll
-        for (int t = 0; t < kStage / 64; ++t) {
-            // what the next step needs is requested before this step's products; the compiler would gather all reads of the stage
-            // at its beginning, where nothing hides them
-            __builtin_amdgcn_sched_barrier(0);
-            if (t + 1 < kStage / 64) {
-                read_codes(s, t + 1, (t + 1) & 1);
-            } else if constexpr (!decltype(is_last)::value) {
-                lds_barrier();
-                read_scales(s + 1);
-                read_codes(s + 1, 0, 0);
-                request(s + 2); // (past the last stage: nobody reads it)
-            }
-            __builtin_amdgcn_sched_barrier(0);
+        for (int t = 0; t < steps; ++t) {
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i)
+            for (int p = 0; p < S::products; ++p) {
+                const int i = p / S::TN, j = p % S::TN;
+                if (t & 1)
+                    acc[i][j] = mfma_32x32x64<2>(b[t & 1][j], a[t & 1][i], acc[i][j], ub[t >> 1][j], ua[t >> 1][i]);
+                else
+                    acc[i][j] = mfma_32x32x64<0>(b[t & 1][j], a[t & 1][i], acc[i][j], ub[t >> 1][j], ua[t >> 1][i]);
+                // (the compiler keeps this order: left to itself it gathers the reads where nothing hides them)
+                __builtin_amdgcn_sched_barrier(0);
+                if (t + 1 < steps) {
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j) {
-                    if (t & 1)
-                        acc[i][j] = mfma_32x32x64<2>(b[t & 1][j], a[t & 1][i], acc[i][j], ub[t >> 1][j], ua[t >> 1][i]);
-                    else
-                        acc[i][j] = mfma_32x32x64<0>(b[t & 1][j], a[t & 1][i], acc[i][j], ub[t >> 1][j], ua[t >> 1][i]);
+                    for (int r = 0; r < reads; ++r)
+                        if (S::read_place(r) == p) read_codes(s, t + 1, r);
                 }
+                if constexpr (more) {
+                    if (t == steps - 2 && p == S::freed) read_barrier();
+                    const int place = t == steps - 2 ? p - S::freed : t == steps - 1 ? S::products - S::freed + p : -1;
+#pragma unroll
+                    for (int q = 0; q < S::loads; ++q)
+                        if (S::load_place(q) == place) request(s + 2, q);
+                    if (t == steps - 1 && p == S::arrived) {
+                        loaded_barrier<S::loads_before_arrival()>();
+#pragma unroll
+                        for (int r = 0; r < reads; ++r) read_scales(s + 1, r);
+                    }
+                    if (t == steps - 1 && p >= S::arrived) {
+                        constexpr int left = S::products - S::arrived;
+#pragma unroll
+                        for (int r = 0; r < reads; ++r)
+                            if (r * left / reads == p - S::arrived) read_codes(s + 1, 0, r);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
     if (first < last) {
-        request(first);
+#pragma unroll
+        for (int q = 0; q < S::loads; ++q) request(first, q);
         lds_barrier();
-        request(first + 1);
-        read_scales(first);
-        read_codes(first, 0, 0);
+#pragma unroll
+        for (int q = 0; q < S::loads; ++q) request(first + 1, q);
+#pragma unroll
+        for (int r = 0; r < S::TM + S::TN; ++r) read_scales(first, r), read_codes(first, 0, r);
         for (int s = first; s + 1 < last; ++s) compute(s, std::false_type{});
         compute(last - 1, std::true_type{});
     }
