@@ -52,8 +52,8 @@ __device__ __forceinline__ void load_first(const T *p, int n, float (&v)[kChunk]
 
 // values c .. c + 7 of a row of `cols`; those past its end are 0.  `inside`: the 8 values lie inside the matrix's memory, so they
 // may be loaded as one vector also where some belong to what follows the row.
-template <typename T>
-__device__ __forceinline__ void load_chunk(const T *row, int64_t c, int64_t cols, bool inside, float (&v)[kChunk])
+template <typename T, typename I>
+__device__ __forceinline__ void load_chunk(const T *row, I c, I cols, bool inside, float (&v)[kChunk])
 {
     if (c + kChunk <= cols) {
         load8(row + c, v);
@@ -69,8 +69,8 @@ __device__ __forceinline__ void load_chunk(const T *row, int64_t c, int64_t cols
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void store_chunk(T *row, int64_t c, int64_t cols, const float (&v)[kChunk])
+template <typename T, typename I>
+__device__ __forceinline__ void store_chunk(T *row, I c, I cols, const float (&v)[kChunk])
 {
     if (c + kChunk <= cols) {
         Vec8<T> t;

@@ -129,36 +129,39 @@ void launch_quant_rows(int32_t dtype, QuantArgs a, hipStream_t st)
 }
 
 // ---- layer norm ----------------------------------------------------------------------------------------------------------
-constexpr int64_t kNormRegisterCols = 16384; // longer rows are read more than once
+// Rows of 8 to 16384 values stay in registers; others are read more than once (shorter ones have no vector of 8).
+bool norm_in_registers(int64_t cols) { return cols >= kChunk && cols <= 16384; }
 
-// f(threads per row, chunks per thread) for rows of `cols` <= kNormRegisterCols
-template <typename F>
-void with_norm_shape(int64_t cols, F f)
+// How a row that stays in registers is laid over threads: f(shape) for the narrowest one that holds it.
+template <int TPR_, int CH_, int BLOCK_>
+struct NormShape {
+    static constexpr int TPR = TPR_, CH = CH_, BLOCK = BLOCK_, cols = TPR * CH * kChunk, rows = BLOCK / TPR;
+};
+
+template <typename... S, typename F>
+void with_first_that_holds(int64_t cols, F f)
 {
-#define DQRM_SHAPE(TPR, CH) \
-    if (cols <= (int64_t)TPR * CH * kChunk) return f(std::integral_constant<int, TPR>{}, std::integral_constant<int, CH>{})
-    DQRM_SHAPE(16, 1);
-    DQRM_SHAPE(64, 1);
-    DQRM_SHAPE(64, 2);
-    DQRM_SHAPE(256, 1);
-    DQRM_SHAPE(256, 2);
-    DQRM_SHAPE(256, 4);
-    DQRM_SHAPE(512, 4);
-#undef DQRM_SHAPE
+    (void)((cols <= S::cols ? (f(S{}), true) : false) || ...);
 }
 
-int norm_rows_per_block(int64_t cols)
+template <typename F>
+void with_norm_fwd_shape(int64_t cols, F f)
 {
-    int n = 1;
-    with_norm_shape(cols, [&](auto tpr, auto) { n = norm_block(decltype(tpr)::value) / decltype(tpr)::value; });
-    return n;
+    with_first_that_holds<NormShape<16, 1, 256>, NormShape<64, 1, 256>, NormShape<64, 2, 256>, NormShape<256, 1, 256>, NormShape<256, 2, 256>,
+                          NormShape<512, 2, 512>, NormShape<1024, 2, 1024>>(cols, f);
+}
+
+template <typename F>
+void with_norm_bwd_shape(int64_t cols, F f)
+{
+    with_first_that_holds<NormShape<16, 1, 1024>, NormShape<64, 1, 1024>, NormShape<64, 2, 512>, NormShape<256, 1, 1024>, NormShape<512, 1, 1024>,
+                          NormShape<1024, 1, 1024>, NormShape<1024, 2, 1024>>(cols, f);
 }
 
 void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
 {
-    const bool in_registers = a.cols <= kNormRegisterCols;
-    const int per_block = in_registers ? norm_rows_per_block(a.cols) : 1;
-    const int64_t step = kMaxBlocks * per_block;
+    const bool in_registers = norm_in_registers(a.cols);
+    const int64_t step = kMaxBlocks;
     const size_t es = size_of(dtype);
     for (int64_t r0 = 0; r0 < a.rows; r0 += step) {
         NormArgs b = a;
@@ -168,16 +171,18 @@ void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
         if (a.mean) b.mean += r0;
         if (a.rstd) b.rstd += r0;
         if (a.codes) b.codes += r0 * codes_pitch(a.cols), b.scales += r0 * scales_pitch(a.cols);
-        const dim3 grid((unsigned)ceil_div(b.rows, per_block));
         with_type(dtype, [&](auto t) {
             constexpr int DT = decltype(t)::value;
             if (!in_registers) {
-                hipLaunchKernelGGL(norm_fwd_long_kernel<DT>, grid, dim3(256), 0, st, b);
+                hipLaunchKernelGGL(norm_fwd_long_kernel<DT>, dim3((unsigned)b.rows), dim3(256), 0, st, b);
                 return;
             }
-            with_norm_shape(a.cols, [&](auto tpr, auto ch) {
-                constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
-                hipLaunchKernelGGL((norm_fwd_kernel<DT, TPR, CH>), grid, dim3(norm_block(TPR)), 0, st, b);
+            with_norm_fwd_shape(a.cols, [&](auto shape) {
+                using S = decltype(shape);
+                // as many workgroups as the chip holds: each keeps its columns' gain and offset for all of its rows
+                const int64_t most = (int64_t)num_cus() * (4 * 4 * kWaveSize / S::BLOCK);
+                hipLaunchKernelGGL((norm_fwd_kernel<DT, S::TPR, S::CH, S::BLOCK>), dim3((unsigned)std::min(ceil_div(b.rows, S::rows), most)), dim3(S::BLOCK),
+                                   0, st, b);
             });
         });
     }
@@ -187,8 +192,10 @@ void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
 int norm_bwd_blocks(int64_t rows, int64_t cols)
 {
     if (rows < 1 || cols < 1) return 0;
-    if (cols > kNormRegisterCols) return (int)std::min<int64_t>(ceil_div(rows, 32), 64);
-    return (int)std::min<int64_t>(ceil_div(rows, norm_rows_per_block(cols)), 512);
+    if (!norm_in_registers(cols)) return (int)std::min<int64_t>(ceil_div(rows, 32), 64);
+    int64_t n = 0;
+    with_norm_bwd_shape(cols, [&](auto shape) { n = std::min<int64_t>(ceil_div(rows, decltype(shape)::rows), num_cus() * (1024 / decltype(shape)::BLOCK)); });
+    return (int)n;
 }
 
 size_t norm_bwd_workspace(int64_t rows, int64_t cols) { return align_up((size_t)norm_bwd_blocks(rows, cols) * 2 * (size_t)cols * sizeof(float), 256); }
@@ -510,10 +517,10 @@ int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void
     const int blocks = norm_bwd_blocks(rows, cols);
     with_type(dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
-        if (cols <= kNormRegisterCols) {
-            with_norm_shape(cols, [&](auto tpr, auto ch) {
-                constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
-                hipLaunchKernelGGL((norm_bwd_kernel<DT, TPR, CH>), dim3((unsigned)blocks), dim3(norm_block(TPR)), 0, st, a);
+        if (norm_in_registers(cols)) {
+            with_norm_bwd_shape(cols, [&](auto shape) {
+                using S = decltype(shape);
+                hipLaunchKernelGGL((norm_bwd_kernel<DT, S::TPR, S::CH, S::BLOCK>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, st, a);
             });
             return;
         }

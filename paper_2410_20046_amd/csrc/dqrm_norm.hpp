@@ -21,7 +21,8 @@ struct NormArgs {
     uint8_t *codes, *scales; // MXFP4 of y (before its rounding to the element type), or null
 };
 
-// sum over the TPR threads of a row; every one of them gets it.  TPR > 64: over the waves of a workgroup by way of LDS.
+// sum over the TPR threads of a row; every one of them gets it.  TPR > 64: over the waves of a workgroup by way of s_part (a place
+// to each wave of the workgroup), which the next call must not take again before another barrier (two places in turn will do).
 template <int TPR, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float (*s_part)[N])
 {
@@ -31,9 +32,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*s_part)[N])
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d, kWaveSize);
     }
     if constexpr (TPR > kWaveSize) {
-        constexpr int waves = TPR / kWaveSize;
-        const int wave = threadIdx.x / kWaveSize;
-        __syncthreads(); // the sums of before are read
+        constexpr int waves = TPR / kWaveSize; // of a row
+        const int wave = threadIdx.x / kWaveSize, first = wave & ~(waves - 1);
         if ((threadIdx.x & (kWaveSize - 1)) == 0) {
 #pragma unroll
             for (int i = 0; i < N; ++i) s_part[wave][i] = v[i];
@@ -41,15 +41,16 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*s_part)[N])
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float t = s_part[0][i];
+            float t = s_part[first][i];
 #pragma unroll
-            for (int w = 1; w < waves; ++w) t += s_part[w][i];
+            for (int w = 1; w < waves; ++w) t += s_part[first + w][i];
             v[i] = t;
         }
     }
 }
 
-__device__ __forceinline__ void load_gain(const float *p, int64_t c, int64_t cols, float without, float (&v)[kChunk])
+template <typename I>
+__device__ __forceinline__ void load_gain(const float *p, I c, I cols, float without, float (&v)[kChunk])
 {
     if (p) {
         load_chunk(p, c, cols, false, v);
@@ -59,58 +60,105 @@ __device__ __forceinline__ void load_gain(const float *p, int64_t c, int64_t col
     }
 }
 
-constexpr int norm_block(int tpr) { return tpr > 256 ? tpr : 256; }
+// A row's chunk as it lies in memory, requested one row ahead of its use.  Where fewer than 8 values are left, it is the last 8 of
+// the row (cols >= 8): a load without a branch, which nothing has to wait for.
+template <typename T> struct Raw { unsigned w[kChunk * sizeof(T) / 4]; };
 
-// TPR threads to a row, CH chunks of 8 values to a thread: the row stays in registers (cols <= TPR * CH * 8).
-template <int DT, int TPR, int CH>
-__global__ __launch_bounds__(norm_block(TPR)) void norm_fwd_kernel(NormArgs a)
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T *row, int c, int cols)
 {
-    using T = elem_t<DT>;
-    constexpr int rows_per_block = norm_block(TPR) / TPR;
-    __shared__ float s_part[TPR > kWaveSize ? TPR / kWaveSize : 1][1];
-    const int t = threadIdx.x % TPR;
-    const int64_t r_own = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
-    const bool own = r_own < a.rows;
-    const int64_t r = own ? r_own : a.rows - 1; // (a group past the last row works on that row and writes nothing)
-    const T *row = static_cast<const T *>(a.x) + r * a.ldx;
-    float x[CH][kChunk];
-    float sum[1] = {0.0f};
+    Raw<T> t;
+    __builtin_memcpy(&t, row + min(c, cols - kChunk), sizeof(t));
+    return t;
+}
+
+// ... and its values c .. c + 7; those past the row's end are 0
+template <typename T>
+__device__ __forceinline__ void values_of(const Raw<T> &raw, int c, int cols, float (&v)[kChunk])
+{
+    Vec8<T> t;
+    __builtin_memcpy(&t, &raw, sizeof(t));
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-        load_chunk(row, (int64_t)(j * TPR + t) * kChunk, a.cols, r + 1 < a.rows, x[j]);
+    for (int i = 0; i < kChunk; ++i) v[i] = (float)t.v[i];
+    const int skip = c + kChunk - cols; // of the 8 belong to the chunk before
+    if (skip > 0) {
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) sum[0] += x[j][i];
-    }
-    row_sums<TPR>(sum, s_part);
-    const float mean = sum[0] / (float)a.cols;
-    float sq[1] = {0.0f};
+        for (int s = 1; s < 2 * kChunk; s *= 2) {
+            if (skip & s || (s == kChunk && skip > kChunk)) {
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-        const int64_t c = (int64_t)(j * TPR + t) * kChunk;
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) {
-            x[j][i] -= mean;
-            if (c + i < a.cols) sq[0] += x[j][i] * x[j][i];
+                for (int i = 0; i < kChunk; ++i) v[i] = i + s < kChunk ? v[i + s < kChunk ? i + s : 0] : 0.0f;
+            }
         }
     }
-    row_sums<TPR>(sq, s_part);
-    const float rstd = 1.0f / sqrtf(sq[0] / (float)a.cols + a.eps);
-    if (own && t == 0) {
-        if (a.mean) a.mean[r] = mean;
-        if (a.rstd) a.rstd[r] = rstd;
-    }
+}
+
+// TPR threads to a row, CH chunks of 8 values to a thread: the row stays in registers (8 <= cols <= TPR * CH * 8), and so do the
+// columns' gain and offset for all rows of a workgroup.
+template <int DT, int TPR, int CH, int BLOCK>
+__global__ __launch_bounds__(BLOCK, 4) void norm_fwd_kernel(NormArgs a)
+{
+    using T = elem_t<DT>;
+    constexpr int rows_per_block = BLOCK / TPR;
+    __shared__ float s_part[2][BLOCK / kWaveSize][1];
+    const int t = threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * rows_per_block;
+    const int cols = (int)a.cols;
+    const int64_t cp = codes_pitch(cols), sp = scales_pitch(cols);
+    // (a group past the last row works on that row and writes nothing)
+    auto row_of = [&](int64_t r) { return static_cast<const T *>(a.x) + min(r, a.rows - 1) * a.ldx; };
+    auto column = [&](int j) { return (j * TPR + t) * kChunk; };
+    int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
+    Raw<T> next[CH];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) next[j] = load_raw(row_of(r), column(j), cols);
+    float gamma[CH][kChunk], beta[CH][kChunk];
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
-        const int64_t c = (int64_t)(j * TPR + t) * kChunk;
-        float g[kChunk], b[kChunk];
-        load_gain(a.gamma, c, a.cols, 1.0f, g);
-        load_gain(a.beta, c, a.cols, 0.0f, b);
+        load_gain(a.gamma, column(j), cols, 1.0f, gamma[j]);
+        load_gain(a.beta, column(j), cols, 0.0f, beta[j]);
+    }
+    for (; r - threadIdx.x / TPR < a.rows; r += step) {
+        const bool own = r < a.rows;
+        float x[CH][kChunk];
+        float sum[1] = {0.0f};
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) x[j][i] = c + i < a.cols ? x[j][i] * rstd * g[i] + b[i] : 0.0f;
+        for (int j = 0; j < CH; ++j) {
+            values_of(next[j], column(j), cols, x[j]);
+            sum[0] += ((x[j][0] + x[j][1]) + (x[j][2] + x[j][3])) + ((x[j][4] + x[j][5]) + (x[j][6] + x[j][7]));
+        }
+        {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) next[j] = load_raw(row_of(r + step), column(j), cols);
+        }
+        row_sums<TPR>(sum, s_part[0]);
+        const float mean = sum[0] / (float)cols;
+        float sq[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) x[j][i] -= mean;
+            if (column(j) + kChunk > cols) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) x[j][i] = column(j) + i < cols ? x[j][i] : 0.0f;
+            }
+            sq[0] += ((x[j][0] * x[j][0] + x[j][1] * x[j][1]) + (x[j][2] * x[j][2] + x[j][3] * x[j][3])) +
+                     ((x[j][4] * x[j][4] + x[j][5] * x[j][5]) + (x[j][6] * x[j][6] + x[j][7] * x[j][7]));
+        }
+        row_sums<TPR>(sq, s_part[1]);
+        const float rstd = 1.0f / sqrtf(sq[0] / (float)cols + a.eps);
         if (!own) continue;
-        if (a.y && c < a.cols) store_chunk(static_cast<T *>(a.y) + r * a.ldy, c, a.cols, x[j]);
-        if (a.codes && c < groups_of(a.cols) * kRowPad)
-            write_chunk(a.codes + r * codes_pitch(a.cols), a.scales + r * scales_pitch(a.cols), (unsigned)(c / kChunk), x[j]);
+        if (t == 0) {
+            if (a.mean) a.mean[r] = mean;
+            if (a.rstd) a.rstd[r] = rstd;
+        }
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int c = column(j);
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) x[j][i] = x[j][i] * rstd * gamma[j][i] + beta[j][i]; // (past the row's end 0, as beta is)
+            if (a.y && c < cols) store_chunk(static_cast<T *>(a.y) + r * a.ldy, c, cols, x[j]);
+            if (a.codes && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), x[j]);
+        }
     }
 }
 
@@ -119,7 +167,7 @@ template <int DT>
 __global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
 {
     using T = elem_t<DT>;
-    __shared__ float s_part[4][1];
+    __shared__ float s_part[2][4][1];
     const int64_t r = blockIdx.x;
     const T *row = static_cast<const T *>(a.x) + r * a.ldx;
     const int64_t step = 256 * kChunk, end = groups_of(a.cols) * kRowPad;
@@ -129,7 +177,7 @@ __global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
         load_chunk(row, c, a.cols, false, x);
         sum[0] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
     }
-    row_sums<256>(sum, s_part);
+    row_sums<256>(sum, s_part[0]);
     const float mean = sum[0] / (float)a.cols;
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += step) {
         load_chunk(row, c, a.cols, false, x);
@@ -138,7 +186,7 @@ __global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
         for (int i = 0; i < kChunk; ++i) q += c + i < a.cols ? (x[i] - mean) * (x[i] - mean) : 0.0f;
         sq[0] += q;
     }
-    row_sums<256>(sq, s_part);
+    row_sums<256>(sq, s_part[1]);
     const float rstd = 1.0f / sqrtf(sq[0] / (float)a.cols + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[r] = mean;
@@ -166,51 +214,80 @@ struct NormBwdArgs {
     float *partial; // [blocks][2][cols]: the workgroups' sums for dgamma and dbeta, or null
 };
 
-// The row of dy and of x in registers; a thread has the same columns in every row of its workgroup's slice, and keeps their sums.
-template <int DT, int TPR, int CH>
-__global__ __launch_bounds__(norm_block(TPR)) void norm_bwd_kernel(NormBwdArgs a)
+// The row of dy and of x in registers, the next one on its way; a thread has the same columns in every row of its workgroup's
+// slice, and keeps their sums.
+template <int DT, int TPR, int CH, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 {
     using T = elem_t<DT>;
-    constexpr int rows_per_block = norm_block(TPR) / TPR;
-    __shared__ float s_part[TPR > kWaveSize ? TPR / kWaveSize : 1][2];
+    constexpr int rows_per_block = BLOCK / TPR;
+    constexpr bool ahead = TPR * CH < 2048; // (rows longer than that take all registers)
+    __shared__ float s_part[2][BLOCK / kWaveSize][2];
     const int t = threadIdx.x % TPR;
-    const float inv_n = 1.0f / (float)a.cols;
-    float dg[CH][kChunk] = {}, db[CH][kChunk] = {}, gamma[CH][kChunk];
+    const int cols = (int)a.cols;
+    const float inv_n = 1.0f / (float)cols;
+    const int64_t step = (int64_t)gridDim.x * rows_per_block;
+    auto column = [&](int j) { return (j * TPR + t) * kChunk; };
+    int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
+    Raw<T> next_dy[CH], next_x[CH];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    // (a group past the last row works on that row with a gradient of 0)
+    auto request = [&](int64_t at) {
+        const int64_t q = min(at, a.rows - 1);
+        next_mean = a.mean[q], next_rstd = a.rstd[q];
 #pragma unroll
-    for (int j = 0; j < CH; ++j) load_gain(a.gamma, (int64_t)(j * TPR + t) * kChunk, a.cols, 1.0f, gamma[j]);
-    for (int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR; r - threadIdx.x / TPR < a.rows; r += (int64_t)gridDim.x * rows_per_block) {
+        for (int j = 0; j < CH; ++j) {
+            next_dy[j] = load_raw(static_cast<const T *>(a.dy) + q * a.lddy, column(j), cols);
+            next_x[j] = load_raw(static_cast<const T *>(a.x) + q * a.ldx, column(j), cols);
+        }
+    };
+    if (ahead) request(r);
+    float dg[CH][kChunk] = {}, db[CH][kChunk] = {}, gamma[ahead ? CH : 1][kChunk];
+#pragma unroll
+    for (int j = 0; ahead && j < CH; ++j) load_gain(a.gamma, column(j), cols, 1.0f, gamma[j]);
+    int turn = 0;
+    for (; r - threadIdx.x / TPR < a.rows; r += step) {
         const bool own = r < a.rows;
+        if (!ahead) request(r);
+        const float mean = next_mean, rstd = next_rstd;
         float dy[CH][kChunk], xh[CH][kChunk];
         float s[2] = {0.0f, 0.0f};
-        float rstd = 0.0f;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            values_of(next_dy[j], column(j), cols, dy[j]);
+            values_of(next_x[j], column(j), cols, xh[j]);
+        }
+        if (ahead) request(r + step);
         if (own) {
-            const float mean = a.mean[r];
-            rstd = a.rstd[r];
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const int64_t c = (int64_t)(j * TPR + t) * kChunk;
-                load_chunk(static_cast<const T *>(a.dy) + r * a.lddy, c, a.cols, r + 1 < a.rows, dy[j]);
-                load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, r + 1 < a.rows, xh[j]);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) xh[j][i] = (xh[j][i] - mean) * rstd;
+                if (column(j) + kChunk > cols) {
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i) xh[j][i] = column(j) + i < cols ? xh[j][i] : 0.0f;
+                }
+                if (!ahead) load_gain(a.gamma, column(j), cols, 1.0f, gamma[0]);
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) {
-                    xh[j][i] = c + i < a.cols ? (xh[j][i] - mean) * rstd : 0.0f;
                     dg[j][i] += dy[j][i] * xh[j][i];
                     db[j][i] += dy[j][i];
-                    dy[j][i] *= gamma[j][i];
+                    dy[j][i] *= gamma[ahead ? j : 0][i];
                     s[0] += dy[j][i];
                     s[1] += dy[j][i] * xh[j][i];
                 }
             }
         }
         if (!a.dx) continue;
-        row_sums<TPR>(s, s_part);
+        row_sums<TPR>(s, s_part[turn]); // (two places in turn: no wave overwrites what another still reads)
+        turn ^= 1;
         if (own) {
+            const float c0 = s[0] * inv_n, c1 = s[1] * inv_n;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const int64_t c = (int64_t)(j * TPR + t) * kChunk;
 #pragma unroll
-                for (int i = 0; i < kChunk; ++i) dy[j][i] = rstd * (dy[j][i] - s[0] * inv_n - xh[j][i] * (s[1] * inv_n));
-                if (c < a.cols) store_chunk(static_cast<T *>(a.dx) + r * a.lddx, c, a.cols, dy[j]);
+                for (int i = 0; i < kChunk; ++i) dy[j][i] = rstd * (dy[j][i] - c0 - xh[j][i] * c1);
+                if (column(j) < cols) store_chunk(static_cast<T *>(a.dx) + r * a.lddx, column(j), cols, dy[j]);
             }
         }
     }
@@ -219,10 +296,10 @@ __global__ __launch_bounds__(norm_block(TPR)) void norm_bwd_kernel(NormBwdArgs a
     if constexpr (rows_per_block == 1) {
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            const int64_t c = (int64_t)(j * TPR + t) * kChunk;
-            if (c < a.cols) {
-                store_chunk(out, c, a.cols, dg[j]);
-                store_chunk(out + a.cols, c, a.cols, db[j]);
+            const int c = column(j);
+            if (c < cols) {
+                store_chunk(out, c, cols, dg[j]);
+                store_chunk(out + cols, c, cols, db[j]);
             }
         }
     } else {
@@ -236,7 +313,7 @@ __global__ __launch_bounds__(norm_block(TPR)) void norm_bwd_kernel(NormBwdArgs a
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) s_acc[threadIdx.x / TPR][t * kChunk + i] = k ? db[j][i] : dg[j][i];
                 __syncthreads();
-                for (int c = threadIdx.x; c < TPR * kChunk; c += norm_block(TPR)) {
+                for (int c = threadIdx.x; c < TPR * kChunk; c += BLOCK) {
                     float v = s_acc[0][c];
                     for (int w = 1; w < rows_per_block; ++w) v += s_acc[w][c];
                     const int64_t col = (int64_t)j * TPR * kChunk + c;
