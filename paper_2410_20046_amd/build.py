@@ -8,7 +8,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdqrm.so")
-_SHARED = ["dqrm_host.hpp", os.path.join(ROOT, "include", "dqrm.h")]
+_SHARED = ["dqrm_host.hpp", "dqrm_fastdiv.hpp", os.path.join(ROOT, "include", "dqrm.h")]
 # each translation unit and the headers it includes
 UNITS = {
     "dqrm_api.hip": ["dqrm_device.hpp", "dqrm_fwd.hpp", "dqrm_dedupe.hpp", "dqrm_bwd.hpp", "dqrm_update.hpp", "dqrm_merge.hpp",

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "dqrm.h"
+#include "dqrm_fastdiv.hpp"
 
 // one rounding per operation everywhere: results are compared bit for bit
 #pragma clang fp contract(off)
@@ -88,24 +89,6 @@ __device__ __forceinline__ unsigned pack_bytes(int q0, int q1, int q2, int q3)
 {
     return ((unsigned)q0 & 0xFFu) | (((unsigned)q1 & 0xFFu) << 8) | (((unsigned)q2 & 0xFFu) << 16) | ((unsigned)q3 << 24);
 }
-
-// unsigned division of numbers below 2^31 by a fixed divisor (host-side set-up)
-struct FastDiv {
-    unsigned magic, shift, d;
-    __host__ static FastDiv make(unsigned divisor)
-    {
-        FastDiv f;
-        unsigned l = 0;
-        while ((1u << l) < divisor) ++l;
-        // ceil(2^(31 + l) / d) < 2^32 for d >= 2; exact quotients for every dividend below 2^31
-        const unsigned long long p = 1ull << (31 + l);
-        f.magic = divisor > 1 ? (unsigned)((p + divisor - 1) / divisor) : 0u;
-        f.shift = l > 0 ? l - 1 : 0;
-        f.d = divisor;
-        return f;
-    }
-    __device__ __forceinline__ unsigned div(unsigned x) const { return d > 1 ? __umulhi(x, magic) >> shift : x; }
-};
 
 // sign-extend the low 4 bits of v
 __device__ __forceinline__ int nibble_code(unsigned v) { return (int)((v & 0xFu) ^ 8u) - 8; }

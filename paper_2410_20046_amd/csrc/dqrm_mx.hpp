@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include "dqrm.h"
+#include "dqrm_fastdiv.hpp"
 
 #pragma clang fp contract(off)
 
@@ -32,6 +33,22 @@ template <> struct Elem<DQRM_F16> { using T = _Float16; };
 template <int DT> using elem_t = typename Elem<DT>::T;
 
 template <typename T> struct Vec8 { T v[kChunk]; };
+
+// 16 bytes past the caches, at the elements' alignment
+template <typename T, typename V>
+__device__ __forceinline__ void store_stream(T *p, const V &v)
+{
+    static_assert(sizeof(V) == 16);
+    typedef unsigned u4 __attribute__((ext_vector_type(4)));
+    typedef u4 u4_by_2 __attribute__((aligned(2)));
+    typedef u4 u4_by_4 __attribute__((aligned(4)));
+    u4 w;
+    __builtin_memcpy(&w, &v, 16);
+    if constexpr (alignof(T) == 2)
+        __builtin_nontemporal_store(w, reinterpret_cast<u4_by_2 *>(p));
+    else
+        __builtin_nontemporal_store(w, reinterpret_cast<u4_by_4 *>(p));
+}
 
 template <typename T>
 __device__ __forceinline__ void load8(const T *p, float (&v)[kChunk])
@@ -66,6 +83,38 @@ __device__ __forceinline__ void load_chunk(const T *row, I c, I cols, bool insid
         for (int i = 0; i < kChunk; ++i) v[i] = c + i < cols ? v[i] : 0.0f;
     } else {
         load_first(row + c, (int)(cols - c), v);
+    }
+}
+
+// A row's chunk as it lies in memory, to be requested long before its use.  Where fewer than 8 values are left, it is the last 8
+// of the row (cols >= 8): a load without a branch, which nothing has to wait for.
+template <typename T> struct Raw { unsigned w[kChunk * sizeof(T) / 4]; };
+
+template <typename T, typename I>
+__device__ __forceinline__ Raw<T> load_raw(const T *row, I c, I cols)
+{
+    Raw<T> t;
+    __builtin_memcpy(&t, row + min(c, cols - (I)kChunk), sizeof(t));
+    return t;
+}
+
+// ... and its values c .. c + 7; those past the row's end are 0
+template <typename T, typename I>
+__device__ __forceinline__ void values_of(const Raw<T> &raw, I c, I cols, float (&v)[kChunk])
+{
+    Vec8<T> t;
+    __builtin_memcpy(&t, &raw, sizeof(t));
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) v[i] = (float)t.v[i];
+    const int skip = (int)min(c + (I)kChunk - cols, (I)(2 * kChunk)); // of the 8 belong to the chunk before
+    if (skip > 0) {
+#pragma unroll
+        for (int s = 1; s < 2 * kChunk; s *= 2) {
+            if (skip & s || (s == kChunk && skip > kChunk)) { // (8 and more: nothing of the row)
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) v[i] = i + s < kChunk ? v[i + s < kChunk ? i + s : 0] : 0.0f;
+            }
+        }
     }
 }
 
@@ -161,17 +210,12 @@ __device__ __forceinline__ void load_gated(const QuantArgs &a, int64_t r, int64_
     }
 }
 
-// One chunk to a lane, rows' chunks one after another.
+// One chunk to a lane, rows' chunks one after another; per_row: chunks of a row, of fewer than 2^31 in all.
 template <int DT>
-__global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a)
+__global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a, dqrm::FastDiv per_row)
 {
     using T = elem_t<DT>;
-    const unsigned per_row = (unsigned)groups_of(a.cols) * (kRowPad / kChunk);
-    const int64_t first = (int64_t)blockIdx.x * 256;
-    const int64_t r0 = first / per_row;
-    const unsigned at = (unsigned)(first - r0 * per_row) + threadIdx.x;
-    const unsigned down = at / per_row, chunk = at - down * per_row;
-    const int64_t r = r0 + down;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, r = per_row.div(at), chunk = at - r * per_row.d;
     if (r >= a.rows) return; // (whole blocks of 32 values: a row has a multiple of 16 chunks)
     float v[kChunk];
     load_gated<T>(a, r, (int64_t)chunk * kChunk, v);
@@ -185,10 +229,11 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a)
 constexpr int kTile = 128;
 
 template <int DT>
-__global__ __launch_bounds__(256) void quant_tile_kernel(QuantArgs a)
+__global__ __launch_bounds__(256, DT == DQRM_F32 ? 2 : 4) void quant_tile_kernel(QuantArgs a)
 {
     using T = elem_t<DT>;
     struct alignas(2 * sizeof(T)) Pair { T v[2]; };
+    constexpr int passes = kTile / 16;
     __shared__ __align__(16) T tile[kTile][kTile];
     __shared__ unsigned s_scale[kTile];
     __shared__ float s_sum[4][kTile];
@@ -196,22 +241,49 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(QuantArgs a)
     const int64_t r0 = (int64_t)row_tile * kTile, c0 = (int64_t)(blockIdx.x - row_tile * a.col_tiles) * kTile;
     const int tid = threadIdx.x;
     const int lane_chunk = tid & 15;
-    for (int i = 0; i < kTile / 16; ++i) {
-        const int dr = i * 16 + (tid >> 4);
-        const int64_t r = r0 + dr, c = c0 + lane_chunk * kChunk;
-        float v[kChunk];
-        if (r < a.rows) {
-            load_gated<T>(a, r, c, v);
-            if (a.codes)
-                write_chunk(a.codes + r * codes_pitch(a.cols), a.scales + r * scales_pitch(a.cols), (unsigned)(c / kChunk), v);
-        } else {
-#pragma unroll
-            for (int k = 0; k < kChunk; ++k) v[k] = 0.0f;
-        }
+    const int64_t c = c0 + lane_chunk * kChunk;
+    auto finish_chunk = [&](int dr, float (&v)[kChunk]) {
+        if (a.codes && r0 + dr < a.rows)
+            write_chunk(a.codes + (r0 + dr) * codes_pitch(a.cols), a.scales + (r0 + dr) * scales_pitch(a.cols), (unsigned)(c / kChunk), v);
         Vec8<T> t;
 #pragma unroll
         for (int k = 0; k < kChunk; ++k) t.v[k] = (T)v[k];
         __builtin_memcpy(__builtin_assume_aligned(&tile[dr][lane_chunk * kChunk], 16), &t, sizeof(t));
+    };
+    if (a.cols >= kChunk) {
+        // (rows past the last one repeat it and then count as zeros)
+        auto row = [&](const void *p, int64_t ld, int i) { return static_cast<const T *>(p) + min(r0 + i * 16 + (tid >> 4), a.rows - 1) * ld; };
+        Raw<T> x[passes], gate[passes];
+#pragma unroll
+        for (int i = 0; i < passes; ++i) x[i] = load_raw(row(a.x, a.ldx, i), c, a.cols);
+        if (a.gate) {
+#pragma unroll
+            for (int i = 0; i < passes; ++i) gate[i] = load_raw(row(a.gate, a.ldgate, i), c, a.cols);
+        }
+#pragma unroll
+        for (int i = 0; i < passes; ++i) {
+            const int dr = i * 16 + (tid >> 4);
+            float v[kChunk];
+            values_of<T>(x[i], c, a.cols, v);
+            if (a.gate) {
+                float g[kChunk];
+                values_of<T>(gate[i], c, a.cols, g);
+#pragma unroll
+                for (int k = 0; k < kChunk; ++k) v[k] = g[k] > 0.0f ? v[k] : 0.0f;
+            }
+            if (r0 + dr >= a.rows) {
+#pragma unroll
+                for (int k = 0; k < kChunk; ++k) v[k] = 0.0f;
+            }
+            finish_chunk(dr, v);
+        }
+    } else {
+        for (int i = 0; i < passes; ++i) {
+            const int dr = i * 16 + (tid >> 4);
+            float v[kChunk] = {};
+            if (r0 + dr < a.rows) load_gated<T>(a, r0 + dr, c, v);
+            finish_chunk(dr, v);
+        }
     }
     __syncthreads();
     const int lane = tid & 63, wave = tid >> 6;
@@ -228,7 +300,11 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(QuantArgs a)
     for (int j = 0; j < 2; ++j) {
         unsigned m = 0;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) m = max(m, abs_bits(v[j][k])), sum[j] += v[j][k];
+        for (int k = 0; k < 32; ++k) m = max(m, abs_bits(v[j][k]));
+        if (a.partial) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) sum[j] += v[j][k];
+        }
         scale[j] = scale_byte(m);
         unsigned w[4];
 #pragma unroll
@@ -245,7 +321,7 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(QuantArgs a)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int c = lane * 2 + j;
-        s_codes[c * 4 + wave] = codes[j];
+        s_codes[c * 4 + (wave ^ (lane & 3))] = codes[j]; // (columns apart in LDS's banks)
         reinterpret_cast<uint8_t *>(&s_scale[c])[wave] = (uint8_t)scale[j];
         s_sum[wave][c] = sum[j];
     }
@@ -255,7 +331,7 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(QuantArgs a)
         for (int i = 0; i < 2; ++i) {
             const int at = i * 256 + tid, c = at >> 2;
             if (c0 + c < a.cols)
-                *reinterpret_cast<uint4 *>(a.codes_t + (c0 + c) * codes_pitch(a.rows) + r0 / 2 + (at & 3) * 16) = s_codes[at];
+                *reinterpret_cast<uint4 *>(a.codes_t + (c0 + c) * codes_pitch(a.rows) + r0 / 2 + (at & 3) * 16) = s_codes[at ^ ((c >> 1) & 3)];
         }
         if (tid < kTile && c0 + tid < a.cols)
             *reinterpret_cast<unsigned *>(a.scales_t + (c0 + tid) * scales_pitch(a.rows) + r0 / 32) = s_scale[tid];
@@ -294,16 +370,13 @@ __device__ __forceinline__ void unpack_codes(unsigned w, float scale, float (&v)
     v[4] = c.x * scale, v[5] = c.y * scale, v[6] = d.x * scale, v[7] = d.y * scale;
 }
 
+// per_row: chunks of a row that hold values, of fewer than 2^31 in all
 template <int DT>
-__global__ __launch_bounds__(256) void dequant_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out, int64_t ldo)
+__global__ __launch_bounds__(256) void dequant_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out, int64_t ldo,
+                                                      dqrm::FastDiv per_row)
 {
     using T = elem_t<DT>;
-    const unsigned per_row = (unsigned)((cols + kChunk - 1) / kChunk);
-    const int64_t first = (int64_t)blockIdx.x * 256;
-    const int64_t r0 = first / per_row;
-    const unsigned at = (unsigned)(first - r0 * per_row) + threadIdx.x;
-    const unsigned down = at / per_row, chunk = at - down * per_row;
-    const int64_t r = r0 + down;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, r = per_row.div(at), chunk = at - r * per_row.d;
     if (r >= rows) return;
     const unsigned w = *reinterpret_cast<const unsigned *>(codes + r * codes_pitch(cols) + (size_t)chunk * 4);
     float v[kChunk];

@@ -123,7 +123,8 @@ void launch_quant_rows(int32_t dtype, QuantArgs a, hipStream_t st)
         if (a.gate) b.gate = static_cast<const char *>(a.gate) + r0 * a.ldgate * es;
         b.codes += r0 * codes_pitch(a.cols), b.scales += r0 * scales_pitch(a.cols);
         with_type(dtype, [&](auto t) {
-            hipLaunchKernelGGL(quant_rows_kernel<decltype(t)::value>, dim3((unsigned)ceil_div(b.rows * per_row, 256)), dim3(256), 0, st, b);
+            hipLaunchKernelGGL(quant_rows_kernel<decltype(t)::value>, dim3((unsigned)ceil_div(b.rows * per_row, 256)), dim3(256), 0, st, b,
+                               dqrm::FastDiv::make((unsigned)per_row));
         });
     }
 }
@@ -201,9 +202,11 @@ int norm_bwd_blocks(int64_t rows, int64_t cols)
 size_t norm_bwd_workspace(int64_t rows, int64_t cols) { return align_up((size_t)norm_bwd_blocks(rows, cols) * 2 * (size_t)cols * sizeof(float), 256); }
 
 // ---- products --------------------------------------------------------------------------------------------------------------
-using Tile256 = TileShape<4, 4, 2, 2>;
-using Tile128 = TileShape<2, 2, 2, 2>;
-using Tile64 = TileShape<1, 1, 2, 2>;
+constexpr int64_t kMinStages = 4; // of a slice of k
+
+using Tile256 = TileShape<4, 2, 2, 4, 2>;
+using Tile128 = TileShape<2, 1, 2, 4, 4>;
+using Tile64 = TileShape<1, 1, 2, 2, 2>;
 
 struct MatmulPlan {
     int tile;        // 256, 128 or 64; 0: few_kernel
@@ -217,13 +220,17 @@ bool is_few(int64_t m, int64_t n, int64_t k) { return m <= 64 && (n >= 512 || k 
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
     if (is_few(m, n, k)) return MatmulPlan{0, 1, 0};
-    const auto tiles = [&](int64_t t) { return ceil_div(m, t) * ceil_div(n, t); };
+    const int64_t cus = num_cus(), stages = std::max<int64_t>(1, ceil_div(groups_of(k), 2));
+    const auto tiles = [&](int64_t t) { return std::max<int64_t>(1, ceil_div(m, t) * ceil_div(n, t)); };
     MatmulPlan p{};
-    p.tile = tiles(256) >= num_cus() ? 256 : tiles(128) >= num_cus() / 2 || k >= 4096 ? 128 : 64;
-    const int64_t stages = std::max<int64_t>(1, ceil_div(groups_of(k), 2));
-    const int64_t want = std::max<int64_t>(1, num_cus() / std::max<int64_t>(1, tiles(p.tile)));
-    const int64_t most = std::max<int64_t>(1, stages / 4); // four stages to a slice at least
-    const int64_t slices = std::min(want, most);
+    // the largest tile of which there is one to (nearly) each CU; tiles of 128 also where k can be cut until there is
+    if (tiles(256) * 8 >= cus * 7)
+        p.tile = 256;
+    else if (tiles(128) * 4 >= cus * 3 || (tiles(64) < cus && tiles(128) * stages >= cus * kMinStages))
+        p.tile = 128;
+    else
+        p.tile = 64;
+    const int64_t slices = std::max<int64_t>(1, std::min(cus / tiles(p.tile), stages / kMinStages));
     p.stages_per_slice = (unsigned)ceil_div(stages, slices);
     p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
     return p;
@@ -287,7 +294,7 @@ int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t 
         MatmulArgs part = g;
         part.c = workspace;
         launch_tiles<float>(p, part, st);
-        const unsigned blocks = (unsigned)ceil_div(g.m * g.n, 1024);
+        const unsigned blocks = (unsigned)ceil_div(g.m * g.n, 256);
         with_type(dtype, [&](auto t) {
             hipLaunchKernelGGL(matmul_join_kernel<decltype(t)::value>, dim3(blocks), dim3(256), 0, st, static_cast<const float *>(workspace), g);
         });
@@ -380,7 +387,7 @@ int32_t dqrm_mxfp4_dequant(const dqrm_mxfp4_t *q, int32_t dtype, void *out, int6
         with_type(dtype, [&](auto t) {
             hipLaunchKernelGGL(dequant_kernel<decltype(t)::value>, dim3((unsigned)ceil_div(rows * per_row, 256)), dim3(256), 0, st,
                                q->codes + r0 * codes_pitch(q->cols), q->scales + r0 * scales_pitch(q->cols), rows, q->cols,
-                               static_cast<char *>(out) + r0 * ldo * size_of(dtype), ldo);
+                               static_cast<char *>(out) + r0 * ldo * size_of(dtype), ldo, dqrm::FastDiv::make((unsigned)per_row));
         });
     }
     DQRM_HIP_CHECK(hipGetLastError());

@@ -33,7 +33,7 @@ struct MatmulArgs {
     unsigned stages_per_slice;
 };
 
-constexpr unsigned kParts = 8;              // of the chip, each with a second-level cache
+constexpr unsigned kParts = 8;     // of the chip, each with a second-level cache
 constexpr unsigned kTileRows = 8;
 constexpr int kStage = 256;                // values of k that a stage holds of each row: 128 bytes of codes, 8 of scales
 constexpr int kStageCodes = kStage / 2, kStageScales = kStage / 32;
@@ -72,21 +72,28 @@ __device__ __forceinline__ void read_barrier() { asm volatile("s_waitcnt lgkmcnt
 // every wave's loads are in LDS but for its last N
 template <int N>
 __device__ __forceinline__ void loaded_barrier() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
+// both
+template <int N>
+__device__ __forceinline__ void loaded_and_read_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ unsigned lds_address(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
-// A tile of WM * TM * 32 rows of A by WN * TN * 32 of B: WM by WN waves, each TM by TN accumulators of 32 by 32.
-template <int TM_, int TN_, int WM_, int WN_>
+// A tile of WM * TM * 32 rows of A by WN * TN * 32 of B: WM by WN waves, each TM by TN accumulators of 32 by 32; memory for `ring`
+// stages of k in LDS.
+template <int TM_, int TN_, int WM_, int WN_, int RING_>
 struct TileShape {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, waves = WM * WN, BM = TM * WM * 32, BN = TN * WN * 32;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, ring = RING_, waves = WM * WN, BM = TM * WM * 32, BN = TN * WN * 32;
     static constexpr int rows = BM + BN;
+    static constexpr int per_simd = TM * TN > 8 ? 1 : 2; // waves that the accumulators leave room for
     static constexpr int code_bytes = rows * kStageCodes, stage_bytes = code_bytes + rows * kStageScales;
     // loads of a wave in a stage: vectors of A's and of B's codes, scales
     static constexpr int a_loads = BM / 8 / waves, b_loads = BN / 8 / waves, loads = a_loads + b_loads + (rows / 32 + waves - 1) / waves;
     // Order of a stage's instructions, in places behind each of a step's products: reads for the next step in the first half; in the
-    // last step but one, behind place `freed`, every wave has read the stage and the loads of the stage after the next go into its
+    // last step but one, behind place `freed`, every wave has read the stage and the loads of the stage `ring` later go into its
     // memory, spread evenly; in the last step, behind place `arrived`, the next stage is there.
     static constexpr int products = TM * TN, freed = products * 3 / 4 - (products > 1), arrived = products / 2 - (products > 1);
+    // A wave with few products in a step has no time to hide reads of LDS behind them: it reads a whole stage ahead.
+    static constexpr bool stage_ahead = products <= 4;
     static constexpr int load_places = 2 * products - freed;
     static constexpr int load_place(int q) { return q * load_places / loads; }
     static constexpr int read_place(int r) { return r * products / (TM + TN) / 2; }
@@ -94,7 +101,7 @@ struct TileShape {
     {
         int n = 0;
         for (int q = 0; q < loads; ++q) n += load_place(q) <= products - freed + arrived;
-        return n;
+        return n + (ring - 2) * loads; // (and those of the stages in between)
     }
 };
 
@@ -133,7 +140,7 @@ __device__ __forceinline__ void store_tile(const MatmulArgs &g, T *c, int64_t ld
             if (m >= g.m) continue;
             T *to = c + m * ldc + n;
             if (n + per <= g.n) {
-                __builtin_memcpy(to, &x, sizeof(x));
+                store_stream(to, x);
             } else {
 #pragma unroll
                 for (int e = 0; e < per; ++e)
@@ -145,10 +152,10 @@ __device__ __forceinline__ void store_tile(const MatmulArgs &g, T *c, int64_t ld
 }
 
 template <typename T, typename S>
-__global__ __launch_bounds__(S::waves *kWaveSize, 1) void matmul_kernel(MatmulArgs g)
+__global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kernel(MatmulArgs g)
 {
     constexpr int pitch_out = S::TN * 32 * sizeof(T) + 16;
-    constexpr int lds_bytes = 2 * S::stage_bytes > S::waves * 32 * pitch_out ? 2 * S::stage_bytes : S::waves * 32 * pitch_out;
+    constexpr int lds_bytes = S::ring * S::stage_bytes > S::waves * 32 * pitch_out ? S::ring * S::stage_bytes : S::waves * 32 * pitch_out;
     __shared__ __align__(1024) char lds[lds_bytes];
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = (int)uniform(threadIdx.x >> 6);
@@ -169,14 +176,16 @@ __global__ __launch_bounds__(S::waves *kWaveSize, 1) void matmul_kernel(MatmulAr
     // operand memory from the tile's first row on; what lies past the matrix reads as zeros
     const rsrc_t ra = buffer_of(g.a_codes + m0 * cp, (g.m - m0) * cp), rb = buffer_of(g.b_codes + n0 * cp, (g.n - n0) * cp);
     const rsrc_t rsa = buffer_of(g.a_scales + m0 * sp, (g.m - m0) * sp), rsb = buffer_of(g.b_scales + n0 * sp, (g.n - n0) * sp);
-    // codes in LDS: 8 vectors of 16 bytes to a row, vector v of row r in place v ^ (r & 7)
-    const unsigned code_at = (unsigned)(lane >> 3) * (unsigned)cp + (unsigned)(((lane & 7) ^ (lane >> 3)) * 16);
+    // Codes in LDS: 8 vectors of 16 bytes to a row, vector v of row r in place v ^ (r / 2 % 8): the 16 rows that are read together
+    // lie in different banks.  (A load has 8 rows from an 8-fold on, an odd one in odd waves.)
+    static_assert(S::waves % 2 == 0);
+    const unsigned code_at = (unsigned)(lane >> 3) * (unsigned)cp + (unsigned)(((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16);
     const unsigned scale_at = (unsigned)(lane >> 1) * (unsigned)sp + (unsigned)(lane & 1) * 4;
     const unsigned lds0 = uniform(lds_address(lds));
 
     // Load q of the S::loads that a wave has in stage s.  A stage past the last one is requested from a buffer without bytes.
     auto request = [&](int s, int q) {
-        const unsigned to = lds0 + (unsigned)((s - first) & 1) * S::stage_bytes;
+        const unsigned to = lds0 + (unsigned)((s - first) & (S::ring - 1)) * S::stage_bytes;
         auto here = [&](rsrc_t r) {
             r.z = uniform(s < last ? r.z : 0u);
             return r;
@@ -201,23 +210,31 @@ __global__ __launch_bounds__(S::waves *kWaveSize, 1) void matmul_kernel(MatmulAr
 
     const int wm = wave / S::WN, wn = wave % S::WN;
     const int row_a = wm * S::TM * 32 + (lane & 31), row_b = S::BM + wn * S::TN * 32 + (lane & 31);
-    uint4 a[2][S::TM], b[2][S::TN];
-    // operand r of a step: A's rows, then B's
-    auto read_codes = [&](int s, int t, int r) {
-        const char *now = lds + ((s - first) & 1) * S::stage_bytes;
-        const int at = ((2 * t + half) ^ (lane & 7)) * 16;
+    constexpr int steps = kStage / 64, reads = S::TM + S::TN;
+    constexpr int sets = S::stage_ahead ? 2 * steps : 2; // of operands in registers
+    uint4 a[sets][S::TM], b[sets][S::TN];
+    // operand r of step t, A's rows, then B's, into a set
+    auto read_codes = [&](int s, int t, int r, int set) {
+        const char *now = lds + ((s - first) & (S::ring - 1)) * S::stage_bytes;
+        const int at = ((2 * t + half) ^ ((lane >> 1) & 7)) * 16;
         if (r < S::TM)
-            a[t & 1][r] = *reinterpret_cast<const uint4 *>(now + (row_a + r * 32) * kStageCodes + at);
+            a[set][r] = *reinterpret_cast<const uint4 *>(now + (row_a + r * 32) * kStageCodes + at);
         else
-            b[t & 1][r - S::TM] = *reinterpret_cast<const uint4 *>(now + (row_b + (r - S::TM) * 32) * kStageCodes + at);
+            b[set][r - S::TM] = *reinterpret_cast<const uint4 *>(now + (row_b + (r - S::TM) * 32) * kStageCodes + at);
     };
-    uint2 sa[S::TM], sb[S::TN];
+    uint2 raw_scales[reads];
     auto read_scales = [&](int s, int r) {
-        const char *now = lds + ((s - first) & 1) * S::stage_bytes + S::code_bytes;
-        if (r < S::TM)
-            sa[r] = *reinterpret_cast<const uint2 *>(now + (row_a + r * 32) * kStageScales);
-        else
-            sb[r - S::TM] = *reinterpret_cast<const uint2 *>(now + (row_b + (r - S::TM) * 32) * kStageScales);
+        const char *now = lds + ((s - first) & (S::ring - 1)) * S::stage_bytes + S::code_bytes;
+        const int row = r < S::TM ? row_a + r * 32 : row_b + (r - S::TM) * 32;
+        raw_scales[r] = *reinterpret_cast<const uint2 *>(now + row * kStageScales);
+    };
+    // The lane's bytes: block 2 t + half of the stage.  Past the row's end (the second half of an odd last stage) scales of 0 on both
+    // sides give 0.
+    unsigned scales[reads][2];
+    auto take_scales = [&](int s) {
+        const bool odd_end = (int64_t)(s + 1) * 2 > groups;
+#pragma unroll
+        for (int r = 0; r < reads; ++r) scales[r][0] = raw_scales[r].x >> (8 * half), scales[r][1] = odd_end ? 0u : raw_scales[r].y >> (8 * half);
     };
     // the sums begin with the bias
     const bool finish = g.slices <= 1;
@@ -233,39 +250,34 @@ __global__ __launch_bounds__(S::waves *kWaveSize, 1) void matmul_kernel(MatmulAr
                 for (int t = 0; t < S::TM; ++t) acc[t][j][i] = v;
             }
     }
+    auto multiply = [&](int t, int p, int set) {
+        const int i = p / S::TN, j = p % S::TN;
+        if (t & 1)
+            acc[i][j] = mfma_32x32x64<2>(b[set][j], a[set][i], acc[i][j], scales[S::TM + j][t >> 1], scales[i][t >> 1]);
+        else
+            acc[i][j] = mfma_32x32x64<0>(b[set][j], a[set][i], acc[i][j], scales[S::TM + j][t >> 1], scales[i][t >> 1]);
+    };
+    // (sched_barrier: the compiler keeps this order; left to itself it gathers the reads where nothing hides them)
     auto compute = [&](int s, auto is_last) {
-        // the lane's bytes: block 2 t + half of the stage; past the row's end (the second half of an odd last stage) scales of 0 on
-        // both sides give 0
-        const bool odd_end = (int64_t)(s + 1) * 2 > groups;
-        unsigned ua[2][S::TM], ub[2][S::TN];
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i) ua[0][i] = sa[i].x >> (8 * half), ua[1][i] = odd_end ? 0u : sa[i].y >> (8 * half);
-#pragma unroll
-        for (int i = 0; i < S::TN; ++i) ub[0][i] = sb[i].x >> (8 * half), ub[1][i] = odd_end ? 0u : sb[i].y >> (8 * half);
-constexpr int steps = kStage / 64, reads = S::TM + S::TN;
         constexpr bool more = !decltype(is_last)::value;
+        take_scales(s);
 #pragma unroll
         for (int t = 0; t < steps; ++t) {
 #pragma unroll
             for (int p = 0; p < S::products; ++p) {
-                const int i = p / S::TN, j = p % S::TN;
-                if (t & 1)
-                    acc[i][j] = mfma_32x32x64<2>(b[t & 1][j], a[t & 1][i], acc[i][j], ub[t >> 1][j], ua[t >> 1][i]);
-                else
-                    acc[i][j] = mfma_32x32x64<0>(b[t & 1][j], a[t & 1][i], acc[i][j], ub[t >> 1][j], ua[t >> 1][i]);
-                // (the compiler keeps this order: left to itself it gathers the reads where nothing hides them)
+                multiply(t, p, t & 1);
                 __builtin_amdgcn_sched_barrier(0);
                 if (t + 1 < steps) {
 #pragma unroll
                     for (int r = 0; r < reads; ++r)
-                        if (S::read_place(r) == p) read_codes(s, t + 1, r);
+                        if (S::read_place(r) == p) read_codes(s, t + 1, r, (t + 1) & 1);
                 }
                 if constexpr (more) {
                     if (t == steps - 2 && p == S::freed) read_barrier();
                     const int place = t == steps - 2 ? p - S::freed : t == steps - 1 ? S::products - S::freed + p : -1;
 #pragma unroll
                     for (int q = 0; q < S::loads; ++q)
-                        if (S::load_place(q) == place) request(s + 2, q);
+                        if (S::load_place(q) == place) request(s + S::ring, q);
                     if (t == steps - 1 && p == S::arrived) {
                         loaded_barrier<S::loads_before_arrival()>();
 #pragma unroll
@@ -275,8 +287,39 @@ constexpr int steps = kStage / 64, reads = S::TM + S::TN;
                         constexpr int left = S::products - S::arrived;
 #pragma unroll
                         for (int r = 0; r < reads; ++r)
-                            if (r * left / reads == p - S::arrived) read_codes(s + 1, 0, r);
+                            if (r * left / reads == p - S::arrived) read_codes(s + 1, 0, r, 0);
                     }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    // stage_ahead: stage s from the sets of its parity, stage s + 1 into the others
+    auto compute_ahead = [&](int s, auto parity, auto is_last) {
+        constexpr int now = decltype(parity)::value * steps, next = steps - now;
+        constexpr bool more = !decltype(is_last)::value;
+        take_scales(s);
+        if constexpr (more) loaded_and_read_barrier<(S::ring - 2) * S::loads>(); // stage s is in registers everywhere, stage s + 1 in LDS
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < steps; ++t) {
+#pragma unroll
+            for (int p = 0; p < S::products; ++p) {
+                multiply(t, p, now + t);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (more) {
+                    constexpr int all = steps * S::products;
+                    const int place = t * S::products + p;
+                    if (place == 0) {
+#pragma unroll
+                        for (int r = 0; r < reads; ++r) read_scales(s + 1, r);
+                    }
+#pragma unroll
+                    for (int k = 0; k < steps * reads; ++k)
+                        if (k * all / (steps * reads) == place) read_codes(s + 1, k / reads, k % reads, next + k / reads);
+#pragma unroll
+                    for (int q = 0; q < S::loads; ++q)
+                        if (q * all / S::loads == place) request(s + S::ring, q);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -284,14 +327,33 @@ constexpr int steps = kStage / 64, reads = S::TM + S::TN;
     };
     if (first < last) {
 #pragma unroll
-        for (int q = 0; q < S::loads; ++q) request(first, q);
-        lds_barrier();
+        for (int k = 0; k < S::ring; ++k) {
 #pragma unroll
-        for (int q = 0; q < S::loads; ++q) request(first + 1, q);
+            for (int q = 0; q < S::loads; ++q) request(first + k, q);
+        }
+        loaded_barrier<(S::ring - 1) * S::loads>();
 #pragma unroll
-        for (int r = 0; r < S::TM + S::TN; ++r) read_scales(first, r), read_codes(first, 0, r);
-        for (int s = first; s + 1 < last; ++s) compute(s, std::false_type{});
-        compute(last - 1, std::true_type{});
+        for (int r = 0; r < reads; ++r) read_scales(first, r);
+#pragma unroll
+        for (int k = 0; k < (S::stage_ahead ? steps : 1) * reads; ++k) read_codes(first, k / reads, k % reads, k / reads);
+        const std::integral_constant<int, 0> even;
+        const std::integral_constant<int, 1> odd;
+        if constexpr (S::stage_ahead) {
+            int s = first;
+            for (; s + 2 < last; s += 2) {
+                compute_ahead(s, even, std::false_type{});
+                compute_ahead(s + 1, odd, std::false_type{});
+            }
+            if (s + 1 < last) {
+                compute_ahead(s, even, std::false_type{});
+                compute_ahead(s + 1, odd, std::true_type{});
+            } else {
+                compute_ahead(s, even, std::true_type{});
+            }
+        } else {
+            for (int s = first; s + 1 < last; ++s) compute(s, std::false_type{});
+            compute(last - 1, std::true_type{});
+        }
     }
     lds_barrier(); // the last stage is read
     T *c = static_cast<T *>(g.c) + (finish ? 0 : (int64_t)slice * g.m * g.n);
@@ -303,27 +365,22 @@ template <int DT>
 __global__ __launch_bounds__(256) void matmul_join_kernel(const float *partial, MatmulArgs g)
 {
     using T = elem_t<DT>;
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = g.m * g.n;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, all = g.m * g.n;
     if (at >= all) return;
-    const int count = (int)min((int64_t)4, all - at);
-    float v[4] = {};
-    for (unsigned s = 0; s < g.slices; ++s) {
-        const float *p = partial + (int64_t)s * all + at;
-        if (count == 4) {
-            float4 x;
-            __builtin_memcpy(&x, p, 16);
-            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-        } else {
-            for (int i = 0; i < count; ++i) v[i] += p[i];
-        }
+    const unsigned m = (unsigned)(at / g.n), n = (unsigned)(at - m * g.n);
+    float v = g.bias ? g.bias[n] : 0.0f;
+    constexpr int ahead = 8; // loads in flight
+    unsigned s = 0;
+    for (; s + ahead <= g.slices; s += ahead) {
+        float x[ahead];
+#pragma unroll
+        for (int i = 0; i < ahead; ++i) x[i] = partial[(int64_t)(s + i) * all + at];
+#pragma unroll
+        for (int i = 0; i < ahead; ++i) v += x[i];
     }
-    int64_t m = at / g.n, n = at - m * g.n;
-    for (int i = 0; i < count; ++i) {
-        float x = v[i] + (g.bias ? g.bias[n] : 0.0f);
-        if (g.relu) x = x < 0.0f ? 0.0f : x;
-        static_cast<T *>(g.c)[m * g.ldc + n] = (T)x;
-        if (++n == g.n) n = 0, ++m;
-    }
+    for (; s < g.slices; ++s) v += partial[(int64_t)s * all + at];
+    if (g.relu) v = v < 0.0f ? 0.0f : v; // (a NaN stays)
+    static_cast<T *>(g.c)[m * g.ldc + n] = (T)v;
 }
 
 } // namespace dqrm_mx

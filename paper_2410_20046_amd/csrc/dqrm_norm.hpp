@@ -60,38 +60,6 @@ __device__ __forceinline__ void load_gain(const float *p, I c, I cols, float wit
     }
 }
 
-// A row's chunk as it lies in memory, requested one row ahead of its use.  Where fewer than 8 values are left, it is the last 8 of
-// the row (cols >= 8): a load without a branch, which nothing has to wait for.
-template <typename T> struct Raw { unsigned w[kChunk * sizeof(T) / 4]; };
-
-template <typename T>
-__device__ __forceinline__ Raw<T> load_raw(const T *row, int c, int cols)
-{
-    Raw<T> t;
-    __builtin_memcpy(&t, row + min(c, cols - kChunk), sizeof(t));
-    return t;
-}
-
-// ... and its values c .. c + 7; those past the row's end are 0
-template <typename T>
-__device__ __forceinline__ void values_of(const Raw<T> &raw, int c, int cols, float (&v)[kChunk])
-{
-    Vec8<T> t;
-    __builtin_memcpy(&t, &raw, sizeof(t));
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i) v[i] = (float)t.v[i];
-    const int skip = c + kChunk - cols; // of the 8 belong to the chunk before
-    if (skip > 0) {
-#pragma unroll
-        for (int s = 1; s < 2 * kChunk; s *= 2) {
-            if (skip & s || (s == kChunk && skip > kChunk)) {
-#pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[i] = i + s < kChunk ? v[i + s < kChunk ? i + s : 0] : 0.0f;
-            }
-        }
-    }
-}
-
 // TPR threads to a row, CH chunks of 8 values to a thread: the row stays in registers (8 <= cols <= TPR * CH * 8), and so do the
 // columns' gain and offset for all rows of a workgroup.
 template <int DT, int TPR, int CH, int BLOCK>
