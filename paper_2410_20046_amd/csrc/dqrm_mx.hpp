@@ -118,14 +118,21 @@ __device__ __forceinline__ void values_of(const Raw<T> &raw, I c, I cols, float 
     }
 }
 
-template <typename T, typename I>
+// STREAM: past the caches (for outputs that are not read again soon)
+template <bool STREAM = false, typename T, typename I>
 __device__ __forceinline__ void store_chunk(T *row, I c, I cols, const float (&v)[kChunk])
 {
     if (c + kChunk <= cols) {
         Vec8<T> t;
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) t.v[i] = (T)v[i];
-        __builtin_memcpy(row + c, &t, sizeof(t));
+        if constexpr (STREAM) {
+            struct Half { T v[16 / sizeof(T)]; };
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(t) / 16; ++i) store_stream(row + c + i * (16 / sizeof(T)), reinterpret_cast<const Half *>(&t)[i]);
+        } else {
+            __builtin_memcpy(row + c, &t, sizeof(t));
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kChunk; ++i)
@@ -331,7 +338,7 @@ __global__ __launch_bounds__(256, DT == DQRM_F32 ? 2 : 4) void quant_tile_kernel
         for (int i = 0; i < 2; ++i) {
             const int at = i * 256 + tid, c = at >> 2;
             if (c0 + c < a.cols)
-                *reinterpret_cast<uint4 *>(a.codes_t + (c0 + c) * codes_pitch(a.rows) + r0 / 2 + (at & 3) * 16) = s_codes[at ^ ((c >> 1) & 3)];
+                store_stream(reinterpret_cast<unsigned *>(a.codes_t + (c0 + c) * codes_pitch(a.rows) + r0 / 2 + (at & 3) * 16), s_codes[at ^ ((c >> 1) & 3)]);
         }
         if (tid < kTile && c0 + tid < a.cols)
             *reinterpret_cast<unsigned *>(a.scales_t + (c0 + tid) * scales_pitch(a.rows) + r0 / 32) = s_scale[tid];
@@ -381,7 +388,7 @@ __global__ __launch_bounds__(256) void dequant_kernel(const uint8_t *codes, cons
     const unsigned w = *reinterpret_cast<const unsigned *>(codes + r * codes_pitch(cols) + (size_t)chunk * 4);
     float v[kChunk];
     unpack_codes(w, scale_value(scales[r * scales_pitch(cols) + (chunk >> 2)]), v);
-    store_chunk(static_cast<T *>(out) + r * ldo, (int64_t)chunk * kChunk, cols, v);
+    store_chunk<true>(static_cast<T *>(out) + r * ldo, (int64_t)chunk * kChunk, cols, v);
 }
 
 } // namespace dqrm_mx

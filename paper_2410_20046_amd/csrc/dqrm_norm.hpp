@@ -124,7 +124,7 @@ __global__ __launch_bounds__(BLOCK, 4) void norm_fwd_kernel(NormArgs a)
             const int c = column(j);
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) x[j][i] = x[j][i] * rstd * gamma[j][i] + beta[j][i]; // (past the row's end 0, as beta is)
-            if (a.y && c < cols) store_chunk(static_cast<T *>(a.y) + r * a.ldy, c, cols, x[j]);
+            if (a.y && c < cols) store_chunk<true>(static_cast<T *>(a.y) + r * a.ldy, c, cols, x[j]);
             if (a.codes && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), x[j]);
         }
     }
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
             for (int j = 0; j < CH; ++j) {
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) dy[j][i] = rstd * (dy[j][i] - c0 - xh[j][i] * c1);
-                if (column(j) < cols) store_chunk(static_cast<T *>(a.dx) + r * a.lddx, column(j), cols, dy[j]);
+                if (column(j) < cols) store_chunk<true>(static_cast<T *>(a.dx) + r * a.lddx, column(j), cols, dy[j]);
             }
         }
     }
