@@ -265,10 +265,21 @@ void launch_few(const FewArgs &a, hipStream_t st)
 {
     const int64_t strips = ceil_div(a.g.n, 16);
     const size_t lds = SRC == kFewCodes ? 0 : (size_t)(a.g.m * (codes_pitch(a.g.k) + scales_pitch(a.g.k)));
-    if (strips > num_cus())
-        hipLaunchKernelGGL((few_kernel<DT, SRC, MT, 2>), dim3((unsigned)ceil_div(strips, 2)), dim3(kFewBlock), lds, st, a);
+    const auto go = [&](auto st_, auto ring) {
+        constexpr int ST = decltype(st_)::value, RING = decltype(ring)::value;
+        hipLaunchKernelGGL((few_kernel<DT, SRC, MT, ST, RING>), dim3((unsigned)ceil_div(strips, ST)), dim3(kFewBlock), lds, st, a);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    // Two strips to a workgroup where there are many, so that A is read half as often (16 rows, 32768 x 2048: 15.1 -> 10.7 us; 64
+    // rows, 8192 x 8192: 21 -> 16 us), one strip where there are fewer (16 rows, 4096 x 4096: 5.0 -> 4.2 us).  A second unit in flight
+    // pays where a workgroup's LDS is small (16 rows, 8192 x 8192: 12.0 -> 11.6 us; 32 rows: 13.7 -> 15.7 us).
+    if (strips >= num_cus() * (MT > 2 ? 2 : 4))
+        go(two, one);
+    else if constexpr (MT == 1)
+        go(one, two);
     else
-        hipLaunchKernelGGL((few_kernel<DT, SRC, MT, 1>), dim3((unsigned)strips), dim3(kFewBlock), lds, st, a);
+        go(one, one);
 }
 
 int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t st)
@@ -305,11 +316,13 @@ int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t 
     return DQRM_OK;
 }
 
-// Whether the product quantises the activations itself, every workgroup all of them: as far as quantise_few's registers go.
+// Whether the product quantises the activations itself, every workgroup all of them: saves a launch where they are few (with a norm,
+// from a graph, against two launches: 1 x 367 for 512 outputs 5.3 and 5.8 us, 1 x 8192 for 8192 14.7 and 15.2, 2 x 4096 for 4096 8.4 and
+// 8.4; 4 x 4096 11.0 and 8.6).
 bool linear_in_one(int64_t m, int64_t n, int64_t k)
 {
-    const int64_t waves = m <= 1 ? 8 : m <= 2 ? 4 : m <= 4 ? 2 : 1;
-    return m <= 8 && k > 0 && k <= waves * kWaveSize * kFewChunks * kChunk && is_few(m, n, k);
+    const int64_t waves = m <= 1 ? 4 : m <= 2 ? 2 : 1;
+    return m <= kFewRows && m * k <= 8192 && k >= kChunk && k <= waves * kWaveSize * kFewChunks * kChunk && is_few(m, n, k);
 }
 
 struct LinearWs {

@@ -1,9 +1,10 @@
 // Products of MXFP4 matrices with few rows of A (requests), from codes or from activations as they are (gfx950, wave64).
 //
-// What such a product costs is W's bytes, read once.  A workgroup has ST strips of 16 rows of W; its eight waves cut k between
-// them and read W straight into the operand registers of v_mfma_scale_f32_16x16x128_f8f6f4 (lane l: row l % 16, block l / 16 of 128
-// values), no LDS on the way, the next batch of groups in flight while this one is multiplied.  The waves' sums meet in LDS in a fixed
-// order.
+// What such a product costs is W's bytes, read once.  A workgroup has ST strips of 16 rows of W; its four waves take every fourth
+// unit of 512 values of k.  A wave's loads go straight into LDS of its own, where no other wave looks (so it waits for its loads, but
+// for no barrier): a load has whole lines of 4 rows, while the operands of v_mfma_scale_f32_16x16x128_f8f6f4 (lane l: row l % 16,
+// block l / 16 of 128 values) would have halves of 16 rows' lines; what a load costs the address unit is its lines.  The waves' sums
+// meet in LDS in a fixed order.
 #pragma once
 
 #include "dqrm_mx_gemm.hpp"
@@ -13,8 +14,10 @@ namespace dqrm_mx {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int kFewWaves = 8, kFewBlock = kFewWaves * kWaveSize;
+constexpr int kFewWaves = 4, kFewBlock = kFewWaves * kWaveSize;
 constexpr int kFewChunks = 4; // chunks of 8 activations to a thread, where the product quantises them itself
+constexpr int kFewRows = 4;   // rows that it quantises itself, at most
+constexpr int kUnitGroups = 4, kUnitBytes = 16 * kUnitGroups * 64, kUnitTile = kUnitBytes + 16 * kUnitGroups * 4; // 16 rows' codes and scales
 
 __device__ __forceinline__ v4f mfma_16x16x128(uint4 a, uint4 b, v4f c, unsigned scale_a, unsigned scale_b)
 {
@@ -30,20 +33,38 @@ struct FewArgs {
     NormArgs x;   // activations, and the norm's gain and offset: for the others
 };
 
-// kFewPlain, kFewNorm: the m <= 8 rows of x to codes and scales in LDS, by 8 / m waves to a row, each thread's values in registers
-// (k <= waves of a row * 64 * 4 * 8).  Rows past the last one repeat it.
+// kFewPlain, kFewNorm: the rows of x (kFewRows at most) to codes and scales in LDS, by as many waves to a row as there are, each
+// thread's values in registers (k <= waves of a row * 64 * kFewChunks * 8).
 template <typename T, bool NORM>
 __device__ __forceinline__ void quantise_few(const NormArgs &a, uint8_t *codes, uint8_t *scales, float (*s_sum)[2])
 {
     const int rows = (int)a.rows;
-    const int log_waves = rows <= 1 ? 3 : rows <= 2 ? 2 : rows <= 4 ? 1 : 0; // of a row
+    const int log_waves = rows <= 1 ? 2 : rows <= 2 ? 1 : 0; // of a row
     const int wave = threadIdx.x / kWaveSize, waves = 1 << log_waves;
     const int own = wave >> log_waves, r = min(own, rows - 1);
     const int t = threadIdx.x & ((kWaveSize << log_waves) - 1), stride = kWaveSize << log_waves;
     const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+    const int cols = (int)a.cols, pitch = (int)codes_pitch(cols), spitch = (int)scales_pitch(cols);
+    auto column = [&](int j) { return (j * stride + t) * kChunk; };
+    auto used = [&](int j) { return j * stride * kChunk < cols; }; // by any thread
+    Raw<T> raw[kFewChunks];
+#pragma unroll
+    for (int j = 0; j < kFewChunks; ++j)
+        if (used(j)) raw[j] = load_raw(row, column(j), cols);
+    float gamma[NORM ? kFewChunks : 1][kChunk], beta[NORM ? kFewChunks : 1][kChunk];
+    if constexpr (NORM) {
+#pragma unroll
+        for (int j = 0; j < kFewChunks; ++j) {
+            if (!used(j)) continue;
+            // (the last 8 of a row that ends within the chunk are asked for, and moved like the row's own)
+            if (a.gamma) values_of<float>(load_raw(a.gamma, column(j), cols), column(j), cols, gamma[j]);
+            if (a.beta) values_of<float>(load_raw(a.beta, column(j), cols), column(j), cols, beta[j]);
+        }
+    }
     float x[kFewChunks][kChunk];
 #pragma unroll
-    for (int j = 0; j < kFewChunks; ++j) load_chunk(row, (int64_t)(j * stride + t) * kChunk, a.cols, r + 1 < rows, x[j]);
+    for (int j = 0; j < kFewChunks; ++j)
+        if (used(j)) values_of<T>(raw[j], column(j), cols, x[j]);
     if constexpr (NORM) {
         auto row_sum = [&](float v, int k) {
 #pragma unroll
@@ -57,56 +78,58 @@ __device__ __forceinline__ void quantise_few(const NormArgs &a, uint8_t *codes, 
         };
         float v = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kFewChunks; ++j)
+        for (int j = 0; j < kFewChunks; ++j) {
+            if (!used(j)) continue;
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) v += x[j][i];
-        const float mean = row_sum(v, 0) / (float)a.cols;
+        }
+        const float mean = row_sum(v, 0) / (float)cols;
         v = 0.0f;
 #pragma unroll
         for (int j = 0; j < kFewChunks; ++j) {
-            const int64_t c = (int64_t)(j * stride + t) * kChunk;
+            if (!used(j)) continue;
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) {
-                x[j][i] -= mean;
-                if (c + i < a.cols) v += x[j][i] * x[j][i];
+            for (int i = 0; i < kChunk; ++i) x[j][i] -= mean;
+            if (column(j) + kChunk > cols) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) x[j][i] = column(j) + i < cols ? x[j][i] : 0.0f;
             }
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) v += x[j][i] * x[j][i];
         }
-        const float rstd = 1.0f / sqrtf(row_sum(v, 1) / (float)a.cols + a.eps);
+        const float rstd = 1.0f / sqrtf(row_sum(v, 1) / (float)cols + a.eps);
 #pragma unroll
         for (int j = 0; j < kFewChunks; ++j) {
-            const int64_t c = (int64_t)(j * stride + t) * kChunk;
-            if (c >= a.cols) continue;
-            float g[kChunk], b[kChunk];
-            load_gain(a.gamma, c, a.cols, 1.0f, g);
-            load_gain(a.beta, c, a.cols, 0.0f, b);
+            if (!used(j)) continue;
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) x[j][i] = c + i < a.cols ? x[j][i] * rstd * g[i] + b[i] : 0.0f;
+            for (int i = 0; i < kChunk; ++i) x[j][i] = x[j][i] * rstd * (a.gamma ? gamma[j][i] : 1.0f) + (a.beta ? beta[j][i] : 0.0f);
         }
-        // (a chunk past the row's end: x - mean must not count)
-#pragma unroll
-        for (int j = 0; j < kFewChunks; ++j)
-            if ((int64_t)(j * stride + t) * kChunk >= a.cols) {
-#pragma unroll
-                for (int i = 0; i < kChunk; ++i) x[j][i] = 0.0f;
-            }
     }
-    const int64_t pitch = codes_pitch(a.cols), spitch = scales_pitch(a.cols), chunks = pitch / 4;
 #pragma unroll
     for (int j = 0; j < kFewChunks; ++j) {
         const int chunk = j * stride + t;
-        if (chunk < chunks && own < rows) write_chunk(codes + r * pitch, scales + r * spitch, (unsigned)chunk, x[j]);
+        // (the padding behind a row may begin in a chunk that no value is in)
+        if (j * stride < pitch / 4 && chunk < pitch / 4 && own < rows) {
+            if (!used(j)) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) x[j][i] = 0.0f;
+            }
+            write_chunk(codes + r * pitch, scales + r * spitch, (unsigned)chunk, x[j]);
+        }
     }
     __syncthreads();
 }
 
-// MT: groups of 16 rows of A.
-template <int DT, FewSource SRC, int MT, int ST>
+// MT: groups of 16 rows of A; RING: units of a wave that are in flight or in use.
+template <int DT, FewSource SRC, int MT, int ST, int RING>
 __global__ __launch_bounds__(kFewBlock) void few_kernel(FewArgs a)
 {
     using T = elem_t<DT>;
-    static_assert(SRC == kFewCodes || MT == 1, "quantise_few has up to 8 rows");
-    constexpr int batch = MT * ST > 4 ? 2 : 4; // groups of 128 values that are in flight together
-    __shared__ v4f s_acc[kFewWaves][ST][MT][kWaveSize];
+    static_assert(SRC == kFewCodes || MT == 1, "quantise_few has a few rows");
+    constexpr int tiles = ST + (SRC == kFewCodes ? MT : 0); // of 16 rows that a unit loads: W's, then A's
+    constexpr int loads = 5;                                // of a tile: four of codes, one of scales
+    constexpr int ring_bytes = kFewWaves * RING * tiles * kUnitTile, sum_bytes = kFewWaves * ST * MT * kWaveSize * (int)sizeof(v4f);
+    __shared__ __align__(1024) uint8_t s_ring[ring_bytes > sum_bytes ? ring_bytes : sum_bytes];
     __shared__ float s_sum[kFewWaves][2];
     extern __shared__ __align__(16) uint8_t s_x[]; // codes, then scales, of x
     const MatmulArgs &g = a.g;
@@ -114,75 +137,86 @@ __global__ __launch_bounds__(kFewBlock) void few_kernel(FewArgs a)
     const int row = lane & 15, block = lane >> 4;
     const int64_t groups = groups_of(g.k), cp = groups * 64, sp = groups * 4;
     const int64_t n0 = (int64_t)blockIdx.x * (ST * 16);
-    const int from = (int)(groups * wave / kFewWaves), to = (int)(groups * (wave + 1) / kFewWaves);
+    const int units = (int)((groups + kUnitGroups - 1) / kUnitGroups);
+    const int mine = (units - wave + kFewWaves - 1) / kFewWaves; // the wave's units: wave, wave + 4, ...
 
-    struct Batch {
-        uint4 w[ST][batch], x[MT][batch];
-        unsigned ws[ST][batch], xs[MT][batch];
-    };
-    const uint8_t *w_codes[ST], *w_scales[ST];
+    // memory from a tile's first row on; what lies past the matrix reads as zeros
+    rsrc_t codes[tiles], scales[tiles];
 #pragma unroll
-    for (int s = 0; s < ST; ++s) {
-        const int64_t n = min(n0 + s * 16 + row, g.n - 1);
-        w_codes[s] = g.b_codes + n * cp + block * 16, w_scales[s] = g.b_scales + n * sp + block;
+    for (int t = 0; t < tiles; ++t) {
+        const int64_t r0 = t < ST ? n0 + t * 16 : (int64_t)(t - ST) * 16;
+        const int64_t left = max((t < ST ? g.n : g.m) - r0, (int64_t)0);
+        codes[t] = buffer_of((t < ST ? g.b_codes : g.a_codes) + r0 * cp, min(left, (int64_t)16) * cp);
+        scales[t] = buffer_of((t < ST ? g.b_scales : g.a_scales) + r0 * sp, min(left, (int64_t)16) * sp);
     }
-    const uint8_t *x_codes[MT], *x_scales[MT];
+    // a row's 16 vectors of a unit, vector v of row r in place v ^ r; load j has rows 4 j .. 4 j + 3
+    unsigned code_at[4];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int64_t r = min((int64_t)(m * 16 + row), g.m - 1);
-        const uint8_t *codes = SRC == kFewCodes ? g.a_codes : s_x, *scales = SRC == kFewCodes ? g.a_scales : s_x + g.m * cp;
-        x_codes[m] = codes + r * cp + block * 16, x_scales[m] = scales + r * sp + block;
-    }
-    // (groups past the wave's last one repeat it: loaded, not multiplied)
-    auto load_w = [&](int k, Batch &b) {
+    for (int j = 0; j < 4; ++j) code_at[j] = (unsigned)(j * 4 + block) * (unsigned)cp + (unsigned)((row ^ (j * 4 + block)) * 16);
+    const unsigned scale_at = (unsigned)(lane >> 2) * (unsigned)sp + (unsigned)(lane & 3) * 4;
+    const unsigned lds0 = uniform(lds_address(s_ring)) + (unsigned)wave * (RING * tiles * kUnitTile);
+    // unit i of the wave; one past its last is requested from a buffer without bytes, so that every unit is as many loads
+    auto request = [&](int i) {
+        const unsigned unit = (unsigned)(wave + i * kFewWaves), to = lds0 + (unsigned)(i % RING) * (tiles * kUnitTile);
+        auto here = [&](rsrc_t r) {
+            r.z = uniform(i < mine ? r.z : 0u);
+            return r;
+        };
 #pragma unroll
-        for (int i = 0; i < batch; ++i) {
-            const int at = min(k + i, to - 1);
+        for (int t = 0; t < tiles; ++t) {
 #pragma unroll
-            for (int s = 0; s < ST; ++s) {
-                typedef unsigned u4 __attribute__((ext_vector_type(4)));
-                const u4 v = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(w_codes[s] + (int64_t)at * 64));
-                b.w[s][i] = make_uint4(v.x, v.y, v.z, v.w);
-                b.ws[s][i] = w_scales[s][(int64_t)at * 4];
-            }
+            for (int j = 0; j < 4; ++j) load16_to_lds(here(codes[t]), code_at[j], unit * (kUnitGroups * 64), to + t * kUnitTile + j * 1024);
+            load4_to_lds(here(scales[t]), scale_at, unit * (kUnitGroups * 4), to + t * kUnitTile + kUnitBytes);
         }
     };
-    auto load_x = [&](int k, Batch &b) {
+    auto tile_of = [&](int i, int t) { return s_ring + (wave * RING + i % RING) * (tiles * kUnitTile) + t * kUnitTile; };
 #pragma unroll
-        for (int i = 0; i < batch; ++i) {
-            const int at = min(k + i, to - 1);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                b.x[m][i] = *reinterpret_cast<const uint4 *>(x_codes[m] + (int64_t)at * 64);
-                b.xs[m][i] = x_scales[m][(int64_t)at * 4];
-            }
-        }
-    };
-    v4f acc[ST][MT] = {};
-    auto multiply = [&](int k, const Batch &b) {
-#pragma unroll
-        for (int i = 0; i < batch; ++i)
-            if (k + i < to) {
-#pragma unroll
-                for (int s = 0; s < ST; ++s)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[s][m] = mfma_16x16x128(b.w[s][i], b.x[m][i], acc[s][m], b.ws[s][i], b.xs[m][i]);
-            }
-    };
-    Batch now, next;
-    if (from < to) load_w(from, now);
+    for (int i = 0; i < RING; ++i) request(i);
     if constexpr (SRC != kFewCodes) quantise_few<T, SRC == kFewNorm>(a.x, s_x, s_x + g.m * cp, s_sum);
-    if (from < to) {
-        load_x(from, now);
-        for (int k = from; k < to; k += batch) {
-            if (k + batch < to) {
-                load_w(k + batch, next);
-                load_x(k + batch, next);
+
+    v4f acc[ST][MT] = {};
+    for (int i = 0; i < mine; ++i) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * tiles * loads) : "memory"); // unit i is in LDS
+        const int first = (wave + i * kFewWaves) * kUnitGroups;
+        uint4 w[ST][kUnitGroups], x[MT][kUnitGroups];
+        uint4 ws[ST], xs[MT];
+#pragma unroll
+        for (int t = 0; t < ST + MT; ++t) {
+            if (t < ST || SRC == kFewCodes) {
+                const uint8_t *tile = tile_of(i, t);
+                const uint4 s = *reinterpret_cast<const uint4 *>(tile + kUnitBytes + row * 16);
+                (t < ST ? ws[t < ST ? t : 0] : xs[t < ST ? 0 : t - ST]) = s;
+#pragma unroll
+                for (int k = 0; k < kUnitGroups; ++k) {
+                    const uint4 c = *reinterpret_cast<const uint4 *>(tile + row * 256 + (((k * 4 + block) ^ row) * 16));
+                    (t < ST ? w[t < ST ? t : 0][k] : x[t < ST ? 0 : t - ST][k]) = c;
+                }
+            } else {
+                const int64_t r = min((int64_t)row, g.m - 1);
+                unsigned d[kUnitGroups];
+#pragma unroll
+                for (int k = 0; k < kUnitGroups; ++k) {
+                    const int64_t at = min((int64_t)(first + k), groups - 1); // (a group past the last one is not multiplied)
+                    x[0][k] = *reinterpret_cast<const uint4 *>(s_x + r * cp + at * 64 + block * 16);
+                    d[k] = *reinterpret_cast<const unsigned *>(s_x + g.m * cp + r * sp + at * 4);
+                }
+                xs[0] = make_uint4(d[0], d[1], d[2], d[3]);
             }
-            multiply(k, now);
-            now = next;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // the unit is in registers: its memory may be loaded into
+        request(i + RING);
+#pragma unroll
+        for (int k = 0; k < kUnitGroups; ++k) {
+            if (first + k >= groups) break;
+            auto byte = [&](const uint4 &v) { return (k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w) >> (8 * block); };
+#pragma unroll
+            for (int s = 0; s < ST; ++s)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[s][m] = mfma_16x16x128(w[s][k], x[m][k], acc[s][m], byte(ws[s]), byte(xs[m]));
         }
     }
+    lds_barrier(); // no load is on its way any more
+    v4f(*s_acc)[ST][MT][kWaveSize] = reinterpret_cast<v4f(*)[ST][MT][kWaveSize]>(s_ring);
 #pragma unroll
     for (int s = 0; s < ST; ++s)
 #pragma unroll
