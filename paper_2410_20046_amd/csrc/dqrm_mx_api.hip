@@ -231,7 +231,7 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
     else
         p.tile = 64;
     const int64_t slices = std::max<int64_t>(1, std::min(cus / tiles(p.tile), stages / kMinStages));
-    p.stages_per_slice = (unsigned)ceil_div(stages, slices);
+    p.stages_per_slice = (unsigned)ceil_div(ceil_div(stages, slices), 2) * 2; // (a slice begins with a pair of stages' scales)
     p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
     return p;
 }

@@ -35,8 +35,11 @@ struct MatmulArgs {
 
 constexpr unsigned kParts = 8;     // of the chip, each with a second-level cache
 constexpr unsigned kTileRows = 8;
-constexpr int kStage = 256;                // values of k that a stage holds of each row: 128 bytes of codes, 8 of scales
-constexpr int kStageCodes = kStage / 2, kStageScales = kStage / 32;
+constexpr int kStage = 256; // values of k that a stage holds of each row: 128 bytes of codes
+constexpr int kStageCodes = kStage / 2;
+// Scales come for two stages at a time, 16 bytes of a row: what a load costs is its lines, and a row's scales of one stage are 8 bytes
+// of a line.  A's of a pair of stages are requested with the stage before the pair, B's with the pair's first one.
+constexpr int kPairScales = 2 * kStage / 32;
 
 // ---- loads from memory straight into LDS -------------------------------------------------------------------------------
 // The instructions are written out because the compiler, which cannot tell the stages' halves of LDS apart, would wait for every
@@ -85,9 +88,11 @@ struct TileShape {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, ring = RING_, waves = WM * WN, BM = TM * WM * 32, BN = TN * WN * 32;
     static constexpr int rows = BM + BN;
     static constexpr int per_simd = TM * TN > 8 ? 1 : 2; // waves that the accumulators leave room for
-    static constexpr int code_bytes = rows * kStageCodes, stage_bytes = code_bytes + rows * kStageScales;
+    static_assert(BM == BN, "A's and B's scales are as many loads");
+    static constexpr int pairs = ring / 2 + 2; // of stages whose scales are in LDS: from the one in use to the one that is loaded
+    static constexpr int stage_bytes = rows * kStageCodes, pair_bytes = rows * kPairScales, lds_bytes = ring * stage_bytes + pairs * pair_bytes;
     // loads of a wave in a stage: vectors of A's and of B's codes, scales
-    static constexpr int a_loads = BM / 8 / waves, b_loads = BN / 8 / waves, loads = a_loads + b_loads + (rows / 32 + waves - 1) / waves;
+    static constexpr int a_loads = BM / 8 / waves, b_loads = BN / 8 / waves, scale_loads = BM / 16 / waves, loads = a_loads + b_loads + scale_loads;
     // Order of a stage's instructions, in places behind each of a step's products: reads for the next step in the first half; in the
     // last step but one, behind place `freed`, every wave has read the stage and the loads of the stage `ring` later go into its
     // memory, spread evenly; in the last step, behind place `arrived`, the next stage is there.
@@ -155,7 +160,7 @@ template <typename T, typename S>
 __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kernel(MatmulArgs g)
 {
     constexpr int pitch_out = S::TN * 32 * sizeof(T) + 16;
-    constexpr int lds_bytes = S::ring * S::stage_bytes > S::waves * 32 * pitch_out ? S::ring * S::stage_bytes : S::waves * 32 * pitch_out;
+    constexpr int lds_bytes = S::lds_bytes > S::waves * 32 * pitch_out ? S::lds_bytes : S::waves * 32 * pitch_out;
     __shared__ __align__(1024) char lds[lds_bytes];
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = (int)uniform(threadIdx.x >> 6);
@@ -180,31 +185,30 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
     // lie in different banks.  (A load has 8 rows from an 8-fold on, an odd one in odd waves.)
     static_assert(S::waves % 2 == 0);
     const unsigned code_at = (unsigned)(lane >> 3) * (unsigned)cp + (unsigned)(((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16);
-    const unsigned scale_at = (unsigned)(lane >> 1) * (unsigned)sp + (unsigned)(lane & 1) * 4;
+    const unsigned scale_at = (unsigned)(lane >> 2) * (unsigned)sp + (unsigned)(lane & 3) * 4;
     const unsigned lds0 = uniform(lds_address(lds));
 
-    // Load q of the S::loads that a wave has in stage s.  A stage past the last one is requested from a buffer without bytes.
+    // what is past `last` is requested from a buffer without bytes, so that every stage is as many loads
+    auto until_last = [&](rsrc_t r, int s) {
+        r.z = uniform(s < last ? r.z : 0u);
+        return r;
+    };
+    const unsigned lds_scales = lds0 + S::ring * S::stage_bytes;
+    // load k of the S::scale_loads that a wave has of A's or B's scales of a pair of stages
+    auto request_scales = [&](int pair, bool of_a, int k) {
+        const unsigned j = (unsigned)(k * S::waves + wave);
+        load4_to_lds(until_last(of_a ? rsa : rsb, 2 * pair), scale_at, (unsigned)pair * kPairScales + j * 16 * (unsigned)sp,
+                     lds_scales + (unsigned)(pair % S::pairs) * S::pair_bytes + (of_a ? 0 : S::BM * kPairScales) + j * 256);
+    };
+    // load q of the S::loads that a wave has with stage s
     auto request = [&](int s, int q) {
-        const unsigned to = lds0 + (unsigned)((s - first) & (S::ring - 1)) * S::stage_bytes;
-        auto here = [&](rsrc_t r) {
-            r.z = uniform(s < last ? r.z : 0u);
-            return r;
-        };
         if (q < S::a_loads + S::b_loads) {
             const bool of_a = q < S::a_loads;
             const unsigned j = (unsigned)((of_a ? q : q - S::a_loads) * S::waves + wave);
-            load16_to_lds(here(of_a ? ra : rb), code_at, (unsigned)s * kStageCodes + j * 8 * (unsigned)cp, to + (of_a ? 0 : S::BM * kStageCodes) + j * 1024);
-        } else if constexpr (S::BM / 32 % S::waves == 0) {
-            constexpr int each = S::BM / 32 / S::waves;
-            const int k = q - S::a_loads - S::b_loads;
-            const bool of_a = k < each;
-            const unsigned j = (unsigned)((of_a ? k : k - each) * S::waves + wave);
-            load4_to_lds(here(of_a ? rsa : rsb), scale_at, (unsigned)s * kStageScales + j * 32 * (unsigned)sp, to + S::code_bytes + (of_a ? 0 : S::BM * kStageScales) + j * 256);
+            load16_to_lds(until_last(of_a ? ra : rb, s), code_at, (unsigned)s * kStageCodes + j * 8 * (unsigned)cp,
+                          lds0 + (unsigned)((s - first) & (S::ring - 1)) * S::stage_bytes + (of_a ? 0 : S::BM * kStageCodes) + j * 1024);
         } else {
-            static_assert(S::BM / 32 % S::waves == 0 || S::rows / 32 == S::waves, "one load of scales to a wave");
-            const bool of_a = wave < S::BM / 32;
-            const unsigned j = (unsigned)(of_a ? wave : wave - S::BM / 32);
-            load4_to_lds(here(of_a ? rsa : rsb), scale_at, (unsigned)s * kStageScales + j * 32 * (unsigned)sp, to + S::code_bytes + wave * 256);
+            request_scales((s + 1) >> 1, s & 1, q - S::a_loads - S::b_loads);
         }
     };
 
@@ -224,9 +228,9 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
     };
     uint2 raw_scales[reads];
     auto read_scales = [&](int s, int r) {
-        const char *now = lds + ((s - first) & (S::ring - 1)) * S::stage_bytes + S::code_bytes;
+        const char *now = lds + S::ring * S::stage_bytes + (s >> 1) % S::pairs * S::pair_bytes + (s & 1) * (kPairScales / 2);
         const int row = r < S::TM ? row_a + r * 32 : row_b + (r - S::TM) * 32;
-        raw_scales[r] = *reinterpret_cast<const uint2 *>(now + row * kStageScales);
+        raw_scales[r] = *reinterpret_cast<const uint2 *>(now + row * kPairScales);
     };
     // The lane's bytes: block 2 t + half of the stage.  Past the row's end (the second half of an odd last stage) scales of 0 on both
     // sides give 0.
@@ -325,7 +329,9 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
             }
         }
     };
-    if (first < last) {
+    if (first < last) { // (first is even)
+#pragma unroll
+        for (int k = 0; k < S::scale_loads; ++k) request_scales(first >> 1, true, k);
 #pragma unroll
         for (int k = 0; k < S::ring; ++k) {
 #pragma unroll
