@@ -34,7 +34,7 @@ struct MatmulArgs {
 };
 
 constexpr unsigned kParts = 8;     // of the chip, each with a second-level cache
-constexpr unsigned kTileRows = 8;
+constexpr unsigned kTileRows = 4;
 constexpr int kStage = 256; // values of k that a stage holds of each row: 128 bytes of codes
 constexpr int kStageCodes = kStage / 2;
 // Scales come for two stages at a time, 16 bytes of a row: what a load costs is its lines, and a row's scales of one stage are 8 bytes
@@ -93,79 +93,100 @@ struct TileShape {
     static constexpr int stage_bytes = rows * kStageCodes, pair_bytes = rows * kPairScales, lds_bytes = ring * stage_bytes + pairs * pair_bytes;
     // loads of a wave in a stage: vectors of A's and of B's codes, scales
     static constexpr int a_loads = BM / 8 / waves, b_loads = BN / 8 / waves, scale_loads = BM / 16 / waves, loads = a_loads + b_loads + scale_loads;
-    // Order of a stage's instructions, in places behind each of a step's products: reads for the next step in the first half; in the
-    // last step but one, behind place `freed`, every wave has read the stage and the loads of the stage `ring` later go into its
-    // memory, spread evenly; in the last step, behind place `arrived`, the next stage is there.
-    static constexpr int products = TM * TN, freed = products * 3 / 4 - (products > 1), arrived = products / 2 - (products > 1);
+    // Order of a stage's instructions, in places behind each of a step's products.  Reads of LDS: the operands of steps 1 and 2 in step
+    // 0, those of step 3 in the first half of step 1, so that a stage's memory is free early; behind place `freed` of step 1 every wave
+    // has read the stage, and the loads of the stage `ring` later go into its memory, spread evenly over the rest.  In the last step,
+    // behind place `arrived`, the next stage is there, and the operands of its step 0 are read.
+    static constexpr int steps = kStage / 64, products = TM * TN, free_step = 1, freed = products * 3 / 4 - (products > 1), arrived = products / 4 - (products > 3);
     // A wave with few products in a step has no time to hide reads of LDS behind them: it reads a whole stage ahead.
     static constexpr bool stage_ahead = products <= 4;
-    static constexpr int load_places = 2 * products - freed;
+    static constexpr int load_places = (steps - free_step) * products - freed;
     static constexpr int load_place(int q) { return q * load_places / loads; }
-    static constexpr int read_place(int r) { return r * products / (TM + TN) / 2; }
     static constexpr int loads_before_arrival()
     {
         int n = 0;
-        for (int q = 0; q < loads; ++q) n += load_place(q) <= products - freed + arrived;
+        for (int q = 0; q < loads; ++q) n += load_place(q) <= (steps - 1 - free_step) * products - freed + arrived;
         return n + (ring - 2) * loads; // (and those of the stages in between)
     }
+    static constexpr int read_place(int r) { return r * products / (TM + TN) / 2; } // in half a step
 };
 
 // Rows m by columns n of a wave's accumulators through LDS to memory: the lane has four neighbouring columns of one row in
 // four registers, and stores 16 bytes of a row beside its neighbours'.
 template <typename T, typename S>
-__device__ __forceinline__ void store_tile(const MatmulArgs &g, T *c, int64_t ldc, const v16f (&acc)[S::TM][S::TN], char *lds, int64_t m0, int64_t n0, bool finish)
-{
-    constexpr int per = 16 / sizeof(T);             // values of a vector
-    constexpr int cols = S::TN * 32, pitch = cols * sizeof(T) + 16;
-    const int lane = threadIdx.x & 63, half = lane >> 5;
+struct StoreTile {
+    static constexpr int per = 16 / sizeof(T);                       // values of a vector
+    static constexpr int cols = S::TN * 32, pitch = cols * sizeof(T) + 16;
+    static constexpr int vectors = cols / per, rows_each = kWaveSize / vectors; // of a row; rows that a wave stores at a time
+    static constexpr int block_bytes = 32 * pitch;                   // 32 rows of a wave's accumulators
+    static constexpr int fit = S::lds_bytes / (S::waves * block_bytes);
+    static constexpr int together = fit >= S::TM ? S::TM : fit > 0 ? fit : 1; // such blocks that are in LDS together
+    static constexpr int wave_bytes = together * block_bytes;
+    static_assert(S::TM % together == 0);
+
+    static __device__ __forceinline__ void run(const MatmulArgs &g, T *c, int64_t ldc, v16f (&acc)[S::TM][S::TN], char *lds, int64_t m0, int64_t n0, bool relu)
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        if (relu) {
 #pragma unroll
-    for (int t = 0; t < S::TM; ++t) {
-        struct alignas(4 * sizeof(T)) Four { T v[4]; };
+            for (int t = 0; t < S::TM; ++t)
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j)
+                for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                Four f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v = acc[t][j][q * 4 + i];
-                    if (finish && g.relu) v = v < 0.0f ? 0.0f : v; // (a NaN stays)
-                    f.v[i] = (T)v;
-                }
-                *reinterpret_cast<Four *>(lds + (lane & 31) * pitch + (j * 32 + q * 8 + half * 4) * sizeof(T)) = f;
-            }
-        __builtin_amdgcn_wave_barrier();
-        constexpr int vectors = cols / per; // of a row
-#pragma unroll
-        for (int i = 0; i < 32 * vectors / kWaveSize; ++i) {
-            const int at = i * kWaveSize + lane, r = at / vectors, v = at % vectors;
-            struct alignas(16) Many { T v[per]; };
-            const Many x = *reinterpret_cast<const Many *>(lds + r * pitch + v * 16);
-            const int64_t m = m0 + t * 32 + r, n = n0 + v * per;
-            if (m >= g.m) continue;
-            T *to = c + m * ldc + n;
-            if (n + per <= g.n) {
-                store_stream(to, x);
-            } else {
-#pragma unroll
-                for (int e = 0; e < per; ++e)
-                    if (n + e < g.n) to[e] = x.v[e];
-            }
+                    for (int i = 0; i < 16; ++i) acc[t][j][i] = acc[t][j][i] < 0.0f ? 0.0f : acc[t][j][i]; // (a NaN stays)
         }
-        __builtin_amdgcn_wave_barrier();
+        char *write = lds + (lane & 31) * pitch + half * 4 * sizeof(T);
+        const int r = lane / vectors, v = lane % vectors;
+        const char *read = lds + r * pitch + v * 16;
+        const int64_t m = m0 + r, n = n0 + v * per;
+        T *to = c + m * ldc + n;
+        const bool inside = m0 + S::TM * 32 <= g.m && n0 + cols <= g.n; // of the whole wave
+#pragma unroll
+        for (int first = 0; first < S::TM; first += together) {
+#pragma unroll
+            for (int t = 0; t < together; ++t)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        struct alignas(4 * sizeof(T)) Four { T v[4]; } f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) f.v[i] = (T)acc[first + t][j][q * 4 + i];
+                        *reinterpret_cast<Four *>(write + t * block_bytes + (j * 32 + q * 8) * sizeof(T)) = f;
+                    }
+            __builtin_amdgcn_wave_barrier();
+            struct alignas(16) Many { T v[per]; };
+            if (inside) {
+#pragma unroll
+                for (int i = 0; i < together * 32 / rows_each; ++i)
+                    store_stream(to + (int64_t)(first * 32 + i * rows_each) * ldc, *reinterpret_cast<const Many *>(read + i * rows_each * pitch));
+            } else {
+                for (int i = 0; i < together * 32 / rows_each; ++i) {
+                    const Many x = *reinterpret_cast<const Many *>(read + i * rows_each * pitch);
+                    if (m + first * 32 + i * rows_each >= g.m) break;
+                    T *at = to + (int64_t)(first * 32 + i * rows_each) * ldc;
+                    if (n + per <= g.n) {
+                        store_stream(at, x);
+                    } else {
+                        for (int e = 0; e < per; ++e)
+                            if (n + e < g.n) at[e] = x.v[e];
+                    }
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
     }
-}
+};
 
 template <typename T, typename S>
 __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kernel(MatmulArgs g)
 {
-    constexpr int pitch_out = S::TN * 32 * sizeof(T) + 16;
-    constexpr int lds_bytes = S::lds_bytes > S::waves * 32 * pitch_out ? S::lds_bytes : S::waves * 32 * pitch_out;
+    constexpr int out_bytes = S::waves * StoreTile<T, S>::wave_bytes, lds_bytes = S::lds_bytes > out_bytes ? S::lds_bytes : out_bytes;
     __shared__ __align__(1024) char lds[lds_bytes];
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = (int)uniform(threadIdx.x >> 6);
     const unsigned tiles = g.tiles_m * g.tiles_n;
-    // Workgroups are dealt to the chip's parts in turn: each part gets a run of tiles, in columns of up to 8 rows of tiles, so
+    // Workgroups are dealt to the chip's parts in turn: each part gets a run of tiles, in columns of up to 4 rows of tiles, so
     // that the operands its second-level cache holds are read by several.
     const unsigned part = blockIdx.x % kParts, per_part = gridDim.x / kParts, more = gridDim.x % kParts;
     const unsigned place = part * per_part + min(part, more) + blockIdx.x / kParts;
@@ -214,8 +235,8 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
 
     const int wm = wave / S::WN, wn = wave % S::WN;
     const int row_a = wm * S::TM * 32 + (lane & 31), row_b = S::BM + wn * S::TN * 32 + (lane & 31);
-    constexpr int steps = kStage / 64, reads = S::TM + S::TN;
-    constexpr int sets = S::stage_ahead ? 2 * steps : 2; // of operands in registers
+    constexpr int steps = S::steps, reads = S::TM + S::TN;
+    constexpr int sets = S::stage_ahead ? 2 * steps : steps; // of operands in registers
     uint4 a[sets][S::TM], b[sets][S::TN];
     // operand r of step t, A's rows, then B's, into a set
     auto read_codes = [&](int s, int t, int r, int set) {
@@ -249,7 +270,7 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int64_t n = n0 + (wn * S::TN + j) * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-                const float v = n < g.n ? g.bias[n] : 0.0f;
+                const float v = g.bias[min(n, g.n - 1)]; // (a column past the last one is not stored)
 #pragma unroll
                 for (int t = 0; t < S::TM; ++t) acc[t][j][i] = v;
             }
@@ -269,16 +290,18 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
         for (int t = 0; t < steps; ++t) {
 #pragma unroll
             for (int p = 0; p < S::products; ++p) {
-                multiply(t, p, t & 1);
+                multiply(t, p, t);
                 __builtin_amdgcn_sched_barrier(0);
-                if (t + 1 < steps) {
+                if (t < 2) {
 #pragma unroll
-                    for (int r = 0; r < reads; ++r)
-                        if (S::read_place(r) == p) read_codes(s, t + 1, r, (t + 1) & 1);
+                    for (int r = 0; r < reads; ++r) {
+                        if (S::read_place(r) == p) read_codes(s, t == 0 ? 1 : 3, r, t == 0 ? 1 : 3);
+                        if (t == 0 && S::read_place(r) + S::products / 2 == p) read_codes(s, 2, r, 2);
+                    }
                 }
                 if constexpr (more) {
-                    if (t == steps - 2 && p == S::freed) read_barrier();
-                    const int place = t == steps - 2 ? p - S::freed : t == steps - 1 ? S::products - S::freed + p : -1;
+                    if (t == S::free_step && p == S::freed) read_barrier();
+                    const int place = (t - S::free_step) * S::products + p - S::freed; // (negative before)
 #pragma unroll
                     for (int q = 0; q < S::loads; ++q)
                         if (S::load_place(q) == place) request(s + S::ring, q);
@@ -363,7 +386,7 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
     }
     lds_barrier(); // the last stage is read
     T *c = static_cast<T *>(g.c) + (finish ? 0 : (int64_t)slice * g.m * g.n);
-    store_tile<T, S>(g, c, finish ? g.ldc : g.n, acc, lds + wave * 32 * pitch_out, m0 + wm * S::TM * 32, n0 + wn * S::TN * 32, finish);
+    StoreTile<T, S>::run(g, c, finish ? g.ldc : g.n, acc, lds + wave * StoreTile<T, S>::wave_bytes, m0 + wm * S::TM * 32, n0 + wn * S::TN * 32, finish && g.relu);
 }
 
 // the slices' partial sums in turn, bias, relu, rounding
