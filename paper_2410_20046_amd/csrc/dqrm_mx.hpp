@@ -207,11 +207,12 @@ struct QuantArgs {
 template <typename T>
 __device__ __forceinline__ void load_gated(const QuantArgs &a, int64_t r, int64_t c, float (&v)[kChunk])
 {
-    const bool inside = r + 1 < a.rows;
-    load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, inside, v);
+    // (are there 8 values from this one on before the matrix's memory ends?  Rows may be shorter than that.)
+    auto inside = [&](int64_t ld) { return (a.rows - 1 - r) * ld + a.cols >= c + kChunk; };
+    load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, inside(a.ldx), v);
     if (a.gate) {
         float g[kChunk];
-        load_chunk(static_cast<const T *>(a.gate) + r * a.ldgate, c, a.cols, inside, g);
+        load_chunk(static_cast<const T *>(a.gate) + r * a.ldgate, c, a.cols, inside(a.ldgate), g);
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) v[i] = g[i] > 0.0f ? v[i] : 0.0f;
     }

@@ -165,8 +165,8 @@ __global__ __launch_bounds__(kFewBlock) void few_kernel(FewArgs a)
 #pragma unroll
         for (int t = 0; t < tiles; ++t) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) load16_to_lds(here(codes[t]), code_at[j], unit * (kUnitGroups * 64), to + t * kUnitTile + j * 1024);
-            load4_to_lds(here(scales[t]), scale_at, unit * (kUnitGroups * 4), to + t * kUnitTile + kUnitBytes);
+            for (int j = 0; j < 4; ++j) load16_to_lds(here(codes[t]), code_at[j] + unit * (kUnitGroups * 64), to + t * kUnitTile + j * 1024);
+            load4_to_lds(here(scales[t]), scale_at + unit * (kUnitGroups * 4), to + t * kUnitTile + kUnitBytes);
         }
     };
     auto tile_of = [&](int i, int t) { return s_ring + (wave * RING + i % RING) * (tiles * kUnitTile) + t * kUnitTile; };

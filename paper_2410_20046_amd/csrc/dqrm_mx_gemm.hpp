@@ -59,14 +59,15 @@ __device__ __forceinline__ rsrc_t buffer_of(const uint8_t *p, int64_t bytes)
     return r;
 }
 
-// lane l's 16 (4) bytes at offset + base come to LDS address lds + 16 l (4 l); lds and base are the wave's
-__device__ __forceinline__ void load16_to_lds(rsrc_t r, unsigned offset, unsigned base, unsigned lds)
+// Lane l's 16 (4) bytes at `offset` come to LDS address lds + 16 l (4 l); lds is the wave's.  All of the offset is in the vector register:
+// that is what the bounds check looks at (an offset from a scalar register is not part of it).
+__device__ __forceinline__ void load16_to_lds(rsrc_t r, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(uniform(lds)), "v"(offset), "s"(r), "s"(uniform(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform(lds)), "v"(offset), "s"(r) : "memory");
 }
-__device__ __forceinline__ void load4_to_lds(rsrc_t r, unsigned offset, unsigned base, unsigned lds)
+__device__ __forceinline__ void load4_to_lds(rsrc_t r, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(uniform(lds)), "v"(offset), "s"(r), "s"(uniform(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(uniform(lds)), "v"(offset), "s"(r) : "memory");
 }
 // every load of this wave is in LDS and every read of LDS has its data; then every wave's
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
     // load k of the S::scale_loads that a wave has of A's or B's scales of a pair of stages
     auto request_scales = [&](int pair, bool of_a, int k) {
         const unsigned j = (unsigned)(k * S::waves + wave);
-        load4_to_lds(until_last(of_a ? rsa : rsb, 2 * pair), scale_at, (unsigned)pair * kPairScales + j * 16 * (unsigned)sp,
+        load4_to_lds(until_last(of_a ? rsa : rsb, 2 * pair), scale_at + (unsigned)pair * kPairScales + j * 16 * (unsigned)sp,
                      lds_scales + (unsigned)(pair % S::pairs) * S::pair_bytes + (of_a ? 0 : S::BM * kPairScales) + j * 256);
     };
     // load q of the S::loads that a wave has with stage s
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(S::waves *kWaveSize, S::per_simd) void matmul_kerne
         if (q < S::a_loads + S::b_loads) {
             const bool of_a = q < S::a_loads;
             const unsigned j = (unsigned)((of_a ? q : q - S::a_loads) * S::waves + wave);
-            load16_to_lds(until_last(of_a ? ra : rb, s), code_at, (unsigned)s * kStageCodes + j * 8 * (unsigned)cp,
+            load16_to_lds(until_last(of_a ? ra : rb, s), code_at + (unsigned)s * kStageCodes + j * 8 * (unsigned)cp,
                           lds0 + (unsigned)((s - first) & (S::ring - 1)) * S::stage_bytes + (of_a ? 0 : S::BM * kStageCodes) + j * 1024);
         } else {
             request_scales((s + 1) >> 1, s & 1, q - S::a_loads - S::b_loads);

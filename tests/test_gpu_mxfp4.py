@@ -390,6 +390,46 @@ def test_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(results, want)), k
 
 
+@pytest.mark.parametrize("cols", [1, 3, 7, 65])
+def test_operands_that_end_where_their_memory_ends(cols):
+    """Allocations of whole mebibytes that a matrix fills to the last byte: vectors of rows shorter than a vector, half stages of k and
+    rows past the last one must not be asked for."""
+    dq = _dq()
+    rng = np.random.default_rng(cols)
+    R = (20 << 20) // 2 // cols // 64 * 64
+    x = torch.empty(R * cols, dtype=torch.bfloat16, device="cuda").view(R, cols)
+    x.normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    few = [0, 1, R // 2, R - 9, R - 2, R - 1]
+    _said("quantise", R, cols)
+    q, qt = dq.MxMatrix(R, cols, "cuda"), dq.MxMatrix(cols, R, "cuda")
+    sums, ws = torch.empty(cols, device="cuda"), _workspace(dq.dqrm_mxfp4_quant_workspace_bytes(R, cols))
+    dq.dqrm_mxfp4_quant(x, q)
+    dq.dqrm_mxfp4_quant(x, None, qt, gate=x, col_sums=sums, workspace=ws)
+    code, scale = ref.quantise(f64(x[few]))
+    np.testing.assert_array_equal(q.scales[few].cpu().numpy(), scale)
+    np.testing.assert_array_equal(q.codes[few].cpu().numpy(), ref.pack(code))
+    code, scale = ref.quantise(np.maximum(f64(x), 0).T)
+    np.testing.assert_array_equal(qt.scales.cpu().numpy(), scale)
+    np.testing.assert_array_equal(qt.codes.cpu().numpy(), ref.pack(code))
+    # W of 20 MiB of codes (one group of 128 values to a row), as the second operand of a large and of a small product
+    N = (20 << 20) // 64
+    w = dq.MxMatrix(N, cols, "cuda")
+    wv = rng.choice(ref.MAGNITUDES, (N, cols)) * rng.choice([-1.0, 1.0], (N, cols))
+    dq.dqrm_mxfp4_quant(torch.from_numpy(wv).to(torch.bfloat16).cuda(), w)
+    wv = ref.quantised_values(wv)
+    for m in (70, 3):
+        a, av = _held(rng.standard_normal((m, cols)))
+        out = torch.empty((m, N), dtype=torch.bfloat16, device="cuda")
+        _said("product", m, N, cols)
+        dq.dqrm_mxfp4_matmul(a, w, out, workspace=_workspace(dq.dqrm_mxfp4_matmul_workspace_bytes(m, N, cols)))
+        want = av @ wv.T
+        assert np.all(np.abs(f64(out) - want) <= _bound(av, wv, np.zeros(N), want, "bf16"))
+        out = torch.empty((N, m), dtype=torch.bfloat16, device="cuda")
+        _said("product", N, m, cols)
+        dq.dqrm_mxfp4_matmul(w, a, out, workspace=_workspace(dq.dqrm_mxfp4_matmul_workspace_bytes(N, m, cols)))
+        assert np.all(np.abs(f64(out) - want.T) <= _bound(wv, av, np.zeros(m), want.T, "bf16"))
+
+
 def test_offsets_past_32_bits():
     dq = _dq()
     R, C = 70001, 65600  # 4.6 G values
