@@ -183,12 +183,13 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# the current stream's handle without making a Stream object (2.8 us)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        if _raw_stream is not None and torch.cuda.is_initialized():  # (a tenth of the time of making a Stream object)
+        if _raw_stream is not None and torch.cuda.is_initialized():
             return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
@@ -481,27 +482,40 @@ def dqrm_fwd_bwd_step(tables: Tables, bufs: StepBuffers, indices: torch.Tensor, 
 # ---- layer norm and MXFP4 linear layers ---------------------------------------------------------------------------------
 
 
+# (These run on every call, and a call on little data is as long as they are: no tuples, no formatting unless something is wrong.)
 def _matrix(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
     """(dtype, address, row stride) of a matrix whose rows' elements lie one behind the other."""
-    assert t.dim() == 2 and t.dtype in _DTYPES, f"{what}: a matrix of float32, bfloat16 or float16"
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None or t.dim() != 2:
+        raise AssertionError(f"{what}: a matrix of float32, bfloat16 or float16")
     ld, step = t.stride()
-    assert step == 1 or t.shape[1] <= 1, f"{what}: the elements of a row must be contiguous"
-    return _DTYPES[t.dtype], t.data_ptr(), ld
+    if step != 1 and t.shape[1] > 1:
+        raise AssertionError(f"{what}: the elements of a row must be contiguous")
+    return dtype, t.data_ptr(), ld
 
 
 def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
     if t is None:
         return None
-    assert t.dtype == torch.float32 and t.shape == (n,) and t.is_contiguous(), f"{what}: {n} contiguous float32 values"
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise AssertionError(f"{what}: {n} contiguous float32 values")
     return t.data_ptr()
 
 
-def _like(t: torch.Tensor, shape, dtype, what: str) -> None:
-    assert tuple(t.shape) == tuple(shape) and t.dtype == dtype, f"{what}: {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}"
+def _like(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> None:
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise AssertionError(f"{what}: ({rows}, {cols}) of {dtype}, got {tuple(t.shape)} of {t.dtype}")
 
 
 def _space(ws: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
-    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+    return (None, 0) if ws is None else (_ptr(ws), ws.nbytes)
+
+
+def _stream_of(t: torch.Tensor, stream) -> Optional[int]:
+    """The stream asked for, or the current one of the device that `t` is on."""
+    if stream is None and _raw_stream is not None and t.is_cuda:
+        return _raw_stream(t.get_device())
+    return _stream(stream)
 
 
 class MxMatrix:
@@ -515,7 +529,7 @@ class MxMatrix:
         self.codes = codes if codes is not None else byte(64 * groups)
         self.scales = scales if scales is not None else byte(4 * groups)
         for t, n in ((self.codes, 64 * groups), (self.scales, 4 * groups)):
-            _like(t, (self.rows, n), torch.uint8, "MxMatrix")
+            _like(t, self.rows, n, torch.uint8, "MxMatrix")
         self.c = dqrm_mxfp4_t(self.rows, self.cols, _ptr(self.codes), _ptr(self.scales))
         self.ref = C.byref(self.c)
 
@@ -534,15 +548,15 @@ def dqrm_mxfp4_quant(x: torch.Tensor, by_rows: Optional[MxMatrix] = None, by_col
     dtype, p, ld = _matrix(x, "x")
     pg, ldg = None, 0
     if gate is not None:
-        _like(gate, x.shape, x.dtype, "gate")
+        _like(gate, *x.shape, x.dtype, "gate")
         _, pg, ldg = _matrix(gate, "gate")
     _check(lib().dqrm_mxfp4_quant(dtype, x.shape[0], x.shape[1], p, ld, pg, ldg, _mx(by_rows), _mx(by_cols),
-                                  _vector(col_sums, x.shape[1], "col_sums"), *_space(workspace), _stream(stream)), "dqrm_mxfp4_quant")
+                                  _vector(col_sums, x.shape[1], "col_sums"), *_space(workspace), _stream_of(x, stream)), "dqrm_mxfp4_quant")
 
 
 def dqrm_mxfp4_dequant(q: MxMatrix, out: torch.Tensor, stream=None) -> None:
-    _like(out, (q.rows, q.cols), out.dtype, "out")
-    _check(lib().dqrm_mxfp4_dequant(q.ref, *_matrix(out, "out"), _stream(stream)), "dqrm_mxfp4_dequant")
+    _like(out, q.rows, q.cols, out.dtype, "out")
+    _check(lib().dqrm_mxfp4_dequant(q.ref, *_matrix(out, "out"), _stream_of(out, stream)), "dqrm_mxfp4_dequant")
 
 
 def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -551,9 +565,9 @@ def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def dqrm_mxfp4_matmul(a: MxMatrix, b: MxMatrix, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    _like(out, (a.rows, b.rows), out.dtype, "out")
+    _like(out, a.rows, b.rows, out.dtype, "out")
     _check(lib().dqrm_mxfp4_matmul(a.ref, b.ref, _vector(bias, b.rows, "bias"), relu, *_matrix(out, "out"), *_space(workspace),
-                                   _stream(stream)), "dqrm_mxfp4_matmul")
+                                   _stream_of(out, stream)), "dqrm_mxfp4_matmul")
 
 
 def dqrm_mxfp4_linear_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -565,12 +579,13 @@ def dqrm_mxfp4_linear(x: torch.Tensor, w: MxMatrix, out: torch.Tensor, bias: Opt
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """``eps`` given: x goes through a layer norm (with ``gamma`` and ``beta`` if given) first."""
     dtype, p, ld = _matrix(x, "x")
-    _like(x, (x.shape[0], w.cols), x.dtype, "x")
-    _like(out, (x.shape[0], w.rows), x.dtype, "out")
+    m = x.shape[0]
+    _like(x, m, w.cols, x.dtype, "x")
+    _like(out, m, w.rows, x.dtype, "out")
     _, po, ldo = _matrix(out, "out")
-    _check(lib().dqrm_mxfp4_linear(dtype, x.shape[0], p, ld, eps is not None, _vector(gamma, w.cols, "gamma"),
+    _check(lib().dqrm_mxfp4_linear(dtype, m, p, ld, eps is not None, _vector(gamma, w.cols, "gamma"),
                                    _vector(beta, w.cols, "beta"), eps or 0.0, w.ref, _vector(bias, w.rows, "bias"), relu, po, ldo,
-                                   *_space(workspace), _stream(stream)), "dqrm_mxfp4_linear")
+                                   *_space(workspace), _stream_of(x, stream)), "dqrm_mxfp4_linear")
 
 
 def dqrm_layernorm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
@@ -580,10 +595,10 @@ def dqrm_layernorm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Opt
     R, D = x.shape
     py, ldy = None, 0
     if y is not None:
-        _like(y, x.shape, x.dtype, "y")
+        _like(y, R, D, x.dtype, "y")
         _, py, ldy = _matrix(y, "y")
     _check(lib().dqrm_layernorm_fwd(dtype, R, D, p, ld, _vector(gamma, D, "gamma"), _vector(beta, D, "beta"), eps, py, ldy,
-                                    _vector(mean, R, "mean"), _vector(rstd, R, "rstd"), _mx(q), _stream(stream)), "dqrm_layernorm_fwd")
+                                    _vector(mean, R, "mean"), _vector(rstd, R, "rstd"), _mx(q), _stream_of(x, stream)), "dqrm_layernorm_fwd")
 
 
 def dqrm_layernorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
@@ -595,12 +610,12 @@ def dqrm_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
                        dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     dtype, p, ld = _matrix(x, "x")
     R, D = x.shape
-    _like(dy, x.shape, x.dtype, "dy")
+    _like(dy, R, D, x.dtype, "dy")
     _, pdy, lddy = _matrix(dy, "dy")
     pdx, lddx = None, 0
     if dx is not None:
-        _like(dx, x.shape, x.dtype, "dx")
+        _like(dx, R, D, x.dtype, "dx")
         _, pdx, lddx = _matrix(dx, "dx")
     _check(lib().dqrm_layernorm_bwd(dtype, R, D, pdy, lddy, p, ld, _vector(mean, R, "mean"), _vector(rstd, R, "rstd"),
                                     _vector(gamma, D, "gamma"), pdx, lddx, _vector(dgamma, D, "dgamma"), _vector(dbeta, D, "dbeta"),
-                                    *_space(workspace), _stream(stream)), "dqrm_layernorm_bwd")
+                                    *_space(workspace), _stream_of(x, stream)), "dqrm_layernorm_bwd")
