@@ -152,11 +152,13 @@ void with_norm_fwd_shape(int64_t cols, F f)
                           NormShape<512, 2, 512>, NormShape<1024, 2, 1024>>(cols, f);
 }
 
+// (16001 x 8190 bfloat16: 512 threads with two chunks 141 us, 1024 with one 166; 64000 x 2047: 128 threads with two chunks 150 us, 256 with
+// one 201)
 template <typename F>
 void with_norm_bwd_shape(int64_t cols, F f)
 {
-    with_first_that_holds<NormShape<16, 1, 1024>, NormShape<64, 1, 1024>, NormShape<64, 2, 512>, NormShape<256, 1, 1024>, NormShape<512, 1, 1024>,
-                          NormShape<1024, 1, 1024>, NormShape<1024, 2, 1024>>(cols, f);
+    with_first_that_holds<NormShape<16, 1, 1024>, NormShape<64, 1, 1024>, NormShape<64, 2, 512>, NormShape<128, 2, 512>, NormShape<256, 2, 512>,
+                          NormShape<512, 2, 512>, NormShape<1024, 2, 1024>>(cols, f);
 }
 
 void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
@@ -195,7 +197,8 @@ int norm_bwd_blocks(int64_t rows, int64_t cols)
     if (rows < 1 || cols < 1) return 0;
     if (!norm_in_registers(cols)) return (int)std::min<int64_t>(ceil_div(rows, 32), 64);
     int64_t n = 0;
-    with_norm_bwd_shape(cols, [&](auto shape) { n = std::min<int64_t>(ceil_div(rows, decltype(shape)::rows), num_cus() * (1024 / decltype(shape)::BLOCK)); });
+    // (one to a CU: twice as many write and join twice the partial sums, 145 instead of 141 us for 16001 x 8190)
+    with_norm_bwd_shape(cols, [&](auto shape) { n = std::min<int64_t>(ceil_div(rows, decltype(shape)::rows), num_cus()); });
     return (int)n;
 }
 
