@@ -51,39 +51,35 @@ __device__ __forceinline__ void store_stream(T *p, const V &v)
 }
 
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&v)[kChunk])
+__device__ __forceinline__ void to_float(const Vec8<T> &t, float (&v)[kChunk])
 {
-    Vec8<T> t;
-    __builtin_memcpy(&t, p, sizeof(t));
 #pragma unroll
     for (int i = 0; i < kChunk; ++i) v[i] = (float)t.v[i];
 }
 
-// the first n of 8 values, the others 0
-template <typename T>
-__device__ __forceinline__ void load_first(const T *p, int n, float (&v)[kChunk])
-{
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
-}
-
-// values c .. c + 7 of a row of `cols`; those past its end are 0.  `inside`: the 8 values lie inside the matrix's memory, so they
+// Values c .. c + 7 of a row of `cols`; those past its end are 0.  `inside`: the 8 values lie inside the matrix's memory, so they
 // may be loaded as one vector also where some belong to what follows the row.
 template <typename T, typename I>
-__device__ __forceinline__ void load_chunk(const T *row, I c, I cols, bool inside, float (&v)[kChunk])
+__device__ __forceinline__ Vec8<T> load_vec(const T *row, I c, I cols, bool inside)
 {
-    if (c + kChunk <= cols) {
-        load8(row + c, v);
-    } else if (c >= cols) {
+    Vec8<T> t;
+    if (c + kChunk <= cols || (inside && c < cols)) {
+        __builtin_memcpy(&t, row + c, sizeof(t));
+        if (c + kChunk > cols) {
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = 0.0f;
-    } else if (inside) {
-        load8(row + c, v);
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = c + i < cols ? v[i] : 0.0f;
+            for (int i = 0; i < kChunk; ++i) t.v[i] = c + i < cols ? t.v[i] : (T)0.0f;
+        }
     } else {
-        load_first(row + c, (int)(cols - c), v);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) t.v[i] = c + i < cols ? row[c + i] : (T)0.0f;
     }
+    return t;
+}
+
+template <typename T, typename I>
+__device__ __forceinline__ void load_chunk(const T *row, I c, I cols, float (&v)[kChunk])
+{
+    to_float(load_vec(row, c, cols, false), v);
 }
 
 // A row's chunk as it lies in memory, to be requested long before its use.  Where fewer than 8 values are left, it is the last 8
@@ -99,23 +95,37 @@ __device__ __forceinline__ Raw<T> load_raw(const T *row, I c, I cols)
 }
 
 // ... and its values c .. c + 7; those past the row's end are 0
-template <typename T, typename I>
-__device__ __forceinline__ void values_of(const Raw<T> &raw, I c, I cols, float (&v)[kChunk])
+template <typename V, typename I>
+__device__ __forceinline__ void drop_before(V (&v)[kChunk], I c, I cols)
 {
-    Vec8<T> t;
-    __builtin_memcpy(&t, &raw, sizeof(t));
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i) v[i] = (float)t.v[i];
     const int skip = (int)min(c + (I)kChunk - cols, (I)(2 * kChunk)); // of the 8 belong to the chunk before
     if (skip > 0) {
 #pragma unroll
         for (int s = 1; s < 2 * kChunk; s *= 2) {
             if (skip & s || (s == kChunk && skip > kChunk)) { // (8 and more: nothing of the row)
 #pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[i] = i + s < kChunk ? v[i + s < kChunk ? i + s : 0] : 0.0f;
+                for (int i = 0; i < kChunk; ++i) v[i] = i + s < kChunk ? v[i + s < kChunk ? i + s : 0] : (V)0.0f;
             }
         }
     }
+}
+
+template <typename T, typename I>
+__device__ __forceinline__ Vec8<T> vec_of(const Raw<T> &raw, I c, I cols)
+{
+    Vec8<T> t;
+    __builtin_memcpy(&t, &raw, sizeof(t));
+    drop_before(t.v, c, cols);
+    return t;
+}
+
+template <typename T, typename I>
+__device__ __forceinline__ void values_of(const Raw<T> &raw, I c, I cols, float (&v)[kChunk])
+{
+    Vec8<T> t;
+    __builtin_memcpy(&t, &raw, sizeof(t));
+    to_float(t, v);
+    drop_before(v, c, cols);
 }
 
 // STREAM: past the caches (for outputs that are not read again soon)
@@ -150,32 +160,77 @@ __device__ __forceinline__ unsigned scale_byte(unsigned amax_bits)
     return e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
 }
 
-// 2^-e for a scale byte of a finite block (0 .. 252)
-__device__ __forceinline__ float inverse_scale(unsigned s) { return __uint_as_float((254u - s) << 23); }
 // 2^e; 255 is NaN
 __device__ __forceinline__ float scale_value(unsigned s)
 {
     return __uint_as_float(s == 255u ? 0x7FC00000u : s == 0u ? 0x00400000u : s << 23);
 }
 
-// eight codes, value 0 in the low four bits; the conversion rounds to even and saturates
-__device__ __forceinline__ unsigned pack_codes(const float (&v)[kChunk], unsigned s)
+// Eight codes, value 0 in the low four bits.  The conversion divides by the scale, rounds to even and saturates.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ unsigned convert8(const float (&v)[kChunk], float scale)
 {
-    const float inv = inverse_scale(s & 0xFFu);
-    unsigned r = 0;
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0] * inv, v[1] * inv, 1.0f, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2] * inv, v[3] * inv, 1.0f, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4] * inv, v[5] * inv, 1.0f, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6] * inv, v[7] * inv, 1.0f, 3);
+    unsigned r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], scale, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], scale, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], scale, 3);
+}
+__device__ __forceinline__ unsigned convert8(const __bf16 (&v)[kChunk], float scale)
+{
+    unsigned r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, bf16x2{v[0], v[1]}, scale, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, bf16x2{v[2], v[3]}, scale, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, bf16x2{v[4], v[5]}, scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, bf16x2{v[6], v[7]}, scale, 3);
+}
+__device__ __forceinline__ unsigned convert8(const _Float16 (&v)[kChunk], float scale)
+{
+    unsigned r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(0u, f16x2{v[0], v[1]}, scale, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, f16x2{v[2], v[3]}, scale, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, f16x2{v[4], v[5]}, scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, f16x2{v[6], v[7]}, scale, 3);
+}
+
+template <typename T>
+__device__ __forceinline__ unsigned pack_codes(const T (&v)[kChunk], unsigned s)
+{
+    const unsigned r = convert8(v, __uint_as_float(s << 23)); // (of the scale only the exponent's field counts, 0 being 2^-127)
     return s == 255u ? 0u : r;
 }
 
+// bits, as a float's, of the largest magnitude of eight values
 __device__ __forceinline__ unsigned max8(const float (&v)[kChunk])
 {
     unsigned m = abs_bits(v[0]);
 #pragma unroll
     for (int i = 1; i < kChunk; ++i) m = max(m, abs_bits(v[i]));
     return m;
+}
+
+// ... of 16-bit types: magnitudes order like their bits, two to a register
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 abs_pair(unsigned w)
+{
+    u16x2 r;
+    w &= 0x7FFF7FFFu;
+    __builtin_memcpy(&r, &w, 4);
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ unsigned bits_of_16(unsigned short m)
+{
+    T t;
+    __builtin_memcpy(&t, &m, 2);
+    return __float_as_uint((float)t);
+}
+template <typename T>
+__device__ __forceinline__ unsigned max8(const T (&v)[kChunk])
+{
+    unsigned w[4];
+    __builtin_memcpy(w, v, 16);
+    const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(abs_pair(w[0]), abs_pair(w[1])), __builtin_elementwise_max(abs_pair(w[2]), abs_pair(w[3])));
+    return bits_of_16<T>(m.x > m.y ? m.x : m.y);
 }
 
 // the largest over the four lanes of a block
@@ -187,7 +242,8 @@ __device__ __forceinline__ unsigned quad_max(unsigned m)
 
 // A chunk of a row's codes and, from the first lane of each block, its scale byte.  All four lanes of a block take part.
 // chunk: index of the 8 values in the padded row.  (A block of the padding has zeros: its scale byte is 0.)
-__device__ __forceinline__ void write_chunk(uint8_t *codes_row, uint8_t *scales_row, unsigned chunk, const float (&v)[kChunk])
+template <typename T>
+__device__ __forceinline__ void write_chunk(uint8_t *codes_row, uint8_t *scales_row, unsigned chunk, const T (&v)[kChunk])
 {
     const unsigned s = scale_byte(quad_max(max8(v)));
     *reinterpret_cast<unsigned *>(codes_row + (size_t)chunk * 4) = pack_codes(v, s);
@@ -204,18 +260,22 @@ struct QuantArgs {
     unsigned col_tiles;          // of quant_tile_kernel's grid
 };
 
+// x where gate > 0
 template <typename T>
-__device__ __forceinline__ void load_gated(const QuantArgs &a, int64_t r, int64_t c, float (&v)[kChunk])
+__device__ __forceinline__ void apply_gate(Vec8<T> &v, const Vec8<T> &gate)
+{
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) v.v[i] = gate.v[i] > (T)0.0f ? v.v[i] : (T)0.0f;
+}
+
+template <typename T>
+__device__ __forceinline__ Vec8<T> load_gated(const QuantArgs &a, int64_t r, int64_t c)
 {
     // (are there 8 values from this one on before the matrix's memory ends?  Rows may be shorter than that.)
     auto inside = [&](int64_t ld) { return (a.rows - 1 - r) * ld + a.cols >= c + kChunk; };
-    load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, inside(a.ldx), v);
-    if (a.gate) {
-        float g[kChunk];
-        load_chunk(static_cast<const T *>(a.gate) + r * a.ldgate, c, a.cols, inside(a.ldgate), g);
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = g[i] > 0.0f ? v[i] : 0.0f;
-    }
+    Vec8<T> v = load_vec(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, inside(a.ldx));
+    if (a.gate) apply_gate(v, load_vec(static_cast<const T *>(a.gate) + r * a.ldgate, c, a.cols, inside(a.ldgate)));
+    return v;
 }
 
 // One chunk to a lane, rows' chunks one after another; per_row: chunks of a row, of fewer than 2^31 in all.
@@ -225,9 +285,8 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a, dqrm::Fast
     using T = elem_t<DT>;
     const unsigned at = blockIdx.x * 256 + threadIdx.x, r = per_row.div(at), chunk = at - r * per_row.d;
     if (r >= a.rows) return; // (whole blocks of 32 values: a row has a multiple of 16 chunks)
-    float v[kChunk];
-    load_gated<T>(a, r, (int64_t)chunk * kChunk, v);
-    write_chunk(a.codes + r * codes_pitch(a.cols), a.scales + r * scales_pitch(a.cols), chunk, v);
+    const Vec8<T> v = load_gated<T>(a, r, (int64_t)chunk * kChunk);
+    write_chunk(a.codes + r * codes_pitch(a.cols), a.scales + r * scales_pitch(a.cols), chunk, v.v);
 }
 
 // ---- along columns, and both ways from one read ----------------------------------------------------------------------------
@@ -250,13 +309,10 @@ __global__ __launch_bounds__(256, DT == DQRM_F32 ? 2 : 4) void quant_tile_kernel
     const int tid = threadIdx.x;
     const int lane_chunk = tid & 15;
     const int64_t c = c0 + lane_chunk * kChunk;
-    auto finish_chunk = [&](int dr, float (&v)[kChunk]) {
+    auto finish_chunk = [&](int dr, const Vec8<T> &v) {
         if (a.codes && r0 + dr < a.rows)
-            write_chunk(a.codes + (r0 + dr) * codes_pitch(a.cols), a.scales + (r0 + dr) * scales_pitch(a.cols), (unsigned)(c / kChunk), v);
-        Vec8<T> t;
-#pragma unroll
-        for (int k = 0; k < kChunk; ++k) t.v[k] = (T)v[k];
-        __builtin_memcpy(__builtin_assume_aligned(&tile[dr][lane_chunk * kChunk], 16), &t, sizeof(t));
+            write_chunk(a.codes + (r0 + dr) * codes_pitch(a.cols), a.scales + (r0 + dr) * scales_pitch(a.cols), (unsigned)(c / kChunk), v.v);
+        __builtin_memcpy(__builtin_assume_aligned(&tile[dr][lane_chunk * kChunk], 16), &v, sizeof(v));
     };
     if (a.cols >= kChunk) {
         // (rows past the last one repeat it and then count as zeros)
@@ -271,58 +327,52 @@ __global__ __launch_bounds__(256, DT == DQRM_F32 ? 2 : 4) void quant_tile_kernel
 #pragma unroll
         for (int i = 0; i < passes; ++i) {
             const int dr = i * 16 + (tid >> 4);
-            float v[kChunk];
-            values_of<T>(x[i], c, a.cols, v);
-            if (a.gate) {
-                float g[kChunk];
-                values_of<T>(gate[i], c, a.cols, g);
-#pragma unroll
-                for (int k = 0; k < kChunk; ++k) v[k] = g[k] > 0.0f ? v[k] : 0.0f;
-            }
+            Vec8<T> v = vec_of<T>(x[i], c, a.cols);
+            if (a.gate) apply_gate(v, vec_of<T>(gate[i], c, a.cols));
             if (r0 + dr >= a.rows) {
 #pragma unroll
-                for (int k = 0; k < kChunk; ++k) v[k] = 0.0f;
+                for (int k = 0; k < kChunk; ++k) v.v[k] = (T)0.0f;
             }
             finish_chunk(dr, v);
         }
     } else {
         for (int i = 0; i < passes; ++i) {
             const int dr = i * 16 + (tid >> 4);
-            float v[kChunk] = {};
-            if (r0 + dr < a.rows) load_gated<T>(a, r0 + dr, c, v);
+            Vec8<T> v{};
+            if (r0 + dr < a.rows) v = load_gated<T>(a, r0 + dr, c);
             finish_chunk(dr, v);
         }
     }
     __syncthreads();
     const int lane = tid & 63, wave = tid >> 6;
-    uint4 codes[2] = {};
-    unsigned scale[2] = {0, 0};
+    uint4 codes[2];
+    unsigned scale[2];
     float sum[2] = {0.0f, 0.0f};
-    float v[2][32];
+    T v[2][4][kChunk];
+    unsigned most[2];
+    u16x2 pair_most = {0, 0};
+    most[0] = most[1] = 0;
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
         const Pair p = *reinterpret_cast<const Pair *>(&tile[wave * 32 + k][lane * 2]);
-        v[0][k] = (float)p.v[0], v[1][k] = (float)p.v[1];
+        v[0][k / kChunk][k % kChunk] = p.v[0], v[1][k / kChunk][k % kChunk] = p.v[1];
+        if constexpr (sizeof(T) == 2) {
+            unsigned w;
+            __builtin_memcpy(&w, &p, 4);
+            pair_most = __builtin_elementwise_max(pair_most, abs_pair(w));
+        } else {
+            most[0] = max(most[0], abs_bits(p.v[0])), most[1] = max(most[1], abs_bits(p.v[1]));
+        }
     }
+    if (a.partial) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) sum[0] += (float)v[0][k / kChunk][k % kChunk], sum[1] += (float)v[1][k / kChunk][k % kChunk];
+    }
+    if constexpr (sizeof(T) == 2) most[0] = bits_of_16<T>(pair_most.x), most[1] = bits_of_16<T>(pair_most.y);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        unsigned m = 0;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) m = max(m, abs_bits(v[j][k]));
-        if (a.partial) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) sum[j] += v[j][k];
-        }
-        scale[j] = scale_byte(m);
-        unsigned w[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float t[kChunk];
-#pragma unroll
-            for (int k = 0; k < kChunk; ++k) t[k] = v[j][q * kChunk + k];
-            w[q] = pack_codes(t, scale[j]);
-        }
-        codes[j] = make_uint4(w[0], w[1], w[2], w[3]);
+        scale[j] = scale_byte(most[j]);
+        codes[j] = make_uint4(pack_codes(v[j][0], scale[j]), pack_codes(v[j][1], scale[j]), pack_codes(v[j][2], scale[j]), pack_codes(v[j][3], scale[j]));
     }
     __syncthreads(); // the tile is read; its memory takes the codes: [128 columns][64 bytes]
     uint4 *s_codes = reinterpret_cast<uint4 *>(&tile[0][0]);

@@ -53,7 +53,7 @@ template <typename I>
 __device__ __forceinline__ void load_gain(const float *p, I c, I cols, float without, float (&v)[kChunk])
 {
     if (p) {
-        load_chunk(p, c, cols, false, v);
+        load_chunk(p, c, cols, v);
     } else {
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) v[i] = without;
@@ -142,13 +142,13 @@ __global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
     float sum[1] = {0.0f}, sq[1] = {0.0f};
     float x[kChunk];
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += step) {
-        load_chunk(row, c, a.cols, false, x);
+        load_chunk(row, c, a.cols, x);
         sum[0] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
     }
     row_sums<256>(sum, s_part[0]);
     const float mean = sum[0] / (float)a.cols;
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += step) {
-        load_chunk(row, c, a.cols, false, x);
+        load_chunk(row, c, a.cols, x);
         float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) q += c + i < a.cols ? (x[i] - mean) * (x[i] - mean) : 0.0f;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
     if (!a.y && !a.codes) return;
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < end; c += step) {
         float g[kChunk], b[kChunk];
-        load_chunk(row, c, a.cols, false, x);
+        load_chunk(row, c, a.cols, x);
         load_gain(a.gamma, c, a.cols, 1.0f, g);
         load_gain(a.beta, c, a.cols, 0.0f, b);
 #pragma unroll
@@ -304,8 +304,8 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
     float s[2] = {0.0f, 0.0f};
     float dy[kChunk], x[kChunk], g[kChunk];
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += 256 * kChunk) {
-        load_chunk(pdy, c, a.cols, false, dy);
-        load_chunk(px, c, a.cols, false, x);
+        load_chunk(pdy, c, a.cols, dy);
+        load_chunk(px, c, a.cols, x);
         load_gain(a.gamma, c, a.cols, 1.0f, g);
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
@@ -318,8 +318,8 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
     }
     row_sums<256>(s, s_part);
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += 256 * kChunk) {
-        load_chunk(pdy, c, a.cols, false, dy);
-        load_chunk(px, c, a.cols, false, x);
+        load_chunk(pdy, c, a.cols, dy);
+        load_chunk(px, c, a.cols, x);
         load_gain(a.gamma, c, a.cols, 1.0f, g);
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) x[i] = rstd * (dy[i] * g[i] - s[0] * inv_n - (x[i] - mean) * rstd * (s[1] * inv_n));
@@ -339,8 +339,8 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(NormBwdArgs a, in
     for (int64_t r = r0; r < r1; ++r) {
         const float mean = a.mean[r], rstd = a.rstd[r];
         float dy[kChunk], x[kChunk];
-        load_chunk(static_cast<const T *>(a.dy) + r * a.lddy, c, a.cols, false, dy);
-        load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, false, x);
+        load_chunk(static_cast<const T *>(a.dy) + r * a.lddy, c, a.cols, dy);
+        load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, x);
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) dg[i] += c + i < a.cols ? dy[i] * ((x[i] - mean) * rstd) : 0.0f, db[i] += dy[i];
     }
