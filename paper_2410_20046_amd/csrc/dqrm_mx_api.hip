@@ -57,7 +57,7 @@ int32_t check_matrix(const void *p, int64_t ld, int32_t dtype, int64_t rows, int
 {
     if (rows == 0 || cols == 0) return DQRM_OK;
     if (!p || !aligned(p, size_of(dtype)) || (rows > 1 && ld < cols)) return DQRM_ERR_INVALID_ARG;
-    if (rows > 1 && ld > (int64_t)1 << 40) return DQRM_ERR_UNSUPPORTED;
+    if (rows > 1 && (ld > (int64_t)1 << 40 || ld > ((int64_t)1 << 48) / rows)) return DQRM_ERR_UNSUPPORTED;
     return DQRM_OK;
 }
 
@@ -217,8 +217,10 @@ struct MatmulPlan {
     unsigned stages_per_slice;
 };
 
-// Few rows of A, and W's strips enough to keep the chip's memory busy or k short.
-bool is_few(int64_t m, int64_t n, int64_t k) { return m <= 64 && (n >= 512 || k <= 16384); }
+// Few rows of A, and strips of W enough to keep the chip's memory busy or k short: W straight from memory.  Against tiles, of which
+// k can be cut: 64 x 4096 x 4096 7.0 and 10.6 us, 64 x 8192 x 8192 16.2 and 17.4, 16 x 256 x 32768 8.4 and 9.3; 16 x 512 x 65536 21.8 and 15.3,
+// 64 x 256 x 16384 12.2 and 8.4.
+bool is_few(int64_t m, int64_t n, int64_t k) { return m <= 64 && (n >= 4096 || k <= (m <= 16 ? 32768 : 8192)); }
 
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
@@ -226,7 +228,9 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
     const int64_t cus = num_cus(), stages = std::max<int64_t>(1, ceil_div(groups_of(k), 2));
     const auto tiles = [&](int64_t t) { return std::max<int64_t>(1, ceil_div(m, t) * ceil_div(n, t)); };
     MatmulPlan p{};
-    // the largest tile of which there is one to (nearly) each CU; tiles of 128 also where k can be cut until there is
+    // The largest tile of which there is one to (nearly) each CU; tiles of 128 also where k can be cut until there is.  Sides of 256, 128
+    // and 64: 8192 x 2048 x 2048 24, 34 and 36 us; 2048 x 2048 x 8192 48, 26 and 35; 8192 x 512 x 415 9.0, 5.8 and 6.1; 1024 x 1024 x 1024
+    // 9.8, 5.8 and 4.4.
     if (tiles(256) * 8 >= cus * 7)
         p.tile = 256;
     else if (tiles(128) * 4 >= cus * 3 || (tiles(64) < cus && tiles(128) * stages >= cus * kMinStages))
@@ -270,7 +274,14 @@ void launch_few(const FewArgs &a, hipStream_t st)
     const size_t lds = SRC == kFewCodes ? 0 : (size_t)(a.g.m * (codes_pitch(a.g.k) + scales_pitch(a.g.k)));
     const auto go = [&](auto st_, auto ring) {
         constexpr int ST = decltype(st_)::value, RING = decltype(ring)::value;
-        hipLaunchKernelGGL((few_kernel<DT, SRC, MT, ST, RING>), dim3((unsigned)ceil_div(strips, ST)), dim3(kFewBlock), lds, st, a);
+        for (int64_t n0 = 0; n0 < a.g.n; n0 += kMaxBlocks * 16) { // (W's rows of one launch)
+            FewArgs b = a;
+            b.g.n = std::min(kMaxBlocks * 16, a.g.n - n0);
+            b.g.b_codes += n0 * codes_pitch(a.g.k), b.g.b_scales += n0 * scales_pitch(a.g.k);
+            b.g.c = static_cast<elem_t<DT> *>(a.g.c) + n0;
+            if (a.g.bias) b.g.bias += n0;
+            hipLaunchKernelGGL((few_kernel<DT, SRC, MT, ST, RING>), dim3((unsigned)ceil_div(b.g.n, 16 * ST)), dim3(kFewBlock), lds, st, b);
+        }
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 2> two;
@@ -288,6 +299,7 @@ void launch_few(const FewArgs &a, hipStream_t st)
 int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t st)
 {
     const MatmulPlan p = matmul_plan(g.m, g.n, g.k);
+    if (p.tile > 0 && ceil_div(g.m, p.tile) * ceil_div(g.n, p.tile) > kMaxBlocks) return DQRM_ERR_UNSUPPORTED;
     if (p.tile == 0) {
         FewArgs a{};
         a.g = g;
@@ -364,7 +376,7 @@ int32_t dqrm_mxfp4_quant(int32_t dtype, int64_t rows, int64_t cols, const void *
     if (col_sums) DQRM_CHECK(check_workspace(workspace, workspace_bytes, quant_workspace(rows, cols)));
     const int64_t row_tiles = ceil_div(rows, kTile), col_tiles = ceil_div(cols, kTile);
     const bool tiles = by_cols || col_sums;
-    if (tiles && row_tiles * col_tiles > kMaxBlocks * 4) return DQRM_ERR_UNSUPPORTED;
+    if (tiles && row_tiles * col_tiles > 2 * kMaxBlocks) return DQRM_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (rows == 0 || cols == 0) {
         fill_zero(col_sums, cols, st);
