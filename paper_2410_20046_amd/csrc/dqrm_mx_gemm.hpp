@@ -142,6 +142,8 @@ struct StoreTile {
         const int64_t m = m0 + r, n = n0 + v * per;
         T *to = c + m * ldc + n;
         const bool inside = m0 + S::TM * 32 <= g.m && n0 + cols <= g.n; // of the whole wave
+        // whole lines go past the caches; parts of lines meet their other parts there
+        const bool lines = (ldc * sizeof(T)) % 128 == 0 && reinterpret_cast<uintptr_t>(c) % 128 == 0;
 #pragma unroll
         for (int first = 0; first < S::TM; first += together) {
 #pragma unroll
@@ -157,17 +159,21 @@ struct StoreTile {
                     }
             __builtin_amdgcn_wave_barrier();
             struct alignas(16) Many { T v[per]; };
-            if (inside) {
+            if (inside && lines) {
 #pragma unroll
                 for (int i = 0; i < together * 32 / rows_each; ++i)
                     store_stream(to + (int64_t)(first * 32 + i * rows_each) * ldc, *reinterpret_cast<const Many *>(read + i * rows_each * pitch));
+            } else if (inside) {
+#pragma unroll
+                for (int i = 0; i < together * 32 / rows_each; ++i)
+                    __builtin_memcpy(to + (int64_t)(first * 32 + i * rows_each) * ldc, read + i * rows_each * pitch, 16);
             } else {
                 for (int i = 0; i < together * 32 / rows_each; ++i) {
                     const Many x = *reinterpret_cast<const Many *>(read + i * rows_each * pitch);
                     if (m + first * 32 + i * rows_each >= g.m) break;
                     T *at = to + (int64_t)(first * 32 + i * rows_each) * ldc;
                     if (n + per <= g.n) {
-                        store_stream(at, x);
+                        __builtin_memcpy(at, &x, 16);
                     } else {
                         for (int e = 0; e < per; ++e)
                             if (n + e < g.n) at[e] = x.v[e];
