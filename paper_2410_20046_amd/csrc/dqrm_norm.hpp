@@ -179,7 +179,9 @@ struct NormBwdArgs {
     const float *mean, *rstd, *gamma; // gamma or null: 1
     void *dx;                         // or null
     int64_t lddx;
-    float *partial; // [blocks][2][cols]: the workgroups' sums for dgamma and dbeta, or null
+    // the workgroups' sums for dgamma and dbeta, or null: [blocks][2][cols] in the workspace, or those of the only workgroup in place
+    float *sum_gamma, *sum_beta;
+    int64_t block_stride;
 };
 
 // The row of dy and of x in registers, the next one on its way; a thread has the same columns in every row of its workgroup's
@@ -259,15 +261,15 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
             }
         }
     }
-    if (!a.partial) return;
-    float *out = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
+    if (!a.sum_gamma) return;
+    float *out[2] = {a.sum_gamma + blockIdx.x * a.block_stride, a.sum_beta + blockIdx.x * a.block_stride};
     if constexpr (rows_per_block == 1) {
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int c = column(j);
             if (c < cols) {
-                store_chunk(out, c, cols, dg[j]);
-                store_chunk(out + cols, c, cols, db[j]);
+                store_chunk(out[0], c, cols, dg[j]);
+                store_chunk(out[1], c, cols, db[j]);
             }
         }
     } else {
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
                     float v = s_acc[0][c];
                     for (int w = 1; w < rows_per_block; ++w) v += s_acc[w][c];
                     const int64_t col = (int64_t)j * TPR * kChunk + c;
-                    if (col < a.cols) out[k * a.cols + col] = v;
+                    if (col < a.cols) out[k][col] = v;
                 }
             }
         }
@@ -344,9 +346,8 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(NormBwdArgs a, in
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) dg[i] += c + i < a.cols ? dy[i] * ((x[i] - mean) * rstd) : 0.0f, db[i] += dy[i];
     }
-    float *out = a.partial + (int64_t)blockIdx.y * 2 * a.cols;
-    store_chunk(out, c, a.cols, dg);
-    store_chunk(out + a.cols, c, a.cols, db);
+    store_chunk(a.sum_gamma + blockIdx.y * a.block_stride, c, a.cols, dg);
+    store_chunk(a.sum_beta + blockIdx.y * a.block_stride, c, a.cols, db);
 }
 
 } // namespace dqrm_mx
