@@ -398,6 +398,21 @@ __global__ __launch_bounds__(256, DT == DQRM_F32 ? 2 : 4) void quant_tile_kernel
         a.partial[(int64_t)row_tile * a.cols + c0 + tid] = (s_sum[0][tid] + s_sum[1][tid]) + (s_sum[2][tid] + s_sum[3][tid]);
 }
 
+// v + p[0] + p[stride] + ... (n of them, in this order), 16 loads at a time on their way: behind the last one it is asked for again, and
+// not added.
+__device__ __forceinline__ float add_strided(float v, const float *p, int64_t stride, int n)
+{
+    constexpr int ahead = 16;
+    for (int i = 0; i < n; i += ahead) {
+        float x[ahead];
+#pragma unroll
+        for (int j = 0; j < ahead; ++j) x[j] = p[(int64_t)min(i + j, n - 1) * stride];
+#pragma unroll
+        for (int j = 0; j < ahead; ++j) v = i + j < n ? v + x[j] : v;
+    }
+    return v;
+}
+
 // out[c] = sum over p of partial[p][c] (and a second pair of arrays behind it), in a fixed order: 16 lanes take every 16th each, then
 // their sums are added in turn.
 __global__ __launch_bounds__(256) void join_columns_kernel(const float *partial, int64_t stride, int n, int64_t cols, float *out0, float *out1)
@@ -407,8 +422,7 @@ __global__ __launch_bounds__(256) void join_columns_kernel(const float *partial,
     const int slice = threadIdx.x >> 4;
     const float *p = partial + (blockIdx.y ? cols : 0);
     float sum = 0.0f;
-    if (c < cols)
-        for (int i = slice; i < n; i += 16) sum += p[(int64_t)i * stride + c];
+    if (c < cols) sum = add_strided(sum, p + (int64_t)slice * stride + c, 16 * stride, (n - slice + 15) / 16); // (none: n - slice <= 0)
     s[slice][threadIdx.x & 15] = sum;
     __syncthreads();
     if (slice == 0 && c < cols) {
