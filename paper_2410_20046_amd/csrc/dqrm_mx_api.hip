@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <cmath>
 
 #include "dqrm.h"
 #include "dqrm_host.hpp"
@@ -209,7 +210,6 @@ int norm_bwd_blocks(int64_t rows, int64_t cols)
 size_t norm_bwd_workspace(int64_t rows, int64_t cols) { return align_up((size_t)norm_bwd_blocks(rows, cols) * 2 * (size_t)cols * sizeof(float), 256); }
 
 // ---- products --------------------------------------------------------------------------------------------------------------
-constexpr int64_t kMinStages = 4; // of a slice of k
 
 using Tile256 = TileShape<4, 2, 2, 4, 2>;
 using Tile128 = TileShape<2, 1, 2, 4, 4>;
@@ -226,25 +226,43 @@ struct MatmulPlan {
 // 64 x 256 x 16384 12.2 and 8.4.
 bool is_few(int64_t m, int64_t n, int64_t k) { return m <= 64 && (n >= 4096 || k <= (m <= 16 ? 32768 : 8192)); }
 
+// Time of a product's tiles, to choose among them: us, from how many of them there are to a CU and the stages of k that each has.  A
+// workgroup of 64 by 64 shares its CU with three others; larger ones have it to themselves and come in rounds, and where they don't
+// fill the first the rest run faster (less to load, a higher clock).  Coefficients by least squares from 107 products, m 100 to 65536, n 13
+// to 4096 and k 256 to 65536, each with every side and up to 12 numbers of slices (a tenth off, on the average): the plan that
+// it takes is 0.7 % slower than the fastest one measured, geometric mean, 17 % at most.  Sides of 64, 128 and 256, best slices of each:
+// 1024 x 1024 x 1024 5.1, 6.5 and 10.1 us; 1024 x 1024 x 16384 26.9 (3 slices), 24.1 (3) and 31.4 (10); 2048 x 2048 x 4096 20.0, 15.8
+// and 25.1; 3000 x 3000 x 4096 47.4, 41.0 and 31.9; 4096 x 4096 x 4096 77.4, 55.9 and 39.1.
+double matmul_us(int tile, double per_cu, double stages)
+{
+    if (tile == 64) return 2.1 + 0.54 * per_cu + stages * std::max(0.60, 0.27 * per_cu);
+    const double rounds = std::ceil(per_cu);
+    const auto us = [&](double once, double round, double full, double alone) {
+        return once + round * rounds + stages * (per_cu > 1 ? full * rounds : full * per_cu + alone * (1 - per_cu));
+    };
+    return tile == 128 ? us(1.7, 2.8, 0.70, 0.49) : us(6.5, 0.0, 1.75, 1.16);
+}
+
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
     if (is_few(m, n, k)) return MatmulPlan{0, 1, 0};
     const int64_t cus = num_cus(), stages = std::max<int64_t>(1, ceil_div(groups_of(k), 2));
-    const auto tiles = [&](int64_t t) { return std::max<int64_t>(1, ceil_div(m, t) * ceil_div(n, t)); };
-    MatmulPlan p{};
-    // The largest tile of which there is one to (nearly) each CU; tiles of 128 also where k can be cut until there is.  Sides of 256, 128
-    // and 64: 8192 x 2048 x 2048 24, 34 and 36 us; 2048 x 2048 x 8192 48, 26 and 35; 8192 x 512 x 415 9.0, 5.8 and 6.1; 1024 x 1024 x 1024
-    // 9.8, 5.8 and 4.4.
-    if (tiles(256) * 8 >= cus * 7)
-        p.tile = 256;
-    else if (tiles(128) * 4 >= cus * 3 || (tiles(64) < cus && tiles(128) * stages >= cus * kMinStages))
-        p.tile = 128;
-    else
-        p.tile = 64;
-    const int64_t slices = std::max<int64_t>(1, std::min(cus / tiles(p.tile), stages / kMinStages));
-    p.stages_per_slice = (unsigned)ceil_div(ceil_div(stages, slices), 2) * 2; // (a slice begins with a pair of stages' scales)
-    p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
-    return p;
+    MatmulPlan best{};
+    double least = 0;
+    for (int tile : {64, 128, 256})
+        for (int slices : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32}) {
+            const int64_t tiles = std::max<int64_t>(1, ceil_div(m, tile) * ceil_div(n, tile));
+            if ((tile < 256 && tiles > kMaxBlocks) || (slices > 1 && (tiles * slices > 4 * cus || stages < 2 * slices))) break;
+            MatmulPlan p{tile, 1, (unsigned)stages};
+            if (slices > 1) {
+                p.stages_per_slice = (unsigned)ceil_div(ceil_div(stages, slices), 2) * 2; // (a slice begins with a pair of stages' scales)
+                p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
+            }
+            double us = matmul_us(tile, (double)(tiles * p.slices) / (double)cus, p.stages_per_slice);
+            if (p.slices > 1) us += 3.1 + 0.45e-6 * sizeof(float) * p.slices * (double)m * (double)n; // partial sums: another launch, their bytes
+            if (best.tile == 0 || us < least) best = p, least = us;
+        }
+    return best;
 }
 
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k)
