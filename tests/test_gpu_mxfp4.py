@@ -219,6 +219,30 @@ def test_product(shape, dtype):
         assert torch.equal(out._base.nan_to_num(7.0), around.nan_to_num(7.0))
 
 
+@pytest.mark.parametrize("shape", [(130, 70, 40000), (70, 600, 33333), (520, 367, 60001), (1030, 770, 40100), (2048, 1000, 60001), (3000, 1100, 700)])
+def test_product_of_long_sums_and_of_more_tiles(shape):
+    """Slices of k for every side of the tiles, the last one shorter; the plain product in 64 bits on the GPU."""
+    dq = _dq()
+    m, n, k = shape
+    _said("long product", shape)
+    gen = torch.Generator("cuda").manual_seed(m + n + k)
+    held = []
+    for rows in (m, n):
+        x = torch.randn((rows, k), device="cuda", generator=gen) * 0.25
+        q = dq.MxMatrix(rows, k, "cuda")
+        dq.dqrm_mxfp4_quant(x, q)
+        dq.dqrm_mxfp4_dequant(q, x)
+        held.append((q, x.double()))
+    (a, av), (b, bv) = held
+    bias = torch.randn(n, device="cuda", generator=gen)
+    out = torch.full((m, n), float("nan"), device="cuda")
+    dq.dqrm_mxfp4_matmul(a, b, out, bias=bias, relu=True, workspace=_workspace(dq.dqrm_mxfp4_matmul_workspace_bytes(m, n, k)))
+    want = (av @ bv.T + bias.double()).clamp_min(0.0)
+    size = av.abs() @ bv.abs().T + bias.double().abs()
+    bound = (k / 64 + 40) * 2.0 ** -22 * size + 1.01 * HALF_ULP["f32"] * want + TINY["f32"]
+    assert bool(((out.double() - want).abs() <= bound).all()), (shape, float((out.double() - want).abs().max()))
+
+
 @pytest.mark.parametrize("shape", [(3, 70, 300), (200, 150, 600), (40, 30, 9000)])
 def test_product_keeps_nans_to_the_rows_that_hold_them(shape):
     dq = _dq()
