@@ -213,10 +213,15 @@ size_t norm_bwd_workspace(int64_t rows, int64_t cols) { return align_up((size_t)
 
 using Tile256 = TileShape<4, 2, 2, 4, 2>;
 using Tile128 = TileShape<2, 1, 2, 4, 4>;
+using TilePair = TileShape<2, 2, 2, 2, 2>; // two to a CU
 using Tile64 = TileShape<1, 1, 2, 2, 2>;
 
+enum class Tiles { few, by64, by128, by128_pair, by256 }; // few: few_kernel
+
+int side_of(Tiles t) { return t == Tiles::by256 ? 256 : t == Tiles::by64 ? 64 : 128; }
+
 struct MatmulPlan {
-    int tile;        // 256, 128 or 64; 0: few_kernel
+    Tiles tiles;
     unsigned slices; // of k
     unsigned stages_per_slice;
 };
@@ -226,41 +231,45 @@ struct MatmulPlan {
 // 64 x 256 x 16384 12.2 and 8.4.
 bool is_few(int64_t m, int64_t n, int64_t k) { return m <= 64 && (n >= 4096 || k <= (m <= 16 ? 32768 : 8192)); }
 
-// Time of a product's tiles, to choose among them: us, from how many of them there are to a CU and the stages of k that each has.  A
-// workgroup of 64 by 64 shares its CU with three others; larger ones have it to themselves and come in rounds, and where they don't
-// fill the first the rest run faster (less to load, a higher clock).  Coefficients by least squares from 107 products, m 100 to 65536, n 13
-// to 4096 and k 256 to 65536, each with every side and up to 12 numbers of slices (a tenth off, on the average): the plan that
-// it takes is 0.7 % slower than the fastest one measured, geometric mean, 17 % at most.  Sides of 64, 128 and 256, best slices of each:
-// 1024 x 1024 x 1024 5.1, 6.5 and 10.1 us; 1024 x 1024 x 16384 26.9 (3 slices), 24.1 (3) and 31.4 (10); 2048 x 2048 x 4096 20.0, 15.8
-// and 25.1; 3000 x 3000 x 4096 47.4, 41.0 and 31.9; 4096 x 4096 x 4096 77.4, 55.9 and 39.1.
-double matmul_us(int tile, double per_cu, double stages)
+// Time of a product's tiles, to choose among them: us, from how many of them there are to a CU and the stages of k that each has.
+// Sides of 64: four workgroups to a CU.  128: two that have the least to read from LDS and hide each other's waits (by128_pair), or
+// one whose loads are further ahead, for long sums of few tiles (by128).  256: one; the least to load of all.  Where
+// workgroups don't fill the CUs the rest run faster (less to load, a higher clock).  The coefficients are from 112 products, m 100 to
+// 65536, n 13 to 4096 and k 256 to 65536, each with every side and up to 12 numbers of slices: the plan that it takes is 0.8 % slower
+// than the fastest one measured, geometric mean, 18 % at most.  64, 128, 128 in pairs and 256, best slices of each:
+// 4096 x 2048 x 4096 39.8, 29.6, 23.9 and 27.3 us; 4096 x 4096 x 4096 77.8, 58.0, 46.0 and 39.2; 8192 x 512 x 16384 91.6, 56.1, 69.1 and
+// 69.1; without pairs 1024 x 1024 x 1024 5.1, 6.5 and 10.1; 1024 x 1024 x 16384 26.9 (3 slices), 24.1 (3) and 31.4 (10).
+double matmul_us(Tiles shape, double per_cu, double stages)
 {
-    if (tile == 64) return 2.1 + 0.54 * per_cu + stages * std::max(0.60, 0.27 * per_cu);
-    const double rounds = std::ceil(per_cu);
-    const auto us = [&](double once, double round, double full, double alone) {
-        return once + round * rounds + stages * (per_cu > 1 ? full * rounds : full * per_cu + alone * (1 - per_cu));
-    };
-    return tile == 128 ? us(1.7, 2.8, 0.70, 0.49) : us(6.5, 0.0, 1.75, 1.16);
+    const double rounds = std::ceil(per_cu), part = std::min(per_cu, 1.0);
+    switch (shape) {
+    case Tiles::by128: return 1.57 + 2.94 * rounds + stages * (per_cu > 1 ? 0.72 * rounds : 0.72 * part + 0.50 * (1 - part));
+    case Tiles::by128_pair:
+        return 2.35 + 1.12 * per_cu +
+               stages * (per_cu > 2 ? 1.20 * std::ceil(per_cu / 2) : per_cu > 1 ? 0.98 + 0.22 * (per_cu - 1) : 0.98 * part + 0.85 * (1 - part));
+    case Tiles::by256: return 8.72 + 0.21 * rounds + stages * (per_cu > 1 ? 1.77 * rounds : 1.77 * part + 1.06 * (1 - part));
+    default: return 2.11 + 0.55 * per_cu + stages * std::max(0.60, 0.28 * per_cu);
+    }
 }
 
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
-    if (is_few(m, n, k)) return MatmulPlan{0, 1, 0};
+    if (is_few(m, n, k)) return MatmulPlan{Tiles::few, 1, 0};
     const int64_t cus = num_cus(), stages = std::max<int64_t>(1, ceil_div(groups_of(k), 2));
     MatmulPlan best{};
     double least = 0;
-    for (int tile : {64, 128, 256})
+    for (Tiles shape : {Tiles::by64, Tiles::by128, Tiles::by128_pair, Tiles::by256})
         for (int slices : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32}) {
-            const int64_t tiles = std::max<int64_t>(1, ceil_div(m, tile) * ceil_div(n, tile));
-            if ((tile < 256 && tiles > kMaxBlocks) || (slices > 1 && (tiles * slices > 4 * cus || stages < 2 * slices))) break;
-            MatmulPlan p{tile, 1, (unsigned)stages};
+            const int64_t side = side_of(shape), tiles = std::max<int64_t>(1, ceil_div(m, side) * ceil_div(n, side));
+            if ((side < 256 && tiles > kMaxBlocks) || (slices > 1 && (tiles * slices > 4 * cus || stages < 2 * slices))) break;
+            MatmulPlan p{shape, 1, (unsigned)stages};
             if (slices > 1) {
                 p.stages_per_slice = (unsigned)ceil_div(ceil_div(stages, slices), 2) * 2; // (a slice begins with a pair of stages' scales)
                 p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
             }
-            double us = matmul_us(tile, (double)(tiles * p.slices) / (double)cus, p.stages_per_slice);
-            if (p.slices > 1) us += 3.1 + 0.45e-6 * sizeof(float) * p.slices * (double)m * (double)n; // partial sums: another launch, their bytes
-            if (best.tile == 0 || us < least) best = p, least = us;
+            double us = matmul_us(shape, (double)(tiles * p.slices) / (double)cus, p.stages_per_slice);
+            if (p.slices > 1) us += 3.3 + 0.46e-6 * sizeof(float) * p.slices * (double)m * (double)n; // partial sums: another launch, their bytes
+            if (best.slices == 0 || us < least) best = p, least = us;
         }
     return best;
 }
@@ -279,12 +288,12 @@ void launch_tiles(const MatmulPlan &p, MatmulArgs g, hipStream_t st)
         g.tiles_m = (unsigned)ceil_div(g.m, S::BM), g.tiles_n = (unsigned)ceil_div(g.n, S::BN);
         hipLaunchKernelGGL((matmul_kernel<T, S>), dim3(g.tiles_m * g.tiles_n * g.slices), dim3(S::waves * kWaveSize), 0, st, g);
     };
-    if (p.tile == 256)
-        go(Tile256{});
-    else if (p.tile == 128)
-        go(Tile128{});
-    else
-        go(Tile64{});
+    switch (p.tiles) {
+    case Tiles::by256: return go(Tile256{});
+    case Tiles::by128: return go(Tile128{});
+    case Tiles::by128_pair: return go(TilePair{});
+    default: return go(Tile64{});
+    }
 }
 
 constexpr int64_t kMaxInner = 1 << 24; // a tile's rows of codes are addressed with 32 bits
@@ -321,8 +330,8 @@ void launch_few(const FewArgs &a, hipStream_t st)
 int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t st)
 {
     const MatmulPlan p = matmul_plan(g.m, g.n, g.k);
-    if (p.tile > 0 && ceil_div(g.m, p.tile) * ceil_div(g.n, p.tile) > kMaxBlocks) return DQRM_ERR_UNSUPPORTED;
-    if (p.tile == 0) {
+    if (p.tiles != Tiles::few && ceil_div(g.m, side_of(p.tiles)) * ceil_div(g.n, side_of(p.tiles)) > kMaxBlocks) return DQRM_ERR_UNSUPPORTED;
+    if (p.tiles == Tiles::few) {
         FewArgs a{};
         a.g = g;
         with_type(dtype, [&](auto t) {

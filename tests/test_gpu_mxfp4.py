@@ -219,7 +219,7 @@ def test_product(shape, dtype):
         assert torch.equal(out._base.nan_to_num(7.0), around.nan_to_num(7.0))
 
 
-@pytest.mark.parametrize("shape", [(130, 70, 40000), (70, 600, 33333), (520, 367, 60001), (1030, 770, 40100), (2048, 1000, 60001), (3000, 1100, 700)])
+@pytest.mark.parametrize("shape", [(130, 70, 40000), (70, 600, 33333), (520, 367, 60001), (1030, 770, 40100), (2048, 1000, 60001), (4000, 1000, 65000), (3000, 1100, 700)])
 def test_product_of_long_sums_and_of_more_tiles(shape):
     """Slices of k for every side of the tiles, the last one shorter; the plain product in 64 bits on the GPU."""
     dq = _dq()
