@@ -154,12 +154,13 @@ void with_norm_fwd_shape(int64_t cols, F f)
 }
 
 // (16001 x 8190 bfloat16: 512 threads with two chunks 141 us, 1024 with one 166; 64000 x 2047: 128 threads with two chunks 150 us, 256 with
-// one 201)
+// one 201; 8000 x 8200: 512 threads with three chunks 78 us, 1024 with two 126; 8000 x 16000: 512 with four, though some of the compiler's
+// registers are in memory then, 153 us, 1024 with two, and the next row not ahead, 197)
 template <typename F>
 void with_norm_bwd_shape(int64_t cols, F f)
 {
     with_first_that_holds<NormShape<16, 1, 1024>, NormShape<64, 1, 1024>, NormShape<64, 2, 512>, NormShape<128, 2, 512>, NormShape<256, 2, 512>,
-                          NormShape<512, 2, 512>, NormShape<1024, 2, 1024>>(cols, f);
+                          NormShape<512, 2, 512>, NormShape<512, 3, 512>, NormShape<512, 4, 512>>(cols, f);
 }
 
 void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)

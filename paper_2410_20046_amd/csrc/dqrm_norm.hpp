@@ -191,7 +191,6 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 {
     using T = elem_t<DT>;
     constexpr int rows_per_block = BLOCK / TPR;
-    constexpr bool ahead = TPR * CH < 2048; // (rows longer than that take all registers)
     __shared__ float s_part[2][BLOCK / kWaveSize][2];
     const int t = threadIdx.x % TPR;
     const int cols = (int)a.cols;
@@ -211,14 +210,13 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
             next_x[j] = load_raw(static_cast<const T *>(a.x) + q * a.ldx, column(j), cols);
         }
     };
-    if (ahead) request(r);
-    float dg[CH][kChunk] = {}, db[CH][kChunk] = {}, gamma[ahead ? CH : 1][kChunk];
+    request(r);
+    float dg[CH][kChunk] = {}, db[CH][kChunk] = {}, gamma[CH][kChunk];
 #pragma unroll
-    for (int j = 0; ahead && j < CH; ++j) load_gain(a.gamma, column(j), cols, 1.0f, gamma[j]);
+    for (int j = 0; j < CH; ++j) load_gain(a.gamma, column(j), cols, 1.0f, gamma[j]);
     int turn = 0;
     for (; r - threadIdx.x / TPR < a.rows; r += step) {
         const bool own = r < a.rows;
-        if (!ahead) request(r);
         const float mean = next_mean, rstd = next_rstd;
         float dy[CH][kChunk], xh[CH][kChunk];
         float s[2] = {0.0f, 0.0f};
@@ -227,7 +225,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
             values_of(next_dy[j], column(j), cols, dy[j]);
             values_of(next_x[j], column(j), cols, xh[j]);
         }
-        if (ahead) request(r + step);
+        request(r + step);
         if (own) {
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
@@ -237,12 +235,11 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 #pragma unroll
                     for (int i = 0; i < kChunk; ++i) xh[j][i] = column(j) + i < cols ? xh[j][i] : 0.0f;
                 }
-                if (!ahead) load_gain(a.gamma, column(j), cols, 1.0f, gamma[0]);
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) {
                     dg[j][i] += dy[j][i] * xh[j][i];
                     db[j][i] += dy[j][i];
-                    dy[j][i] *= gamma[ahead ? j : 0][i];
+                    dy[j][i] *= gamma[j][i];
                     s[0] += dy[j][i];
                     s[1] += dy[j][i] * xh[j][i];
                 }
