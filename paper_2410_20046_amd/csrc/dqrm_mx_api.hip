@@ -146,19 +146,38 @@ void with_first_that_holds(int64_t cols, F f)
     (void)((cols <= S::cols ? (f(S{}), true) : false) || ...);
 }
 
-template <typename F>
-void with_norm_fwd_shape(int64_t cols, F f)
+// 16-bit types with this many values: shapes of which a row leaves few threads without values.  Those have more chunks to a
+// thread or more rows to a workgroup, whose latency few rows don't hide, and 32-bit rows have bytes enough.  Forward, the shapes below
+// for many values and the others: 8000 x 8200 52 and 79 us, 32000 x 1200 31 and 49, 100000 x 300 30 and 38, 500 x 300 4.9 and 3.5; in float
+// 32000 x 1200 62 and 50.
+constexpr int64_t kNormMany = 1 << 22;
+
+template <int DT, typename F>
+void with_norm_fwd_shape(int64_t rows, int64_t cols, F f)
 {
+    if constexpr (DT != DQRM_F32) {
+        if (rows * cols >= kNormMany)
+            return with_first_that_holds<NormShape<16, 1, 256>, NormShape<16, 2, 256>, NormShape<16, 3, 256>, NormShape<64, 1, 256>, NormShape<64, 2, 256>,
+                                         NormShape<64, 3, 256>, NormShape<128, 2, 256>, NormShape<128, 3, 256>, NormShape<256, 2, 256>,
+                                         NormShape<256, 3, 256>, NormShape<512, 2, 512>, NormShape<512, 3, 512>, NormShape<1024, 2, 1024>>(cols, f);
+    }
     with_first_that_holds<NormShape<16, 1, 256>, NormShape<64, 1, 256>, NormShape<64, 2, 256>, NormShape<256, 1, 256>, NormShape<256, 2, 256>,
                           NormShape<512, 2, 512>, NormShape<1024, 2, 1024>>(cols, f);
 }
 
 // (16001 x 8190 bfloat16: 512 threads with two chunks 141 us, 1024 with one 166; 64000 x 2047: 128 threads with two chunks 150 us, 256 with
 // one 201; 8000 x 8200: 512 threads with three chunks 78 us, 1024 with two 126; 8000 x 16000: 512 with four, though some of the compiler's
-// registers are in memory then, 153 us, 1024 with two, and the next row not ahead, 197)
-template <typename F>
-void with_norm_bwd_shape(int64_t cols, F f)
+// registers are in memory then, 153 us, 1024 with two, and the next row not ahead, 197.  The shapes for many values and the others: 16000 x
+// 4100 79 and 106 us, 16000 x 1200 26 and 32, 4000 x 300 9.5 and 7.9; in float 16000 x 4100 168 and 156)
+template <int DT, typename F>
+void with_norm_bwd_shape(int64_t rows, int64_t cols, F f)
 {
+    if constexpr (DT != DQRM_F32) {
+        if (rows * cols >= kNormMany)
+            return with_first_that_holds<NormShape<16, 1, 1024>, NormShape<16, 2, 512>, NormShape<16, 3, 512>, NormShape<64, 1, 1024>, NormShape<64, 2, 512>,
+                                         NormShape<64, 3, 512>, NormShape<128, 2, 512>, NormShape<128, 3, 512>, NormShape<256, 2, 512>,
+                                         NormShape<256, 3, 512>, NormShape<512, 2, 512>, NormShape<512, 3, 512>, NormShape<512, 4, 512>>(cols, f);
+    }
     with_first_that_holds<NormShape<16, 1, 1024>, NormShape<64, 1, 1024>, NormShape<64, 2, 512>, NormShape<128, 2, 512>, NormShape<256, 2, 512>,
                           NormShape<512, 2, 512>, NormShape<512, 3, 512>, NormShape<512, 4, 512>>(cols, f);
 }
@@ -182,7 +201,7 @@ void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
                 hipLaunchKernelGGL(norm_fwd_long_kernel<DT>, dim3((unsigned)b.rows), dim3(256), 0, st, b);
                 return;
             }
-            with_norm_fwd_shape(a.cols, [&](auto shape) {
+            with_norm_fwd_shape<DT>(a.rows, a.cols, [&](auto shape) {
                 using S = decltype(shape);
                 // as many workgroups as the chip holds: each keeps its columns' gain and offset for all of its rows
                 const int64_t most = (int64_t)num_cus() * (4 * 4 * kWaveSize / S::BLOCK);
@@ -198,17 +217,24 @@ void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
 // 64 x 512 7.27 and 5.91).
 constexpr int64_t kNormAlone = 2;
 
-int norm_bwd_blocks(int64_t rows, int64_t cols)
+int norm_bwd_blocks(int32_t dtype, int64_t rows, int64_t cols)
 {
     if (rows < 1 || cols < 1) return 0;
     if (!norm_in_registers(cols)) return (int)std::min<int64_t>(ceil_div(rows, 32), 64);
     int64_t n = 0;
     // (one to a CU: twice as many write and join twice the partial sums, 145 instead of 141 us for 16001 x 8190)
-    with_norm_bwd_shape(cols, [&](auto shape) { n = std::min<int64_t>(ceil_div(rows, decltype(shape)::rows), num_cus()); });
+    with_type(dtype, [&](auto t) {
+        with_norm_bwd_shape<decltype(t)::value>(rows, cols, [&](auto shape) { n = std::min<int64_t>(ceil_div(rows, decltype(shape)::rows), num_cus()); });
+    });
     return n <= kNormAlone ? 1 : (int)n;
 }
 
-size_t norm_bwd_workspace(int64_t rows, int64_t cols) { return align_up((size_t)norm_bwd_blocks(rows, cols) * 2 * (size_t)cols * sizeof(float), 256); }
+// (of any type)
+size_t norm_bwd_workspace(int64_t rows, int64_t cols)
+{
+    const int blocks = std::max(norm_bwd_blocks(DQRM_F32, rows, cols), norm_bwd_blocks(DQRM_BF16, rows, cols));
+    return align_up((size_t)blocks * 2 * (size_t)cols * sizeof(float), 256);
+}
 
 // ---- products --------------------------------------------------------------------------------------------------------------
 
@@ -581,7 +607,7 @@ int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void
         DQRM_HIP_CHECK(hipGetLastError());
         return DQRM_OK;
     }
-    const int blocks = norm_bwd_blocks(rows, cols);
+    const int blocks = norm_bwd_blocks(dtype, rows, cols);
     float *partial = static_cast<float *>(workspace);
     NormBwdArgs a{dy, x, lddy, ldx, rows, cols, mean, rstd, gamma, dx, lddx, nullptr, nullptr, 0};
     if (dgamma && blocks > 1)
@@ -591,7 +617,7 @@ int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void
     with_type(dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
         if (norm_in_registers(cols)) {
-            with_norm_bwd_shape(cols, [&](auto shape) {
+            with_norm_bwd_shape<DT>(rows, cols, [&](auto shape) {
                 using S = decltype(shape);
                 hipLaunchKernelGGL((norm_bwd_kernel<DT, S::TPR, S::CH, S::BLOCK>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, st, a);
             });

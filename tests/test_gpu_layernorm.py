@@ -85,6 +85,38 @@ def test_forward(shape, dtype):
         assert torch.equal(y._base.nan_to_num(7.0), around.nan_to_num(7.0))
 
 
+@pytest.mark.parametrize("cols", [100, 250, 384, 500, 1024, 1500, 2048, 2500, 4096, 5001, 8191, 10001, 16384])
+def test_many_values_of_16_bits(cols):
+    """The ways that a row is laid over threads where there are many values; the plain form in 64 bits on the GPU."""
+    dq = _dq()
+    dtype = "bf16" if cols % 2 else "f16"
+    R = (1 << 22) // cols + 5
+    print("norm of many values", (R, cols), dtype, flush=True)
+    gen = torch.Generator("cuda").manual_seed(cols)
+    rand = lambda *s: torch.randn(s, device="cuda", generator=gen)
+    x, dy = (rand(R, cols) * 2 + 1).to(TYPES[dtype]), rand(R, cols).to(TYPES[dtype])
+    g, b = 1 + 0.4 * rand(cols), rand(cols)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd, dgamma, dbeta = torch.empty(R, device="cuda"), torch.empty(R, device="cuda"), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    dq.dqrm_layernorm_fwd(x, g, b, EPS, y=y, mean=mean, rstd=rstd)
+    ws = torch.full((dq.dqrm_layernorm_bwd_workspace_bytes(R, cols),), 0xFF, dtype=torch.uint8, device="cuda")
+    dq.dqrm_layernorm_bwd(dy, x, mean, rstd, g, dx, dgamma, dbeta, ws)
+    # some of the rows, the last ones among them, against the bounds of each value
+    at = torch.cat([torch.arange(0, R, max(R // 40, 1)), torch.arange(R - 8, R)]).cuda()
+    xv, dyv, gv = f64(x[at]), f64(dy[at]), f64(g)
+    want, m, r = ref.norm(xv, gv, f64(b), EPS)
+    b_mean, b_rstd, b_y = _forward_bounds(xv, gv, f64(b), want, m, r, dtype)
+    assert np.all(np.abs(f64(mean[at]) - m) <= b_mean) and np.all(np.abs(f64(rstd[at]) - r) <= b_rstd) and np.all(np.abs(f64(y[at]) - want) <= b_y)
+    wdx, _, _ = ref.norm_backward(dyv, xv, f64(mean[at]), f64(rstd[at]), gv)
+    b_dx, _, _ = backward_bounds(dyv, xv, f64(mean[at]), f64(rstd[at]), gv, wdx, dtype, 0)
+    assert np.all(np.abs(f64(dx[at]) - wdx) <= b_dx)
+    # every row is in the sums
+    xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    chain = min(R, 64) + R / 64 + 64
+    for got, terms in ((dgamma, dy.double() * xh), (dbeta, dy.double())):
+        assert bool(((got.double() - terms.sum(0)).abs() <= 1.01 * (chain + 3) * ULP * terms.abs().sum(0) + 1e-45).all())
+
+
 @pytest.mark.parametrize("cols", [5, 200, 3000, 20000])
 def test_rows_of_one_value_and_rows_that_are_not_finite(cols):
     dq = _dq()
