@@ -134,6 +134,13 @@ void launch_quant_rows(int32_t dtype, QuantArgs a, hipStream_t st)
 // Rows of 8 to 16384 values stay in registers; others are read more than once (shorter ones have no vector of 8).
 bool norm_in_registers(int64_t cols) { return cols >= kChunk && cols <= 16384; }
 
+// threads of such another row
+template <typename F>
+void with_norm_long_block(int64_t cols, F f)
+{
+    cols < kChunk ? f(std::integral_constant<int, kWaveSize>{}) : f(std::integral_constant<int, 1024>{});
+}
+
 // How a row that stays in registers is laid over threads: f(shape) for the narrowest one that holds it.
 template <int TPR_, int CH_, int BLOCK_>
 struct NormShape {
@@ -198,7 +205,10 @@ void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
         with_type(dtype, [&](auto t) {
             constexpr int DT = decltype(t)::value;
             if (!in_registers) {
-                hipLaunchKernelGGL(norm_fwd_long_kernel<DT>, dim3((unsigned)b.rows), dim3(256), 0, st, b);
+                with_norm_long_block(a.cols, [&](auto block) {
+                    constexpr int BLOCK = decltype(block)::value;
+                    hipLaunchKernelGGL((norm_fwd_long_kernel<DT, BLOCK>), dim3((unsigned)b.rows), dim3(BLOCK), 0, st, b);
+                });
                 return;
             }
             with_norm_fwd_shape<DT>(a.rows, a.cols, [&](auto shape) {
@@ -220,7 +230,8 @@ constexpr int64_t kNormAlone = 2;
 int norm_bwd_blocks(int32_t dtype, int64_t rows, int64_t cols)
 {
     if (rows < 1 || cols < 1) return 0;
-    if (!norm_in_registers(cols)) return (int)std::min<int64_t>(ceil_div(rows, 32), 64);
+    // (a short row's columns are one thread's)
+    if (!norm_in_registers(cols)) return (int)std::min<int64_t>(ceil_div(rows, 32), cols < kChunk ? 1024 : 64);
     int64_t n = 0;
     // (one to a CU: twice as many write and join twice the partial sums, 145 instead of 141 us for 16001 x 8190)
     with_type(dtype, [&](auto t) {
@@ -624,16 +635,23 @@ int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void
             return;
         }
         // (the columns' sums first: dx may be dy's or x's own memory)
-        if (dgamma)
-            hipLaunchKernelGGL(norm_bwd_columns_kernel<DT>, dim3((unsigned)ceil_div(cols, 256 * kChunk), (unsigned)blocks), dim3(256), 0, st, a,
-                               ceil_div(rows, blocks));
+        if (dgamma) {
+            const dim3 grid((unsigned)ceil_div(cols, 256 * kChunk), (unsigned)blocks);
+            if (cols < kChunk)
+                hipLaunchKernelGGL((norm_bwd_columns_kernel<DT, true>), grid, dim3(256), 0, st, a, ceil_div(rows, blocks));
+            else
+                hipLaunchKernelGGL((norm_bwd_columns_kernel<DT, false>), grid, dim3(256), 0, st, a, ceil_div(rows, blocks));
+        }
         const size_t es = size_of(dtype);
         for (int64_t r0 = 0; dx && r0 < rows; r0 += kMaxBlocks) {
             NormBwdArgs b = a;
             b.rows = std::min(kMaxBlocks, rows - r0);
             b.dy = static_cast<const char *>(dy) + r0 * lddy * es, b.x = static_cast<const char *>(x) + r0 * ldx * es;
             b.dx = static_cast<char *>(dx) + r0 * lddx * es, b.mean = mean + r0, b.rstd = rstd + r0;
-            hipLaunchKernelGGL(norm_bwd_long_kernel<DT>, dim3((unsigned)b.rows), dim3(256), 0, st, b);
+            with_norm_long_block(cols, [&](auto block) {
+                constexpr int BLOCK = decltype(block)::value;
+                hipLaunchKernelGGL((norm_bwd_long_kernel<DT, BLOCK>), dim3((unsigned)b.rows), dim3(BLOCK), 0, st, b);
+            });
         }
     });
     if (dgamma && blocks > 1) join_columns(partial, 2 * cols, blocks, cols, dgamma, dbeta, st);

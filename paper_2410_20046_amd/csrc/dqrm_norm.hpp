@@ -131,21 +131,21 @@ __global__ __launch_bounds__(BLOCK, 4) void norm_fwd_kernel(NormArgs a)
 }
 
 // Rows of any length, a workgroup to each: three passes over the row.
-template <int DT>
-__global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
+template <int DT, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void norm_fwd_long_kernel(NormArgs a)
 {
     using T = elem_t<DT>;
-    __shared__ float s_part[2][4][1];
+    __shared__ float s_part[2][BLOCK / kWaveSize][1];
     const int64_t r = blockIdx.x;
     const T *row = static_cast<const T *>(a.x) + r * a.ldx;
-    const int64_t step = 256 * kChunk, end = groups_of(a.cols) * kRowPad;
+    const int64_t step = BLOCK * kChunk, end = groups_of(a.cols) * kRowPad;
     float sum[1] = {0.0f}, sq[1] = {0.0f};
     float x[kChunk];
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += step) {
         load_chunk(row, c, a.cols, x);
         sum[0] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
     }
-    row_sums<256>(sum, s_part[0]);
+    row_sums<BLOCK>(sum, s_part[0]);
     const float mean = sum[0] / (float)a.cols;
     for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += step) {
         load_chunk(row, c, a.cols, x);
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256) void norm_fwd_long_kernel(NormArgs a)
         for (int i = 0; i < kChunk; ++i) q += c + i < a.cols ? (x[i] - mean) * (x[i] - mean) : 0.0f;
         sq[0] += q;
     }
-    row_sums<256>(sq, s_part[1]);
+    row_sums<BLOCK>(sq, s_part[1]);
     const float rstd = 1.0f / sqrtf(sq[0] / (float)a.cols + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[r] = mean;
@@ -292,17 +292,17 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 }
 
 // Rows of any length: dx from two passes over the row, a workgroup to each.
-template <int DT>
-__global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
+template <int DT, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void norm_bwd_long_kernel(NormBwdArgs a)
 {
     using T = elem_t<DT>;
-    __shared__ float s_part[4][2];
+    __shared__ float s_part[BLOCK / kWaveSize][2];
     const int64_t r = blockIdx.x;
     const float mean = a.mean[r], rstd = a.rstd[r], inv_n = 1.0f / (float)a.cols;
     const T *pdy = static_cast<const T *>(a.dy) + r * a.lddy, *px = static_cast<const T *>(a.x) + r * a.ldx;
     float s[2] = {0.0f, 0.0f};
     float dy[kChunk], x[kChunk], g[kChunk];
-    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += 256 * kChunk) {
+    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += BLOCK * kChunk) {
         load_chunk(pdy, c, a.cols, dy);
         load_chunk(px, c, a.cols, x);
         load_gain(a.gamma, c, a.cols, 1.0f, g);
@@ -315,8 +315,8 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
         }
         s[0] += s0, s[1] += s1;
     }
-    row_sums<256>(s, s_part);
-    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += 256 * kChunk) {
+    row_sums<BLOCK>(s, s_part);
+    for (int64_t c = (int64_t)threadIdx.x * kChunk; c < a.cols; c += BLOCK * kChunk) {
         load_chunk(pdy, c, a.cols, dy);
         load_chunk(px, c, a.cols, x);
         load_gain(a.gamma, c, a.cols, 1.0f, g);
@@ -326,22 +326,44 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
     }
 }
 
-// ... and the sums over a slice of rows, eight columns to a thread.
-template <int DT>
+// ... and the sums over a slice of rows, eight columns to a thread, the loads of four rows on their way at a time (rows of fewer than 8
+// values: of one).
+template <int DT, bool SHORT>
 __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(NormBwdArgs a, int64_t rows_per_slice)
 {
     using T = elem_t<DT>;
+    constexpr int together = SHORT ? 1 : 4;
     const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * kChunk;
     if (c >= a.cols) return;
     const int64_t r0 = (int64_t)blockIdx.y * rows_per_slice, r1 = min(r0 + rows_per_slice, a.rows);
     float dg[kChunk] = {}, db[kChunk] = {};
-    for (int64_t r = r0; r < r1; ++r) {
-        const float mean = a.mean[r], rstd = a.rstd[r];
-        float dy[kChunk], x[kChunk];
-        load_chunk(static_cast<const T *>(a.dy) + r * a.lddy, c, a.cols, dy);
-        load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, x);
+    for (int64_t r = r0; r < r1; r += together) {
+        float dy[together][kChunk], x[together][kChunk], mean[together], rstd[together];
+        if constexpr (SHORT) {
+            load_chunk(static_cast<const T *>(a.dy) + r * a.lddy, c, a.cols, dy[0]);
+            load_chunk(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, x[0]);
+            mean[0] = a.mean[r], rstd[0] = a.rstd[r];
+        } else {
+            Raw<T> raw_dy[together], raw_x[together];
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) dg[i] += c + i < a.cols ? dy[i] * ((x[i] - mean) * rstd) : 0.0f, db[i] += dy[i];
+            for (int k = 0; k < together; ++k) {
+                const int64_t q = min(r + k, r1 - 1);
+                raw_dy[k] = load_raw(static_cast<const T *>(a.dy) + q * a.lddy, c, a.cols);
+                raw_x[k] = load_raw(static_cast<const T *>(a.x) + q * a.ldx, c, a.cols);
+                mean[k] = a.mean[q], rstd[k] = a.rstd[q];
+            }
+#pragma unroll
+            for (int k = 0; k < together; ++k) {
+                values_of(raw_dy[k], c, a.cols, dy[k]);
+                values_of(raw_x[k], c, a.cols, x[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < together; ++k) {
+            if (r + k >= r1) break;
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) dg[i] += c + i < a.cols ? dy[k][i] * ((x[k][i] - mean[k]) * rstd[k]) : 0.0f, db[i] += dy[k][i];
+        }
     }
     store_chunk(a.sum_gamma + blockIdx.y * a.block_stride, c, a.cols, dg);
     store_chunk(a.sum_beta + blockIdx.y * a.block_stride, c, a.cols, db);
