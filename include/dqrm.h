@@ -466,7 +466,8 @@ int32_t dqrm_mxfp4_dequant(const dqrm_mxfp4_t *q, int32_t dtype, void *out, int6
 /* out [m][n] = act(sum over k of a[m][k] b[n][k] + bias[n]), act = max(., 0) if relu (a NaN stays), rounded once to the
  * element type.  a->cols = b->cols = k; k = 0 gives act(bias).  With A by rows and B = W by rows it is a linear layer's
  * forward; with dY by rows and W by columns the input's gradient; with dY and X by columns the weights'.  bias: [n] fp32
- * or NULL.  The order of the sums depends on the shape alone.  out must not overlap the operands. */
+ * or NULL.  The order of the sums depends on the shape alone.  out must not overlap the operands.  k > 16777216 is
+ * DQRM_ERR_UNSUPPORTED, here and below. */
 size_t dqrm_mxfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int32_t dqrm_mxfp4_matmul(const dqrm_mxfp4_t *a, const dqrm_mxfp4_t *b, const float *bias, int32_t relu, int32_t dtype,
                           void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
@@ -494,7 +495,7 @@ int32_t dqrm_layernorm_fwd(int32_t dtype, int64_t rows, int64_t cols, const void
  *   dx = rstd (g - mean over the row of g - xhat mean over the row of (g xhat))   or NULL; may be dy's or x's own memory
  *   dgamma [cols] = sum over rows of dy xhat, dbeta [cols] = sum over rows of dy, fp32   both or neither (NULL)
  * dy, x, dx of one type; mean and rstd from the forward.  The workspace (256-byte aligned) is needed for dgamma and dbeta;
- * their order of addition depends on the shape alone.  rows = 0 gives zeros. */
+ * their order of addition depends on shape and type alone.  rows = 0 gives zeros. */
 size_t dqrm_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
 int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void *dy, int64_t lddy, const void *x,
                            int64_t ldx, const float *mean, const float *rstd, const float *gamma, void *dx, int64_t lddx,

@@ -278,7 +278,8 @@ __device__ __forceinline__ Vec8<T> load_gated(const QuantArgs &a, int64_t r, int
     return v;
 }
 
-// One chunk to a lane, rows' chunks one after another; per_row: chunks of a row, of fewer than 2^31 in all.
+// One chunk to a lane, rows' chunks one after another; per_row: chunks of a row, of fewer than 2^31 in all.  Bound by its bytes:
+// 8192 x 512 float (19 MB) 4.6 us, of which the launch and a read's latency are about 3.
 template <int DT>
 __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a, dqrm::FastDiv per_row)
 {
@@ -292,7 +293,9 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a, dqrm::Fast
 // ---- along columns, and both ways from one read ----------------------------------------------------------------------------
 // A workgroup takes 128 rows by 128 columns.  The chunks that its lanes load are blocks of rows already (four lanes to a block);
 // the tile then goes through LDS in its own type, and each wave takes 32 rows of it, two columns to a lane: a block of a column is
-// in one lane's registers.
+// in one lane's registers.  128 because a line of the columns' codes is 64 bytes of 128 values.  Bound by its bytes, then by the
+// columns' stores of half lines: 16384 x 8191 bfloat16 both ways (411 MB) 100 us, 4.1 TB/s, where a copy has 5.1; by rows alone
+// 8192 x 2048 with a gate and column sums 19 us (85 MB).
 constexpr int kTile = 128;
 
 template <int DT>
@@ -414,7 +417,7 @@ __device__ __forceinline__ float add_strided(float v, const float *p, int64_t st
 }
 
 // out[c] = sum over p of partial[p][c] (and a second pair of arrays behind it), in a fixed order: 16 lanes take every 16th each, then
-// their sums are added in turn.
+// their sums are added in turn.  The launch and two reads' latencies: 256 parts of 512 columns twice 2.8 us, of 8190 columns 8.
 __global__ __launch_bounds__(256) void join_columns_kernel(const float *partial, int64_t stride, int n, int64_t cols, float *out0, float *out1)
 {
     __shared__ float s[16][17];
@@ -442,7 +445,7 @@ __device__ __forceinline__ void unpack_codes(unsigned w, float scale, float (&v)
     v[4] = c.x * scale, v[5] = c.y * scale, v[6] = d.x * scale, v[7] = d.y * scale;
 }
 
-// per_row: chunks of a row that hold values, of fewer than 2^31 in all
+// per_row: chunks of a row that hold values, of fewer than 2^31 in all.  Bound by its bytes: 16384 x 8191 bfloat16 (340 MB) 62 us, 5.5 TB/s.
 template <int DT>
 __global__ __launch_bounds__(256) void dequant_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out, int64_t ldo,
                                                       dqrm::FastDiv per_row)

@@ -5,6 +5,9 @@
 // for no barrier): a load has whole lines of 4 rows, while the operands of v_mfma_scale_f32_16x16x128_f8f6f4 (lane l: row l % 16,
 // block l / 16 of 128 values) would have halves of 16 rows' lines; what a load costs the address unit is its lines.  The waves' sums
 // meet in LDS in a fixed order.
+//
+// 16 x 8192 x 8192 takes 11 us (36 MB of W, 3.2 TB/s; 16.4 with the operands' own loads): a workgroup has four units to a wave, and
+// the first one's latency and the launch are a third of it.  1 x 367 for 512 outputs, quantised within: 3.6 us, all latency.
 #pragma once
 
 #include "dqrm_mx_gemm.hpp"
