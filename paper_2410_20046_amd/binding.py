@@ -483,15 +483,23 @@ def dqrm_fwd_bwd_step(tables: Tables, bufs: StepBuffers, indices: torch.Tensor, 
 
 
 # (These run on every call, and a call on little data is as long as they are: no tuples, no formatting unless something is wrong.)
-def _matrix(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
-    """(dtype, address, row stride) of a matrix whose rows' elements lie one behind the other."""
-    dtype = _DTYPES.get(t.dtype)
-    if dtype is None or t.dim() != 2:
+def _kind(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
+    """(element type, rows, columns) of a matrix."""
+    dtype, shape = _DTYPES.get(t.dtype), t.shape
+    if dtype is None or len(shape) != 2:
         raise AssertionError(f"{what}: a matrix of float32, bfloat16 or float16")
+    return dtype, shape[0], shape[1]
+
+
+def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> Tuple[int, int]:
+    """(address, row stride) of a matrix of this kind whose rows' elements lie one behind the other."""
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise AssertionError(f"{what}: ({rows}, {cols}) of {dtype}, got {tuple(shape)} of {t.dtype}")
     ld, step = t.stride()
-    if step != 1 and t.shape[1] > 1:
+    if step != 1 and cols > 1:
         raise AssertionError(f"{what}: the elements of a row must be contiguous")
-    return dtype, t.data_ptr(), ld
+    return t.data_ptr(), ld
 
 
 def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
@@ -502,13 +510,12 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
     return t.data_ptr()
 
 
-def _like(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> None:
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise AssertionError(f"{what}: ({rows}, {cols}) of {dtype}, got {tuple(t.shape)} of {t.dtype}")
-
-
 def _space(ws: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
-    return (None, 0) if ws is None else (_ptr(ws), ws.nbytes)
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous():
+        raise AssertionError("workspace: contiguous memory")
+    return ws.data_ptr(), ws.nbytes
 
 
 def _stream_of(t: torch.Tensor, stream) -> Optional[int]:
@@ -529,7 +536,7 @@ class MxMatrix:
         self.codes = codes if codes is not None else byte(64 * groups)
         self.scales = scales if scales is not None else byte(4 * groups)
         for t, n in ((self.codes, 64 * groups), (self.scales, 4 * groups)):
-            _like(t, self.rows, n, torch.uint8, "MxMatrix")
+            _rows_of(t, self.rows, n, torch.uint8, "MxMatrix")
         self.c = dqrm_mxfp4_t(self.rows, self.cols, _ptr(self.codes), _ptr(self.scales))
         self.ref = C.byref(self.c)
 
@@ -545,18 +552,16 @@ def dqrm_mxfp4_quant_workspace_bytes(rows: int, cols: int) -> int:
 def dqrm_mxfp4_quant(x: torch.Tensor, by_rows: Optional[MxMatrix] = None, by_cols: Optional[MxMatrix] = None,
                      gate: Optional[torch.Tensor] = None, col_sums: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    dtype, p, ld = _matrix(x, "x")
-    pg, ldg = None, 0
-    if gate is not None:
-        _like(gate, *x.shape, x.dtype, "gate")
-        _, pg, ldg = _matrix(gate, "gate")
-    _check(lib().dqrm_mxfp4_quant(dtype, x.shape[0], x.shape[1], p, ld, pg, ldg, _mx(by_rows), _mx(by_cols),
-                                  _vector(col_sums, x.shape[1], "col_sums"), *_space(workspace), _stream_of(x, stream)), "dqrm_mxfp4_quant")
+    dtype, R, D = _kind(x, "x")
+    p, ld = _rows_of(x, R, D, x.dtype, "x")
+    pg, ldg = (None, 0) if gate is None else _rows_of(gate, R, D, x.dtype, "gate")
+    _check(lib().dqrm_mxfp4_quant(dtype, R, D, p, ld, pg, ldg, _mx(by_rows), _mx(by_cols),
+                                  _vector(col_sums, D, "col_sums"), *_space(workspace), _stream_of(x, stream)), "dqrm_mxfp4_quant")
 
 
 def dqrm_mxfp4_dequant(q: MxMatrix, out: torch.Tensor, stream=None) -> None:
-    _like(out, q.rows, q.cols, out.dtype, "out")
-    _check(lib().dqrm_mxfp4_dequant(q.ref, *_matrix(out, "out"), _stream_of(out, stream)), "dqrm_mxfp4_dequant")
+    dtype, _, _ = _kind(out, "out")
+    _check(lib().dqrm_mxfp4_dequant(q.ref, dtype, *_rows_of(out, q.rows, q.cols, out.dtype, "out"), _stream_of(out, stream)), "dqrm_mxfp4_dequant")
 
 
 def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -565,8 +570,9 @@ def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def dqrm_mxfp4_matmul(a: MxMatrix, b: MxMatrix, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    _like(out, a.rows, b.rows, out.dtype, "out")
-    _check(lib().dqrm_mxfp4_matmul(a.ref, b.ref, _vector(bias, b.rows, "bias"), relu, *_matrix(out, "out"), *_space(workspace),
+    dtype, _, _ = _kind(out, "out")
+    po, ldo = _rows_of(out, a.rows, b.rows, out.dtype, "out")
+    _check(lib().dqrm_mxfp4_matmul(a.ref, b.ref, _vector(bias, b.rows, "bias"), relu, dtype, po, ldo, *_space(workspace),
                                    _stream_of(out, stream)), "dqrm_mxfp4_matmul")
 
 
@@ -578,11 +584,9 @@ def dqrm_mxfp4_linear(x: torch.Tensor, w: MxMatrix, out: torch.Tensor, bias: Opt
                       gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: Optional[float] = None,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """``eps`` given: x goes through a layer norm (with ``gamma`` and ``beta`` if given) first."""
-    dtype, p, ld = _matrix(x, "x")
-    m = x.shape[0]
-    _like(x, m, w.cols, x.dtype, "x")
-    _like(out, m, w.rows, x.dtype, "out")
-    _, po, ldo = _matrix(out, "out")
+    dtype, m, _ = _kind(x, "x")
+    p, ld = _rows_of(x, m, w.cols, x.dtype, "x")
+    po, ldo = _rows_of(out, m, w.rows, x.dtype, "out")
     _check(lib().dqrm_mxfp4_linear(dtype, m, p, ld, eps is not None, _vector(gamma, w.cols, "gamma"),
                                    _vector(beta, w.cols, "beta"), eps or 0.0, w.ref, _vector(bias, w.rows, "bias"), relu, po, ldo,
                                    *_space(workspace), _stream_of(x, stream)), "dqrm_mxfp4_linear")
@@ -591,12 +595,9 @@ def dqrm_mxfp4_linear(x: torch.Tensor, w: MxMatrix, out: torch.Tensor, bias: Opt
 def dqrm_layernorm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                        y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
                        q: Optional[MxMatrix] = None, stream=None) -> None:
-    dtype, p, ld = _matrix(x, "x")
-    R, D = x.shape
-    py, ldy = None, 0
-    if y is not None:
-        _like(y, R, D, x.dtype, "y")
-        _, py, ldy = _matrix(y, "y")
+    dtype, R, D = _kind(x, "x")
+    p, ld = _rows_of(x, R, D, x.dtype, "x")
+    py, ldy = (None, 0) if y is None else _rows_of(y, R, D, x.dtype, "y")
     _check(lib().dqrm_layernorm_fwd(dtype, R, D, p, ld, _vector(gamma, D, "gamma"), _vector(beta, D, "beta"), eps, py, ldy,
                                     _vector(mean, R, "mean"), _vector(rstd, R, "rstd"), _mx(q), _stream_of(x, stream)), "dqrm_layernorm_fwd")
 
@@ -608,14 +609,10 @@ def dqrm_layernorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
 def dqrm_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
                        dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
                        dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    dtype, p, ld = _matrix(x, "x")
-    R, D = x.shape
-    _like(dy, R, D, x.dtype, "dy")
-    _, pdy, lddy = _matrix(dy, "dy")
-    pdx, lddx = None, 0
-    if dx is not None:
-        _like(dx, R, D, x.dtype, "dx")
-        _, pdx, lddx = _matrix(dx, "dx")
+    dtype, R, D = _kind(x, "x")
+    p, ld = _rows_of(x, R, D, x.dtype, "x")
+    pdy, lddy = _rows_of(dy, R, D, x.dtype, "dy")
+    pdx, lddx = (None, 0) if dx is None else _rows_of(dx, R, D, x.dtype, "dx")
     _check(lib().dqrm_layernorm_bwd(dtype, R, D, pdy, lddy, p, ld, _vector(mean, R, "mean"), _vector(rstd, R, "rstd"),
                                     _vector(gamma, D, "gamma"), pdx, lddx, _vector(dgamma, D, "dgamma"), _vector(dbeta, D, "dbeta"),
                                     *_space(workspace), _stream_of(x, stream)), "dqrm_layernorm_bwd")
