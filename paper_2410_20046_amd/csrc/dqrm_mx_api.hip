@@ -168,6 +168,11 @@ void with_norm_fwd_shape(int64_t rows, int64_t cols, F f)
                                          NormShape<64, 3, 256>, NormShape<128, 2, 256>, NormShape<128, 3, 256>, NormShape<256, 2, 256>,
                                          NormShape<256, 3, 256>, NormShape<512, 2, 512>, NormShape<512, 3, 512>, NormShape<1024, 2, 1024>>(cols, f);
     }
+    // A row to a CU at most: its latency counts, which is less the more threads it has (from a graph, with codes: 16 x 700 bfloat16 3.4 us, with two
+    // chunks to a thread 4.1; 200 x 2500 3.7 and 4.3; 16 x 6000 4.05 and 4.3)
+    if (rows <= num_cus())
+        return with_first_that_holds<NormShape<16, 1, 256>, NormShape<64, 1, 256>, NormShape<128, 1, 256>, NormShape<256, 1, 256>, NormShape<512, 1, 512>,
+                                     NormShape<1024, 1, 1024>, NormShape<1024, 2, 1024>>(cols, f);
     with_first_that_holds<NormShape<16, 1, 256>, NormShape<64, 1, 256>, NormShape<64, 2, 256>, NormShape<256, 1, 256>, NormShape<256, 2, 256>,
                           NormShape<512, 2, 512>, NormShape<1024, 2, 1024>>(cols, f);
 }

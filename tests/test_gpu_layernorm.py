@@ -42,7 +42,7 @@ def _gain(rng, C, kind):
 
 # every way a row is laid over threads, and both sides of each limit
 SHAPES = [(1, 1), (5, 2), (3, 7), (130, 13), (17, 128), (16, 129), (1000, 64), (33, 512), (9, 513), (6, 1024), (7, 1025), (4, 2048), (5, 2049),
-          (3, 4097), (2, 8191), (3, 8193), (2, 16384), (3, 16385), (2, 50001)]
+          (3, 4097), (2, 8191), (3, 8193), (2, 16384), (3, 16385), (2, 50001), (300, 700), (290, 1500), (280, 2500), (270, 6000)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
