@@ -270,9 +270,14 @@ struct MatmulPlan {
 };
 
 // Few rows of A, and strips of W enough to keep the chip's memory busy or k short: W straight from memory.  Against tiles, of which
-// k can be cut: 64 x 4096 x 4096 7.0 and 10.6 us, 64 x 8192 x 8192 16.2 and 17.4, 16 x 256 x 32768 8.4 and 9.3; 16 x 512 x 65536 21.8 and 15.3,
-// 64 x 256 x 16384 12.2 and 8.4.
-bool is_few(int64_t m, int64_t n, int64_t k) { return m <= 64 && (n >= 4096 || k <= (m <= 16 ? 32768 : 8192)); }
+// k can be cut: 64 x 4096 x 8192 11.8 and 14.9 us, 64 x 8192 x 8192 16.6 and 19.6, 16 x 2048 x 2048 3.4 and 6.8, 16 x 512 x 32768 8.5 and 9.1;
+// 16 x 512 x 65536 21.8 and 15.3, 64 x 256 x 16384 12.2 and 8.4, 64 x 4096 x 32768 31.2 and 27.4.  More than 32 rows are a fixed cost that
+// a short k doesn't cover: 64 x 2048 x 512 3.9 and 3.2, 64 x 8192 x 512 5.7 and 3.8, 64 x 2048 x 2048 5.0 and 6.8.
+bool is_few(int64_t m, int64_t n, int64_t k)
+{
+    if (m > 32) return m <= 64 && (n >= 4096 ? k > 1024 && k <= 16384 : k > 768 && k <= 8192);
+    return n >= 4096 || k <= (m <= 16 ? 32768 : 8192);
+}
 
 // Time of a product's tiles, to choose among them: us, from how many of them there are to a CU and the stages of k that each has.
 // Sides of 64: four workgroups to a CU.  128: two that have the least to read from LDS and hide each other's waits (by128_pair), or
