@@ -188,7 +188,8 @@ def _bound(a, b, bias, out, dtype):
 
 
 PRODUCTS = [(1, 1, 1), (1, 512, 367), (2, 3, 13), (5, 70, 129), (31, 33, 128), (33, 65, 512), (64, 64, 64), (100, 1, 300), (129, 257, 415),
-            (257, 130, 640), (300, 300, 1000), (16, 1000, 2048), (17, 40, 8192), (64, 96, 20000), (512, 367, 8192), (1000, 520, 96), (700, 900, 1537), (60, 300, 3000), (50, 5000, 1100), (30, 5000, 200)]
+            (257, 130, 640), (300, 300, 1000), (16, 1000, 2048), (17, 40, 8192), (64, 96, 20000), (512, 367, 8192), (1000, 520, 96), (700, 900, 1537),
+            (60, 300, 3000), (50, 5000, 1100), (30, 5000, 200)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
