@@ -106,6 +106,11 @@ __device__ __forceinline__ void quantise_few(const NormArgs &a, uint8_t *codes, 
             if (!used(j)) continue;
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) x[j][i] = x[j][i] * rstd * (a.gamma ? gamma[j][i] : 1.0f) + (a.beta ? beta[j][i] : 0.0f);
+            // (past the row's end 0, also where rstd is infinite or a NaN: the padding of the codes)
+            if (column(j) + kChunk > cols) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) x[j][i] = column(j) + i < cols ? x[j][i] : 0.0f;
+            }
         }
     }
 #pragma unroll

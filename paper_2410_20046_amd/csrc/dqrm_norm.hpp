@@ -125,7 +125,12 @@ __global__ __launch_bounds__(BLOCK, 4) void norm_fwd_kernel(NormArgs a)
         for (int j = 0; j < CH; ++j) {
             const int c = column(j);
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) x[j][i] = x[j][i] * rstd * gamma[j][i] + beta[j][i]; // (past the row's end 0, as beta is)
+            for (int i = 0; i < kChunk; ++i) x[j][i] = x[j][i] * rstd * gamma[j][i] + beta[j][i];
+            // (past the row's end 0, also where rstd is infinite or a NaN: the padding of the codes)
+            if (c + kChunk > cols) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) x[j][i] = c + i < cols ? x[j][i] : 0.0f;
+            }
             if (a.y && c < cols) store_chunk<true>(static_cast<T *>(a.y) + r * a.ldy, c, cols, x[j]);
             if (a.codes && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), x[j]);
         }
