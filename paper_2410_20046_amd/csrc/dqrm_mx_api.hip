@@ -29,7 +29,7 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 int64_t ceil_div(int64_t x, int64_t d) { return (x + d - 1) / d; }
 
 constexpr int64_t kMaxDim = 2147483647LL - 1024; // rows, columns and row strides' limit
-constexpr int64_t kMaxBlocks = 1 << 22;          // of one launch (blocks times threads is below 2^32)
+constexpr int64_t kMaxBlocks = 1 << 22;          // of one launch, with up to 512 threads each (a launch has to have fewer than 2^32)
 
 size_t size_of(int32_t dtype) { return dtype == DQRM_F32 ? 4 : 2; }
 
@@ -134,11 +134,18 @@ void launch_quant_rows(int32_t dtype, QuantArgs a, hipStream_t st)
 // Rows of 8 to 16384 values stay in registers; others are read more than once (shorter ones have no vector of 8).
 bool norm_in_registers(int64_t cols) { return cols >= kChunk && cols <= 16384; }
 
-// threads of such another row
+// threads of such another row, a workgroup's; a launch takes as many rows as have 2^31 threads together
 template <typename F>
 void with_norm_long_block(int64_t cols, F f)
 {
     cols < kChunk ? f(std::integral_constant<int, kWaveSize>{}) : f(std::integral_constant<int, 1024>{});
+}
+
+int64_t norm_long_rows(int64_t cols)
+{
+    int64_t rows = 0;
+    with_norm_long_block(cols, [&](auto block) { rows = ((int64_t)1 << 31) / decltype(block)::value; });
+    return rows;
 }
 
 // How a row that stays in registers is laid over threads: f(shape) for the narrowest one that holds it.
@@ -197,7 +204,7 @@ void with_norm_bwd_shape(int64_t rows, int64_t cols, F f)
 void launch_norm_fwd(int32_t dtype, const NormArgs &a, hipStream_t st)
 {
     const bool in_registers = norm_in_registers(a.cols);
-    const int64_t step = kMaxBlocks;
+    const int64_t step = in_registers ? kMaxBlocks : norm_long_rows(a.cols);
     const size_t es = size_of(dtype);
     for (int64_t r0 = 0; r0 < a.rows; r0 += step) {
         NormArgs b = a;
@@ -653,9 +660,10 @@ int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void
                 hipLaunchKernelGGL((norm_bwd_columns_kernel<DT, false>), grid, dim3(256), 0, st, a, ceil_div(rows, blocks));
         }
         const size_t es = size_of(dtype);
-        for (int64_t r0 = 0; dx && r0 < rows; r0 += kMaxBlocks) {
+        const int64_t step = norm_long_rows(cols);
+        for (int64_t r0 = 0; dx && r0 < rows; r0 += step) {
             NormBwdArgs b = a;
-            b.rows = std::min(kMaxBlocks, rows - r0);
+            b.rows = std::min(step, rows - r0);
             b.dy = static_cast<const char *>(dy) + r0 * lddy * es, b.x = static_cast<const char *>(x) + r0 * ldx * es;
             b.dx = static_cast<char *>(dx) + r0 * lddx * es, b.mean = mean + r0, b.rstd = rstd + r0;
             with_norm_long_block(cols, [&](auto block) {

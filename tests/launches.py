@@ -1,0 +1,76 @@
+"""What the library would launch, found out without a GPU.
+
+``would_launch(calls)`` makes C calls in a process of its own in which the HIP runtime's launch calls are those of launch_recorder.cpp: the
+library's host side runs as it is, and every kernel is written down instead of run.  A call is ``(name, *arguments)``: whole numbers (pointers
+among them; nothing is dereferenced), floats, ``None``, and ``mx(rows, cols)`` for an MXFP4 matrix.
+"""
+import ctypes as C
+import json
+import os
+import re
+import subprocess
+import sys
+import tempfile
+from typing import NamedTuple, Tuple
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+LIB = os.path.join(os.path.dirname(HERE), "paper_2410_20046_amd", "libdqrm.so")
+FAKE = 0x10000  # non-null, aligned, never dereferenced
+
+
+class Launch(NamedTuple):
+    kernel: str
+    grid: Tuple[int, int, int]
+    block: Tuple[int, int, int]
+    shared: int
+    failed: bool
+
+
+def mx(rows, cols, codes=FAKE, scales=FAKE):
+    return {"mx": [rows, cols, codes, scales]}
+
+
+def would_launch(calls):
+    """[(return code, [Launch, ...])] of the calls."""
+    with tempfile.TemporaryDirectory() as folder:
+        recorder = os.path.join(folder, "recorder.so")
+        subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-o", recorder, os.path.join(HERE, "launch_recorder.cpp")], check=True)
+        r = subprocess.run([sys.executable, os.path.abspath(__file__), recorder, LIB], input=json.dumps(calls), stdout=subprocess.PIPE, text=True, check=True)
+    out = json.loads(r.stdout)
+    names = sorted({l[0] for _, ls in out for l in ls})
+    plain = subprocess.run(["c++filt"], input="\n".join(names), stdout=subprocess.PIPE, text=True, check=True).stdout.splitlines() if names else []
+    clear = {n: re.sub(r"^void ", "", re.sub(r"\([^()]*\)$", "", p)).replace("dqrm_mx::", "").replace("(anonymous namespace)::", "") for n, p in zip(names, plain)}
+    return [(rc, [Launch(clear[n], tuple(s[:3]), tuple(s[3:6]), s[6], bool(s[7])) for n, s in ls]) for rc, ls in out]
+
+
+class _Mx(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+def _argument(a):
+    if isinstance(a, dict):
+        return C.byref(_Mx(*a["mx"]))
+    return C.c_float(a) if isinstance(a, float) else C.c_int64(a or 0)
+
+
+def _main():
+    recorder = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+    library = C.CDLL(sys.argv[2])
+    recorder.recorded_name.restype = C.c_char_p
+    out = []
+    for name, *args in json.load(sys.stdin):
+        recorder.forget_launches()
+        f = getattr(library, name)
+        f.restype = C.c_size_t if name.endswith("_bytes") else C.c_int32
+        rc = f(*[_argument(a) for a in args])
+        launches = []
+        for i in range(recorder.recorded_launches()):
+            shape = (C.c_uint * 8)()
+            recorder.recorded_shape(i, shape)
+            launches.append((recorder.recorded_name(i).decode(), list(shape)))
+        out.append((rc, launches))
+    json.dump(out, sys.stdout)
+
+
+if __name__ == "__main__":
+    _main()

@@ -1,0 +1,34 @@
+"""CPU-only checks of what the layer norm and MXFP4 calls launch: the host side runs with the HIP runtime's launch calls written down
+instead of made (see launches.py)."""
+import pytest
+
+import paper_2410_20046_amd as dq
+from launches import FAKE, mx, would_launch
+
+OK, INVALID, UNSUPPORTED = dq.OK, dq.ERR_INVALID_ARG, dq.ERR_UNSUPPORTED
+BF16 = dq.BF16
+ROOM = 1 << 60  # bytes of workspace: enough for anything
+
+
+def threads(launch):
+    return max(launch.grid[i] * launch.block[i] for i in range(3))
+
+
+def norm_fwd(rows, cols):
+    return ("dqrm_layernorm_fwd", BF16, rows, cols, FAKE, cols, None, None, 1e-5, FAKE, cols, None, None, None, None)
+
+
+def norm_bwd(rows, cols, dx=FAKE, sums=FAKE):
+    return ("dqrm_layernorm_bwd", BF16, rows, cols, FAKE, cols, FAKE, cols, FAKE, FAKE, None, dx, cols, sums, sums, FAKE, ROOM, None)
+
+
+@pytest.mark.parametrize("call", [norm_fwd, norm_bwd])
+@pytest.mark.parametrize("rows, cols, block", [((1 << 22) - 1, 16385, 1024), (1 << 22, 16385, 1024), ((1 << 22) + 1, 40000, 1024), (5 << 22, 16385, 1024),
+                                               (1 << 25, 3, 64), ((1 << 25) + 1, 7, 64)])
+def test_norms_of_many_rows_that_are_read_more_than_once(call, rows, cols, block):
+    """A workgroup to a row, of 1024 threads where rows are long: a launch has fewer than 2^32 threads, and all launches every row."""
+    (rc, launches), = would_launch([call(rows, cols)])
+    assert rc == OK
+    assert all(threads(l) < 1 << 32 and not l.failed for l in launches)
+    long = [l for l in launches if "_long_kernel" in l.kernel]
+    assert all(l.block[0] == block for l in long) and sum(l.grid[0] for l in long) == rows
