@@ -416,14 +416,15 @@ __device__ __forceinline__ float add_strided(float v, const float *p, int64_t st
     return v;
 }
 
-// out[c] = sum over p of partial[p][c] (and a second pair of arrays behind it), in a fixed order: 16 lanes take every 16th each, then
-// their sums are added in turn.  The launch and two reads' latencies: 256 parts of 512 columns twice 2.8 us, of 8190 columns 8.
-__global__ __launch_bounds__(256) void join_columns_kernel(const float *partial, int64_t stride, int n, int64_t cols, float *out0, float *out1)
+// out[c] = sum over p of partial[p][c], and another such sum from `second` values on, in a fixed order: 16 lanes take every 16th each,
+// then their sums are added in turn.  The launch and two reads' latencies: 256 parts of 512 columns twice 2.8 us, of 8190 columns 8.
+__global__ __launch_bounds__(256) void join_columns_kernel(const float *partial, int64_t stride, int n, int64_t cols, int64_t second, float *out0,
+                                                           float *out1)
 {
     __shared__ float s[16][17];
     const int64_t c = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
     const int slice = threadIdx.x >> 4;
-    const float *p = partial + (blockIdx.y ? cols : 0);
+    const float *p = partial + (blockIdx.y ? second : 0);
     float sum = 0.0f;
     if (c < cols) sum = add_strided(sum, p + (int64_t)slice * stride + c, 16 * stride, (n - slice + 15) / 16); // (none: n - slice <= 0)
     s[slice][threadIdx.x & 15] = sum;

@@ -106,7 +106,12 @@ void fill_zero(float *p, int64_t n, hipStream_t st)
 
 void join_columns(const float *partial, int64_t stride, int n, int64_t cols, float *out0, float *out1, hipStream_t st)
 {
-    hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(cols, 16), out1 ? 2 : 1), dim3(256), 0, st, partial, stride, n, cols, out0, out1);
+    const int64_t step = kMaxBlocks * 16; // columns of a launch
+    for (int64_t c0 = 0; c0 < cols; c0 += step) {
+        const int64_t some = std::min(step, cols - c0);
+        hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(some, 16), out1 ? 2 : 1), dim3(256), 0, st, partial + c0, stride, n, some, cols,
+                           out0 + c0, out1 ? out1 + c0 : nullptr);
+    }
 }
 
 // ---- quantisation ------------------------------------------------------------------------------------------------------

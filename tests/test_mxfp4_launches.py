@@ -32,3 +32,22 @@ def test_norms_of_many_rows_that_are_read_more_than_once(call, rows, cols, block
     assert all(threads(l) < 1 << 32 and not l.failed for l in launches)
     long = [l for l in launches if "_long_kernel" in l.kernel]
     assert all(l.block[0] == block for l in long) and sum(l.grid[0] for l in long) == rows
+
+
+def quant(rows, cols, by_rows=None, by_cols=None, sums=None):
+    return ("dqrm_mxfp4_quant", BF16, rows, cols, FAKE, cols, None, 0, by_rows, by_cols, sums, FAKE, ROOM, None)
+
+
+@pytest.mark.parametrize("cols", [1, 8190, (1 << 28) - 16, (1 << 28) - 15, 1 << 28, (1 << 29) + 17])
+@pytest.mark.parametrize("pair", [False, True])
+def test_column_sums_of_very_wide_matrices(cols, pair):
+    """The join of partial sums has 16 threads to a column, one pair of arrays of sums or one array, and is as many launches as it takes."""
+    (rc, launches), = would_launch([norm_bwd(129, cols, dx=None) if pair else quant(129, cols, sums=FAKE)])
+    if not pair and 2 * -(-cols // 128) > 1 << 23:  # more tiles of 128 by 128 than the quantisation takes
+        assert rc == UNSUPPORTED and not launches
+        return
+    assert rc == OK
+    assert all(threads(l) < 1 << 32 and not l.failed for l in launches)
+    joins = [l for l in launches if l.kernel == "join_columns_kernel"]
+    assert all(l.grid[1] == (2 if pair else 1) for l in joins)
+    assert sum(l.grid[0] for l in joins) == -(-cols // 16)
