@@ -454,7 +454,8 @@ typedef struct {
  *   col_sums  [cols] fp32: the sums of x's columns before quantisation (a bias's gradient), or NULL.  Needs the workspace
  *             (256-byte aligned); their order of addition depends on the shape alone.
  *   gate      [rows][cols] of the same type, or NULL: x counts as 0 where gate > 0 does not hold (a ReLU's backward,
- *             gate being the layer's output) */
+ *             gate being the layer's output)
+ * With by_cols or col_sums, more than 8388608 tiles of 128 by 128 are DQRM_ERR_UNSUPPORTED. */
 size_t dqrm_mxfp4_quant_workspace_bytes(int64_t rows, int64_t cols);
 int32_t dqrm_mxfp4_quant(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *gate,
                          int64_t ldgate, const dqrm_mxfp4_t *by_rows, const dqrm_mxfp4_t *by_cols, float *col_sums,
@@ -466,8 +467,9 @@ int32_t dqrm_mxfp4_dequant(const dqrm_mxfp4_t *q, int32_t dtype, void *out, int6
 /* out [m][n] = act(sum over k of a[m][k] b[n][k] + bias[n]), act = max(., 0) if relu (a NaN stays), rounded once to the
  * element type.  a->cols = b->cols = k; k = 0 gives act(bias).  With A by rows and B = W by rows it is a linear layer's
  * forward; with dY by rows and W by columns the input's gradient; with dY and X by columns the weights'.  bias: [n] fp32
- * or NULL.  The order of the sums depends on the shape alone.  out must not overlap the operands.  k > 16777216 is
- * DQRM_ERR_UNSUPPORTED, here and below. */
+ * or NULL.  The order of the sums depends on the shape alone.  out must not overlap the operands.  DQRM_ERR_UNSUPPORTED,
+ * here and below: k > 16777216, and outputs of more than 4194304 tiles of 256 by 256 (but not where A has up to 32 rows, or
+ * up to 64 and k is from 1025 to 16384). */
 size_t dqrm_mxfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int32_t dqrm_mxfp4_matmul(const dqrm_mxfp4_t *a, const dqrm_mxfp4_t *b, const float *bias, int32_t relu, int32_t dtype,
                           void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);

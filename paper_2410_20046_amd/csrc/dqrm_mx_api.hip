@@ -358,6 +358,13 @@ void launch_tiles(const MatmulPlan &p, MatmulArgs g, hipStream_t st)
 
 constexpr int64_t kMaxInner = 1 << 24; // a tile's rows of codes are addressed with 32 bits
 
+// Whether a product of this shape can be launched: asked before anything is.  (Where tiles of 128 or 64 are too many, the plan has none.)
+int32_t check_product(int64_t m, int64_t n, int64_t k)
+{
+    if (k > kMaxInner) return DQRM_ERR_UNSUPPORTED;
+    return is_few(m, n, k) || ceil_div(m, 256) * ceil_div(n, 256) <= kMaxBlocks ? DQRM_OK : DQRM_ERR_UNSUPPORTED;
+}
+
 template <int DT, FewSource SRC, int MT>
 void launch_few(const FewArgs &a, hipStream_t st)
 {
@@ -390,7 +397,6 @@ void launch_few(const FewArgs &a, hipStream_t st)
 int32_t launch_matmul(int32_t dtype, MatmulArgs g, void *workspace, hipStream_t st)
 {
     const MatmulPlan p = matmul_plan(g.m, g.n, g.k);
-    if (p.tiles != Tiles::few && ceil_div(g.m, side_of(p.tiles)) * ceil_div(g.n, side_of(p.tiles)) > kMaxBlocks) return DQRM_ERR_UNSUPPORTED;
     if (p.tiles == Tiles::few) {
         FewArgs a{};
         a.g = g;
@@ -532,7 +538,7 @@ int32_t dqrm_mxfp4_matmul(const dqrm_mxfp4_t *a, const dqrm_mxfp4_t *b, const fl
     if (bias && !aligned(bias, 4)) return DQRM_ERR_INVALID_ARG;
     DQRM_CHECK(check_matrix(out, ldo, dtype, m, n));
     DQRM_CHECK(check_workspace(workspace, workspace_bytes, matmul_workspace(m, n, k)));
-    if (k > kMaxInner) return DQRM_ERR_UNSUPPORTED;
+    DQRM_CHECK(check_product(m, n, k));
     if (m == 0 || n == 0) return DQRM_OK;
     const MatmulArgs g{a->codes, a->scales, b->codes, b->scales, m, n, k, bias, relu != 0, out, ldo};
     return launch_matmul(dtype, g, workspace, static_cast<hipStream_t>(stream));
@@ -560,7 +566,7 @@ int32_t dqrm_mxfp4_linear(int32_t dtype, int64_t m, const void *x, int64_t ldx, 
     DQRM_CHECK(check_matrix(out, ldo, dtype, m, n));
     const LinearWs L = linear_ws(m, n, k);
     DQRM_CHECK(check_workspace(workspace, workspace_bytes, L.total));
-    if (k > kMaxInner) return DQRM_ERR_UNSUPPORTED;
+    DQRM_CHECK(check_product(m, n, k));
     if (m == 0 || n == 0) return DQRM_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);

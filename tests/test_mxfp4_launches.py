@@ -51,3 +51,24 @@ def test_column_sums_of_very_wide_matrices(cols, pair):
     joins = [l for l in launches if l.kernel == "join_columns_kernel"]
     assert all(l.grid[1] == (2 if pair else 1) for l in joins)
     assert sum(l.grid[0] for l in joins) == -(-cols // 16)
+
+
+def linear(m, n, k, norm=0, ws_bytes=ROOM):
+    return ("dqrm_mxfp4_linear", BF16, m, FAKE, k, norm, None, None, 1e-5, mx(n, k), None, 0, FAKE, n, FAKE, ws_bytes, None)
+
+
+def matmul(m, n, k, ws_bytes=ROOM):
+    return ("dqrm_mxfp4_matmul", mx(m, k), mx(n, k), None, 0, BF16, FAKE, n, FAKE, ws_bytes, None)
+
+
+@pytest.mark.parametrize("m, n, k", [(1 << 20, 1 << 19, 64), (1 << 30, 1000, 300), (1 << 27, 8193, 17), (1 << 20, 1 << 18, (1 << 24) + 1)])
+def test_products_that_are_refused_launch_nothing(m, n, k):
+    """More outputs than 2^22 tiles of 256 by 256 hold, and longer sums than 2^24: the linear layer's activations stay unquantised too."""
+    for rc, launches in would_launch([matmul(m, n, k), linear(m, n, k), linear(m, n, k, norm=1)]):
+        assert rc == UNSUPPORTED and not launches
+
+
+def test_products_up_to_the_limit_are_launched():
+    for rc, launches in would_launch([f(*shape) for shape in ((1 << 20, 1 << 18, 64), (64, (1 << 30) + 5, 1100), (3, (1 << 30) + 5, 64))
+                                      for f in (matmul, linear, lambda *s: linear(*s, norm=1))]):
+        assert rc == OK and launches and all(threads(l) < 1 << 32 and not l.failed for l in launches)
