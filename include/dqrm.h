@@ -427,7 +427,11 @@ int32_t dqrm_dense_step_quant(const dqrm_dense_model_t *model, const dqrm_dense_
  * layer's inputs in the range of few bits.  Sums, statistics and scales are held in 32 bits.
  *
  * Element types of matrices that are not codes.  A matrix has a row stride in elements (ld >= cols; any value if there
- * is one row) and starts at any multiple of its element's size; rows and cols are at most 2147482623. */
+ * is one row) and starts at any multiple of its element's size; rows and cols are at most 2147482623.
+ *
+ * A workspace of dqrm_*_workspace_bytes(rows, ...) is enough for any smaller number of rows of the same columns (n and
+ * k), as dqrm_dense_workspace_bytes is: rows is the first argument, x's rows or a's (m).  These queries belong to set-up: the
+ * product's tries plans (some microseconds, tenths of a millisecond for tall and narrow shapes). */
 #define DQRM_F32 0
 #define DQRM_BF16 1
 #define DQRM_F16 2

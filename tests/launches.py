@@ -4,10 +4,13 @@
 library's host side runs as it is, and every kernel is written down instead of run.  A call is ``(name, *arguments)``: whole numbers (pointers
 among them; nothing is dereferenced), floats, ``None``, and ``mx(rows, cols)`` for an MXFP4 matrix.
 """
+import atexit
 import ctypes as C
+import functools
 import json
 import os
 import re
+import shutil
 import subprocess
 import sys
 import tempfile
@@ -30,12 +33,19 @@ def mx(rows, cols, codes=FAKE, scales=FAKE):
     return {"mx": [rows, cols, codes, scales]}
 
 
+@functools.lru_cache(maxsize=None)
+def _recorder():
+    folder = tempfile.mkdtemp()
+    atexit.register(shutil.rmtree, folder, ignore_errors=True)
+    out = os.path.join(folder, "recorder.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-o", out, os.path.join(HERE, "launch_recorder.cpp")], check=True)
+    return out
+
+
 def would_launch(calls):
     """[(return code, [Launch, ...])] of the calls."""
-    with tempfile.TemporaryDirectory() as folder:
-        recorder = os.path.join(folder, "recorder.so")
-        subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-o", recorder, os.path.join(HERE, "launch_recorder.cpp")], check=True)
-        r = subprocess.run([sys.executable, os.path.abspath(__file__), recorder, LIB], input=json.dumps(calls), stdout=subprocess.PIPE, text=True, check=True)
+    command = [sys.executable, os.path.abspath(__file__), _recorder(), LIB]
+    r = subprocess.run(command, input=json.dumps(calls), stdout=subprocess.PIPE, text=True, check=True)
     out = json.loads(r.stdout)
     names = sorted({l[0] for _, ls in out for l in ls})
     plain = subprocess.run(["c++filt"], input="\n".join(names), stdout=subprocess.PIPE, text=True, check=True).stdout.splitlines() if names else []

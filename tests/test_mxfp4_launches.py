@@ -1,5 +1,7 @@
 """CPU-only checks of what the layer norm and MXFP4 calls launch: the host side runs with the HIP runtime's launch calls written down
 instead of made (see launches.py)."""
+import random
+
 import pytest
 
 import paper_2410_20046_amd as dq
@@ -72,3 +74,33 @@ def test_products_up_to_the_limit_are_launched():
     for rc, launches in would_launch([f(*shape) for shape in ((1 << 20, 1 << 18, 64), (64, (1 << 30) + 5, 1100), (3, (1 << 30) + 5, 64))
                                       for f in (matmul, linear, lambda *s: linear(*s, norm=1))]):
         assert rc == OK and launches and all(threads(l) < 1 << 32 and not l.failed for l in launches)
+
+
+def held(what, *shape):
+    return ("dqrm_" + what + "_workspace_bytes", *shape)
+
+
+def fewer(m, rng):
+    """Numbers of rows up to m: the smallest, those around each multiple of a tile's rows that a plan changes at, and others."""
+    near = {1, 2, 16, 17, 32, 33, 64, 65, 127, 128, 129, 255, 256, 257, 512, 513, 1024, 2048, 4096, m - 1, m, m // 2, m // 3}
+    return sorted(v for v in near | {rng.randint(1, m) for _ in range(30)} if 1 <= v <= m)
+
+
+@pytest.mark.parametrize("n, k", [(512, 8192), (2048, 16384), (1, 65536), (367, 65536), (130, 33000), (1000, 60001), (8192, 8192), (4100, 4099), (77, 40000)])
+@pytest.mark.parametrize("m", [64, 1000, 8192, 20000])
+def test_the_workspace_of_a_product_is_enough_for_fewer_rows(m, n, k):
+    """One workspace for the largest batch serves smaller ones, the last batch of an epoch and single requests among them."""
+    some = fewer(m, random.Random(m + n + k))
+    (product, _), (layer, _) = would_launch([held("mxfp4_matmul", m, n, k), held("mxfp4_linear", m, n, k)])
+    for call, room in ((matmul, product), (linear, layer)):
+        assert [rc for rc, _ in would_launch([call(v, n, k, ws_bytes=room) for v in some])] == [OK] * len(some)
+
+
+@pytest.mark.parametrize("cols", [1, 7, 40, 300, 1200, 4100, 8192, 16384, 16385, 50000])
+@pytest.mark.parametrize("rows", [3, 65, 1000, 4097, 100000])
+def test_the_other_workspaces_are_enough_for_fewer_rows(rows, cols):
+    some = fewer(rows, random.Random(rows + cols))
+    (norm, _), (sums, _) = would_launch([held("layernorm_bwd", rows, cols), held("mxfp4_quant", rows, cols)])
+    back = [("dqrm_layernorm_bwd", t, v, cols, FAKE, cols, FAKE, cols, FAKE, FAKE, None, FAKE, cols, FAKE, FAKE, FAKE, norm, None) for v in some for t in (0, 1, 2)]
+    quantised = [("dqrm_mxfp4_quant", 0, v, cols, FAKE, cols, None, 0, None, None, FAKE, FAKE, sums, None) for v in some]
+    assert {rc for rc, _ in would_launch(back + quantised)} == {OK}
