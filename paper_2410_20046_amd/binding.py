@@ -482,46 +482,63 @@ def dqrm_fwd_bwd_step(tables: Tables, bufs: StepBuffers, indices: torch.Tensor, 
 # ---- layer norm and MXFP4 linear layers ---------------------------------------------------------------------------------
 
 
-# (These run on every call, and a call on little data is as long as they are: no tuples, no formatting unless something is wrong.)
-def _kind(t: torch.Tensor, what: str) -> Tuple[int, int, int]:
-    """(element type, rows, columns) of a matrix."""
+# Operands have to be in the memory of one GPU, that of a call's first matrix: the library cannot see where they are.
+# (These run on every call, and a call on little data is as long as they are: no loops, no formatting unless something is wrong.)
+def _matrix(t: torch.Tensor, what: str) -> Tuple[int, int, int, int, int, int]:
+    """(element type, rows, columns, address, row stride, GPU) of a matrix whose rows' elements lie one behind the other."""
     dtype, shape = _DTYPES.get(t.dtype), t.shape
     if dtype is None or len(shape) != 2:
         raise AssertionError(f"{what}: a matrix of float32, bfloat16 or float16")
-    return dtype, shape[0], shape[1]
+    rows, cols = shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise AssertionError(f"{what}: the elements of a row must be contiguous")
+    return dtype, rows, cols, t.data_ptr(), ld, t.get_device()
 
 
-def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> Tuple[int, int]:
-    """(address, row stride) of a matrix of this kind whose rows' elements lie one behind the other."""
+def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, what: str, gpu: int) -> Tuple[int, int]:
+    """(address, row stride) of another one of this kind."""
     shape = t.shape
     if t.dtype is not dtype or len(shape) != 2 or shape[0] != rows or shape[1] != cols:
         raise AssertionError(f"{what}: ({rows}, {cols}) of {dtype}, got {tuple(shape)} of {t.dtype}")
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise AssertionError(f"{what}: the elements of a row must be contiguous")
+    if t.get_device() != gpu:
+        raise _elsewhere(what)
     return t.data_ptr(), ld
 
 
-def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], n: int, what: str, gpu: int) -> Optional[int]:
     if t is None:
         return None
     if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise AssertionError(f"{what}: {n} contiguous float32 values")
+    if t.get_device() != gpu:
+        raise _elsewhere(what)
     return t.data_ptr()
 
 
-def _space(ws: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+def _space(ws: Optional[torch.Tensor], gpu: int) -> Tuple[Optional[int], int]:
     if ws is None:
         return None, 0
     if not ws.is_contiguous():
         raise AssertionError("workspace: contiguous memory")
+    if ws.get_device() != gpu:
+        raise _elsewhere("workspace")
     return ws.data_ptr(), ws.nbytes
 
 
-def _stream_of(t: torch.Tensor, stream) -> Optional[int]:
-    """The stream asked for, or the current one of the device that `t` is on."""
-    if stream is None and _raw_stream is not None and t.is_cuda:
-        return _raw_stream(t.get_device())
+def _elsewhere(what: str) -> DqrmError:
+    return DqrmError(ERR_INVALID_ARG, what, "not in the memory that the other operands are in")
+
+
+def _stream_of(gpu: int, stream) -> Optional[int]:
+    """The stream asked for, or the current one of the GPU that the operands are on."""
+    if gpu < 0:
+        raise DqrmError(ERR_INVALID_ARG, "operands", "in host memory")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(gpu)
     return _stream(stream)
 
 
@@ -535,14 +552,19 @@ class MxMatrix:
         byte = lambda n: torch.empty((self.rows, n), dtype=torch.uint8, device=device)  # noqa: E731
         self.codes = codes if codes is not None else byte(64 * groups)
         self.scales = scales if scales is not None else byte(4 * groups)
+        self.gpu = self.codes.get_device()  # -1: host memory
         for t, n in ((self.codes, 64 * groups), (self.scales, 4 * groups)):
-            _rows_of(t, self.rows, n, torch.uint8, "MxMatrix")
+            _rows_of(t, self.rows, n, torch.uint8, "MxMatrix", self.gpu)
         self.c = dqrm_mxfp4_t(self.rows, self.cols, _ptr(self.codes), _ptr(self.scales))
         self.ref = C.byref(self.c)
 
 
-def _mx(q: Optional[MxMatrix]):
-    return None if q is None else q.ref
+def _mx(q: Optional[MxMatrix], what: str, gpu: int):
+    if q is None:
+        return None
+    if q.gpu != gpu:
+        raise _elsewhere(what)
+    return q.ref
 
 
 def dqrm_mxfp4_quant_workspace_bytes(rows: int, cols: int) -> int:
@@ -552,16 +574,17 @@ def dqrm_mxfp4_quant_workspace_bytes(rows: int, cols: int) -> int:
 def dqrm_mxfp4_quant(x: torch.Tensor, by_rows: Optional[MxMatrix] = None, by_cols: Optional[MxMatrix] = None,
                      gate: Optional[torch.Tensor] = None, col_sums: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    dtype, R, D = _kind(x, "x")
-    p, ld = _rows_of(x, R, D, x.dtype, "x")
-    pg, ldg = (None, 0) if gate is None else _rows_of(gate, R, D, x.dtype, "gate")
-    _check(lib().dqrm_mxfp4_quant(dtype, R, D, p, ld, pg, ldg, _mx(by_rows), _mx(by_cols),
-                                  _vector(col_sums, D, "col_sums"), *_space(workspace), _stream_of(x, stream)), "dqrm_mxfp4_quant")
+    dtype, R, D, p, ld, gpu = _matrix(x, "x")
+    pg, ldg = (None, 0) if gate is None else _rows_of(gate, R, D, x.dtype, "gate", gpu)
+    _check(lib().dqrm_mxfp4_quant(dtype, R, D, p, ld, pg, ldg, _mx(by_rows, "by_rows", gpu), _mx(by_cols, "by_cols", gpu),
+                                  _vector(col_sums, D, "col_sums", gpu), *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_mxfp4_quant")
 
 
 def dqrm_mxfp4_dequant(q: MxMatrix, out: torch.Tensor, stream=None) -> None:
-    dtype, _, _ = _kind(out, "out")
-    _check(lib().dqrm_mxfp4_dequant(q.ref, dtype, *_rows_of(out, q.rows, q.cols, out.dtype, "out"), _stream_of(out, stream)), "dqrm_mxfp4_dequant")
+    dtype, R, D, p, ld, gpu = _matrix(out, "out")
+    if R != q.rows or D != q.cols:
+        raise AssertionError(f"out: ({q.rows}, {q.cols}), got ({R}, {D})")
+    _check(lib().dqrm_mxfp4_dequant(_mx(q, "q", gpu), dtype, p, ld, _stream_of(gpu, stream)), "dqrm_mxfp4_dequant")
 
 
 def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -570,10 +593,11 @@ def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def dqrm_mxfp4_matmul(a: MxMatrix, b: MxMatrix, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    dtype, _, _ = _kind(out, "out")
-    po, ldo = _rows_of(out, a.rows, b.rows, out.dtype, "out")
-    _check(lib().dqrm_mxfp4_matmul(a.ref, b.ref, _vector(bias, b.rows, "bias"), relu, dtype, po, ldo, *_space(workspace),
-                                   _stream_of(out, stream)), "dqrm_mxfp4_matmul")
+    dtype, m, n, po, ldo, gpu = _matrix(out, "out")
+    if m != a.rows or n != b.rows:
+        raise AssertionError(f"out: ({a.rows}, {b.rows}), got ({m}, {n})")
+    _check(lib().dqrm_mxfp4_matmul(_mx(a, "a", gpu), _mx(b, "b", gpu), _vector(bias, n, "bias", gpu), relu, dtype, po, ldo,
+                                   *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_mxfp4_matmul")
 
 
 def dqrm_mxfp4_linear_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -584,22 +608,23 @@ def dqrm_mxfp4_linear(x: torch.Tensor, w: MxMatrix, out: torch.Tensor, bias: Opt
                       gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: Optional[float] = None,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """``eps`` given: x goes through a layer norm (with ``gamma`` and ``beta`` if given) first."""
-    dtype, m, _ = _kind(x, "x")
-    p, ld = _rows_of(x, m, w.cols, x.dtype, "x")
-    po, ldo = _rows_of(out, m, w.rows, x.dtype, "out")
-    _check(lib().dqrm_mxfp4_linear(dtype, m, p, ld, eps is not None, _vector(gamma, w.cols, "gamma"),
-                                   _vector(beta, w.cols, "beta"), eps or 0.0, w.ref, _vector(bias, w.rows, "bias"), relu, po, ldo,
-                                   *_space(workspace), _stream_of(x, stream)), "dqrm_mxfp4_linear")
+    dtype, m, k, p, ld, gpu = _matrix(x, "x")
+    if k != w.cols:
+        raise AssertionError(f"x: ({m}, {w.cols}), got ({m}, {k})")
+    po, ldo = _rows_of(out, m, w.rows, x.dtype, "out", gpu)
+    _check(lib().dqrm_mxfp4_linear(dtype, m, p, ld, eps is not None, _vector(gamma, k, "gamma", gpu), _vector(beta, k, "beta", gpu),
+                                   eps or 0.0, _mx(w, "w", gpu), _vector(bias, w.rows, "bias", gpu), relu, po, ldo,
+                                   *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_mxfp4_linear")
 
 
 def dqrm_layernorm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                        y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
                        q: Optional[MxMatrix] = None, stream=None) -> None:
-    dtype, R, D = _kind(x, "x")
-    p, ld = _rows_of(x, R, D, x.dtype, "x")
-    py, ldy = (None, 0) if y is None else _rows_of(y, R, D, x.dtype, "y")
-    _check(lib().dqrm_layernorm_fwd(dtype, R, D, p, ld, _vector(gamma, D, "gamma"), _vector(beta, D, "beta"), eps, py, ldy,
-                                    _vector(mean, R, "mean"), _vector(rstd, R, "rstd"), _mx(q), _stream_of(x, stream)), "dqrm_layernorm_fwd")
+    dtype, R, D, p, ld, gpu = _matrix(x, "x")
+    py, ldy = (None, 0) if y is None else _rows_of(y, R, D, x.dtype, "y", gpu)
+    _check(lib().dqrm_layernorm_fwd(dtype, R, D, p, ld, _vector(gamma, D, "gamma", gpu), _vector(beta, D, "beta", gpu), eps, py, ldy,
+                                    _vector(mean, R, "mean", gpu), _vector(rstd, R, "rstd", gpu), _mx(q, "q", gpu),
+                                    _stream_of(gpu, stream)), "dqrm_layernorm_fwd")
 
 
 def dqrm_layernorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
@@ -609,10 +634,9 @@ def dqrm_layernorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
 def dqrm_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
                        dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
                        dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    dtype, R, D = _kind(x, "x")
-    p, ld = _rows_of(x, R, D, x.dtype, "x")
-    pdy, lddy = _rows_of(dy, R, D, x.dtype, "dy")
-    pdx, lddx = (None, 0) if dx is None else _rows_of(dx, R, D, x.dtype, "dx")
-    _check(lib().dqrm_layernorm_bwd(dtype, R, D, pdy, lddy, p, ld, _vector(mean, R, "mean"), _vector(rstd, R, "rstd"),
-                                    _vector(gamma, D, "gamma"), pdx, lddx, _vector(dgamma, D, "dgamma"), _vector(dbeta, D, "dbeta"),
-                                    *_space(workspace), _stream_of(x, stream)), "dqrm_layernorm_bwd")
+    dtype, R, D, p, ld, gpu = _matrix(x, "x")
+    pdy, lddy = _rows_of(dy, R, D, x.dtype, "dy", gpu)
+    pdx, lddx = (None, 0) if dx is None else _rows_of(dx, R, D, x.dtype, "dx", gpu)
+    _check(lib().dqrm_layernorm_bwd(dtype, R, D, pdy, lddy, p, ld, _vector(mean, R, "mean", gpu), _vector(rstd, R, "rstd", gpu),
+                                    _vector(gamma, D, "gamma", gpu), pdx, lddx, _vector(dgamma, D, "dgamma", gpu),
+                                    _vector(dbeta, D, "dbeta", gpu), *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_layernorm_bwd")
