@@ -543,12 +543,19 @@ def _stream_of(gpu: int, stream) -> Optional[int]:
 
 
 class MxMatrix:
-    """A matrix in MXFP4 (see ``dqrm_mxfp4_t``): the device buffers of its codes and scales and the C descriptor."""
+    """A matrix in MXFP4 (see ``dqrm_mxfp4_t``): the device buffers of its codes and scales and the C descriptor.  Buffers that are not
+    given are made on ``device``: by default where the given one is, or else on torch's default device, or, that being the host, on the
+    current GPU (host memory where there is none: no call takes such a matrix)."""
 
     def __init__(self, rows: int, cols: int, device=None, codes: Optional[torch.Tensor] = None,
                  scales: Optional[torch.Tensor] = None):
         self.rows, self.cols = int(rows), int(cols)
         groups = -(-self.cols // 128)
+        if device is None and (codes is None or scales is None):
+            given = codes if codes is not None else scales
+            device = given.device if given is not None else torch.get_default_device()
+            if given is None and device.type == "cpu" and torch.cuda.is_available():
+                device = "cuda"
         byte = lambda n: torch.empty((self.rows, n), dtype=torch.uint8, device=device)  # noqa: E731
         self.codes = codes if codes is not None else byte(64 * groups)
         self.scales = scales if scales is not None else byte(4 * groups)

@@ -1,4 +1,5 @@
-"""CPU-only checks of where the operands of the layer norm and MXFP4 calls may be: in the memory of one GPU.  Tensors say that they are on a GPU, the library's calls are written down, and nothing is launched."""
+"""CPU-only checks of where the operands of the layer norm and MXFP4 calls may be: in the memory of one GPU.  Tensors say
+that they are on a GPU, the library's calls are written down, and nothing is launched."""
 import contextlib
 
 import pytest
@@ -124,3 +125,20 @@ def test_rows_on_top_of_each_other_are_left_to_the_library(monkeypatch):
     with pytest.raises(dq.DqrmError) as e:
         dq.dqrm_mxfp4_quant(on(0, 1, 64).expand(4, 64), matrix(0, 4, 64), stream=0)
     assert e.value.code == dq.ERR_INVALID_ARG and "operands" not in str(e.value)
+
+
+def test_a_matrix_is_made_where_its_calls_need_it(monkeypatch):
+    """On the current GPU if there is one and the default device is the host; beside the codes that are given."""
+    made = []
+    real = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: made.append(device) or real(*a, **k))
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    dq.MxMatrix(4, 64)
+    assert [torch.device(d).type for d in made] == ["cuda", "cuda"]
+    made.clear()
+    dq.MxMatrix(4, 64, codes=torch.zeros(4, 64, dtype=torch.uint8))
+    assert [torch.device(d).type for d in made] == ["cpu"]
+    made.clear()
+    monkeypatch.setattr(torch, "get_default_device", lambda: torch.device("cuda:1"))
+    dq.MxMatrix(4, 64)
+    assert [torch.device(d) for d in made] == [torch.device("cuda:1")] * 2
