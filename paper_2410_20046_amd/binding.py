@@ -512,7 +512,7 @@ def _rows_of(t: torch.Tensor, rows: int, cols: int, dtype, what: str, gpu: int) 
 def _vector(t: Optional[torch.Tensor], n: int, what: str, gpu: int) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not torch.float32 or t.shape != (n,) or not t.is_contiguous():
         raise AssertionError(f"{what}: {n} contiguous float32 values")
     if t.get_device() != gpu:
         raise _elsewhere(what)
@@ -531,6 +531,15 @@ def _space(ws: Optional[torch.Tensor], gpu: int) -> Tuple[Optional[int], int]:
 
 def _elsewhere(what: str) -> DqrmError:
     return DqrmError(ERR_INVALID_ARG, what, "not in the memory that the other operands are in")
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _there(gpu: int, call, *args) -> None:
+    """The call again with the operands' GPU the current one: a default stream's handle is null for every GPU."""
+    with torch.cuda.device(gpu):
+        call(*args)
 
 
 def _stream_of(gpu: int, stream) -> Optional[int]:
@@ -582,16 +591,26 @@ def dqrm_mxfp4_quant(x: torch.Tensor, by_rows: Optional[MxMatrix] = None, by_col
                      gate: Optional[torch.Tensor] = None, col_sums: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     dtype, R, D, p, ld, gpu = _matrix(x, "x")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_mxfp4_quant, x, by_rows, by_cols, gate, col_sums, workspace, stream)
     pg, ldg = (None, 0) if gate is None else _rows_of(gate, R, D, x.dtype, "gate", gpu)
-    _check(lib().dqrm_mxfp4_quant(dtype, R, D, p, ld, pg, ldg, _mx(by_rows, "by_rows", gpu), _mx(by_cols, "by_cols", gpu),
-                                  _vector(col_sums, D, "col_sums", gpu), *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_mxfp4_quant")
+    rc = lib().dqrm_mxfp4_quant(
+        dtype, R, D, p, ld, pg, ldg, _mx(by_rows, "by_rows", gpu), _mx(by_cols, "by_cols", gpu),
+        _vector(col_sums, D, "col_sums", gpu), *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_mxfp4_quant")
 
 
 def dqrm_mxfp4_dequant(q: MxMatrix, out: torch.Tensor, stream=None) -> None:
     dtype, R, D, p, ld, gpu = _matrix(out, "out")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_mxfp4_dequant, q, out, stream)
     if R != q.rows or D != q.cols:
         raise AssertionError(f"out: ({q.rows}, {q.cols}), got ({R}, {D})")
-    _check(lib().dqrm_mxfp4_dequant(_mx(q, "q", gpu), dtype, p, ld, _stream_of(gpu, stream)), "dqrm_mxfp4_dequant")
+    rc = lib().dqrm_mxfp4_dequant(
+        _mx(q, "q", gpu), dtype, p, ld, _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_mxfp4_dequant")
 
 
 def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -601,10 +620,15 @@ def dqrm_mxfp4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 def dqrm_mxfp4_matmul(a: MxMatrix, b: MxMatrix, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     dtype, m, n, po, ldo, gpu = _matrix(out, "out")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_mxfp4_matmul, a, b, out, bias, relu, workspace, stream)
     if m != a.rows or n != b.rows:
         raise AssertionError(f"out: ({a.rows}, {b.rows}), got ({m}, {n})")
-    _check(lib().dqrm_mxfp4_matmul(_mx(a, "a", gpu), _mx(b, "b", gpu), _vector(bias, n, "bias", gpu), relu, dtype, po, ldo,
-                                   *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_mxfp4_matmul")
+    rc = lib().dqrm_mxfp4_matmul(
+        _mx(a, "a", gpu), _mx(b, "b", gpu), _vector(bias, n, "bias", gpu), relu, dtype, po, ldo,
+        *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_mxfp4_matmul")
 
 
 def dqrm_mxfp4_linear_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -616,22 +640,30 @@ def dqrm_mxfp4_linear(x: torch.Tensor, w: MxMatrix, out: torch.Tensor, bias: Opt
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """``eps`` given: x goes through a layer norm (with ``gamma`` and ``beta`` if given) first."""
     dtype, m, k, p, ld, gpu = _matrix(x, "x")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_mxfp4_linear, x, w, out, bias, relu, gamma, beta, eps, workspace, stream)
     if k != w.cols:
         raise AssertionError(f"x: ({m}, {w.cols}), got ({m}, {k})")
     po, ldo = _rows_of(out, m, w.rows, x.dtype, "out", gpu)
-    _check(lib().dqrm_mxfp4_linear(dtype, m, p, ld, eps is not None, _vector(gamma, k, "gamma", gpu), _vector(beta, k, "beta", gpu),
-                                   eps or 0.0, _mx(w, "w", gpu), _vector(bias, w.rows, "bias", gpu), relu, po, ldo,
-                                   *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_mxfp4_linear")
+    rc = lib().dqrm_mxfp4_linear(
+        dtype, m, p, ld, eps is not None, _vector(gamma, k, "gamma", gpu), _vector(beta, k, "beta", gpu),
+        eps or 0.0, _mx(w, "w", gpu), _vector(bias, w.rows, "bias", gpu), relu, po, ldo, *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_mxfp4_linear")
 
 
 def dqrm_layernorm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                        y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
                        q: Optional[MxMatrix] = None, stream=None) -> None:
     dtype, R, D, p, ld, gpu = _matrix(x, "x")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_layernorm_fwd, x, gamma, beta, eps, y, mean, rstd, q, stream)
     py, ldy = (None, 0) if y is None else _rows_of(y, R, D, x.dtype, "y", gpu)
-    _check(lib().dqrm_layernorm_fwd(dtype, R, D, p, ld, _vector(gamma, D, "gamma", gpu), _vector(beta, D, "beta", gpu), eps, py, ldy,
-                                    _vector(mean, R, "mean", gpu), _vector(rstd, R, "rstd", gpu), _mx(q, "q", gpu),
-                                    _stream_of(gpu, stream)), "dqrm_layernorm_fwd")
+    rc = lib().dqrm_layernorm_fwd(
+        dtype, R, D, p, ld, _vector(gamma, D, "gamma", gpu), _vector(beta, D, "beta", gpu), eps, py, ldy,
+        _vector(mean, R, "mean", gpu), _vector(rstd, R, "rstd", gpu), _mx(q, "q", gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_layernorm_fwd")
 
 
 def dqrm_layernorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
@@ -642,8 +674,13 @@ def dqrm_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
                        dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
                        dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     dtype, R, D, p, ld, gpu = _matrix(x, "x")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_layernorm_bwd, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, workspace, stream)
     pdy, lddy = _rows_of(dy, R, D, x.dtype, "dy", gpu)
     pdx, lddx = (None, 0) if dx is None else _rows_of(dx, R, D, x.dtype, "dx", gpu)
-    _check(lib().dqrm_layernorm_bwd(dtype, R, D, pdy, lddy, p, ld, _vector(mean, R, "mean", gpu), _vector(rstd, R, "rstd", gpu),
-                                    _vector(gamma, D, "gamma", gpu), pdx, lddx, _vector(dgamma, D, "dgamma", gpu),
-                                    _vector(dbeta, D, "dbeta", gpu), *_space(workspace, gpu), _stream_of(gpu, stream)), "dqrm_layernorm_bwd")
+    rc = lib().dqrm_layernorm_bwd(
+        dtype, R, D, pdy, lddy, p, ld, _vector(mean, R, "mean", gpu), _vector(rstd, R, "rstd", gpu),
+        _vector(gamma, D, "gamma", gpu), pdx, lddx, _vector(dgamma, D, "dgamma", gpu), _vector(dbeta, D, "dbeta", gpu),
+        *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_layernorm_bwd")

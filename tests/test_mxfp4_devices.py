@@ -1,5 +1,6 @@
-"""CPU-only checks of where the operands of the layer norm and MXFP4 calls may be: in the memory of one GPU.  Tensors say
-that they are on a GPU, the library's calls are written down, and nothing is launched."""
+"""CPU-only checks of where the operands of the layer norm and MXFP4 calls may be: in the memory of one GPU, which
+is the current device while the call is made.  Tensors say that they are on a GPU, the library's calls are written down, and nothing is
+launched."""
 import contextlib
 
 import pytest
@@ -125,6 +126,17 @@ def test_rows_on_top_of_each_other_are_left_to_the_library(monkeypatch):
     with pytest.raises(dq.DqrmError) as e:
         dq.dqrm_mxfp4_quant(on(0, 1, 64).expand(4, 64), matrix(0, 4, 64), stream=0)
     assert e.value.code == dq.ERR_INVALID_ARG and "operands" not in str(e.value)
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_a_call_is_made_on_the_gpu_that_holds_its_operands(call, library):
+    for current in (0, 1):
+        for gpu in (0, 1, 3):
+            library.current, library.calls = current, []
+            make(call, {"all": gpu})
+            make(call, {"all": gpu}, stream=77)
+            assert [c[1:] for c in library.calls] == [(0 if gpu == 0 else 100 + gpu, gpu), (77, gpu)]
+            assert library.current == current
 
 
 def test_a_matrix_is_made_where_its_calls_need_it(monkeypatch):
