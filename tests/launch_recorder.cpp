@@ -3,6 +3,7 @@
 // does on the card.
 #include <cstddef>
 #include <cstring>
+#include <iterator>
 #include <map>
 #include <string>
 #include <vector>
@@ -76,6 +77,13 @@ int hipDeviceGetAttribute(int *value, int, int)
     return 0;
 }
 
+int known_kernels() { return (int)names().size(); }
+const char *known_kernel(int i) // of the library
+{
+    auto it = names().begin();
+    std::advance(it, i);
+    return it->second.c_str();
+}
 int recorded_launches() { return (int)launches.size(); }
 const char *recorded_name(int i) { return launches[i].name.c_str(); }
 void recorded_shape(int i, unsigned *out) // grid, block, shared memory, whether it failed

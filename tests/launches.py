@@ -44,13 +44,30 @@ def _recorder():
 
 def would_launch(calls):
     """[(return code, [Launch, ...])] of the calls."""
-    command = [sys.executable, os.path.abspath(__file__), _recorder(), LIB]
-    r = subprocess.run(command, input=json.dumps(calls), stdout=subprocess.PIPE, text=True, check=True)
-    out = json.loads(r.stdout)
-    names = sorted({l[0] for _, ls in out for l in ls})
-    plain = subprocess.run(["c++filt"], input="\n".join(names), stdout=subprocess.PIPE, text=True, check=True).stdout.splitlines() if names else []
-    clear = {n: re.sub(r"^void ", "", re.sub(r"\([^()]*\)$", "", p)).replace("dqrm_mx::", "").replace("(anonymous namespace)::", "") for n, p in zip(names, plain)}
+    out = _ask(calls)["calls"]
+    clear = _readable({l[0] for _, ls in out for l in ls})
     return [(rc, [Launch(clear[n], tuple(s[:3]), tuple(s[3:6]), s[6], bool(s[7])) for n, s in ls]) for rc, ls in out]
+
+
+def library_kernels():
+    """The names of all kernels that the library has."""
+    return set(_readable(set(_ask([])["kernels"])).values())
+
+
+def _ask(calls):
+    command = [sys.executable, os.path.abspath(__file__), _recorder(), LIB]
+    return json.loads(subprocess.run(command, input=json.dumps(calls), stdout=subprocess.PIPE, text=True, check=True).stdout)
+
+
+def _readable(names):
+    """Without types of arguments and namespaces; element types as they are in C (the demangler may not know the 16-bit ones)."""
+    names = sorted(names)
+    if not names:
+        return {}
+    known = "\n".join(n.replace("IDF16b", "I4bf16").replace("IDF16_", "I4half") for n in names)
+    plain = subprocess.run(["c++filt"], input=known, stdout=subprocess.PIPE, text=True, check=True).stdout.splitlines()
+    short = [re.sub(r"^void ", "", re.sub(r"\([^()]*\)$", "", p)) for p in plain]
+    return {n: p.replace("dqrm_mx::", "").replace("(anonymous namespace)::", "").replace("(FewSource)", "") for n, p in zip(names, short)}
 
 
 class _Mx(C.Structure):
@@ -79,7 +96,8 @@ def _main():
             recorder.recorded_shape(i, shape)
             launches.append((recorder.recorded_name(i).decode(), list(shape)))
         out.append((rc, launches))
-    json.dump(out, sys.stdout)
+    recorder.known_kernel.restype = C.c_char_p
+    json.dump({"calls": out, "kernels": [recorder.known_kernel(i).decode() for i in range(recorder.known_kernels())]}, sys.stdout)
 
 
 if __name__ == "__main__":
