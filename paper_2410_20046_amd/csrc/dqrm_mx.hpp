@@ -294,8 +294,9 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a, dqrm::Fast
 // A workgroup takes 128 rows by 128 columns.  The chunks that its lanes load are blocks of rows already (four lanes to a block);
 // the tile then goes through LDS in its own type, and each wave takes 32 rows of it, two columns to a lane: a block of a column is
 // in one lane's registers.  128 because a line of the columns' codes is 64 bytes of 128 values.  Bound by its bytes, then by the
-// columns' stores of half lines: 16384 x 8191 bfloat16 both ways (411 MB) 100 us, 4.1 TB/s, where a copy has 5.1; by rows alone
-// 8192 x 2048 with a gate and column sums 19 us (85 MB).
+// columns' stores of half lines: 16384 x 8191 bfloat16 both ways (411 MB) 100 us, 4.1 TB/s, where a copy has 5.1; 8192 x 2048 with a
+// gate and column sums 19 us (85 MB).  By columns alone 71 us (340 MB, 4.8 TB/s), of 8192 x 2048 11.5 us (42 MB).  Float, which has half the
+// workgroups to a CU: both ways 149 us (679 MB, 4.6 TB/s), by columns 125 (608 MB); 2048 x 2048 6 us.
 constexpr int kTile = 128;
 
 template <int DT>

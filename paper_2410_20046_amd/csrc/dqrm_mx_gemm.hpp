@@ -3,10 +3,11 @@
 // v_mfma_scale_f32_32x32x64_f8f6f4 takes 32 codes of a row from each lane, one block with one scale byte: lane l holds row l % 32,
 // block l / 32 of the 64 values.  Sums are held in 32 bits.
 //
-// What bounds them: from registers alone the instruction reaches 8.4 PFLOP/s with one code throughout and 6.4 with random ones, at which
-// the card lowers its clock.  16384 x 8192 x 8192 takes 490 to 510 us, 4.3 to 4.5 PFLOP/s: behind tiles of 256 a wave reads 6 operands
-// from LDS for 8 products, and the barriers of a stage (256 values of k) cost the rest.  A tile of 128 reads 4 for 4 or 3 for 2 and is
-// bound by LDS.  Short sums are bound by the launch, the first loads' latency and the output's stores: 8192 x 512 x 415 in float, 8 us.
+// What bounds them: from registers alone the instruction reaches 9.6 PFLOP/s with one code throughout and 6.2 with random ones, at which
+// the card lowers its clock.  16384 x 8192 x 8192 takes 490 to 515 us, 4.3 to 4.5 PFLOP/s: tiles of 256 (6 operands read from LDS for 8
+// products, two barriers to a stage of 256 values of k) keep the matrix cores at work for 67 % of the time and LDS for 41 %.  Tiles of 128 (4
+// operands for 4 products, or 3 for 2) have one barrier to a stage and few products between two of them: 2048 x 2048 x 8192, 27 us, matrix
+// cores 36 %, LDS 40 %; no unit is at its limit, what is left is waiting.  Short sums are bound by the launch, the first loads' latency and the output's stores: 8192 x 512 x 415 in float, 8 us.
 #pragma once
 
 #include <type_traits>
