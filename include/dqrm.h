@@ -16,7 +16,9 @@
  *   dqrm_dense_step      every step      MLPs, interaction, loss, their backward, dense SGD
  *   dqrm_dense_step_quant  the same with channel-wise INT4 weights and / or INT8 gradients + error compensation
  * Apart from that step, for wider dense parts than it has: layer norm (dqrm_layernorm_fwd, _bwd) and linear layers whose
- * operands are held in 4 bits with a scale to every 32 values (dqrm_mxfp4_quant, _dequant, _matmul, _linear).
+ * operands are held in 4 bits with a scale to every 32 values (dqrm_mxfp4_quant, _dequant, _matmul, _linear); the join of a block with
+ * its residual stream and the norms around it (dqrm_residual_norm_fwd, _bwd); a loss over many classes (dqrm_softmax_xent_fwd, _bwd);
+ * and, behind any of the backward passes, the clip of all gradients by their norm (dqrm_grad_norm, _scale, _clip).
  *
  * Conventions common to every entry point
  *   - Returns 0 (DQRM_OK) or a negative DQRM_ERR_* code.  Never throws, never aborts.
@@ -34,7 +36,7 @@
  *     the first problem in a per-device status word that dqrm_check_status()
  *     reads and clears.
  *   - All floating point is IEEE binary32, one rounding per operation (no fused
- *     multiply-add), true division; the layer norm and the MXFP4 calls state theirs.
+ *     multiply-add), true division; the layer norm, the MXFP4 calls and what follows them state theirs.
  *
  * The quantiser (the paper states "uniform", "one scale per table"; the formula
  * is this library's reading): scale = max(absmax / (2^(b-1) - 1), 1e-8),
@@ -506,6 +508,100 @@ size_t dqrm_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
 int32_t dqrm_layernorm_bwd(int32_t dtype, int64_t rows, int64_t cols, const void *dy, int64_t lddy, const void *x,
                            int64_t ldx, const float *mean, const float *rstd, const float *gamma, void *dx, int64_t lddx,
                            float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- residual norms -----------------------------------------------------------------------------------------------
+ * The join of a block's output u with the residual stream r, and the norms around it:
+ *   out = res_scale r + gate N1(u)      (post: the norm behind the block)
+ *   y   = N2(out)                       (pre: the norm before the next block; of out before its rounding)
+ * N(v) = (v - mean) rstd gamma + beta over a row, rstd = 1 / sqrt(sum (v - mean)^2 / cols + eps); DQRM_NORM_LAYER: mean = sum v / cols,
+ * DQRM_NORM_RMS: mean = 0, DQRM_NORM_NONE: no norm (N(v) = v; without `pre` there is no y).  gate, gammas and betas are [cols] fp32 or
+ * NULL (1 and 0; a norm that is not there has none).  1 <= cols <= 16384, more are DQRM_ERR_UNSUPPORTED.  The struct is read on the host
+ * during the call. */
+#define DQRM_NORM_NONE 0
+#define DQRM_NORM_LAYER 1
+#define DQRM_NORM_RMS 2
+typedef struct {
+    int32_t post, pre;
+    const float *post_gamma, *post_beta, *gate, *pre_gamma, *pre_beta;
+    float res_scale, post_eps, pre_eps;
+} dqrm_residual_norm_t;
+
+/* u, r, out, y: [rows][cols] of one type; out may be r's or u's own memory, with the same stride.  y and q (y in MXFP4, quantised from its
+ * 32-bit values) may be NULL.  stats: [4][rows] fp32 or NULL: mean and rstd of N1, mean and rstd of N2 (what the backward needs); those of
+ * a norm that is not there are not written. */
+int32_t dqrm_residual_norm_fwd(int32_t dtype, int64_t rows, int64_t cols, const dqrm_residual_norm_t *norm, const void *u, int64_t ldu, const void *r,
+                               int64_t ldr, void *out, int64_t ldo, void *y, int64_t ldy, float *stats, const dqrm_mxfp4_t *q, void *stream);
+
+/* Its backward, from the gradients of out along the residual stream (dout, or NULL: none) and of y (dy; with `pre` alone):
+ *   g = dout + N2'(dy), dr = res_scale g, du = N1'(gate g)     du, dr: or NULL
+ *   dparams [5][cols] fp32 or NULL: the gradients of post_gamma, post_beta, gate, pre_gamma, pre_beta, whether those are given or
+ *   NULL; of a norm that is not there zeros.  Needs the workspace (256-byte aligned); the order of addition depends on the shape alone.
+ * N' takes the statistics, u and out as the forward left them; u may be NULL without `post` and dparams.  du and dr may be the memory of a
+ * matrix that is read, with the same stride, but not each other's.  rows = 0 gives dparams of zeros. */
+size_t dqrm_residual_norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+int32_t dqrm_residual_norm_bwd(int32_t dtype, int64_t rows, int64_t cols, const dqrm_residual_norm_t *norm, const void *dout, int64_t lddout, const void *dy,
+                               int64_t lddy, const void *u, int64_t ldu, const void *out, int64_t ldo, const float *stats, void *du, int64_t lddu, void *dr,
+                               int64_t lddr, float *dparams, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- softmax cross entropy over many classes ------------------------------------------------------------------------
+ * The loss of a linear classifier whose classes are the rows of w (the items of a table, say), without the logits in memory:
+ *   l[i][j] = scale (x_i . w_j) + bias[j], lse_i = log sum over j of exp(l[i][j]), loss_i = lse_i - l[i][targets[i]]
+ * x [rows][width], w [classes][width] of one type; bias [classes] fp32 or NULL (0; -infinity takes a class out); scale finite;
+ * targets [rows] int64.  A negative target: the row has none, its loss is 0 and it has no gradient.  A target >= classes is recorded as
+ * DQRM_ERR_INDEX_OUT_OF_RANGE (table -1, the target) by the forward and counts as none.  lse [rows] fp32 is what the backward needs.
+ * A row with all its classes taken out has lse = -infinity, loss = +infinity and no gradient; a row with a target that alone is taken out
+ * has loss = +infinity and the gradient of lse, less that of the target's logit.  An infinity in x or w counts as a NaN, and one in a logit
+ * other than by bias = -infinity gives NaN.
+ * Products are of 16-bit values as they are and of fp32 values as sums of three bfloat16 (six of the nine products, as in the dense step);
+ * sums, maxima and exponentials are fp32.  classes >= 1 unless rows = 0; rows, classes and width up to 2147482623, the tiles of 256 by 256
+ * of any two of them up to 4194304, width and row strides up to 4194304; more are DQRM_ERR_UNSUPPORTED.  The order of all sums depends on shape,
+ * strides and type alone. */
+size_t dqrm_softmax_xent_fwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);
+int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                              const float *bias, float scale, const int64_t *targets, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                              void *stream);
+
+/* Its backward, for the gradients grad [rows] fp32 of the rows' losses: with d[i][j] = grad_i (exp(l[i][j] - lse_i) - (1 if j = targets[i])),
+ *   dx = scale d w, dw = scale d^T x (of x's type), dbias[j] = sum over i of d[i][j] (fp32)     each may be NULL, but not all
+ * The logits are computed again, some classes at a time.  d is rounded to the type (fp16: times a power of two that puts the largest |grad| at
+ * 2^15; fp32: kept as three bfloat16) for the products, not for dbias. */
+size_t dqrm_softmax_xent_bwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);
+int32_t dqrm_softmax_xent_bwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                              const float *bias, float scale, const int64_t *targets, const float *lse, const float *grad, void *dx, int64_t lddx, void *dw,
+                              int64_t lddw, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- the norm of all gradients, and the clip ------------------------------------------------------------------------
+ * A gradient tensor: [rows][cols] of `dtype` with a row stride (ld >= cols; any value if there is one row; a flat buffer is one row).
+ *   out    where the scaled values go, [rows][cols] of the same type with stride ld_out; NULL: in place.  Not to overlap other tensors' memory.
+ *   count  device int32, or NULL: only the first `count` rows are there (clamped to 0 .. rows), what lies behind them is neither read
+ *          nor written: the `values` of a table's sparse gradient with their num_unique
+ * The array of these is HOST memory, read during the call; up to 65536 tensors of 2^44 values in all. */
+typedef struct {
+    void *data;
+    int64_t rows, cols, ld;
+    void *out;
+    int64_t ld_out;
+    const int32_t *count;
+    int32_t dtype;
+} dqrm_grad_t;
+
+#define DQRM_GRAD_NORM_2 0   /* sqrt of the sum of all squares (squares and sums in 64 bits) */
+#define DQRM_GRAD_NORM_MAX 1 /* the largest magnitude */
+
+/* norm [1] fp32: of all tensors together; norms [n] fp32 or NULL: of each.  A NaN anywhere gives NaN.  No tensors, or none with
+ * values: 0.  The order of addition depends on the shapes alone (rows behind a count add nothing). */
+size_t dqrm_grad_workspace_bytes(const dqrm_grad_t *grads, int32_t n);
+int32_t dqrm_grad_norm(const dqrm_grad_t *grads, int32_t n, int32_t kind, float *norm, float *norms, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Each value times max_norm / norm (a 32-bit quotient, product rounded once to the type) where norm > max_norm >= 0.  Where it is not, and where
+ * norm is infinite or NaN (the caller sees it and drops the step), values keep their bits; `out` then is a copy.  `norm`: device memory, from
+ * dqrm_grad_norm, or joined over several GPUs.  Tensors that are written must not overlap: the same memory twice is
+ * DQRM_ERR_INVALID_ARG; rows may lie in the gaps between another tensor's rows. */
+int32_t dqrm_grad_scale(const dqrm_grad_t *grads, int32_t n, const float *norm, float max_norm, void *stream);
+
+/* dqrm_grad_norm and dqrm_grad_scale in one call. */
+int32_t dqrm_grad_clip(const dqrm_grad_t *grads, int32_t n, int32_t kind, float max_norm, float *norm, float *norms, void *workspace, size_t workspace_bytes,
+                       void *stream);
 
 /* Synchronises `stream`, returns the first data-dependent problem recorded on
  * the current device since the last call (DQRM_OK if none) and clears it.

@@ -16,5 +16,8 @@ from .binding import (  # noqa: F401
     F32, BF16, F16, MxMatrix, dqrm_mxfp4_t, dqrm_mxfp4_quant_workspace_bytes, dqrm_mxfp4_quant, dqrm_mxfp4_dequant,
     dqrm_mxfp4_matmul_workspace_bytes, dqrm_mxfp4_matmul, dqrm_mxfp4_linear_workspace_bytes, dqrm_mxfp4_linear,
     dqrm_layernorm_fwd, dqrm_layernorm_bwd_workspace_bytes, dqrm_layernorm_bwd,
+    NORM_NONE, NORM_LAYER, NORM_RMS, ResidualNorm, dqrm_residual_norm_t, dqrm_residual_norm_fwd, dqrm_residual_norm_bwd_workspace_bytes,
+    dqrm_residual_norm_bwd, dqrm_softmax_xent_fwd_workspace_bytes, dqrm_softmax_xent_fwd, dqrm_softmax_xent_bwd_workspace_bytes,
+    dqrm_softmax_xent_bwd, GRAD_NORM_2, GRAD_NORM_MAX, Grads, dqrm_grad_t, dqrm_grad_workspace_bytes, dqrm_grad_norm, dqrm_grad_scale, dqrm_grad_clip,
 )
 from .build import build_library  # noqa: F401

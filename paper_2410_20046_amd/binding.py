@@ -43,7 +43,10 @@ EXPORTS = ("dqrm_find_scale", "dqrm_pack_int4", "dqrm_embbag_fwd", "dqrm_embbag_
            "dqrm_quant_update", "dqrm_fwd_bwd_step", "dqrm_dense_workspace_bytes", "dqrm_dense_step",
            "dqrm_dense_param_count", "dqrm_dense_step_quant", "dqrm_mxfp4_quant_workspace_bytes", "dqrm_mxfp4_quant",
            "dqrm_mxfp4_dequant", "dqrm_mxfp4_matmul_workspace_bytes", "dqrm_mxfp4_matmul", "dqrm_mxfp4_linear_workspace_bytes",
-           "dqrm_mxfp4_linear", "dqrm_layernorm_fwd", "dqrm_layernorm_bwd_workspace_bytes", "dqrm_layernorm_bwd", "dqrm_check_status", "dqrm_last_hip_error", "dqrm_version")
+           "dqrm_mxfp4_linear", "dqrm_layernorm_fwd", "dqrm_layernorm_bwd_workspace_bytes", "dqrm_layernorm_bwd",
+           "dqrm_residual_norm_fwd", "dqrm_residual_norm_bwd_workspace_bytes", "dqrm_residual_norm_bwd",
+           "dqrm_softmax_xent_fwd_workspace_bytes", "dqrm_softmax_xent_fwd", "dqrm_softmax_xent_bwd_workspace_bytes", "dqrm_softmax_xent_bwd",
+           "dqrm_grad_workspace_bytes", "dqrm_grad_norm", "dqrm_grad_scale", "dqrm_grad_clip", "dqrm_check_status", "dqrm_last_hip_error", "dqrm_version")
 
 
 class DqrmError(RuntimeError):
@@ -99,6 +102,18 @@ class dqrm_mxfp4_t(C.Structure):
     _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
+class dqrm_residual_norm_t(C.Structure):
+    _fields_ = [("post", C.c_int32), ("pre", C.c_int32), ("post_gamma", C.c_void_p), ("post_beta", C.c_void_p), ("gate", C.c_void_p),
+                ("pre_gamma", C.c_void_p), ("pre_beta", C.c_void_p), ("res_scale", C.c_float), ("post_eps", C.c_float), ("pre_eps", C.c_float)]
+
+
+class dqrm_grad_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("out", C.c_void_p), ("ld_out", C.c_int64),
+                ("count", C.c_void_p), ("dtype", C.c_int32)]
+
+
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+GRAD_NORM_2, GRAD_NORM_MAX = 0, 1
 F32, BF16, F16 = 0, 1, 2
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
@@ -166,6 +181,21 @@ def lib() -> C.CDLL:
             getattr(L, f"dqrm_mxfp4_{n}_workspace_bytes").restype = sz
         L.dqrm_mxfp4_dequant.restype = L.dqrm_layernorm_fwd.restype = L.dqrm_layernorm_bwd.restype = i32
         L.dqrm_layernorm_bwd_workspace_bytes.restype = sz
+        np_, gp = C.POINTER(dqrm_residual_norm_t), C.POINTER(dqrm_grad_t)
+        L.dqrm_residual_norm_fwd.argtypes = [i32, i64, i64, np_, vp, i64, vp, i64, vp, i64, vp, i64, vp, qp, vp]
+        L.dqrm_residual_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.dqrm_residual_norm_bwd.argtypes = [i32, i64, i64, np_] + [vp, i64] * 4 + [vp] + [vp, i64] * 2 + [vp, vp, sz, vp]
+        L.dqrm_softmax_xent_fwd_workspace_bytes.argtypes = L.dqrm_softmax_xent_bwd_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.dqrm_softmax_xent_fwd.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, f32, vp, vp, vp, vp, sz, vp]
+        L.dqrm_softmax_xent_bwd.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, f32, vp, vp, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.dqrm_grad_workspace_bytes.argtypes = [gp, i32]
+        L.dqrm_grad_norm.argtypes = [gp, i32, i32, vp, vp, vp, sz, vp]
+        L.dqrm_grad_scale.argtypes = [gp, i32, vp, f32, vp]
+        L.dqrm_grad_clip.argtypes = [gp, i32, i32, f32, vp, vp, vp, sz, vp]
+        for n in ("residual_norm_fwd", "residual_norm_bwd", "softmax_xent_fwd", "softmax_xent_bwd", "grad_norm", "grad_scale", "grad_clip"):
+            getattr(L, f"dqrm_{n}").restype = i32
+        for n in ("residual_norm_bwd", "softmax_xent_fwd", "softmax_xent_bwd", "grad"):
+            getattr(L, f"dqrm_{n}_workspace_bytes").restype = sz
         L.dqrm_check_status.argtypes = [vp, C.POINTER(i32), C.POINTER(i64)]
         for n in ("dqrm_find_scale", "dqrm_pack_int4", "dqrm_embbag_fwd", "dqrm_embbag_bwd", "dqrm_dedupe", "dqrm_segment_sum",
                   "dqrm_quant_update", "dqrm_grad_quant_int8", "dqrm_sparse_update", "dqrm_check_status"):
@@ -684,3 +714,214 @@ def dqrm_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
         *_space(workspace, gpu), _stream_of(gpu, stream))
     if rc != OK:
         _check(rc, "dqrm_layernorm_bwd")
+
+
+# ---- residual norms, a loss over many classes, the clip of all gradients -----------------------------------------------------
+
+
+class ResidualNorm:
+    """Descriptor of the norms around a residual join (see ``dqrm_residual_norm_t``); the vectors (device, float32) stay owned by the
+    caller.  They have to be contiguous, of one length and in one GPU's memory."""
+
+    def __init__(self, post: int = NORM_NONE, pre: int = NORM_RMS, post_gamma: Optional[torch.Tensor] = None, post_beta: Optional[torch.Tensor] = None,
+                 gate: Optional[torch.Tensor] = None, pre_gamma: Optional[torch.Tensor] = None, pre_beta: Optional[torch.Tensor] = None,
+                 res_scale: float = 1.0, post_eps: float = 1e-5, pre_eps: float = 1e-5):
+        vectors = (post_gamma, post_beta, gate, pre_gamma, pre_beta)
+        given = [v for v in vectors if v is not None]
+        self.cols = given[0].numel() if given else None  # None: any
+        self.gpu = given[0].get_device() if given else None
+        self._keep = vectors
+        p = [_vector(v, self.cols, "ResidualNorm", self.gpu) for v in vectors]
+        self.c = dqrm_residual_norm_t(post, pre, *p, res_scale, post_eps, pre_eps)
+        self.ref = C.byref(self.c)
+
+
+def _norm_of(norm: ResidualNorm, cols: int, gpu: int):
+    if norm.cols is not None and norm.cols != cols:
+        raise AssertionError(f"norm: vectors of {cols}, got {norm.cols}")
+    if norm.gpu is not None and norm.gpu != gpu:
+        raise _elsewhere("norm")
+    return norm.ref
+
+
+def _rows_block(t: Optional[torch.Tensor], n: int, cols: int, what: str, gpu: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.shape != (n, cols) or not t.is_contiguous():
+        raise AssertionError(f"{what}: ({n}, {cols}) contiguous float32 values")
+    if t.get_device() != gpu:
+        raise _elsewhere(what)
+    return t.data_ptr()
+
+
+def dqrm_residual_norm_fwd(norm: ResidualNorm, u: torch.Tensor, r: torch.Tensor, out: torch.Tensor, y: Optional[torch.Tensor] = None,
+                           stats: Optional[torch.Tensor] = None, q: Optional[MxMatrix] = None, stream=None) -> None:
+    dtype, R, D, p, ld, gpu = _matrix(u, "u")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_residual_norm_fwd, norm, u, r, out, y, stats, q, stream)
+    pr, ldr = _rows_of(r, R, D, u.dtype, "r", gpu)
+    po, ldo = _rows_of(out, R, D, u.dtype, "out", gpu)
+    py, ldy = (None, 0) if y is None else _rows_of(y, R, D, u.dtype, "y", gpu)
+    rc = lib().dqrm_residual_norm_fwd(
+        dtype, R, D, _norm_of(norm, D, gpu), p, ld, pr, ldr, po, ldo, py, ldy, _rows_block(stats, 4, R, "stats", gpu), _mx(q, "q", gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_residual_norm_fwd")
+
+
+def dqrm_residual_norm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().dqrm_residual_norm_bwd_workspace_bytes(rows, cols))
+
+
+def dqrm_residual_norm_bwd(norm: ResidualNorm, dout: Optional[torch.Tensor], dy: Optional[torch.Tensor], u: Optional[torch.Tensor],
+                           out: Optional[torch.Tensor], stats: Optional[torch.Tensor], du: Optional[torch.Tensor] = None,
+                           dr: Optional[torch.Tensor] = None, dparams: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                           stream=None) -> None:
+    """``u`` may be None without a norm behind the block and without ``dparams``, ``dy`` and ``out`` without one before the next."""
+    first = dout if dout is not None else dy
+    if first is None:
+        raise AssertionError("dout or dy: a gradient")
+    dtype, R, D, _, _, gpu = _matrix(first, "dout" if dout is not None else "dy")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_residual_norm_bwd, norm, dout, dy, u, out, stats, du, dr, dparams, workspace, stream)
+    at = lambda t, what: (None, 0) if t is None else _rows_of(t, R, D, first.dtype, what, gpu)  # noqa: E731
+    rc = lib().dqrm_residual_norm_bwd(
+        dtype, R, D, _norm_of(norm, D, gpu), *at(dout, "dout"), *at(dy, "dy"), *at(u, "u"), *at(out, "out"), _rows_block(stats, 4, R, "stats", gpu),
+        *at(du, "du"), *at(dr, "dr"), _rows_block(dparams, 5, D, "dparams", gpu), *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_residual_norm_bwd")
+
+
+def _targets_of(t: torch.Tensor, rows: int, gpu: int) -> int:
+    if t.dtype is not torch.int64 or t.shape != (rows,) or not t.is_contiguous():
+        raise AssertionError(f"targets: {rows} contiguous int64 values")
+    if t.get_device() != gpu:
+        raise _elsewhere("targets")
+    return t.data_ptr()
+
+
+def dqrm_softmax_xent_fwd_workspace_bytes(rows: int, classes: int, width: int, dtype: torch.dtype) -> int:
+    return int(lib().dqrm_softmax_xent_fwd_workspace_bytes(rows, classes, width, _DTYPES[dtype]))
+
+
+def dqrm_softmax_xent_fwd(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                          bias: Optional[torch.Tensor] = None, scale: float = 1.0, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    dtype, M, K, p, ld, gpu = _matrix(x, "x")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_softmax_xent_fwd, x, w, targets, loss, lse, bias, scale, workspace, stream)
+    V = w.shape[0]
+    pw, ldw = _rows_of(w, V, K, x.dtype, "w", gpu)
+    rc = lib().dqrm_softmax_xent_fwd(
+        dtype, M, V, K, p, ld, pw, ldw, _vector(bias, V, "bias", gpu), scale, _targets_of(targets, M, gpu), _vector(loss, M, "loss", gpu),
+        _vector(lse, M, "lse", gpu), *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_softmax_xent_fwd")
+
+
+def dqrm_softmax_xent_bwd_workspace_bytes(rows: int, classes: int, width: int, dtype: torch.dtype) -> int:
+    return int(lib().dqrm_softmax_xent_bwd_workspace_bytes(rows, classes, width, _DTYPES[dtype]))
+
+
+def dqrm_softmax_xent_bwd(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad: torch.Tensor,
+                          dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                          bias: Optional[torch.Tensor] = None, scale: float = 1.0, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``lse``: the forward's; ``grad``: the gradients of the rows' losses (1 / rows each for their mean)."""
+    dtype, M, K, p, ld, gpu = _matrix(x, "x")
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_softmax_xent_bwd, x, w, targets, lse, grad, dx, dw, dbias, bias, scale, workspace, stream)
+    V = w.shape[0]
+    pw, ldw = _rows_of(w, V, K, x.dtype, "w", gpu)
+    pdx, lddx = (None, 0) if dx is None else _rows_of(dx, M, K, x.dtype, "dx", gpu)
+    pdw, lddw = (None, 0) if dw is None else _rows_of(dw, V, K, x.dtype, "dw", gpu)
+    rc = lib().dqrm_softmax_xent_bwd(
+        dtype, M, V, K, p, ld, pw, ldw, _vector(bias, V, "bias", gpu), scale, _targets_of(targets, M, gpu), _vector(lse, M, "lse", gpu),
+        _vector(grad, M, "grad", gpu), pdx, lddx, pdw, lddw, _vector(dbias, V, "dbias", gpu), *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_softmax_xent_bwd")
+
+
+def _grad_rows(t: torch.Tensor) -> Tuple[int, int, int]:
+    """(rows, columns, row stride): a tensor whose values lie one behind the other is one row, but a matrix keeps its rows."""
+    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1):
+        return t.shape[0], t.shape[1], t.stride(0)
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() == 1:  # a column
+        return t.shape[0], 1, t.stride(0)
+    raise AssertionError("a gradient: contiguous, or a matrix whose rows are")
+
+
+class Grads:
+    """Gradient tensors of any shapes, float32, bfloat16 and float16 mixed, in one GPU's memory, and the C descriptors (see ``dqrm_grad_t``):
+    made once for the buffers that a program keeps its gradients in, which stay owned by the caller.  ``out``: as many tensors of the same
+    shapes and types, or None: scaled in place.  ``counts``: {number of a tensor (a matrix): int32 tensor of one value, how many of its rows
+    are there}."""
+
+    def __init__(self, tensors, out=None, counts=None):
+        tensors = list(tensors)
+        outs = [None] * len(tensors) if out is None else list(out)
+        counts = dict(counts or {})
+        if len(outs) != len(tensors) or not all(0 <= k < len(tensors) for k in counts):
+            raise AssertionError("Grads: an output to each tensor, counts of tensors that are there")
+        self._keep = (tensors, outs, counts)
+        self.n = len(tensors)
+        self.gpu = tensors[0].get_device() if tensors else None
+        self.c = (dqrm_grad_t * max(self.n, 1))()
+        for k, (t, o) in enumerate(zip(tensors, outs)):
+            dtype = _DTYPES.get(t.dtype)
+            if dtype is None or (o is not None and (o.dtype is not t.dtype or o.shape != t.shape)):
+                raise AssertionError("Grads: float32, bfloat16 or float16, and outputs of the same shapes and types")
+            count = counts.get(k)
+            if count is not None and (count.dtype is not torch.int32 or count.numel() != 1 or t.dim() != 2):
+                raise AssertionError("Grads: a count is one int32 value, of a matrix")
+            if any(v is not None and v.get_device() != self.gpu for v in (t, o, count)):
+                raise _elsewhere("Grads")
+            rows, cols, ld = _grad_rows(t)
+            ld_out = 0
+            if o is not None:
+                same = _grad_rows(o)
+                if same[:2] != (rows, cols):
+                    raise AssertionError("Grads: an output laid out like its tensor")
+                ld_out = same[2]
+            self.c[k] = dqrm_grad_t(t.data_ptr(), rows, cols, ld, None if o is None else o.data_ptr(), ld_out, None if count is None else count.data_ptr(), dtype)
+
+
+def dqrm_grad_workspace_bytes(grads: Grads) -> int:
+    return int(lib().dqrm_grad_workspace_bytes(grads.c, grads.n))
+
+
+def _scalar(t: torch.Tensor, what: str, gpu: Optional[int]) -> Tuple[int, int]:
+    """(address, GPU) of one float32 value"""
+    if t.dtype is not torch.float32 or t.numel() != 1:
+        raise AssertionError(f"{what}: one float32 value")
+    if gpu is not None and t.get_device() != gpu:
+        raise _elsewhere(what)
+    return t.data_ptr(), t.get_device()
+
+
+def dqrm_grad_norm(grads: Grads, norm: torch.Tensor, kind: int = GRAD_NORM_2, norms: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    p, gpu = _scalar(norm, "norm", grads.gpu)
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_grad_norm, grads, norm, kind, norms, workspace, stream)
+    rc = lib().dqrm_grad_norm(grads.c, grads.n, kind, p, _vector(norms, grads.n, "norms", gpu), *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_grad_norm")
+
+
+def dqrm_grad_scale(grads: Grads, norm: torch.Tensor, max_norm: float, stream=None) -> None:
+    p, gpu = _scalar(norm, "norm", grads.gpu)
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_grad_scale, grads, norm, max_norm, stream)
+    rc = lib().dqrm_grad_scale(grads.c, grads.n, p, max_norm, _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_grad_scale")
+
+
+def dqrm_grad_clip(grads: Grads, max_norm: float, norm: torch.Tensor, kind: int = GRAD_NORM_2, norms: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    p, gpu = _scalar(norm, "norm", grads.gpu)
+    if gpu >= 0 and gpu != _current_device():
+        return _there(gpu, dqrm_grad_clip, grads, max_norm, norm, kind, norms, workspace, stream)
+    rc = lib().dqrm_grad_clip(grads.c, grads.n, kind, max_norm, p, _vector(norms, grads.n, "norms", gpu), *_space(workspace, gpu), _stream_of(gpu, stream))
+    if rc != OK:
+        _check(rc, "dqrm_grad_clip")

@@ -12,8 +12,10 @@ _SHARED = ["dqrm_host.hpp", "dqrm_fastdiv.hpp", os.path.join(ROOT, "include", "d
 # each translation unit and the headers it includes
 UNITS = {
     "dqrm_api.hip": ["dqrm_device.hpp", "dqrm_fwd.hpp", "dqrm_dedupe.hpp", "dqrm_bwd.hpp", "dqrm_update.hpp", "dqrm_merge.hpp",
-                     "dqrm_dense.hpp", "dqrm_step.hpp"] + _SHARED,
-    "dqrm_mx_api.hip": ["dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_mx_few.hpp", "dqrm_norm.hpp"] + _SHARED,
+                     "dqrm_dense.hpp", "dqrm_step.hpp", "dqrm_xent_join.hpp"] + _SHARED,
+    "dqrm_mx_api.hip": ["dqrm_checks.hpp", "dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_mx_few.hpp", "dqrm_norm.hpp"] + _SHARED,
+    "dqrm_train_api.hip": ["dqrm_checks.hpp", "dqrm_mx.hpp", "dqrm_norm.hpp", "dqrm_grad.hpp", "dqrm_resnorm.hpp"] + _SHARED,
+    "dqrm_xent_api.hip": ["dqrm_checks.hpp", "dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_xent_gemm.hpp", "dqrm_xent.hpp"] + _SHARED,
 }
 SOURCES = [os.path.join(CSRC, f) for f in UNITS]
 HEADERS = sorted({os.path.join(CSRC, f) for headers in UNITS.values() for f in headers})

@@ -19,6 +19,7 @@
 #include "dqrm_merge.hpp"
 #include "dqrm_dense.hpp"
 #include "dqrm_step.hpp"
+#include "dqrm_xent_join.hpp"
 
 // Scratch of dqrm_embbag_bwd_noalloc: one copy per GPU, held until the process ends.  In host code
 // this name is only a handle for hipGetSymbolAddress; kernels receive the address that call returns.
@@ -30,6 +31,13 @@ int32_t dqrm_host::hip_fail(hipError_t e, const char *what)
 {
     std::snprintf(t_hip_error, sizeof(t_hip_error), "%s: %s", what, hipGetErrorString(e));
     return DQRM_ERR_HIP;
+}
+
+void dqrm_host::launch_xent_join(const void *parts, int64_t tiles, int64_t rows, const float *at, const int64_t *targets, int64_t classes, float *loss,
+                                 float *lse, hipStream_t st)
+{
+    hipLaunchKernelGGL(dqrm::xent_join_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, static_cast<const float2 *>(parts), tiles, rows, at,
+                       targets, classes, loss, lse);
 }
 
 namespace {

@@ -419,7 +419,7 @@ __device__ __forceinline__ float add_strided(float v, const float *p, int64_t st
 
 // out[c] = sum over p of partial[p][c], and another such sum from `second` values on, in a fixed order: 16 lanes take every 16th each,
 // then their sums are added in turn.  The launch and two reads' latencies: 256 parts of 512 columns twice 2.8 us, of 8190 columns 8.
-__global__ __launch_bounds__(256) void join_columns_kernel(const float *partial, int64_t stride, int n, int64_t cols, int64_t second, float *out0,
+static __global__ __launch_bounds__(256) void join_columns_kernel(const float *partial, int64_t stride, int n, int64_t cols, int64_t second, float *out0,
                                                            float *out1)
 {
     __shared__ float s[16][17];

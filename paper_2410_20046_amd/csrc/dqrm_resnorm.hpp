@@ -1,0 +1,375 @@
+// The join of a block with its residual stream, and the norms around it, forward and backward (gfx950, wave64).
+//
+//   out = res_scale r + gate N1(u), y = N2(out);  N(v) = (v - mean) rstd gamma + beta, rstd = 1 / sqrt(sum (v - mean)^2 / n + eps), a layer
+//   norm's mean = sum v / n, an RMS norm's mean = 0
+//   With z the normalised values: of y's gradient dy, e = dy gamma2, g = dout + rstd2 (e - mean(e) - z2 mean(e z2)) (RMS: without mean(e)),
+//   dr = res_scale g, and the same with e = g gate gamma1 gives du.  The vectors' gradients follow from four sums over rows:
+//   S0 = sum g, S1 = sum g z1, S2 = sum dy z2, S3 = sum dy; dgamma1 = gate S1, dbeta1 = gate S0, dgate = gamma1 S1 + beta1 S0, dgamma2 = S2,
+//   dbeta2 = S3 (no N1: z1 = u, dgate = S1).
+//
+// All in 32 bits; a variance is taken about the mean, from values in registers.  N2 sees out before its rounding.
+#pragma once
+
+#include "dqrm_norm.hpp"
+
+namespace dqrm_resnorm {
+
+using namespace dqrm_mx;
+
+struct Params {
+    int post, pre; // DQRM_NORM_*
+    const float *post_gamma, *post_beta, *gate, *pre_gamma, *pre_beta; // or null: 1 and 0
+    float res_scale, post_eps, pre_eps;
+};
+
+struct FwdArgs {
+    Params p;
+    const void *u, *r;
+    int64_t ldu, ldr, rows, cols;
+    void *out, *y; // y or null
+    int64_t ldo, ldy;
+    float *stats;            // [4][all_rows], from this launch's first row on; or null
+    int64_t all_rows;
+    uint8_t *codes, *scales; // MXFP4 of y, or null
+};
+
+// A chunk on its way.  Rows of fewer than 8 values (SHORT) are loaded value by value.
+template <bool SHORT, typename T>
+__device__ __forceinline__ Raw<T> request(const T *row, int c, int cols)
+{
+    if constexpr (SHORT) {
+        const Vec8<T> v = load_vec(row, c, cols, false);
+        Raw<T> raw;
+        __builtin_memcpy(&raw, &v, sizeof(v));
+        return raw;
+    } else {
+        return load_raw(row, c, cols);
+    }
+}
+template <bool SHORT, typename T>
+__device__ __forceinline__ void arrived(const Raw<T> &raw, int c, int cols, float (&v)[kChunk])
+{
+    if constexpr (SHORT) {
+        Vec8<T> t;
+        __builtin_memcpy(&t, &raw, sizeof(t));
+        to_float(t, v);
+    } else {
+        values_of(raw, c, cols, v);
+    }
+}
+
+__device__ __forceinline__ float sum8(const float (&v)[kChunk]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+__device__ __forceinline__ float squares8(const float (&v)[kChunk])
+{
+    return ((v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3])) + ((v[4] * v[4] + v[5] * v[5]) + (v[6] * v[6] + v[7] * v[7]));
+}
+
+// v to (v - mean) rstd in place, over the TPR threads of a row
+template <int TPR, int CH, int WAVES, typename F>
+__device__ __forceinline__ void normalise(int kind, float eps, int cols, float (&v)[CH][kChunk], float (*s_part)[WAVES][1], float &mean, float &rstd, F column)
+{
+    mean = 0.0f;
+    if (kind == DQRM_NORM_LAYER) {
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < CH; ++j) sum[0] += sum8(v[j]);
+        row_sums<TPR>(sum, s_part[0]);
+        mean = sum[0] / (float)cols;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) v[j][i] -= mean;
+            if (column(j) + kChunk > cols) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) v[j][i] = column(j) + i < cols ? v[j][i] : 0.0f;
+            }
+        }
+    }
+    float sq[1] = {0.0f};
+#pragma unroll
+    for (int j = 0; j < CH; ++j) sq[0] += squares8(v[j]);
+    row_sums<TPR>(sq, s_part[1]);
+    rstd = 1.0f / sqrtf(sq[0] / (float)cols + eps);
+#pragma unroll
+    for (int j = 0; j < CH; ++j)
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) v[j][i] *= rstd;
+}
+
+// TPR threads to a row, CH chunks of 8 values to a thread, the next row of u and r requested before this one's sums; the columns' vectors
+// stay in registers for all rows of a workgroup.  Bound by its bytes: two reads and two writes.
+template <int DT, int TPR, int CH, int BLOCK, bool SHORT>
+__global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
+{
+    using T = elem_t<DT>;
+    constexpr int rows_per_block = BLOCK / TPR;
+    __shared__ float s_part[2][4][BLOCK / kWaveSize][1]; // (two rows in turn: no wave overwrites what another still reads)
+    const int t = threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * rows_per_block;
+    const int cols = (int)a.cols;
+    const int64_t cp = codes_pitch(cols), sp = scales_pitch(cols);
+    auto column = [&](int j) { return (j * TPR + t) * kChunk; };
+    int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
+    Raw<T> next_u[CH], next_r[CH];
+    // (a group past the last row works on that row and writes nothing)
+    auto ask = [&](int64_t at) {
+        const int64_t q = min(at, a.rows - 1);
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            next_u[j] = request<SHORT>(static_cast<const T *>(a.u) + q * a.ldu, column(j), cols);
+            next_r[j] = request<SHORT>(static_cast<const T *>(a.r) + q * a.ldr, column(j), cols);
+        }
+    };
+    ask(r);
+    // gate N1(u) = z (gate gamma1) + gate beta1
+    float gain[CH][kChunk], offset[CH][kChunk], gamma[CH][kChunk], beta[CH][kChunk];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        float gate[kChunk];
+        load_gain(a.p.gate, column(j), cols, 1.0f, gate);
+        load_gain(a.p.post_gamma, column(j), cols, 1.0f, gain[j]);
+        load_gain(a.p.post_beta, column(j), cols, 0.0f, offset[j]);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) gain[j][i] *= gate[i], offset[j][i] *= gate[i];
+        load_gain(a.p.pre_gamma, column(j), cols, 1.0f, gamma[j]);
+        load_gain(a.p.pre_beta, column(j), cols, 0.0f, beta[j]);
+    }
+    int turn = 0;
+    for (; r - threadIdx.x / TPR < a.rows; r += step, turn ^= 1) {
+        const bool own = r < a.rows;
+        float v[CH][kChunk], res[CH][kChunk];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            arrived<SHORT>(next_u[j], column(j), cols, v[j]);
+            arrived<SHORT>(next_r[j], column(j), cols, res[j]);
+        }
+        ask(r + step);
+        float mean1 = 0.0f, rstd1 = 0.0f, mean2 = 0.0f, rstd2 = 0.0f;
+        if (a.p.post != DQRM_NORM_NONE) normalise<TPR>(a.p.post, a.p.post_eps, cols, v, s_part[turn], mean1, rstd1, column);
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) {
+                v[j][i] = a.p.res_scale * res[j][i] + (v[j][i] * gain[j][i] + offset[j][i]);
+                if (column(j) + kChunk > cols) v[j][i] = column(j) + i < cols ? v[j][i] : 0.0f;
+            }
+        // (out may be r's or u's memory: a thread stores the values that it alone has taken from there; what else its last vector held it
+        // has dropped)
+        auto store_out = [&] {
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+                if (own && column(j) < cols) store_chunk<true>(static_cast<T *>(a.out) + r * a.ldo, column(j), cols, v[j]);
+        };
+        if (a.p.pre == DQRM_NORM_NONE) {
+            store_out();
+        } else {
+            float out[CH][kChunk];
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) out[j][i] = v[j][i];
+            normalise<TPR>(a.p.pre, a.p.pre_eps, cols, out, s_part[turn] + 2, mean2, rstd2, column);
+            store_out();
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int c = column(j);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) out[j][i] = out[j][i] * gamma[j][i] + beta[j][i];
+                // (past the row's end 0, also where rstd is infinite or a NaN: the padding of the codes)
+                if (c + kChunk > cols) {
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i) out[j][i] = c + i < cols ? out[j][i] : 0.0f;
+                }
+                if (own && a.y && c < cols) store_chunk<true>(static_cast<T *>(a.y) + r * a.ldy, c, cols, out[j]);
+                if (own && a.codes && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), out[j]);
+            }
+        }
+        if (own && t == 0 && a.stats) {
+            if (a.p.post != DQRM_NORM_NONE) a.stats[r] = mean1, a.stats[a.all_rows + r] = rstd1;
+            if (a.p.pre != DQRM_NORM_NONE) a.stats[2 * a.all_rows + r] = mean2, a.stats[3 * a.all_rows + r] = rstd2;
+        }
+    }
+}
+
+struct BwdArgs {
+    Params p;
+    const void *dout, *dy, *u, *out; // dout or null: 0; dy, out where there is N2; u where there is N1 or the vectors' gradients are wanted
+    int64_t lddout, lddy, ldu, ldo, rows, cols;
+    const float *stats;
+    void *du, *dr; // or null
+    int64_t lddu, lddr;
+    float *partial; // [workgroups][4][cols] of S0 .. S3, or null
+};
+
+// The rows of dout, dy, u and out in registers, the next ones on their way; a thread has the same columns in every row of its workgroup's
+// slice and keeps their sums, so that all is read once.  Bound by its bytes: four reads and two writes.
+template <int DT, int TPR, int CH, int BLOCK, bool SHORT>
+__global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
+{
+    using T = elem_t<DT>;
+    constexpr int rows_per_block = BLOCK / TPR;
+    __shared__ float s_part[2][2][BLOCK / kWaveSize][2]; // (two rows in turn)
+    const int t = threadIdx.x % TPR;
+    const int cols = (int)a.cols;
+    const float inv_n = 1.0f / (float)cols;
+    const int64_t step = (int64_t)gridDim.x * rows_per_block;
+    const bool pre = a.p.pre != DQRM_NORM_NONE, post = a.p.post != DQRM_NORM_NONE;
+    auto column = [&](int j) { return (j * TPR + t) * kChunk; };
+    int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
+    Raw<T> next_dout[CH], next_dy[CH], next_u[CH], next_out[CH];
+    float next_mean1 = 0.0f, next_rstd1 = 1.0f, next_mean2 = 0.0f, next_rstd2 = 1.0f;
+    auto ask = [&](int64_t at) {
+        const int64_t q = min(at, a.rows - 1);
+        if (post) next_mean1 = a.stats[q], next_rstd1 = a.stats[a.rows + q];
+        if (pre) next_mean2 = a.stats[2 * a.rows + q], next_rstd2 = a.stats[3 * a.rows + q];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            if (a.dout) next_dout[j] = request<SHORT>(static_cast<const T *>(a.dout) + q * a.lddout, column(j), cols);
+            if (a.u) next_u[j] = request<SHORT>(static_cast<const T *>(a.u) + q * a.ldu, column(j), cols);
+            if (pre) {
+                next_dy[j] = request<SHORT>(static_cast<const T *>(a.dy) + q * a.lddy, column(j), cols);
+                next_out[j] = request<SHORT>(static_cast<const T *>(a.out) + q * a.ldo, column(j), cols);
+            }
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < CH; ++j) next_dout[j] = next_dy[j] = next_u[j] = next_out[j] = Raw<T>{};
+    ask(r);
+    float s0[CH][kChunk] = {}, s1[CH][kChunk] = {}, s2[CH][kChunk] = {}, s3[CH][kChunk] = {};
+    float gate[CH][kChunk], post_gamma[CH][kChunk], pre_gamma[CH][kChunk];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        load_gain(a.p.gate, column(j), cols, 1.0f, gate[j]);
+        load_gain(a.p.post_gamma, column(j), cols, 1.0f, post_gamma[j]);
+        load_gain(a.p.pre_gamma, column(j), cols, 1.0f, pre_gamma[j]);
+    }
+    int turn = 0;
+    for (; r - threadIdx.x / TPR < a.rows; r += step, turn ^= 1) {
+        const bool own = r < a.rows;
+        const float mean1 = next_mean1, rstd1 = next_rstd1, mean2 = next_mean2, rstd2 = next_rstd2;
+        float g[CH][kChunk], dy[CH][kChunk], z1[CH][kChunk], z2[CH][kChunk];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            arrived<SHORT>(next_dout[j], column(j), cols, g[j]);
+            arrived<SHORT>(next_dy[j], column(j), cols, dy[j]);
+            arrived<SHORT>(next_u[j], column(j), cols, z1[j]);
+            arrived<SHORT>(next_out[j], column(j), cols, z2[j]);
+        }
+        ask(r + step);
+        if (pre) {
+            float s[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) {
+                    z2[j][i] = (z2[j][i] - mean2) * rstd2;
+                    if (column(j) + kChunk > cols) z2[j][i] = column(j) + i < cols ? z2[j][i] : 0.0f;
+                    if (own) s2[j][i] += dy[j][i] * z2[j][i], s3[j][i] += dy[j][i];
+                    dy[j][i] *= pre_gamma[j][i];
+                    s[0] += dy[j][i];
+                    s[1] += dy[j][i] * z2[j][i];
+                }
+            }
+            row_sums<TPR>(s, s_part[turn][0]);
+            const float c0 = a.p.pre == DQRM_NORM_LAYER ? s[0] * inv_n : 0.0f, c1 = s[1] * inv_n;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) g[j][i] += rstd2 * (dy[j][i] - c0 - z2[j][i] * c1);
+        }
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) {
+                z1[j][i] = (z1[j][i] - mean1) * rstd1;
+                if (column(j) + kChunk > cols) {
+                    z1[j][i] = column(j) + i < cols ? z1[j][i] : 0.0f;
+                    g[j][i] = column(j) + i < cols ? g[j][i] : 0.0f;
+                }
+                if (own) s0[j][i] += g[j][i], s1[j][i] += g[j][i] * z1[j][i];
+                dy[j][i] = g[j][i] * gate[j][i];
+                if (post) dy[j][i] *= post_gamma[j][i];
+                s[0] += dy[j][i];
+                s[1] += dy[j][i] * z1[j][i];
+            }
+        float c0 = 0.0f, c1 = 0.0f, by = 1.0f;
+        if (post) {
+            row_sums<TPR>(s, s_part[turn][1]);
+            c0 = a.p.post == DQRM_NORM_LAYER ? s[0] * inv_n : 0.0f, c1 = s[1] * inv_n, by = rstd1;
+        }
+        // (du and dr may be the memory of a matrix that is read: a thread stores the values that it alone has taken from there)
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            if (!own || column(j) >= cols) continue;
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) {
+                dy[j][i] = by * (dy[j][i] - c0 - z1[j][i] * c1);
+                g[j][i] *= a.p.res_scale;
+            }
+            if (a.du) store_chunk<true>(static_cast<T *>(a.du) + r * a.lddu, column(j), cols, dy[j]);
+            if (a.dr) store_chunk<true>(static_cast<T *>(a.dr) + r * a.lddr, column(j), cols, g[j]);
+        }
+    }
+    if (!a.partial) return;
+    float *out = a.partial + (int64_t)blockIdx.x * 4 * cols;
+    auto store_sums = [&](int k, const float(&v)[CH][kChunk]) {
+        if constexpr (rows_per_block == 1) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+                if (column(j) < cols) store_chunk(out + (int64_t)k * cols, column(j), cols, v[j]);
+        } else {
+            // the rows' groups of the workgroup are added in turn
+            __shared__ float s_acc[rows_per_block][TPR * kChunk];
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) s_acc[threadIdx.x / TPR][t * kChunk + i] = v[j][i];
+                __syncthreads();
+                for (int c = threadIdx.x; c < TPR * kChunk; c += BLOCK) {
+                    float sum = s_acc[0][c];
+                    for (int w = 1; w < rows_per_block; ++w) sum += s_acc[w][c];
+                    const int col = j * TPR * kChunk + c;
+                    if (col < cols) out[(int64_t)k * cols + col] = sum;
+                }
+            }
+        }
+    };
+    store_sums(0, s0);
+    store_sums(1, s1);
+    store_sums(2, s2);
+    store_sums(3, s3);
+}
+
+// The workgroups' sums in turn, 16 lanes with every 16th each, and the five vectors' gradients [5][cols] from them: post gamma and beta,
+// gate, pre gamma and beta; those of a norm that is not there are 0.
+static __global__ __launch_bounds__(256) void resnorm_join_kernel(const float *partial, int n, int cols, Params p, float *dparams)
+{
+    __shared__ float s[4][16][17];
+    const int c = (int)blockIdx.x * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float sum = 0.0f;
+        if (c < cols) sum = add_strided(sum, partial + ((int64_t)slice * 4 + k) * cols + c, (int64_t)16 * 4 * cols, (n - slice + 15) / 16);
+        s[k][slice][threadIdx.x & 15] = sum;
+    }
+    __syncthreads();
+    if (slice != 0 || c >= cols) return;
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[k] = s[k][0][threadIdx.x];
+        for (int i = 1; i < 16; ++i) v[k] += s[k][i][threadIdx.x];
+    }
+    const bool pre = p.pre != DQRM_NORM_NONE, post = p.post != DQRM_NORM_NONE;
+    const float gate = p.gate ? p.gate[c] : 1.0f, gamma = p.post_gamma ? p.post_gamma[c] : 1.0f, beta = p.post_beta ? p.post_beta[c] : 0.0f;
+    const int64_t C = cols;
+    dparams[c] = post ? gate * v[1] : 0.0f;
+    dparams[C + c] = post ? gate * v[0] : 0.0f;
+    dparams[2 * C + c] = post ? gamma * v[1] + beta * v[0] : v[1];
+    dparams[3 * C + c] = pre ? v[2] : 0.0f;
+    dparams[4 * C + c] = pre ? v[3] : 0.0f;
+}
+
+} // namespace dqrm_resnorm

@@ -1,0 +1,416 @@
+// Softmax cross entropy of a linear classifier, without its logits in memory (gfx950, wave64).
+//
+//   l[i][j] = scale x_i . w_j + bias_j, lse_i = log sum_j exp l[i][j], loss_i = lse_i - l[i][target_i]
+//   d[i][j] = grad_i (exp(l[i][j] - lse_i) - (1 if j = target_i)), dx = scale d w, dw = scale d^T x, dbias_j = sum_i d[i][j]
+//
+// Forward, a tile of logits stays in registers and leaves as each row's maximum and sum of exponentials over the tile's classes, which
+// xent_join_kernel joins.  Backward, the tile is computed again and leaves as d for some classes at a time, which two more products read.
+// Exponentials are powers of two (logits times log2 e).  A lane has one row of a block of 32 and 16 classes of each.
+#pragma once
+
+#include "dqrm_xent_gemm.hpp"
+
+namespace dqrm_xent {
+
+constexpr float kLog2e = 1.44269504088896341f;
+
+struct Classifier {
+    Products g;
+    const float *bias; // [n] or null
+    float scale2;      // scale times log2 e
+    const int64_t *targets;
+    int64_t first; // the products' first class
+    int64_t classes;
+};
+
+// The tile's logits, in powers of two, in place of its sums; classes past the last one -infinity, and those that are taken out whatever their sums are.
+template <typename S>
+__device__ __forceinline__ void logits(const Classifier &c, v16f (&acc)[S::TM][S::TN], int64_t n0)
+{
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+        float b[16];
+        bool out = false;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t n = n0 + j * 32 + q * 8 + half * 4;
+            struct Four { float v[4]; } f{};
+            if (c.bias) {
+                if (n + 4 <= c.g.n) {
+                    __builtin_memcpy(&f, c.bias + n, sizeof(f));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f.v[i] = n + i < c.g.n ? c.bias[n + i] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = n + i < c.g.n ? f.v[i] * kLog2e : -__builtin_inff();
+                b[q * 4 + i] = v;
+                out |= v == -__builtin_inff();
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < S::TM; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][j][i] = __builtin_fmaf(acc[t][j][i], c.scale2, b[i]);
+        if (__any(out)) {
+#pragma unroll
+            for (int t = 0; t < S::TM; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[t][j][i] = b[i] == -__builtin_inff() ? b[i] : acc[t][j][i];
+        }
+    }
+}
+
+// f(t, j, i) for the place of the target's class of the lane's row, where the wave's tile has it; target: [TM], relative to the wave's first class
+template <typename S, typename F>
+__device__ __forceinline__ void at_target(const int (&target)[S::TM], F f)
+{
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int t = 0; t < S::TM; ++t) {
+        if (!__any(target[t] >= 0)) continue;
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (target[t] == j * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) f(t, j, i);
+    }
+}
+
+// the row's target as a place among the wave's classes from n0 on, -1: not there
+template <typename S>
+__device__ __forceinline__ int place_of_target(int64_t target, int64_t n0)
+{
+    const int64_t at = target - n0;
+    return at >= 0 && at < S::TN * 32 ? (int)at : -1;
+}
+
+__device__ __forceinline__ float power2(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// maximum and sum of two parts of a row; a part without classes is (-infinity, 0)
+__device__ __forceinline__ float2 join_parts(float2 a, float2 b)
+{
+    const float most = fmaxf(a.x, b.x), base = most == -__builtin_inff() ? 0.0f : most;
+    return make_float2(most, a.y * power2(a.x - base) + b.y * power2(b.x - base));
+}
+
+struct FwdArgs {
+    Classifier c;
+    float2 *parts; // [tiles of classes][rows]: maximum, sum of powers
+    float *at;     // [rows]: the target's logit
+    unsigned first_tile;
+};
+
+template <typename T, typename S>
+__global__ __launch_bounds__(S::threads, S::per_simd) void xent_fwd_kernel(FwdArgs a)
+{
+    static_assert(S::WN * S::BM * sizeof(float2) <= S::lds_bytes);
+    __shared__ __align__(1024) char lds[S::lds_bytes];
+    const Products &g = a.c.g;
+    const Place at = place_of(g);
+    const int64_t m0 = (int64_t)at.tm * S::BM, n0 = (int64_t)at.tn * S::BN;
+    const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+    v16f acc[S::TM][S::TN];
+    multiply_tile<T, S, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), acc);
+    logits<S>(a.c, acc, n0 + wn * S::TN * 32);
+    const int64_t row0 = m0 + wm * S::TM * 32 + (lane & 31);
+    int target[S::TM];
+#pragma unroll
+    for (int t = 0; t < S::TM; ++t)
+        target[t] = place_of_target<S>(row0 + t * 32 < g.m ? a.c.targets[row0 + t * 32] : -1, a.c.first + n0 + wn * S::TN * 32);
+    at_target<S>(target, [&](int t, int j, int i) { a.at[row0 + t * 32] = acc[t][j][i]; });
+    float2 *s_part = reinterpret_cast<float2 *>(lds); // [WN][BM]
+#pragma unroll
+    for (int t = 0; t < S::TM; ++t) {
+        float most = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, acc[t][j][i]);
+        most = fmaxf(most, __shfl_xor(most, 32, kWaveSize));
+        const float base = most == -__builtin_inff() ? 0.0f : most;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            float part = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part += power2(acc[t][j][i] - base);
+            sum += part;
+        }
+        sum += __shfl_xor(sum, 32, kWaveSize);
+        if (lane < 32) s_part[wn * S::BM + (wm * S::TM + t) * 32 + lane] = make_float2(most, sum);
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < S::BM; r += S::threads) {
+        if (m0 + r >= g.m) break;
+        float2 p = s_part[r];
+#pragma unroll
+        for (int w = 1; w < S::WN; ++w) p = join_parts(p, s_part[w * S::BM + r]);
+        a.parts[(int64_t)(a.first_tile + at.tn) * g.m + m0 + r] = p;
+    }
+}
+
+struct GradArgs {
+    Classifier c;
+    const float *lse, *grad;
+    const uint64_t *live;  // rows that have a gradient, a bit each
+    const float *d_scale;  // what d is multiplied by before its rounding, or null: 1
+    char *d;               // [planes][rows][pitch]
+    int64_t plane, pitch;  // bytes
+    int planes;
+    float *sums; // [tiles of rows][classes of the piece]: d's column sums, or null
+};
+
+// v summed over the 32 lanes of a half wave, for 16 values of a lane: lane l ends with the sum of value l / 2 % 16 (in pairs of lanes)
+__device__ __forceinline__ float sum_over_rows(const float (&v)[16])
+{
+    const int lane = threadIdx.x & 63;
+    float a[8], b[4], c[2], d;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool up = lane & 16;
+        a[i] = (up ? v[i + 8] : v[i]) + __shfl_xor(up ? v[i] : v[i + 8], 16, kWaveSize);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool up = lane & 8;
+        b[i] = (up ? a[i + 4] : a[i]) + __shfl_xor(up ? a[i] : a[i + 4], 8, kWaveSize);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool up = lane & 4;
+        c[i] = (up ? b[i + 2] : b[i]) + __shfl_xor(up ? b[i] : b[i + 2], 4, kWaveSize);
+    }
+    d = (lane & 2 ? c[1] : c[0]) + __shfl_xor(lane & 2 ? c[0] : c[1], 2, kWaveSize);
+    return d + __shfl_xor(d, 1, kWaveSize);
+}
+
+template <typename T, typename S>
+__global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(GradArgs a)
+{
+    constexpr int out_bytes = S::waves * TileOut<T, S, false>::wave_bytes, sum_bytes = S::WM * S::BN * (int)sizeof(float);
+    static_assert(out_bytes <= S::lds_bytes && sum_bytes <= S::lds_bytes);
+    __shared__ __align__(1024) char lds[S::lds_bytes];
+    const Products &g = a.c.g;
+    const Place at = place_of(g);
+    const int64_t m0 = (int64_t)at.tm * S::BM, n0 = (int64_t)at.tn * S::BN;
+    const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN, half = lane >> 5;
+    v16f acc[S::TM][S::TN];
+    multiply_tile<T, S, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), acc);
+    logits<S>(a.c, acc, n0 + wn * S::TN * 32);
+    const int64_t row0 = m0 + wm * S::TM * 32 + (lane & 31);
+    int target[S::TM];
+#pragma unroll
+    for (int t = 0; t < S::TM; ++t) {
+        const int64_t row = row0 + t * 32;
+        const bool live = row < g.m && (a.live[row >> 6] >> (row & 63)) & 1;
+        const float lse2 = live ? a.lse[row] * kLog2e : 0.0f, grad = live ? a.grad[row] : 0.0f;
+        target[t] = place_of_target<S>(live ? a.c.targets[row] : -1, a.c.first + n0 + wn * S::TN * 32);
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][j][i] = power2(acc[t][j][i] - lse2);
+        // (the target's place before the gradient's factor)
+        if (__any(target[t] >= 0)) {
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (target[t] == j * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) acc[t][j][i] -= 1.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][j][i] *= grad;
+        // (a row without a gradient is zeros, whatever its logits are)
+        if (__any(!live)) {
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[t][j][i] = live ? acc[t][j][i] : 0.0f;
+        }
+    }
+    if (a.sums) {
+        float *s_sum = reinterpret_cast<float *>(lds); // [WM][BN]
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                v[i] = acc[0][j][i];
+#pragma unroll
+                for (int t = 1; t < S::TM; ++t) v[i] += acc[t][j][i];
+            }
+            const float sum = sum_over_rows(v);
+            const int i = (lane >> 1) & 15; // ... of which value: bits 8, 4, 2, 1 of it came with lane bits 16, 8, 4, 2
+            if (!(lane & 1)) s_sum[wm * S::BN + (wn * S::TN + j) * 32 + (i >> 2) * 8 + half * 4 + (i & 3)] = sum;
+        }
+        __syncthreads();
+        for (int n = threadIdx.x; n < S::BN; n += S::threads) {
+            float sum = s_sum[n];
+#pragma unroll
+            for (int w = 1; w < S::WM; ++w) sum += s_sum[w * S::BN + n];
+            if (n0 + n < g.n) a.sums[(int64_t)at.tm * g.n + n0 + n] = sum;
+        }
+        __syncthreads();
+    }
+    const float by = a.d_scale ? *a.d_scale : 1.0f;
+    const int64_t cols = a.pitch / (int64_t)sizeof(T); // (the padding is zeros)
+    for (int plane = 0; plane < a.planes; ++plane) {
+        TileOut<T, S, false>::run(reinterpret_cast<T *>(a.d + plane * a.plane), cols, acc, lds + wave * TileOut<T, S, false>::wave_bytes, m0 + wm * S::TM * 32,
+                                  n0 + wn * S::TN * 32, g.m, cols, by);
+        if (plane + 1 == a.planes) break;
+#pragma unroll
+        for (int t = 0; t < S::TM; ++t)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[t][j][i] -= (float)(T)acc[t][j][i]; // (exact)
+    }
+}
+
+struct OutArgs {
+    Products g;
+    void *c; // the result, or [slices][m][n] of 32-bit sums
+    int64_t ldc;
+    float scale;
+    const float *by; // and times this, or null
+};
+
+// A gradient's product, B with k as the rows.  ADD: to the sums of the pieces before.
+template <typename T, typename TO, typename S, bool A_BY_K, bool ADD>
+__global__ __launch_bounds__(S::threads, S::per_simd) void xent_out_kernel(OutArgs a)
+{
+    using Out = TileOut<TO, S, ADD>;
+    static_assert(S::waves * Out::wave_bytes <= S::lds_bytes);
+    __shared__ __align__(1024) char lds[S::lds_bytes];
+    const Products &g = a.g;
+    const Place at = place_of(g);
+    const int64_t m0 = (int64_t)at.tm * S::BM, n0 = (int64_t)at.tn * S::BN;
+    const int wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+    const int all = (int)(g.stages * g.pairs), first = (int)(at.slice * g.stages_per_slice), last = min(all, first + (int)g.stages_per_slice);
+    v16f acc[S::TM][S::TN];
+    multiply_tile<T, S, A_BY_K, true>(g, lds, m0, n0, first, last, acc);
+    const float by = a.by ? a.scale * *a.by : a.scale;
+    Out::run(static_cast<TO *>(a.c) + (int64_t)at.slice * g.m * g.n, a.ldc, acc, lds + wave * Out::wave_bytes, m0 + wm * S::TM * 32, n0 + wn * S::TN * 32, g.m, g.n,
+             by);
+}
+
+// The slices' sums (`all` values apart) in turn, times the factors, rounded: bound by their bytes.  One value to a thread, less than 2^31 in all.
+template <typename TO>
+__global__ __launch_bounds__(256) void xent_out_join_kernel(const float *sums, unsigned slices, int64_t all, unsigned m, dqrm::FastDiv n, TO *c, int64_t ldc,
+                                                            float scale, const float *by)
+{
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, r = n.div(at);
+    if (r >= m) return;
+    float v = 0.0f;
+    constexpr unsigned ahead = 8; // loads in flight
+    unsigned s = 0;
+    for (; s + ahead <= slices; s += ahead) {
+        float x[ahead];
+#pragma unroll
+        for (unsigned i = 0; i < ahead; ++i) x[i] = sums[(int64_t)(s + i) * all + at];
+#pragma unroll
+        for (unsigned i = 0; i < ahead; ++i) v += x[i];
+    }
+    for (; s < slices; ++s) v += sums[(int64_t)s * all + at];
+    c[r * ldc + (at - r * n.d)] = (TO)(v * (by ? scale * *by : scale));
+}
+
+// A matrix as the products take it: 16-bit values, rows padded with zeros to a multiple of 64; fp32 as three bfloat16 planes.
+struct PackArgs {
+    const void *x;
+    int64_t ldx, rows, cols;
+    char *out;
+    int64_t plane, pitch; // bytes
+};
+
+// a float as three bfloat16, whose sum it is exactly (of 2^-110 and more); one that would round to infinity is cut instead
+__device__ __forceinline__ void split(float v, __bf16 (&p)[3])
+{
+    p[0] = (__bf16)v;
+    if (__builtin_isinf((float)p[0])) {
+        const unsigned cut = __float_as_uint(v) & 0xFFFF0000u;
+        p[0] = (__bf16)__uint_as_float(cut);
+    }
+    float rest = v - (float)p[0];
+    p[1] = (__bf16)rest;
+    rest -= (float)p[1];
+    p[2] = (__bf16)rest;
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void xent_pack_kernel(PackArgs a, dqrm::FastDiv per_row)
+{
+    using T = elem_t<DT>;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, r = per_row.div(at), chunk = at - r * per_row.d;
+    if (r >= a.rows) return;
+    const Vec8<T> v = load_vec(static_cast<const T *>(a.x) + r * a.ldx, (int64_t)chunk * kChunk, a.cols, false);
+    char *to = a.out + r * a.pitch + (int64_t)chunk * 16;
+    if constexpr (DT == DQRM_F32) {
+        struct alignas(16) Eight { __bf16 v[kChunk]; } p[3];
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            __bf16 s[3];
+            split(v.v[i], s);
+            p[0].v[i] = s[0], p[1].v[i] = s[1], p[2].v[i] = s[2];
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<Eight *>(to + k * a.plane) = p[k];
+    } else {
+        __builtin_memcpy(__builtin_assume_aligned(to, 16), &v, 16);
+    }
+}
+
+// Which rows have a gradient, a bit each, and the largest |grad| of a workgroup's rows as a float's bits (of finite ones).
+static __global__ __launch_bounds__(256) void xent_rows_kernel(const int64_t *targets, int64_t classes, const float *lse, const float *grad, int64_t rows,
+                                                               uint64_t *live, unsigned *most)
+{
+    __shared__ unsigned s_most[4];
+    unsigned top = 0;
+    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r - (threadIdx.x & 63) < rows; r += (int64_t)gridDim.x * 256) {
+        bool has = false;
+        if (r < rows) {
+            const float g = grad[r];
+            has = targets[r] >= 0 && targets[r] < classes && g != 0.0f && lse[r] != -__builtin_inff();
+            if (has && abs_bits(g) < 0x7F800000u) top = max(top, abs_bits(g));
+        }
+        const uint64_t word = __ballot(has);
+        if ((threadIdx.x & 63) == 0) live[r >> 6] = word;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, kWaveSize));
+    if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) most[blockIdx.x] = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+}
+
+// Which classes are not taken out.
+static __global__ __launch_bounds__(256) void xent_classes_kernel(const float *bias, int64_t classes, uint64_t *live)
+{
+    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t word = __ballot(j < classes && bias[min(j, classes - 1)] != -__builtin_inff());
+    if ((threadIdx.x & 63) == 0 && j < classes) live[j >> 6] = word;
+}
+
+// The power of two that brings the largest |grad| to 2^14 .. 2^15, and its reciprocal: d in fp16 then has all its bits down to 2^-29 of that, and is
+// off by 2^-40 of it below.
+static __global__ __launch_bounds__(256) void xent_scale_kernel(const unsigned *most, int n, float *scale)
+{
+    __shared__ unsigned s_most[4];
+    unsigned top = (int)threadIdx.x < n ? most[threadIdx.x] : 0u;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, kWaveSize));
+    if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        top = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+        const int e = min(max(127 + 14 - ((int)(top >> 23) - 127), 1), 253); // (exponents of the power and of its reciprocal)
+        scale[0] = __uint_as_float((unsigned)e << 23), scale[1] = __uint_as_float((unsigned)(254 - e) << 23);
+    }
+}
+
+} // namespace dqrm_xent

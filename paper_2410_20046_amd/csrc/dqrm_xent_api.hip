@@ -1,0 +1,401 @@
+// C ABI of the softmax cross entropy over many classes: host-side validation and kernel dispatch.
+// Every entry point validates on the host first and enqueues nothing on error.
+#include "dqrm_checks.hpp"
+#include "dqrm_xent.hpp"
+
+namespace {
+
+using namespace dqrm_host;
+using namespace dqrm_xent;
+
+constexpr int64_t kMostTiles = 1 << 22;  // of 256 by 256, of any of the products
+constexpr int64_t kMostStride = 1 << 22; // values: a tile's offsets stay below 2^32 bytes
+constexpr int64_t kMostClasses = 1 << 22; // of a piece, for the same reason
+// What a piece of the classes may take of the workspace: its gradients d, and its rows of w where they are laid out anew.  As large as the
+// chip's last-level cache, which d is read from twice.
+constexpr int64_t kPieceBytes = 256LL << 20;
+constexpr int kMostSlices = 64;
+constexpr int64_t kSliceTiles = 512; // tiles times slices
+
+using TileBig = Tile<4, 4, 2, 2, 2>; // 256 by 256, one to a CU
+using TileMid = Tile<2, 2, 2, 2, 2>; // 128 by 128, two to a CU
+using TileFew = Tile<2, 2, 1, 4, 2>; // 64 by 256: few rows
+
+enum class Shape { big, mid, few };
+
+int64_t up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
+int planes_of(int32_t dtype) { return dtype == DQRM_F32 ? 3 : 1; }
+int pairs_of(int32_t dtype) { return dtype == DQRM_F32 ? 6 : 1; }
+int rows_of(Shape s) { return s == Shape::big ? 256 : s == Shape::mid ? 128 : 64; }
+int cols_of(Shape s) { return s == Shape::mid ? 128 : 256; }
+
+template <typename F>
+void with_shape(Shape s, F f)
+{
+    if (s == Shape::big)
+        f(TileBig{});
+    else if (s == Shape::mid)
+        f(TileMid{});
+    else
+        f(TileFew{});
+}
+
+// bfloat16 also stands for fp32's planes
+template <typename F>
+void with_operands(int32_t dtype, F f)
+{
+    if (dtype == DQRM_F16)
+        f((_Float16)0.0f);
+    else
+        f((__bf16)0.0f);
+}
+
+Shape logits_shape(int64_t m, int64_t n)
+{
+    if (m <= 64) return Shape::few;
+    return ceil_div(m, 256) * ceil_div(n, 256) >= num_cus() ? Shape::big : Shape::mid;
+}
+
+// a gradient's product [m][n]
+Shape out_shape(int64_t m, int64_t n)
+{
+    if (m <= 64) return Shape::few;
+    return m > 128 && n > 128 ? Shape::big : Shape::mid;
+}
+
+struct Sliced {
+    Shape shape;
+    unsigned slices, stages_per_slice;
+};
+
+// few tiles: the sum in slices, joined afterwards
+Sliced out_plan(int64_t m, int64_t n, int64_t stages)
+{
+    Sliced p{out_shape(m, n), 1, (unsigned)std::max<int64_t>(stages, 1)};
+    const int64_t tiles = ceil_div(m, rows_of(p.shape)) * ceil_div(n, cols_of(p.shape));
+    if (tiles < 1 || tiles * 2 > num_cus()) return p;
+    const int64_t slices = std::min<int64_t>({num_cus() / tiles, ceil_div(stages, 4), kMostSlices, kSliceTiles / tiles});
+    if (slices < 2) return p;
+    p.stages_per_slice = (unsigned)ceil_div(stages, slices);
+    p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
+    return p;
+}
+
+int64_t slices_room(int64_t m, int64_t n, int64_t stages)
+{
+    return std::min(kSliceTiles * 256 * 256, m * n * std::min<int64_t>(kMostSlices, ceil_div(stages, 4))) * (int64_t)sizeof(float);
+}
+
+// classes of a piece, a multiple of 256
+int64_t most_classes(int64_t classes, int64_t width, int planes)
+{
+    const int64_t fit = kPieceBytes / (std::max<int64_t>(up(width, kDepth), kDepth) * 2 * planes);
+    return std::min(up(std::max<int64_t>(classes, 1), 256), std::max<int64_t>(256, std::min(fit, kMostClasses) / 256 * 256));
+}
+
+int64_t piece_classes(int64_t rows, int64_t classes, int64_t width, int planes, bool with_d)
+{
+    int64_t most = most_classes(classes, width, planes);
+    if (with_d) most = std::min(most, std::max<int64_t>(256, kPieceBytes / (std::max<int64_t>(rows, 1) * 2 * planes) / 256 * 256));
+    return up(ceil_div(classes, ceil_div(classes, most)), 256);
+}
+
+size_t bytes(int64_t n) { return align_up((size_t)n, 256); }
+
+// the regions of the workspace
+struct Space {
+    char *at;
+    size_t used = 0;
+    void *take(size_t n)
+    {
+        void *p = at + used;
+        used += n;
+        return p;
+    }
+};
+
+struct FwdSpace {
+    size_t parts, at, x, w;
+    size_t total() const { return parts + at + x + w; }
+};
+
+FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype, bool room)
+{
+    const int pl = planes_of(dtype);
+    const int64_t wide = ceil_div(v, 256) * m;
+    FwdSpace s{};
+    // (tiles of 128 are fewer than 2^17 times rows, by the rule that chooses them)
+    s.parts = bytes((room ? std::max(wide, std::min<int64_t>(ceil_div(v, 128) * m, 1 << 17)) : logits_shape(m, v) == Shape::mid ? ceil_div(v, 128) * m : wide) * 8);
+    s.at = bytes(m * 4);
+    s.x = bytes(m * up(k, kDepth) * 2 * pl);
+    s.w = bytes(most_classes(v, k, pl) * up(k, kDepth) * 2 * pl);
+    return s;
+}
+
+struct BwdSpace {
+    size_t live, classes, most, scale, x, w, d, sums, dx, dw;
+    size_t total() const { return live + classes + most + scale + x + w + d + sums + dx + dw; }
+};
+
+BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
+{
+    const int pl = planes_of(dtype), pairs = pairs_of(dtype);
+    const int64_t most = most_classes(v, k, pl);
+    // (a piece has at most `most` classes, and at most 256 or those whose d fits)
+    const int64_t d = std::max(m * 256, std::min(m * most, kPieceBytes / (2 * pl)));
+    BwdSpace s{};
+    s.live = bytes(ceil_div(m, 64) * 8), s.classes = bytes(ceil_div(v, 64) * 8), s.most = 1024, s.scale = 256;
+    s.x = bytes(m * up(k, kDepth) * 2 * pl), s.w = bytes(most * up(k, kDepth) * 2 * pl);
+    s.d = bytes(d * 2 * pl);
+    s.sums = bytes((d / 64 + most) * 4);
+    s.dx = bytes(std::max(m * k * 4, slices_room(m, k, most / kDepth * pairs)));
+    s.dw = bytes(slices_room(most, k, ceil_div(m, kDepth) * pairs));
+    return s;
+}
+
+struct Call {
+    int32_t dtype;
+    int64_t m, v, k;
+    const void *x, *w;
+    int64_t ldx, ldw;
+    const float *bias;
+    float scale;
+    const int64_t *targets;
+};
+
+int32_t check_call(const Call &c)
+{
+    DQRM_CHECK(check_shape(c.dtype, c.m, c.v));
+    DQRM_CHECK(check_shape(c.dtype, c.m, c.k));
+    if (c.v < 1 && c.m > 0) return DQRM_ERR_INVALID_ARG;
+    DQRM_CHECK(check_matrix(c.x, c.ldx, c.dtype, c.m, c.k));
+    DQRM_CHECK(check_matrix(c.w, c.ldw, c.dtype, c.v, c.k));
+    if (!std::isfinite(c.scale) || (c.bias && !aligned(c.bias, 4))) return DQRM_ERR_INVALID_ARG;
+    if (c.m > 0 && (!c.targets || !aligned(c.targets, 8))) return DQRM_ERR_INVALID_ARG;
+    if ((c.m > 1 && c.ldx > kMostStride) || (c.v > 1 && c.ldw > kMostStride) || c.k > kMostStride) return DQRM_ERR_UNSUPPORTED;
+    const int64_t tm = ceil_div(c.m, 256), tv = ceil_div(c.v, 256), tk = ceil_div(c.k, 256);
+    if (tm * tv > kMostTiles || tm * tk > kMostTiles || tv * tk > kMostTiles) return DQRM_ERR_UNSUPPORTED;
+    return DQRM_OK;
+}
+
+bool sizes_are_known(int64_t m, int64_t v, int64_t k, int32_t dtype)
+{
+    if (check_shape(dtype, m, v) != DQRM_OK || check_shape(dtype, m, k) != DQRM_OK || k > kMostStride) return false;
+    const int64_t tm = ceil_div(m, 256), tv = ceil_div(v, 256), tk = ceil_div(k, 256);
+    return tm * tv <= kMostTiles && tm * tk <= kMostTiles && tv * tk <= kMostTiles;
+}
+
+// can the products read the matrix where it is?
+bool as_it_is(const void *p, int64_t ld, int32_t dtype, int64_t rows, int64_t cols)
+{
+    return dtype != DQRM_F32 && aligned(p, 16) && cols % kChunk == 0 && (rows <= 1 || ld % kChunk == 0);
+}
+
+// The matrix as an operand, laid out in `space` first if it has to be.
+Operand operand(int32_t dtype, const void *p, int64_t ld, int64_t rows, int64_t cols, void *space, hipStream_t st)
+{
+    if (rows == 0 || cols == 0) return Operand{nullptr, 0, 0, rows, cols, nullptr};
+    if (as_it_is(p, ld, dtype, rows, cols)) return Operand{static_cast<const char *>(p), 0, (rows > 1 ? ld : cols) * 2, rows, cols, nullptr};
+    const int64_t padded = up(cols, kDepth), pitch = padded * 2, per_row = padded / kChunk, step = std::max<int64_t>(1, ((int64_t)1 << 30) / per_row);
+    const Operand o{static_cast<const char *>(space), rows * pitch, pitch, rows, padded, nullptr};
+    for (int64_t r0 = 0; r0 < rows; r0 += step) {
+        PackArgs a{static_cast<const char *>(p) + r0 * ld * (int64_t)size_of(dtype), ld, std::min(step, rows - r0), cols, static_cast<char *>(space) + r0 * pitch,
+                   o.plane, pitch};
+        with_type(dtype, [&](auto t) {
+            hipLaunchKernelGGL(xent_pack_kernel<decltype(t)::value>, dim3((unsigned)ceil_div(a.rows * per_row, 256)), dim3(256), 0, st, a,
+                               dqrm::FastDiv::make((unsigned)per_row));
+        });
+    }
+    return o;
+}
+
+Products products(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int pairs, Shape shape)
+{
+    Products g{};
+    g.a = a, g.b = b, g.m = m, g.n = n, g.stages = (unsigned)ceil_div(k, kDepth), g.pairs = (unsigned)pairs;
+    g.by_stages = dqrm::FastDiv::make(std::max(g.stages, 1u));
+    g.tiles_m = (unsigned)ceil_div(m, rows_of(shape)), g.tiles_n = (unsigned)ceil_div(n, cols_of(shape)), g.slices = 1;
+    g.stages_per_slice = g.stages * g.pairs;
+    return g;
+}
+
+// rows of w as an operand
+Operand classes_of(const Call &c, int64_t first, int64_t n, void *space, hipStream_t st)
+{
+    return operand(c.dtype, static_cast<const char *>(c.w) + first * c.ldw * (int64_t)size_of(c.dtype), c.ldw, n, c.k, space, st);
+}
+
+Classifier classifier(const Call &c, const Products &g, int64_t first)
+{
+    return Classifier{g, c.bias ? c.bias + first : nullptr, c.scale * kLog2e, c.targets, first, c.v};
+}
+
+void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStream_t st)
+{
+    const int pairs = pairs_of(c.dtype);
+    const FwdSpace need = fwd_space(c.m, c.v, c.k, c.dtype, false);
+    Space ws{static_cast<char *>(workspace)};
+    FwdArgs a{};
+    a.parts = static_cast<float2 *>(ws.take(need.parts)), a.at = static_cast<float *>(ws.take(need.at));
+    void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
+    const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
+    const Shape shape = logits_shape(c.m, c.v);
+    const int64_t step = as_it_is(c.w, c.ldw, c.dtype, c.v, c.k) ? c.v : piece_classes(c.m, c.v, c.k, planes_of(c.dtype), false);
+    for (int64_t first = 0; first < c.v; first += step) {
+        const int64_t n = std::min(step, c.v - first);
+        const Products g = products(x, classes_of(c, first, n, w_space, st), c.m, n, c.k, pairs, shape);
+        a.c = classifier(c, g, first), a.first_tile = (unsigned)(first / cols_of(shape));
+        with_operands(c.dtype, [&](auto zero) {
+            with_shape(shape, [&](auto tile) {
+                using S = decltype(tile);
+                hipLaunchKernelGGL((xent_fwd_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
+            });
+        });
+    }
+    launch_xent_join(a.parts, ceil_div(c.v, cols_of(shape)), c.m, a.at, c.targets, c.v, loss, lse, st);
+}
+
+// sums [slices][m][n] to the result
+void launch_out_join(int32_t dtype, const float *sums, unsigned slices, int64_t m, int64_t n, void *c, int64_t ldc, float scale, const float *by, hipStream_t st)
+{
+    const int64_t step = std::max<int64_t>(1, ((int64_t)1 << 30) / n);
+    for (int64_t r0 = 0; r0 < m; r0 += step) {
+        const int64_t some = std::min(step, m - r0);
+        with_type(dtype, [&](auto t) {
+            using TO = elem_t<decltype(t)::value>;
+            hipLaunchKernelGGL(xent_out_join_kernel<TO>, dim3((unsigned)ceil_div(some * n, 256)), dim3(256), 0, st, sums + r0 * n, slices, m * n, (unsigned)some,
+                               dqrm::FastDiv::make((unsigned)n), static_cast<TO *>(c) + r0 * ldc, ldc, scale, by);
+        });
+    }
+}
+
+template <bool A_BY_K>
+void launch_out(int32_t dtype, Shape shape, const OutArgs &a, bool sums, bool add, hipStream_t st)
+{
+    const dim3 grid(a.g.tiles_m * a.g.tiles_n * a.g.slices);
+    with_operands(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        with_shape(shape, [&](auto tile) {
+            using S = decltype(tile);
+            if (add) {
+                if constexpr (!A_BY_K) hipLaunchKernelGGL((xent_out_kernel<T, float, S, A_BY_K, true>), grid, dim3(S::threads), 0, st, a);
+            } else if (sums || dtype == DQRM_F32)
+                hipLaunchKernelGGL((xent_out_kernel<T, float, S, A_BY_K, false>), grid, dim3(S::threads), 0, st, a);
+            else
+                hipLaunchKernelGGL((xent_out_kernel<T, T, S, A_BY_K, false>), grid, dim3(S::threads), 0, st, a);
+        });
+    });
+}
+
+void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, int64_t lddx, void *dw, int64_t lddw, float *dbias, void *workspace, hipStream_t st)
+{
+    const int planes = planes_of(c.dtype), pairs = pairs_of(c.dtype);
+    const BwdSpace need = bwd_space(c.m, c.v, c.k, c.dtype);
+    Space ws{static_cast<char *>(workspace)};
+    uint64_t *live = static_cast<uint64_t *>(ws.take(need.live)), *live_classes = static_cast<uint64_t *>(ws.take(need.classes));
+    unsigned *most = static_cast<unsigned *>(ws.take(need.most));
+    float *power = static_cast<float *>(ws.take(need.scale));
+    void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
+    char *d = static_cast<char *>(ws.take(need.d));
+    float *sums = static_cast<float *>(ws.take(need.sums)), *dx_sums = static_cast<float *>(ws.take(need.dx)), *dw_sums = static_cast<float *>(ws.take(need.dw));
+
+    const int row_blocks = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(c.m, 256), 1), 256);
+    hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)row_blocks), dim3(256), 0, st, c.targets, c.v, lse, grad, c.m, live, most);
+    const bool f16 = c.dtype == DQRM_F16;
+    if (f16) hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(256), 0, st, most, row_blocks, power);
+    if (c.bias && dx) hipLaunchKernelGGL(xent_classes_kernel, dim3((unsigned)ceil_div(c.v, 256)), dim3(256), 0, st, c.bias, c.v, live_classes);
+
+    const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
+    const int64_t step = piece_classes(c.m, c.v, c.k, planes, true);
+    const bool one = step >= c.v;
+    const Sliced dx_plan = out_plan(c.m, c.k, ceil_div(std::min(step, c.v), kDepth) * pairs);
+    for (int64_t first = 0; first < c.v; first += step) {
+        const int64_t n = std::min(step, c.v - first);
+        const Operand w = classes_of(c, first, n, w_space, st);
+        const Shape shape = logits_shape(c.m, n);
+        GradArgs a{};
+        const Products g = products(x, w, c.m, n, c.k, pairs, shape);
+        a.c = classifier(c, g, first), a.lse = lse, a.grad = grad, a.live = live, a.d_scale = f16 ? power : nullptr;
+        a.pitch = up(n, kDepth) * 2, a.plane = c.m * a.pitch, a.planes = planes, a.d = d, a.sums = dbias ? sums : nullptr;
+        if (g.tiles_m > 0)
+            with_operands(c.dtype, [&](auto zero) {
+                with_shape(shape, [&](auto tile) {
+                    using S = decltype(tile);
+                    hipLaunchKernelGGL((xent_grad_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
+                });
+            });
+        if (dbias) hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, st, sums, n, (int)g.tiles_m, n, n, dbias + first, nullptr);
+        if (c.k == 0) continue;
+        const Operand dm{d, a.plane, a.pitch, c.m, a.pitch / 2, nullptr};
+        if (dx && c.m > 0) {
+            Operand by = w;
+            by.live = c.bias ? live_classes + first / 64 : nullptr;
+            OutArgs o{products(dm, by, c.m, c.k, n, pairs, dx_plan.shape), dx, lddx, c.scale, f16 ? power + 1 : nullptr};
+            o.g.slices = dx_plan.slices, o.g.stages_per_slice = dx_plan.stages_per_slice;
+            const bool in_sums = !one || dx_plan.slices > 1;
+            if (in_sums) o.c = dx_sums, o.ldc = c.k, o.scale = 1.0f, o.by = nullptr;
+            launch_out<false>(c.dtype, dx_plan.shape, o, in_sums, first > 0, st);
+        }
+        if (dw) {
+            Operand by = x;
+            by.live = live;
+            const Sliced p = out_plan(n, c.k, ceil_div(c.m, kDepth) * pairs);
+            char *to = static_cast<char *>(dw) + first * lddw * (int64_t)size_of(c.dtype);
+            OutArgs o{products(dm, by, n, c.k, c.m, pairs, p.shape), to, lddw, c.scale, f16 ? power + 1 : nullptr};
+            o.g.slices = p.slices, o.g.stages_per_slice = p.stages_per_slice;
+            if (p.slices > 1) o.c = dw_sums, o.ldc = c.k, o.scale = 1.0f, o.by = nullptr;
+            launch_out<true>(c.dtype, p.shape, o, p.slices > 1, false, st);
+            if (p.slices > 1) launch_out_join(c.dtype, dw_sums, p.slices, n, c.k, to, lddw, c.scale, f16 ? power + 1 : nullptr, st);
+        }
+    }
+    if (dx && c.m > 0 && c.k > 0 && (!one || dx_plan.slices > 1))
+        launch_out_join(c.dtype, dx_sums, dx_plan.slices, c.m, c.k, dx, lddx, c.scale, f16 ? power + 1 : nullptr, st);
+}
+
+} // namespace
+
+extern "C" {
+
+size_t dqrm_softmax_xent_fwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype)
+{
+    return sizes_are_known(rows, classes, width, dtype) ? fwd_space(rows, classes, width, dtype, true).total() : 0;
+}
+
+int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                              const float *bias, float scale, const int64_t *targets, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                              void *stream)
+{
+    const Call c{dtype, rows, classes, width, x, w, ldx, ldw, bias, scale, targets};
+    DQRM_CHECK(check_call(c));
+    if (rows > 0 && (!loss || !lse || !aligned(loss, 4) || !aligned(lse, 4))) return DQRM_ERR_INVALID_ARG;
+    if (rows == 0) return DQRM_OK;
+    DQRM_CHECK(check_workspace(workspace, workspace_bytes, fwd_space(rows, classes, width, dtype, false).total()));
+    launch_fwd(c, loss, lse, workspace, static_cast<hipStream_t>(stream));
+    DQRM_HIP_CHECK(hipGetLastError());
+    return DQRM_OK;
+}
+
+size_t dqrm_softmax_xent_bwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype)
+{
+    return sizes_are_known(rows, classes, width, dtype) ? bwd_space(rows, classes, width, dtype).total() : 0;
+}
+
+int32_t dqrm_softmax_xent_bwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                              const float *bias, float scale, const int64_t *targets, const float *lse, const float *grad, void *dx, int64_t lddx, void *dw,
+                              int64_t lddw, float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const Call c{dtype, rows, classes, width, x, w, ldx, ldw, bias, scale, targets};
+    DQRM_CHECK(check_call(c));
+    if (!dx && !dw && !dbias && rows > 0 && width > 0) return DQRM_ERR_INVALID_ARG; // (an empty output may be null)
+    if (rows > 0 && (!lse || !grad || !aligned(lse, 4) || !aligned(grad, 4))) return DQRM_ERR_INVALID_ARG;
+    if (dx) DQRM_CHECK(check_matrix(dx, lddx, dtype, rows, width));
+    if (dw) DQRM_CHECK(check_matrix(dw, lddw, dtype, classes, width));
+    if (dbias && !aligned(dbias, 4)) return DQRM_ERR_INVALID_ARG;
+    if (classes == 0) return DQRM_OK;
+    DQRM_CHECK(check_workspace(workspace, workspace_bytes, bwd_space(rows, classes, width, dtype).total()));
+    launch_bwd(c, lse, grad, dx, lddx, dw, lddw, dbias, workspace, static_cast<hipStream_t>(stream));
+    DQRM_HIP_CHECK(hipGetLastError());
+    return DQRM_OK;
+}
+
+} // extern "C"

@@ -1,0 +1,49 @@
+// The last step of the softmax cross entropy's forward: the tiles' parts of each row to its lse and its loss (gfx950, wave64).
+#pragma once
+
+#include "dqrm_device.hpp"
+
+namespace dqrm {
+
+// maximum and sum of powers of two of two parts of a row; one without classes is (-infinity, 0)
+__device__ __forceinline__ float2 xent_join_parts(float2 a, float2 b)
+{
+    const float most = fmaxf(a.x, b.x), base = most == -__builtin_inff() ? 0.0f : most;
+    return make_float2(most, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
+}
+
+// 16 rows to a workgroup, 16 lanes to a row with every 16th tile each, eight loads at a time on their way; then their results in turn.  A
+// sum is at least 1 (its largest power) and at most the classes, so log2 of it is exact to the last bits.
+__global__ __launch_bounds__(256) void xent_join_kernel(const float2 *parts, int64_t tiles, int64_t rows, const float *at, const int64_t *targets,
+                                                        int64_t classes, float *loss, float *lse)
+{
+    __shared__ float2 s[16][17];
+    const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+    const int slice = threadIdx.x >> 4;
+    float2 v = make_float2(-__builtin_inff(), 0.0f);
+    if (r < rows) {
+        constexpr int ahead = 8;
+        for (int64_t k = slice; k < tiles; k += 16 * ahead) {
+            float2 x[ahead];
+#pragma unroll
+            for (int i = 0; i < ahead; ++i) x[i] = parts[min(k + 16 * i, tiles - 1) * rows + r];
+#pragma unroll
+            for (int i = 0; i < ahead; ++i)
+                if (k + 16 * i < tiles) v = xent_join_parts(v, x[i]);
+        }
+    }
+    s[slice][threadIdx.x & 15] = v;
+    __syncthreads();
+    if (slice != 0 || r >= rows) return;
+    for (int i = 1; i < 16; ++i) v = xent_join_parts(v, s[i][threadIdx.x]);
+    constexpr float kLn2 = 0.693147180559945309f;
+    const float lse2 = v.x == -__builtin_inff() && v.y == 0.0f ? v.x : v.x + log2f(v.y); // (no classes left; a NaN stays)
+    lse[r] = lse2 * kLn2;
+    const int64_t t = targets[r];
+    float l = 0.0f;
+    if (t >= classes) report(DQRM_ERR_INDEX_OUT_OF_RANGE, -1, t);
+    if (t >= 0 && t < classes) l = lse2 == -__builtin_inff() ? __builtin_inff() : (lse2 - at[r]) * kLn2;
+    loss[r] = l;
+}
+
+} // namespace dqrm
