@@ -35,7 +35,7 @@ struct Batch {
 constexpr int kThreads = 256;
 constexpr int kAhead = 4; // vectors of a thread that are on their way together
 
-__device__ __forceinline__ const Item &item_of(const Batch &b, unsigned piece)
+__device__ __forceinline__ int item_of(const Batch &b, unsigned piece)
 {
     int lo = 0, hi = b.items - 1;
     while (lo < hi) { // the last item that begins at or before the piece
@@ -45,7 +45,7 @@ __device__ __forceinline__ const Item &item_of(const Batch &b, unsigned piece)
         else
             hi = mid - 1;
     }
-    return b.item[lo];
+    return lo;
 }
 
 __device__ __forceinline__ int64_t rows_of(const Item &t)
@@ -55,14 +55,16 @@ __device__ __forceinline__ int64_t rows_of(const Item &t)
     return n < 0 ? 0 : min(n, t.rows);
 }
 
-// f(row, column) for the thread's vectors of vectors [v0, v1) of a tensor, kAhead of them at a time: f(rows, columns, how many)
+// The thread's vectors of vectors [v0, v1) of a tensor, kAhead of them at a time: f(rows, columns, how many)
 template <typename F>
-__device__ __forceinline__ void for_vectors(int64_t v0, int64_t v1, int64_t per_row, F f)
+__device__ __forceinline__ void for_vectors(int64_t rows_of_tensor, int64_t v0, int64_t v1, int64_t per_row, F f)
 {
-    int64_t v = v0 + threadIdx.x;
+    int64_t v = v0 + threadIdx.x, r = 0, c = v, down = 0, right = kThreads;
     if (v >= v1) return;
-    const int64_t down = kThreads / per_row, right = kThreads - down * per_row;
-    int64_t r = v / per_row, c = v - r * per_row;
+    if (rows_of_tensor > 1) { // (a single row needs no divisions: they are most of a small tensor's time)
+        r = v / per_row, c = v - r * per_row;
+        down = kThreads / per_row, right = kThreads - down * per_row;
+    }
     while (v < v1) {
         int64_t rows[kAhead], cols[kAhead];
         int n = 0;
@@ -109,7 +111,6 @@ template <typename F>
 __device__ __forceinline__ void with_item(const Item &t, F f)
 {
     const auto typed = [&](auto zero) {
-        using T = decltype(zero);
         if (t.cols < kChunk)
             f(zero, std::true_type{});
         else
@@ -151,7 +152,15 @@ template <int KIND>
 __device__ __forceinline__ double join_parts(const double *parts, unsigned first, unsigned n, double *s)
 {
     double v = 0.0;
-    for (unsigned i = threadIdx.x; i < n; i += kThreads) v = join<KIND>(v, parts[first + i]);
+    constexpr unsigned ahead = 8; // loads in flight (a part past the last one is the last one again, and not added)
+    for (unsigned i = threadIdx.x; i < n; i += kThreads * ahead) {
+        double x[ahead];
+#pragma unroll
+        for (unsigned k = 0; k < ahead; ++k) x[k] = parts[first + min(i + k * kThreads, n - 1)];
+#pragma unroll
+        for (unsigned k = 0; k < ahead; ++k)
+            if (i + k * kThreads < n) v = join<KIND>(v, x[k]);
+    }
     return join_all<KIND>(v, s);
 }
 
@@ -167,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void grad_part_kernel(Batch b, double *pa
 {
     __shared__ double s[kThreads / kWaveSize];
     const unsigned piece = b.first + blockIdx.x;
-    const Item &t = item_of(b, piece);
+    const Item &t = b.item[item_of(b, piece)];
     const int64_t per_row = (t.cols + kChunk - 1) / kChunk, v0 = (int64_t)(piece - t.first) * b.per_piece;
     const int64_t v1 = min(v0 + b.per_piece, rows_of(t) * per_row);
     double sum = 0.0;
@@ -176,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void grad_part_kernel(Batch b, double *pa
         using T = decltype(zero);
         constexpr bool SHORT = decltype(is_short)::value;
         const T *data = reinterpret_cast<const T *>(t.data);
-        for_vectors(v0, v1, per_row, [&](const int64_t(&r)[kAhead], const int64_t(&c)[kAhead], int n) {
+        for_vectors(t.rows, v0, v1, per_row, [&](const int64_t(&r)[kAhead], const int64_t(&c)[kAhead], int n) {
             Raw<T> raw[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) load_values<T, SHORT>(data + r[i] * t.ld, c[i], t.cols, raw[i]);
@@ -200,37 +209,47 @@ __global__ __launch_bounds__(kThreads) void grad_part_kernel(Batch b, double *pa
     if (threadIdx.x == 0) parts[piece] = sum;
 }
 
+__device__ __forceinline__ unsigned pieces_of(const Batch &b, int item)
+{
+    return (item + 1 < b.items ? b.item[item + 1].first : b.first + b.pieces) - b.item[item].first;
+}
+
 // A workgroup to each tensor's norm, and one to the norm of all.
 template <int KIND>
 __global__ __launch_bounds__(kThreads) void grad_join_kernel(Batch b, const double *parts, float *norms, int first_norm, float *norm)
 {
     __shared__ double s[kThreads / kWaveSize];
     const int at = (int)blockIdx.x;
-    unsigned from = 0, n = b.all;
-    if (norms && at < b.items) {
-        from = b.item[at].first;
-        n = (at + 1 < b.items ? b.item[at + 1].first : b.first + b.pieces) - from;
-    }
-    const double v = join_parts<KIND>(parts, from, n, s);
-    if (threadIdx.x == 0) (norms && at < b.items ? norms[first_norm + at] : *norm) = norm_of<KIND>(v);
+    const bool one = norms && at < b.items;
+    const double v = join_parts<KIND>(parts, one ? b.item[at].first : 0u, one ? pieces_of(b, at) : b.all, s);
+    if (threadIdx.x == 0) (one ? norms[first_norm + at] : *norm) = norm_of<KIND>(v);
 }
 
-// The values times max_norm / norm.  The norm is the joined parts', or given; a workgroup of a tensor that stays as it is ends here.
+// The values times max_norm / norm.  The norm is the joined parts', or given; a workgroup of a tensor that stays as it is ends there.  With
+// parts, each tensor's norm is written beside (`norms`) by the workgroup of its first piece, an empty one's by the first of all.
 template <int KIND>
-__global__ __launch_bounds__(kThreads) void grad_scale_kernel(Batch b, const double *parts, const float *given, float *norm, float max_norm)
+__global__ __launch_bounds__(kThreads) void grad_scale_kernel(Batch b, const double *parts, const float *given, float *norm, float *norms, float max_norm)
 {
-    __shared__ double s[kThreads / kWaveSize];
+    __shared__ double s[2][kThreads / kWaveSize];
+    const unsigned piece = b.first + blockIdx.x;
+    const int item = item_of(b, piece);
+    const Item &t = b.item[item];
     float total;
     if (parts) {
-        total = norm_of<KIND>(join_parts<KIND>(parts, 0, b.all, s));
+        total = norm_of<KIND>(join_parts<KIND>(parts, 0, b.all, s[0]));
         if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = total;
+        if (norms) {
+            if (blockIdx.x == 0 && (int)threadIdx.x < b.items && pieces_of(b, threadIdx.x) == 0) norms[threadIdx.x] = 0.0f;
+            if (piece == t.first) {
+                const double v = join_parts<KIND>(parts, t.first, pieces_of(b, item), s[1]);
+                if (threadIdx.x == 0) norms[item] = norm_of<KIND>(v);
+            }
+        }
     } else {
         total = *given;
     }
     const bool scaled = total > max_norm && total < __builtin_inff(); // (not with a NaN)
     const float by = scaled ? max_norm / total : 1.0f;
-    const unsigned piece = b.first + blockIdx.x;
-    const Item &t = item_of(b, piece);
     if (!scaled && t.out == t.data) return;
     const int64_t per_row = (t.cols + kChunk - 1) / kChunk, v0 = (int64_t)(piece - t.first) * b.per_piece;
     const int64_t v1 = min(v0 + b.per_piece, rows_of(t) * per_row);
@@ -239,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Batch b, const dou
         constexpr bool SHORT = decltype(is_short)::value;
         const T *data = reinterpret_cast<const T *>(t.data);
         T *out = reinterpret_cast<T *>(t.out);
-        for_vectors(v0, v1, per_row, [&](const int64_t(&r)[kAhead], const int64_t(&c)[kAhead], int n) {
+        for_vectors(t.rows, v0, v1, per_row, [&](const int64_t(&r)[kAhead], const int64_t(&c)[kAhead], int n) {
             Raw<T> raw[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) load_values<T, SHORT>(data + r[i] * t.ld, c[i], t.cols, raw[i]);

@@ -7,7 +7,7 @@
 //   S0 = sum g, S1 = sum g z1, S2 = sum dy z2, S3 = sum dy; dgamma1 = gate S1, dbeta1 = gate S0, dgate = gamma1 S1 + beta1 S0, dgamma2 = S2,
 //   dbeta2 = S3 (no N1: z1 = u, dgate = S1).
 //
-// All in 32 bits; a variance is taken about the mean, from values in registers.  N2 sees out before its rounding.
+// All in 32 bits but for the layer norm's sums, which are in 64.  N2 sees out before its rounding.
 #pragma once
 
 #include "dqrm_norm.hpp"
@@ -58,42 +58,123 @@ __device__ __forceinline__ void arrived(const Raw<T> &raw, int c, int cols, floa
     }
 }
 
-__device__ __forceinline__ float sum8(const float (&v)[kChunk]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 __device__ __forceinline__ float squares8(const float (&v)[kChunk])
 {
     return ((v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3])) + ((v[4] * v[4] + v[5] * v[5]) + (v[6] * v[6] + v[7] * v[7]));
 }
 
-// v to (v - mean) rstd in place, over the TPR threads of a row
-template <int TPR, int CH, int WAVES, typename F>
-__device__ __forceinline__ void normalise(int kind, float eps, int cols, float (&v)[CH][kChunk], float (*s_part)[WAVES][1], float &mean, float &rstd, F column)
+// ---- sums over the threads of a row -------------------------------------------------------------------------------------
+// Lanes add what a lane 8, 4, 2, 1 places on in their 16 has (after each of these steps the values repeat with that period, so all lanes
+// get the same bits), then rows of 16 and halves of the wave are exchanged: no step goes through LDS.
+__device__ __forceinline__ float moved(float v, int how)
 {
-    mean = 0.0f;
-    if (kind == DQRM_NORM_LAYER) {
-        float sum[1] = {0.0f};
+    switch (how) {
+    case 8: return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, true));
+    case 4: return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xF, 0xF, true));
+    case 2: return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xF, 0xF, true));
+    default: return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xF, 0xF, true));
+    }
+}
+__device__ __forceinline__ double moved(double v, int how)
+{
+    return __hiloint2double(__float_as_int(moved(__int_as_float(__double2hiint(v)), how)), __float_as_int(moved(__int_as_float(__double2loint(v)), how)));
+}
+// v of this row of 16 lanes and of its neighbour, of this half and of the other one: in the same order in both
+__device__ __forceinline__ float with_other_row(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap((unsigned)__float_as_int(v), (unsigned)__float_as_int(v), false, false);
+    return __int_as_float((int)r[0]) + __int_as_float((int)r[1]);
+}
+__device__ __forceinline__ float with_other_half(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap((unsigned)__float_as_int(v), (unsigned)__float_as_int(v), false, false);
+    return __int_as_float((int)r[0]) + __int_as_float((int)r[1]);
+}
+__device__ __forceinline__ double with_other_row(double v)
+{
+    const auto h = __builtin_amdgcn_permlane16_swap((unsigned)__double2hiint(v), (unsigned)__double2hiint(v), false, false);
+    const auto l = __builtin_amdgcn_permlane16_swap((unsigned)__double2loint(v), (unsigned)__double2loint(v), false, false);
+    return __hiloint2double((int)h[0], (int)l[0]) + __hiloint2double((int)h[1], (int)l[1]);
+}
+__device__ __forceinline__ double with_other_half(double v)
+{
+    const auto h = __builtin_amdgcn_permlane32_swap((unsigned)__double2hiint(v), (unsigned)__double2hiint(v), false, false);
+    const auto l = __builtin_amdgcn_permlane32_swap((unsigned)__double2loint(v), (unsigned)__double2loint(v), false, false);
+    return __hiloint2double((int)h[0], (int)l[0]) + __hiloint2double((int)h[1], (int)l[1]);
+}
+
+// Sums over the TPR threads of a row; every one of them gets them.  TPR > 64: over the row's waves by way of s_part (a place to each wave of
+// the workgroup), which the next call must not take again before another barrier.
+template <int TPR, int N, typename V>
+__device__ __forceinline__ void totals(V (&v)[N], V (*s_part)[N])
+{
 #pragma unroll
-        for (int j = 0; j < CH; ++j) sum[0] += sum8(v[j]);
-        row_sums<TPR>(sum, s_part[0]);
-        mean = sum[0] / (float)cols;
+    for (int i = 0; i < N; ++i) {
+        v[i] += moved(v[i], 8);
+        v[i] += moved(v[i], 4);
+        v[i] += moved(v[i], 2);
+        v[i] += moved(v[i], 1);
+        if constexpr (TPR > 16) v[i] = with_other_half(with_other_row(v[i]));
+    }
+    if constexpr (TPR > kWaveSize) {
+        constexpr int waves = TPR / kWaveSize; // of a row
+        const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x / kWaveSize;
+        if (lane == 0) {
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
+            for (int i = 0; i < N; ++i) s_part[wave][i] = v[i];
+        }
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) v[j][i] -= mean;
-            if (column(j) + kChunk > cols) {
-#pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[j][i] = column(j) + i < cols ? v[j][i] : 0.0f;
-            }
+        for (int i = 0; i < N; ++i) {
+            v[i] = s_part[(wave & ~(waves - 1)) + (lane & (waves - 1))][i];
+            if constexpr (waves > 8) v[i] += moved(v[i], 8);
+            if constexpr (waves > 4) v[i] += moved(v[i], 4);
+            if constexpr (waves > 2) v[i] += moved(v[i], 2);
+            v[i] += moved(v[i], 1);
         }
     }
-    float sq[1] = {0.0f};
+}
+
+// Places for a row's sums of the waves
+template <int WAVES>
+struct Parts {
+    double layer[WAVES][2];
+    float rms[WAVES][1];
+};
+
+// Mean and rstd of a row's values v (0 past its end) over its TPR threads.  One reduction: the layer norm's sums are of the values less
+// `pivot`, the row's first one, and their squares, in 64 bits.  The variance is what is left of the squares' mean without the mean's square, which
+// is at most cols times as large (the pivot itself is one of the values), so of 53 bits at most 14 are lost.
+template <int TPR, int CH, int WAVES, typename F>
+__device__ __forceinline__ void statistics(int kind, float eps, int cols, const float (&v)[CH][kChunk], float pivot, Parts<WAVES> &parts, float &mean,
+                                           float &rstd, F column)
+{
+    if (kind == DQRM_NORM_LAYER) {
+        double sum[2] = {0.0, 0.0};
 #pragma unroll
-    for (int j = 0; j < CH; ++j) sq[0] += squares8(v[j]);
-    row_sums<TPR>(sq, s_part[1]);
-    rstd = 1.0f / sqrtf(sq[0] / (float)cols + eps);
+        for (int j = 0; j < CH; ++j) {
+            if (column(j) >= cols) continue;
+            const bool whole = column(j) + kChunk <= cols;
 #pragma unroll
-    for (int j = 0; j < CH; ++j)
+            for (int i = 0; i < kChunk; ++i) {
+                double d = (double)v[j][i] - (double)pivot;
+                if (!whole) d = column(j) + i < cols ? d : 0.0;
+                sum[0] += d;
+                sum[1] = fma(d, d, sum[1]);
+            }
+        }
+        totals<TPR>(sum, parts.layer);
+        const double off = sum[0] / cols, var = sum[1] / cols - off * off;
+        mean = (float)((double)pivot + off);
+        rstd = 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + eps); // (a NaN stays)
+    } else {
+        float sq[1] = {0.0f};
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[j][i] *= rstd;
+        for (int j = 0; j < CH; ++j) sq[0] += squares8(v[j]);
+        totals<TPR>(sq, parts.rms);
+        mean = 0.0f;
+        rstd = 1.0f / sqrtf(sq[0] / (float)cols + eps);
+    }
 }
 
 // TPR threads to a row, CH chunks of 8 values to a thread, the next row of u and r requested before this one's sums; the columns' vectors
@@ -103,7 +184,7 @@ __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
 {
     using T = elem_t<DT>;
     constexpr int rows_per_block = BLOCK / TPR;
-    __shared__ float s_part[2][4][BLOCK / kWaveSize][1]; // (two rows in turn: no wave overwrites what another still reads)
+    __shared__ Parts<BLOCK / kWaveSize> s_parts[2][2]; // (two rows in turn: no wave overwrites what another still reads)
     const int t = threadIdx.x % TPR;
     const int64_t step = (int64_t)gridDim.x * rows_per_block;
     const int cols = (int)a.cols;
@@ -111,9 +192,11 @@ __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
     auto column = [&](int j) { return (j * TPR + t) * kChunk; };
     int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
     Raw<T> next_u[CH], next_r[CH];
+    T next_u0, next_r0; // the row's first values, for the statistics' pivots
     // (a group past the last row works on that row and writes nothing)
     auto ask = [&](int64_t at) {
         const int64_t q = min(at, a.rows - 1);
+        next_u0 = static_cast<const T *>(a.u)[q * a.ldu], next_r0 = static_cast<const T *>(a.r)[q * a.ldr];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             next_u[j] = request<SHORT>(static_cast<const T *>(a.u) + q * a.ldu, column(j), cols);
@@ -123,6 +206,8 @@ __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
     ask(r);
     // gate N1(u) = z (gate gamma1) + gate beta1
     float gain[CH][kChunk], offset[CH][kChunk], gamma[CH][kChunk], beta[CH][kChunk];
+    const auto first = [](const float *p, float without) { return p ? p[0] : without; };
+    const float gain0 = first(a.p.post_gamma, 1.0f) * first(a.p.gate, 1.0f), offset0 = first(a.p.post_beta, 0.0f) * first(a.p.gate, 1.0f);
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
         float gate[kChunk];
@@ -138,50 +223,44 @@ __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
     for (; r - threadIdx.x / TPR < a.rows; r += step, turn ^= 1) {
         const bool own = r < a.rows;
         float v[CH][kChunk], res[CH][kChunk];
+        const float u0 = (float)next_u0, r0 = (float)next_r0;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             arrived<SHORT>(next_u[j], column(j), cols, v[j]);
             arrived<SHORT>(next_r[j], column(j), cols, res[j]);
         }
         ask(r + step);
-        float mean1 = 0.0f, rstd1 = 0.0f, mean2 = 0.0f, rstd2 = 0.0f;
-        if (a.p.post != DQRM_NORM_NONE) normalise<TPR>(a.p.post, a.p.post_eps, cols, v, s_part[turn], mean1, rstd1, column);
+        float mean1 = 0.0f, rstd1 = 1.0f, mean2 = 0.0f, rstd2 = 1.0f;
+        if (a.p.post != DQRM_NORM_NONE) statistics<TPR>(a.p.post, a.p.post_eps, cols, v, u0, s_parts[turn][0], mean1, rstd1, column);
+        const auto joined = [&](float u, float r, float gain, float offset) { return a.p.res_scale * r + ((u - mean1) * rstd1 * gain + offset); };
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) v[j][i] = joined(v[j][i], res[j][i], gain[j][i], offset[j][i]);
+            if (column(j) + kChunk > cols) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) v[j][i] = column(j) + i < cols ? v[j][i] : 0.0f;
+            }
+        }
+        if (a.p.pre != DQRM_NORM_NONE) statistics<TPR>(a.p.pre, a.p.pre_eps, cols, v, joined(u0, r0, gain0, offset0), s_parts[turn][1], mean2, rstd2, column);
+        // out may be r's or u's memory.  A thread stores the values that it alone has taken from there (what else its last vector held it has
+        // dropped); the row's first values, which all threads have where they are a pivot, went into the sums in front of the last barrier.
 #pragma unroll
         for (int j = 0; j < CH; ++j)
-#pragma unroll
-            for (int i = 0; i < kChunk; ++i) {
-                v[j][i] = a.p.res_scale * res[j][i] + (v[j][i] * gain[j][i] + offset[j][i]);
-                if (column(j) + kChunk > cols) v[j][i] = column(j) + i < cols ? v[j][i] : 0.0f;
-            }
-        // (out may be r's or u's memory: a thread stores the values that it alone has taken from there; what else its last vector held it
-        // has dropped)
-        auto store_out = [&] {
-#pragma unroll
-            for (int j = 0; j < CH; ++j)
-                if (own && column(j) < cols) store_chunk<true>(static_cast<T *>(a.out) + r * a.ldo, column(j), cols, v[j]);
-        };
-        if (a.p.pre == DQRM_NORM_NONE) {
-            store_out();
-        } else {
-            float out[CH][kChunk];
-#pragma unroll
-            for (int j = 0; j < CH; ++j)
-#pragma unroll
-                for (int i = 0; i < kChunk; ++i) out[j][i] = v[j][i];
-            normalise<TPR>(a.p.pre, a.p.pre_eps, cols, out, s_part[turn] + 2, mean2, rstd2, column);
-            store_out();
+            if (own && column(j) < cols) store_chunk<true>(static_cast<T *>(a.out) + r * a.ldo, column(j), cols, v[j]);
+        if (a.p.pre != DQRM_NORM_NONE) {
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
                 const int c = column(j);
 #pragma unroll
-                for (int i = 0; i < kChunk; ++i) out[j][i] = out[j][i] * gamma[j][i] + beta[j][i];
-                // (past the row's end 0, also where rstd is infinite or a NaN: the padding of the codes)
+                for (int i = 0; i < kChunk; ++i) v[j][i] = (v[j][i] - mean2) * rstd2 * gamma[j][i] + beta[j][i];
+                // (past the row's end 0: the padding of the codes)
                 if (c + kChunk > cols) {
 #pragma unroll
-                    for (int i = 0; i < kChunk; ++i) out[j][i] = c + i < cols ? out[j][i] : 0.0f;
+                    for (int i = 0; i < kChunk; ++i) v[j][i] = c + i < cols ? v[j][i] : 0.0f;
                 }
-                if (own && a.y && c < cols) store_chunk<true>(static_cast<T *>(a.y) + r * a.ldy, c, cols, out[j]);
-                if (own && a.codes && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), out[j]);
+                if (own && a.y && c < cols) store_chunk<true>(static_cast<T *>(a.y) + r * a.ldy, c, cols, v[j]);
+                if (own && a.codes && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), v[j]);
             }
         }
         if (own && t == 0 && a.stats) {
@@ -270,7 +349,7 @@ __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
                     s[1] += dy[j][i] * z2[j][i];
                 }
             }
-            row_sums<TPR>(s, s_part[turn][0]);
+            totals<TPR>(s, s_part[turn][0]);
             const float c0 = a.p.pre == DQRM_NORM_LAYER ? s[0] * inv_n : 0.0f, c1 = s[1] * inv_n;
 #pragma unroll
             for (int j = 0; j < CH; ++j)
@@ -295,7 +374,7 @@ __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
             }
         float c0 = 0.0f, c1 = 0.0f, by = 1.0f;
         if (post) {
-            row_sums<TPR>(s, s_part[turn][1]);
+            totals<TPR>(s, s_part[turn][1]);
             c0 = a.p.post == DQRM_NORM_LAYER ? s[0] * inv_n : 0.0f, c1 = s[1] * inv_n, by = rstd1;
         }
         // (du and dr may be the memory of a matrix that is read: a thread stores the values that it alone has taken from there)

@@ -16,8 +16,10 @@ using dqrm_grad::Item;
 using dqrm_mx::kChunk;
 
 constexpr int32_t kMostTensors = 65536;
-// Pieces of all tensors together, apart from each tensor's last: a few workgroups to a CU.  A piece has at least four rounds of vectors.
+// Pieces of the tensors of a launch, on average: a few workgroups to a CU.  A piece has at least four rounds of vectors.
 constexpr int64_t kPieces = 2048, kLeastPiece = dqrm_grad::kThreads * dqrm_grad::kAhead;
+// Up to so many parts every workgroup of the scaling joins them for itself; more are joined by a launch of their own.
+constexpr unsigned kJoinedByAll = 2 * kPieces;
 
 bool empty(const dqrm_grad_t &g) { return g.rows == 0 || g.cols == 0; }
 
@@ -91,7 +93,8 @@ GradPlan grad_plan(const dqrm_grad_t *g, int32_t n)
     int64_t all = 0;
     for (int32_t i = 0; i < n; ++i)
         if (!empty(g[i])) all += vectors_of(item_of(g[i]));
-    GradPlan p{std::max(kLeastPiece, ceil_div(ceil_div(all, kPieces), kLeastPiece) * kLeastPiece), 0};
+    const int64_t pieces = kPieces * std::max<int64_t>(1, ceil_div(n, dqrm_grad::kItems));
+    GradPlan p{std::max(kLeastPiece, ceil_div(ceil_div(all, pieces), kLeastPiece) * kLeastPiece), 0};
     for (int32_t i = 0; i < n; ++i)
         if (!empty(g[i])) p.pieces += (unsigned)ceil_div(vectors_of(item_of(g[i])), p.per_piece);
     return p;
@@ -156,14 +159,14 @@ void launch_joins(const dqrm_grad_t *g, int32_t n, int32_t kind, const GradPlan 
     });
 }
 
-void launch_scale(const dqrm_grad_t *g, int32_t n, int32_t kind, const GradPlan &p, const double *parts, const float *given, float *norm, float max_norm,
-                  hipStream_t st)
+void launch_scale(const dqrm_grad_t *g, int32_t n, int32_t kind, const GradPlan &p, const double *parts, const float *given, float *norm, float *norms,
+                  float max_norm, hipStream_t st)
 {
-    for_batches(g, n, p, [&](const Batch &b, int32_t first, bool) {
+    for_batches(g, n, p, [&](const Batch &b, int32_t, bool) {
         if (!b.pieces) return;
         with_kind(kind, [&](auto k) {
-            hipLaunchKernelGGL(dqrm_grad::grad_scale_kernel<decltype(k)::value>, dim3(b.pieces), dim3(dqrm_grad::kThreads), 0, st, b, parts, given,
-                               b.first == 0 ? norm : nullptr, max_norm);
+            hipLaunchKernelGGL(dqrm_grad::grad_scale_kernel<decltype(k)::value>, dim3(b.pieces), dim3(dqrm_grad::kThreads), 0, st, b, parts, given, norm,
+                               norms, max_norm);
         });
     });
 }
@@ -255,7 +258,7 @@ int32_t dqrm_grad_scale(const dqrm_grad_t *grads, int32_t n, const float *norm, 
     DQRM_CHECK(check_grads(grads, n));
     if (!norm || !aligned(norm, 4) || !(max_norm >= 0.0f)) return DQRM_ERR_INVALID_ARG;
     DQRM_CHECK(check_apart(grads, n));
-    launch_scale(grads, n, DQRM_GRAD_NORM_2, grad_plan(grads, n), nullptr, norm, nullptr, max_norm, static_cast<hipStream_t>(stream));
+    launch_scale(grads, n, DQRM_GRAD_NORM_2, grad_plan(grads, n), nullptr, norm, nullptr, nullptr, max_norm, static_cast<hipStream_t>(stream));
     DQRM_HIP_CHECK(hipGetLastError());
     return DQRM_OK;
 }
@@ -270,8 +273,12 @@ int32_t dqrm_grad_clip(const dqrm_grad_t *grads, int32_t n, int32_t kind, float 
     hipStream_t st = static_cast<hipStream_t>(stream);
     double *parts = static_cast<double *>(workspace);
     launch_parts(grads, n, kind, p, parts, st);
-    if (norms || !p.pieces) launch_joins(grads, n, kind, p, parts, p.pieces ? nullptr : norm, norms, st);
-    launch_scale(grads, n, kind, p, parts, nullptr, norm, max_norm, st);
+    if (n <= dqrm_grad::kItems && p.pieces > 0 && p.pieces <= kJoinedByAll) { // (one launch: it joins the parts as well)
+        launch_scale(grads, n, kind, p, parts, nullptr, norm, norms, max_norm, st);
+    } else {
+        launch_joins(grads, n, kind, p, parts, norm, norms, st);
+        launch_scale(grads, n, kind, p, nullptr, norm, nullptr, nullptr, max_norm, st);
+    }
     DQRM_HIP_CHECK(hipGetLastError());
     return DQRM_OK;
 }

@@ -157,7 +157,8 @@ struct GradArgs {
     Classifier c;
     const float *lse, *grad;
     const uint64_t *live;  // rows that have a gradient, a bit each
-    const float *d_scale;  // what d is multiplied by before its rounding, or null: 1
+    const float *most;     // the largest |grad|: d is held in units of it, times `by`
+    float by;
     char *d;               // [planes][rows][pitch]
     int64_t plane, pitch;  // bytes
     int planes;
@@ -202,12 +203,13 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(Grad
     multiply_tile<T, S, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), acc);
     logits<S>(a.c, acc, n0 + wn * S::TN * 32);
     const int64_t row0 = m0 + wm * S::TM * 32 + (lane & 31);
+    const float most = *a.most;
     int target[S::TM];
 #pragma unroll
     for (int t = 0; t < S::TM; ++t) {
         const int64_t row = row0 + t * 32;
         const bool live = row < g.m && (a.live[row >> 6] >> (row & 63)) & 1;
-        const float lse2 = live ? a.lse[row] * kLog2e : 0.0f, grad = live ? a.grad[row] : 0.0f;
+        const float lse2 = live ? a.lse[row] * kLog2e : 0.0f, grad = live ? a.grad[row] / most : 0.0f;
         target[t] = place_of_target<S>(live ? a.c.targets[row] : -1, a.c.first + n0 + wn * S::TN * 32);
 #pragma unroll
         for (int j = 0; j < S::TN; ++j)
@@ -253,15 +255,14 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(Grad
             float sum = s_sum[n];
 #pragma unroll
             for (int w = 1; w < S::WM; ++w) sum += s_sum[w * S::BN + n];
-            if (n0 + n < g.n) a.sums[(int64_t)at.tm * g.n + n0 + n] = sum;
+            if (n0 + n < g.n) a.sums[(int64_t)at.tm * g.n + n0 + n] = sum * most;
         }
         __syncthreads();
     }
-    const float by = a.d_scale ? *a.d_scale : 1.0f;
     const int64_t cols = a.pitch / (int64_t)sizeof(T); // (the padding is zeros)
     for (int plane = 0; plane < a.planes; ++plane) {
         TileOut<T, S, false>::run(reinterpret_cast<T *>(a.d + plane * a.plane), cols, acc, lds + wave * TileOut<T, S, false>::wave_bytes, m0 + wm * S::TM * 32,
-                                  n0 + wn * S::TN * 32, g.m, cols, by);
+                                  n0 + wn * S::TN * 32, g.m, cols, a.by);
         if (plane + 1 == a.planes) break;
 #pragma unroll
         for (int t = 0; t < S::TM; ++t)
@@ -365,13 +366,29 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(PackArgs a, dqrm::FastDi
     }
 }
 
-// Which rows have a gradient, a bit each, and the largest |grad| of a workgroup's rows as a float's bits (of finite ones).
-static __global__ __launch_bounds__(256) void xent_rows_kernel(const int64_t *targets, int64_t classes, const float *lse, const float *grad, int64_t rows,
-                                                               uint64_t *live, unsigned *most)
+// The largest of 1024 threads' values; thread 0 gets it
+__device__ __forceinline__ unsigned largest(unsigned v)
 {
-    __shared__ unsigned s_most[4];
+    __shared__ unsigned s[16];
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, d, kWaveSize));
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 1; i < 16; ++i) v = max(v, s[i]);
+    return v;
+}
+
+// The gradients' unit: the largest of them (of the finite ones; 1 if there is none).  d in units of it: where all rows weigh the same, as in a
+// mean, the targets' places are close to -1 and lose nothing by their rounding; and fp16, times 2^14, has all its bits down to 2^-28 of the unit.
+__device__ __forceinline__ float unit_of(unsigned bits) { return bits ? __uint_as_float(bits) : 1.0f; }
+
+// Which rows have a gradient, a bit each, and the bits of the largest |grad| of a workgroup's rows; of all rows, by a single workgroup, as the unit.
+static __global__ __launch_bounds__(1024) void xent_rows_kernel(const int64_t *targets, int64_t classes, const float *lse, const float *grad, int64_t rows,
+                                                                uint64_t *live, unsigned *most, float *unit)
+{
     unsigned top = 0;
-    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r - (threadIdx.x & 63) < rows; r += (int64_t)gridDim.x * 256) {
+    for (int64_t r = (int64_t)blockIdx.x * 1024 + threadIdx.x; r - (threadIdx.x & 63) < rows; r += (int64_t)gridDim.x * 1024) {
         bool has = false;
         if (r < rows) {
             const float g = grad[r];
@@ -381,11 +398,16 @@ static __global__ __launch_bounds__(256) void xent_rows_kernel(const int64_t *ta
         const uint64_t word = __ballot(has);
         if ((threadIdx.x & 63) == 0) live[r >> 6] = word;
     }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, kWaveSize));
-    if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) most[blockIdx.x] = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+    top = largest(top);
+    if (threadIdx.x == 0 && gridDim.x == 1) *unit = unit_of(top);
+    if (threadIdx.x == 0 && gridDim.x > 1) most[blockIdx.x] = top;
+}
+
+// ... of several workgroups
+static __global__ __launch_bounds__(1024) void xent_unit_kernel(const unsigned *most, int n, float *unit)
+{
+    const unsigned top = largest((int)threadIdx.x < n ? most[threadIdx.x] : 0u);
+    if (threadIdx.x == 0) *unit = unit_of(top);
 }
 
 // Which classes are not taken out.
@@ -394,23 +416,6 @@ static __global__ __launch_bounds__(256) void xent_classes_kernel(const float *b
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const uint64_t word = __ballot(j < classes && bias[min(j, classes - 1)] != -__builtin_inff());
     if ((threadIdx.x & 63) == 0 && j < classes) live[j >> 6] = word;
-}
-
-// The power of two that brings the largest |grad| to 2^14 .. 2^15, and its reciprocal: d in fp16 then has all its bits down to 2^-29 of that, and is
-// off by 2^-40 of it below.
-static __global__ __launch_bounds__(256) void xent_scale_kernel(const unsigned *most, int n, float *scale)
-{
-    __shared__ unsigned s_most[4];
-    unsigned top = (int)threadIdx.x < n ? most[threadIdx.x] : 0u;
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, kWaveSize));
-    if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        top = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
-        const int e = min(max(127 + 14 - ((int)(top >> 23) - 127), 1), 253); // (exponents of the power and of its reciprocal)
-        scale[0] = __uint_as_float((unsigned)e << 23), scale[1] = __uint_as_float((unsigned)(254 - e) << 23);
-    }
 }
 
 } // namespace dqrm_xent

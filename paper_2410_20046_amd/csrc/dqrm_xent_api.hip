@@ -15,6 +15,7 @@ constexpr int64_t kMostClasses = 1 << 22; // of a piece, for the same reason
 // chip's last-level cache, which d is read from twice.
 constexpr int64_t kPieceBytes = 256LL << 20;
 constexpr int kMostSlices = 64;
+constexpr int64_t kRowsAlone = 16384; // rows that one workgroup looks through for the gradients' unit
 constexpr int64_t kSliceTiles = 512; // tiles times slices
 
 using TileBig = Tile<4, 4, 2, 2, 2>; // 256 by 256, one to a CU
@@ -133,8 +134,8 @@ FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype, bool room)
 }
 
 struct BwdSpace {
-    size_t live, classes, most, scale, x, w, d, sums, dx, dw;
-    size_t total() const { return live + classes + most + scale + x + w + d + sums + dx + dw; }
+    size_t live, classes, most, unit, x, w, d, sums, dx, dw;
+    size_t total() const { return live + classes + most + unit + x + w + d + sums + dx + dw; }
 };
 
 BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
@@ -144,7 +145,7 @@ BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     // (a piece has at most `most` classes, and at most 256 or those whose d fits)
     const int64_t d = std::max(m * 256, std::min(m * most, kPieceBytes / (2 * pl)));
     BwdSpace s{};
-    s.live = bytes(ceil_div(m, 64) * 8), s.classes = bytes(ceil_div(v, 64) * 8), s.most = 1024, s.scale = 256;
+    s.live = bytes(ceil_div(m, 64) * 8), s.classes = bytes(ceil_div(v, 64) * 8), s.most = 1024, s.unit = 256;
     s.x = bytes(m * up(k, kDepth) * 2 * pl), s.w = bytes(most * up(k, kDepth) * 2 * pl);
     s.d = bytes(d * 2 * pl);
     s.sums = bytes((d / 64 + most) * 4);
@@ -294,15 +295,16 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
     Space ws{static_cast<char *>(workspace)};
     uint64_t *live = static_cast<uint64_t *>(ws.take(need.live)), *live_classes = static_cast<uint64_t *>(ws.take(need.classes));
     unsigned *most = static_cast<unsigned *>(ws.take(need.most));
-    float *power = static_cast<float *>(ws.take(need.scale));
+    float *unit = static_cast<float *>(ws.take(need.unit));
     void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
     char *d = static_cast<char *>(ws.take(need.d));
     float *sums = static_cast<float *>(ws.take(need.sums)), *dx_sums = static_cast<float *>(ws.take(need.dx)), *dw_sums = static_cast<float *>(ws.take(need.dw));
 
-    const int row_blocks = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(c.m, 256), 1), 256);
-    hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)row_blocks), dim3(256), 0, st, c.targets, c.v, lse, grad, c.m, live, most);
-    const bool f16 = c.dtype == DQRM_F16;
-    if (f16) hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(256), 0, st, most, row_blocks, power);
+    const int row_blocks = c.m <= kRowsAlone ? 1 : (int)std::min<int64_t>(ceil_div(c.m, 1024), 256);
+    hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)row_blocks), dim3(1024), 0, st, c.targets, c.v, lse, grad, c.m, live, most, unit);
+    if (row_blocks > 1) hipLaunchKernelGGL(xent_unit_kernel, dim3(1), dim3(1024), 0, st, most, row_blocks, unit);
+    // d is held in units of the largest |grad|, in fp16 times 2^14
+    const float by = c.dtype == DQRM_F16 ? 16384.0f : 1.0f, scale = c.scale / by;
     if (c.bias && dx) hipLaunchKernelGGL(xent_classes_kernel, dim3((unsigned)ceil_div(c.v, 256)), dim3(256), 0, st, c.bias, c.v, live_classes);
 
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
@@ -315,7 +317,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
         const Shape shape = logits_shape(c.m, n);
         GradArgs a{};
         const Products g = products(x, w, c.m, n, c.k, pairs, shape);
-        a.c = classifier(c, g, first), a.lse = lse, a.grad = grad, a.live = live, a.d_scale = f16 ? power : nullptr;
+        a.c = classifier(c, g, first), a.lse = lse, a.grad = grad, a.live = live, a.most = unit, a.by = by;
         a.pitch = up(n, kDepth) * 2, a.plane = c.m * a.pitch, a.planes = planes, a.d = d, a.sums = dbias ? sums : nullptr;
         if (g.tiles_m > 0)
             with_operands(c.dtype, [&](auto zero) {
@@ -330,7 +332,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
         if (dx && c.m > 0) {
             Operand by = w;
             by.live = c.bias ? live_classes + first / 64 : nullptr;
-            OutArgs o{products(dm, by, c.m, c.k, n, pairs, dx_plan.shape), dx, lddx, c.scale, f16 ? power + 1 : nullptr};
+            OutArgs o{products(dm, by, c.m, c.k, n, pairs, dx_plan.shape), dx, lddx, scale, unit};
             o.g.slices = dx_plan.slices, o.g.stages_per_slice = dx_plan.stages_per_slice;
             const bool in_sums = !one || dx_plan.slices > 1;
             if (in_sums) o.c = dx_sums, o.ldc = c.k, o.scale = 1.0f, o.by = nullptr;
@@ -341,15 +343,15 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
             by.live = live;
             const Sliced p = out_plan(n, c.k, ceil_div(c.m, kDepth) * pairs);
             char *to = static_cast<char *>(dw) + first * lddw * (int64_t)size_of(c.dtype);
-            OutArgs o{products(dm, by, n, c.k, c.m, pairs, p.shape), to, lddw, c.scale, f16 ? power + 1 : nullptr};
+            OutArgs o{products(dm, by, n, c.k, c.m, pairs, p.shape), to, lddw, scale, unit};
             o.g.slices = p.slices, o.g.stages_per_slice = p.stages_per_slice;
             if (p.slices > 1) o.c = dw_sums, o.ldc = c.k, o.scale = 1.0f, o.by = nullptr;
             launch_out<true>(c.dtype, p.shape, o, p.slices > 1, false, st);
-            if (p.slices > 1) launch_out_join(c.dtype, dw_sums, p.slices, n, c.k, to, lddw, c.scale, f16 ? power + 1 : nullptr, st);
+            if (p.slices > 1) launch_out_join(c.dtype, dw_sums, p.slices, n, c.k, to, lddw, scale, unit, st);
         }
     }
     if (dx && c.m > 0 && c.k > 0 && (!one || dx_plan.slices > 1))
-        launch_out_join(c.dtype, dx_sums, dx_plan.slices, c.m, c.k, dx, lddx, c.scale, f16 ? power + 1 : nullptr, st);
+        launch_out_join(c.dtype, dx_sums, dx_plan.slices, c.m, c.k, dx, lddx, scale, unit, st);
 }
 
 } // namespace

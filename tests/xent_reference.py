@@ -50,12 +50,12 @@ def gradients_and_bounds(x, w, targets, bias, scale, grad):
     d[rows, targets[rows]] -= 1
     off = (off + U * d.abs()) * g.abs()
     d = d * g
-    off = off + 2 * U * d.abs() + 2.0 ** -120
+    off = off + 4 * U * d.abs() + 2.0 ** -120  # (grad over the unit, its product, times the unit again)
     dbias = d.sum(0)
     dbias_off = off.sum(0) + U * (x.shape[0] + 4) * d.abs().sum(0) + 2.0 ** -120
     # d as the products take it
     u, least = HALF_STEP[dtype], 0.0
-    if dtype is torch.float16:  # held times a power of two that brings the largest |grad| to 2^14 and more: half a subnormal step is 2^-25 of that
+    if dtype is torch.float16:  # held in units of the largest |grad| times 2^14: half a subnormal step is 2^-25
         least = 2.0 ** -25 * 2.0 ** -14 * float(g.abs().max())
     off = off * (1 + u) + u * d.abs() + least
     n = terms(w.shape[0], dtype)
