@@ -36,8 +36,14 @@ int32_t dqrm_host::hip_fail(hipError_t e, const char *what)
 void dqrm_host::launch_xent_join(const void *parts, int64_t tiles, int64_t rows, const float *at, const int64_t *targets, int64_t classes, float *loss,
                                  float *lse, hipStream_t st)
 {
-    hipLaunchKernelGGL(dqrm::xent_join_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, static_cast<const float2 *>(parts), tiles, rows, at,
-                       targets, classes, loss, lse);
+    const auto go = [&](auto kernel, int64_t rows_each) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + rows_each - 1) / rows_each)), dim3(256), 0, st, static_cast<const float2 *>(parts), tiles, rows, at,
+                           targets, classes, loss, lse);
+    };
+    if (rows <= 1024)
+        go(dqrm::xent_join_kernel<1>, 1);
+    else
+        go(dqrm::xent_join_kernel<16>, 16);
 }
 
 namespace {

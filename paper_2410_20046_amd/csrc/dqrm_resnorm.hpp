@@ -58,6 +58,7 @@ __device__ __forceinline__ void arrived(const Raw<T> &raw, int c, int cols, floa
     }
 }
 
+__device__ __forceinline__ float sum8(const float (&v)[kChunk]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 __device__ __forceinline__ float squares8(const float (&v)[kChunk])
 {
     return ((v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3])) + ((v[4] * v[4] + v[5] * v[5]) + (v[6] * v[6] + v[7] * v[7]));
@@ -142,30 +143,37 @@ struct Parts {
     float rms[WAVES][1];
 };
 
-// Mean and rstd of a row's values v (0 past its end) over its TPR threads.  One reduction: the layer norm's sums are of the values less
-// `pivot`, the row's first one, and their squares, in 64 bits.  The variance is what is left of the squares' mean without the mean's square, which
-// is at most cols times as large (the pivot itself is one of the values), so of 53 bits at most 14 are lost.
+// Mean and rstd of a row's values v (0 past its end) over its TPR threads.  One reduction: a thread takes the mean m of its own n values, and
+// their squares about it; the sums over threads of n m and of n m^2 + squares are in 64 bits, where the difference that the variance is
+// loses 2^-52 of the mean's square, less than the values' own rounding makes of it.
 template <int TPR, int CH, int WAVES, typename F>
-__device__ __forceinline__ void statistics(int kind, float eps, int cols, const float (&v)[CH][kChunk], float pivot, Parts<WAVES> &parts, float &mean,
-                                           float &rstd, F column)
+__device__ __forceinline__ void statistics(int kind, float eps, int cols, const float (&v)[CH][kChunk], Parts<WAVES> &parts, float &mean, float &rstd, F column)
 {
     if (kind == DQRM_NORM_LAYER) {
-        double sum[2] = {0.0, 0.0};
+        float own = 0.0f, squares = 0.0f;
+        int n = 0;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            if (column(j) >= cols) continue;
-            const bool whole = column(j) + kChunk <= cols;
-#pragma unroll
-            for (int i = 0; i < kChunk; ++i) {
-                double d = (double)v[j][i] - (double)pivot;
-                if (!whole) d = column(j) + i < cols ? d : 0.0;
-                sum[0] += d;
-                sum[1] = fma(d, d, sum[1]);
-            }
+            own += sum8(v[j]);
+            n += min(max(cols - column(j), 0), kChunk);
         }
+        own = n == CH * kChunk ? own * (1.0f / (CH * kChunk)) : n > 0 ? own / (float)n : 0.0f;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            float d[kChunk];
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) d[i] = v[j][i] - own;
+            if (column(j) + kChunk > cols) {
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) d[i] = column(j) + i < cols ? d[i] : 0.0f;
+            }
+            squares += squares8(d);
+        }
+        const double weight = (double)n * (double)own;
+        double sum[2] = {weight, fma(weight, (double)own, (double)squares)};
         totals<TPR>(sum, parts.layer);
-        const double off = sum[0] / cols, var = sum[1] / cols - off * off;
-        mean = (float)((double)pivot + off);
+        const double inv_n = 1.0 / cols, middle = sum[0] * inv_n, var = sum[1] * inv_n - middle * middle;
+        mean = (float)middle;
         rstd = 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + eps); // (a NaN stays)
     } else {
         float sq[1] = {0.0f};
@@ -177,12 +185,17 @@ __device__ __forceinline__ void statistics(int kind, float eps, int cols, const 
     }
 }
 
-// TPR threads to a row, CH chunks of 8 values to a thread, the next row of u and r requested before this one's sums; the columns' vectors
-// stay in registers for all rows of a workgroup.  Bound by its bytes: two reads and two writes.
-template <int DT, int TPR, int CH, int BLOCK, bool SHORT>
+// Where the columns' vectors are for all rows of a workgroup
+enum class Gains { registers, lds, memory };
+
+// TPR threads to a row, CH chunks of 8 values to a thread, the next rows of u and r requested before this one's sums.  Bound by its bytes, two
+// reads and two writes, where a copy has 5.0 TB/s: 65536 x 1024 bfloat16 104 us, 5.2 TB/s, 32768 x 4096 235 us, 4.6; wide rows by the two
+// reductions' latency as well, for as many rows as are in a CU's registers: 16384 x 8192 283 us, 3.8.
+template <int DT, int TPR, int CH, int BLOCK, bool SHORT, Gains GAINS, bool CODES>
 __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
 {
     using T = elem_t<DT>;
+    constexpr bool held = GAINS == Gains::registers;
     constexpr int rows_per_block = BLOCK / TPR;
     __shared__ Parts<BLOCK / kWaveSize> s_parts[2][2]; // (two rows in turn: no wave overwrites what another still reads)
     const int t = threadIdx.x % TPR;
@@ -191,60 +204,90 @@ __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
     const int64_t cp = codes_pitch(cols), sp = scales_pitch(cols);
     auto column = [&](int j) { return (j * TPR + t) * kChunk; };
     int64_t r = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / TPR;
-    Raw<T> next_u[CH], next_r[CH];
-    T next_u0, next_r0; // the row's first values, for the statistics' pivots
+    constexpr int ahead = CH == 1 ? 2 : 1; // rows on their way
+    Raw<T> next_u[ahead][CH], next_r[ahead][CH];
     // (a group past the last row works on that row and writes nothing)
-    auto ask = [&](int64_t at) {
+    auto ask = [&](int slot, int64_t at) {
         const int64_t q = min(at, a.rows - 1);
-        next_u0 = static_cast<const T *>(a.u)[q * a.ldu], next_r0 = static_cast<const T *>(a.r)[q * a.ldr];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            next_u[j] = request<SHORT>(static_cast<const T *>(a.u) + q * a.ldu, column(j), cols);
-            next_r[j] = request<SHORT>(static_cast<const T *>(a.r) + q * a.ldr, column(j), cols);
+            next_u[slot][j] = request<SHORT>(static_cast<const T *>(a.u) + q * a.ldu, column(j), cols);
+            next_r[slot][j] = request<SHORT>(static_cast<const T *>(a.r) + q * a.ldr, column(j), cols);
         }
     };
-    ask(r);
+#pragma unroll
+    for (int k = 0; k < ahead; ++k) ask(k, r + k * step);
     // gate N1(u) = z (gate gamma1) + gate beta1
-    float gain[CH][kChunk], offset[CH][kChunk], gamma[CH][kChunk], beta[CH][kChunk];
-    const auto first = [](const float *p, float without) { return p ? p[0] : without; };
-    const float gain0 = first(a.p.post_gamma, 1.0f) * first(a.p.gate, 1.0f), offset0 = first(a.p.post_beta, 0.0f) * first(a.p.gate, 1.0f);
+    // which: 0 gate gamma1, 1 gate beta1, 2 gamma2, 3 beta2
+    auto fetch = [&](int which, int c, float(&v)[kChunk]) {
+        load_gain(which == 0 ? a.p.post_gamma : which == 1 ? a.p.post_beta : which == 2 ? a.p.pre_gamma : a.p.pre_beta, c, cols, which & 1 ? 0.0f : 1.0f, v);
+        if (which < 2 && a.p.gate) {
+            float gate[kChunk];
+            load_gain(a.p.gate, c, cols, 1.0f, gate);
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-        float gate[kChunk];
-        load_gain(a.p.gate, column(j), cols, 1.0f, gate);
-        load_gain(a.p.post_gamma, column(j), cols, 1.0f, gain[j]);
-        load_gain(a.p.post_beta, column(j), cols, 0.0f, offset[j]);
+            for (int i = 0; i < kChunk; ++i) v[i] *= gate[i];
+        } // (a gate of 1 otherwise)
+    };
+    constexpr int in_lds = GAINS == Gains::lds ? TPR * CH * kChunk : 1;
+    __shared__ __align__(16) float s_gains[4][in_lds];
+    float gains[4][held ? CH : 1][kChunk];
+    if constexpr (held) {
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) gain[j][i] *= gate[i], offset[j][i] *= gate[i];
-        load_gain(a.p.pre_gamma, column(j), cols, 1.0f, gamma[j]);
-        load_gain(a.p.pre_beta, column(j), cols, 0.0f, beta[j]);
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) fetch(k, column(j), gains[k][j]);
+    } else if constexpr (GAINS == Gains::lds) {
+        for (int c = threadIdx.x * kChunk; c < in_lds; c += BLOCK * kChunk)
+            for (int k = 0; k < 4; ++k) {
+                float v[kChunk];
+                fetch(k, c, v);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) s_gains[k][c + i] = v[i];
+            }
+        __syncthreads();
     }
-    int turn = 0;
-    for (; r - threadIdx.x / TPR < a.rows; r += step, turn ^= 1) {
+    auto gain_of = [&](int which, int j, float(&v)[kChunk]) {
+        int c = column(j);
+        asm volatile("" : "+v"(c)); // (a load of this row: taken out of the loop over rows, the vectors would be in registers after all)
+        if constexpr (held) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) v[i] = gains[which][j][i];
+        } else if constexpr (GAINS == Gains::lds) {
+            __builtin_memcpy(v, __builtin_assume_aligned(&s_gains[which][c], 16), sizeof(v));
+        } else {
+            fetch(which, c, v);
+        }
+    };
+    auto one_row = [&](int slot, int turn) __attribute__((always_inline)) {
         const bool own = r < a.rows;
-        float v[CH][kChunk], res[CH][kChunk];
-        const float u0 = (float)next_u0, r0 = (float)next_r0;
+        float v[CH][kChunk];
+        Raw<T> res[CH];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            arrived<SHORT>(next_u[j], column(j), cols, v[j]);
-            arrived<SHORT>(next_r[j], column(j), cols, res[j]);
+            arrived<SHORT>(next_u[slot][j], column(j), cols, v[j]);
+            res[j] = next_r[slot][j];
         }
-        ask(r + step);
+        ask(slot, r + ahead * step);
         float mean1 = 0.0f, rstd1 = 1.0f, mean2 = 0.0f, rstd2 = 1.0f;
-        if (a.p.post != DQRM_NORM_NONE) statistics<TPR>(a.p.post, a.p.post_eps, cols, v, u0, s_parts[turn][0], mean1, rstd1, column);
+        if (a.p.post != DQRM_NORM_NONE) statistics<TPR>(a.p.post, a.p.post_eps, cols, v, s_parts[turn][0], mean1, rstd1, column);
         const auto joined = [&](float u, float r, float gain, float offset) { return a.p.res_scale * r + ((u - mean1) * rstd1 * gain + offset); };
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
+            float x[kChunk], gain[kChunk], offset[kChunk];
+            arrived<SHORT>(res[j], column(j), cols, x);
+            gain_of(0, j, gain);
+            gain_of(1, j, offset);
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) v[j][i] = joined(v[j][i], res[j][i], gain[j][i], offset[j][i]);
+            for (int i = 0; i < kChunk; ++i) v[j][i] = joined(v[j][i], x[i], gain[i], offset[i]);
             if (column(j) + kChunk > cols) {
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) v[j][i] = column(j) + i < cols ? v[j][i] : 0.0f;
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (a.p.pre != DQRM_NORM_NONE) statistics<TPR>(a.p.pre, a.p.pre_eps, cols, v, joined(u0, r0, gain0, offset0), s_parts[turn][1], mean2, rstd2, column);
-        // out may be r's or u's memory.  A thread stores the values that it alone has taken from there (what else its last vector held it has
-        // dropped); the row's first values, which all threads have where they are a pivot, went into the sums in front of the last barrier.
+        if (a.p.pre != DQRM_NORM_NONE) statistics<TPR>(a.p.pre, a.p.pre_eps, cols, v, s_parts[turn][1], mean2, rstd2, column);
+        // (out may be r's or u's memory: a thread stores the values that it alone has taken from there; what else its last vector held it
+        // has dropped)
 #pragma unroll
         for (int j = 0; j < CH; ++j)
             if (own && column(j) < cols) store_chunk<true>(static_cast<T *>(a.out) + r * a.ldo, column(j), cols, v[j]);
@@ -252,21 +295,32 @@ __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
                 const int c = column(j);
+                float gamma[kChunk], beta[kChunk];
+                gain_of(2, j, gamma);
+                gain_of(3, j, beta);
 #pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[j][i] = (v[j][i] - mean2) * rstd2 * gamma[j][i] + beta[j][i];
+                for (int i = 0; i < kChunk; ++i) v[j][i] = (v[j][i] - mean2) * rstd2 * gamma[i] + beta[i];
                 // (past the row's end 0: the padding of the codes)
                 if (c + kChunk > cols) {
 #pragma unroll
                     for (int i = 0; i < kChunk; ++i) v[j][i] = c + i < cols ? v[j][i] : 0.0f;
                 }
                 if (own && a.y && c < cols) store_chunk<true>(static_cast<T *>(a.y) + r * a.ldy, c, cols, v[j]);
-                if (own && a.codes && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), v[j]);
+                if (CODES && own && c < cp * 2) write_chunk(a.codes + r * cp, a.scales + r * sp, (unsigned)(c / kChunk), v[j]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (own && t == 0 && a.stats) {
             if (a.p.post != DQRM_NORM_NONE) a.stats[r] = mean1, a.stats[a.all_rows + r] = rstd1;
             if (a.p.pre != DQRM_NORM_NONE) a.stats[2 * a.all_rows + r] = mean2, a.stats[3 * a.all_rows + r] = rstd2;
         }
+    };
+    while (r - threadIdx.x / TPR < a.rows) {
+        one_row(0, 0);
+        r += step;
+        if (r - threadIdx.x / TPR >= a.rows) break;
+        one_row(ahead - 1, 1);
+        r += step;
     }
 }
 
@@ -281,10 +335,12 @@ struct BwdArgs {
 };
 
 // The rows of dout, dy, u and out in registers, the next ones on their way; a thread has the same columns in every row of its workgroup's
-// slice and keeps their sums, so that all is read once.  Bound by its bytes: four reads and two writes.
-template <int DT, int TPR, int CH, int BLOCK, bool SHORT>
+// slice and keeps their sums, so that all is read once.  Bound by its bytes, four reads and two writes: 32768 x 4096 bfloat16 281 us, 5.7 TB/s,
+// 16384 x 8192 286 us, 5.6, 32768 x 512 float 64 us, 6.2.
+template <int DT, int TPR, int CH, int BLOCK, bool SHORT, Gains GAINS>
 __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
 {
+    constexpr bool held = GAINS == Gains::registers;
     using T = elem_t<DT>;
     constexpr int rows_per_block = BLOCK / TPR;
     __shared__ float s_part[2][2][BLOCK / kWaveSize][2]; // (two rows in turn)
@@ -315,13 +371,46 @@ __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
     for (int j = 0; j < CH; ++j) next_dout[j] = next_dy[j] = next_u[j] = next_out[j] = Raw<T>{};
     ask(r);
     float s0[CH][kChunk] = {}, s1[CH][kChunk] = {}, s2[CH][kChunk] = {}, s3[CH][kChunk] = {};
-    float gate[CH][kChunk], post_gamma[CH][kChunk], pre_gamma[CH][kChunk];
+    // which: 0 gate gamma1 (without N1 the gate), 1 gamma2
+    auto fetch = [&](int which, int c, float(&v)[kChunk]) {
+        load_gain(which ? a.p.pre_gamma : a.p.post_gamma, c, cols, 1.0f, v);
+        if (!which && a.p.gate) {
+            float gate[kChunk];
+            load_gain(a.p.gate, c, cols, 1.0f, gate);
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-        load_gain(a.p.gate, column(j), cols, 1.0f, gate[j]);
-        load_gain(a.p.post_gamma, column(j), cols, 1.0f, post_gamma[j]);
-        load_gain(a.p.pre_gamma, column(j), cols, 1.0f, pre_gamma[j]);
+            for (int i = 0; i < kChunk; ++i) v[i] *= gate[i];
+        }
+    };
+    constexpr int in_lds = GAINS == Gains::lds ? TPR * CH * kChunk : 1;
+    __shared__ __align__(16) float s_gains[2][in_lds];
+    float gains[2][held ? CH : 1][kChunk];
+    if constexpr (held) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) fetch(k, column(j), gains[k][j]);
+    } else if constexpr (GAINS == Gains::lds) {
+        for (int c = threadIdx.x * kChunk; c < in_lds; c += BLOCK * kChunk)
+            for (int k = 0; k < 2; ++k) {
+                float v[kChunk];
+                fetch(k, c, v);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) s_gains[k][c + i] = v[i];
+            }
+        __syncthreads();
     }
+    auto gain_of = [&](int which, int j, float(&v)[kChunk]) {
+        int c = column(j);
+        asm volatile("" : "+v"(c)); // (a load of this row, as in the forward)
+        if constexpr (held) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) v[i] = gains[which][j][i];
+        } else if constexpr (GAINS == Gains::lds) {
+            __builtin_memcpy(v, __builtin_assume_aligned(&s_gains[which][c], 16), sizeof(v));
+        } else {
+            fetch(which, c, v);
+        }
+    };
     int turn = 0;
     for (; r - threadIdx.x / TPR < a.rows; r += step, turn ^= 1) {
         const bool own = r < a.rows;
@@ -339,12 +428,14 @@ __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
             float s[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
+                float gain[kChunk];
+                gain_of(1, j, gain);
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) {
                     z2[j][i] = (z2[j][i] - mean2) * rstd2;
                     if (column(j) + kChunk > cols) z2[j][i] = column(j) + i < cols ? z2[j][i] : 0.0f;
                     if (own) s2[j][i] += dy[j][i] * z2[j][i], s3[j][i] += dy[j][i];
-                    dy[j][i] *= pre_gamma[j][i];
+                    dy[j][i] *= gain[i];
                     s[0] += dy[j][i];
                     s[1] += dy[j][i] * z2[j][i];
                 }
@@ -358,7 +449,9 @@ __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
         }
         float s[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < CH; ++j)
+        for (int j = 0; j < CH; ++j) {
+            float gain[kChunk];
+            gain_of(0, j, gain);
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) {
                 z1[j][i] = (z1[j][i] - mean1) * rstd1;
@@ -367,11 +460,11 @@ __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
                     g[j][i] = column(j) + i < cols ? g[j][i] : 0.0f;
                 }
                 if (own) s0[j][i] += g[j][i], s1[j][i] += g[j][i] * z1[j][i];
-                dy[j][i] = g[j][i] * gate[j][i];
-                if (post) dy[j][i] *= post_gamma[j][i];
+                dy[j][i] = g[j][i] * gain[i];
                 s[0] += dy[j][i];
                 s[1] += dy[j][i] * z1[j][i];
             }
+        }
         float c0 = 0.0f, c1 = 0.0f, by = 1.0f;
         if (post) {
             totals<TPR>(s, s_part[turn][1]);

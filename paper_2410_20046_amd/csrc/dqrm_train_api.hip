@@ -176,9 +176,11 @@ namespace rn = dqrm_resnorm;
 
 constexpr int64_t kMostNormCols = 16384;
 
-template <int TPR_, int CH_, int BLOCK_, bool SHORT_ = false>
+// threads and chunks of 8 values to a row; rows of fewer than 8
+template <int TPR_, int CH_, int BLOCK_, rn::Gains GAINS_ = rn::Gains::registers, bool SHORT_ = false>
 struct RowShape {
     static constexpr int TPR = TPR_, CH = CH_, BLOCK = BLOCK_, cols = TPR * CH * kChunk, rows = BLOCK / TPR;
+    static constexpr rn::Gains GAINS = GAINS_;
     static constexpr bool SHORT = SHORT_;
 };
 
@@ -188,26 +190,43 @@ void with_first_that_holds(int64_t cols, F f)
     (void)((cols <= S::cols ? (f(S{}), true) : false) || ...);
 }
 
-template <typename F>
-void with_resnorm_fwd_shape(int64_t cols, F f)
+// Many rows without codes: several chunks to a thread, and the columns' vectors in LDS, where that is faster (bf16: 16384 x 8192 283 us instead of
+// 300 with 1024 threads to a row, 32768 x 4096 235 and 248, 65536 x 1024 104 and 112; fp32: 8192 x 8192 224 and 248, 16384 x 2048 100 and 111,
+// 32768 x 1024 105 and 113; fp32 16384 x 4096 in LDS 210, in registers 203).  Else a chunk to a thread: a row's latency counts.
+template <int DT, typename F>
+void with_resnorm_fwd_shape(int64_t rows, int64_t cols, bool codes, F f)
 {
-    if (cols < kChunk) return f(RowShape<16, 1, 256, true>{});
+    using rn::Gains;
+    if (cols < kChunk) return f(RowShape<16, 1, 256, Gains::registers, true>{});
+    if (rows >= (int64_t)num_cus() * 16 && !codes) {
+        if constexpr (DT == DQRM_F32)
+            return with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<64, 2, 256>, RowShape<128, 2, 512, Gains::lds>,
+                                         RowShape<512, 1, 512>, RowShape<512, 2, 1024, Gains::lds>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
+        else
+            return with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<64, 2, 256>, RowShape<256, 1, 256>,
+                                         RowShape<128, 4, 256, Gains::lds>, RowShape<512, 2, 1024, Gains::lds>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
+    }
     with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<128, 1, 256>, RowShape<256, 1, 256>, RowShape<512, 1, 512>,
-                          RowShape<1024, 1, 1024>, RowShape<1024, 2, 1024>>(cols, f);
+                          RowShape<1024, 1, 1024>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
 }
 
-template <typename F>
+// (fp32, 8192 x 8192: 1024 threads and the columns' vectors in LDS 297 us, 512 threads with two chunks 390; bf16, 16384 x 8192: 296 and 286.
+// Rows beyond 8192 values keep some of the sums in memory: 10000 x 16384 bf16 1517 us.)
+template <int DT, typename F>
 void with_resnorm_bwd_shape(int64_t cols, F f)
 {
-    if (cols < kChunk) return f(RowShape<16, 1, 512, true>{});
+    using rn::Gains;
+    if (cols < kChunk) return f(RowShape<16, 1, 512, Gains::registers, true>{});
+    if constexpr (DT == DQRM_F32)
+        if (cols > 4096 && cols <= 8192) return f(RowShape<1024, 1, 1024, Gains::lds>{});
     with_first_that_holds<RowShape<16, 1, 512>, RowShape<64, 1, 512>, RowShape<128, 1, 512>, RowShape<256, 1, 512>, RowShape<512, 1, 512>,
-                          RowShape<512, 2, 512>, RowShape<512, 4, 512>>(cols, f);
+                          RowShape<512, 2, 512>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
 }
 
 int resnorm_bwd_blocks(int64_t rows, int64_t cols)
 {
-    int64_t n = 0;
-    if (rows > 0 && cols > 0) with_resnorm_bwd_shape(cols, [&](auto shape) { n = std::min<int64_t>(ceil_div(rows, decltype(shape)::rows), num_cus()); });
+    int64_t n = 0; // (every type's shapes have as many rows to a workgroup)
+    if (rows > 0 && cols > 0) with_resnorm_bwd_shape<DQRM_F32>(cols, [&](auto shape) { n = std::min<int64_t>(ceil_div(rows, decltype(shape)::rows), num_cus()); });
     return (int)n;
 }
 
@@ -305,12 +324,14 @@ int32_t dqrm_residual_norm_fwd(int32_t dtype, int64_t rows, int64_t cols, const 
         if (stats) a.stats = stats + r0;
         if (q) a.codes = q->codes + r0 * dqrm_mx::codes_pitch(cols), a.scales = q->scales + r0 * dqrm_mx::scales_pitch(cols);
         with_type(dtype, [&](auto t) {
-            with_resnorm_fwd_shape(cols, [&](auto shape) {
+            with_resnorm_fwd_shape<decltype(t)::value>(rows, cols, q != nullptr, [&](auto shape) {
                 using S = decltype(shape);
                 // as many workgroups as the chip holds: each keeps the columns' vectors for all of its rows
-                const int64_t most = (int64_t)num_cus() * std::max(1, 1024 / S::BLOCK);
-                hipLaunchKernelGGL((rn::resnorm_fwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT>),
-                                   dim3((unsigned)std::min(ceil_div(a.rows, S::rows), most)), dim3(S::BLOCK), 0, st, a);
+                const int64_t most = (int64_t)num_cus() * (S::GAINS == rn::Gains::lds && S::cols > 4096 ? 1 : std::max(1, 1024 / S::BLOCK));
+                const dim3 grid((unsigned)std::min(ceil_div(a.rows, S::rows), most));
+                if constexpr (S::GAINS != rn::Gains::lds)
+                    if (q) hipLaunchKernelGGL((rn::resnorm_fwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT, S::GAINS, true>), grid, dim3(S::BLOCK), 0, st, a);
+                if (!q) hipLaunchKernelGGL((rn::resnorm_fwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT, S::GAINS, false>), grid, dim3(S::BLOCK), 0, st, a);
             });
         });
     }
@@ -352,9 +373,9 @@ int32_t dqrm_residual_norm_bwd(int32_t dtype, int64_t rows, int64_t cols, const 
     a.partial = dparams ? static_cast<float *>(workspace) : nullptr;
     if (blocks > 0)
         with_type(dtype, [&](auto t) {
-            with_resnorm_bwd_shape(cols, [&](auto shape) {
+            with_resnorm_bwd_shape<decltype(t)::value>(cols, [&](auto shape) {
                 using S = decltype(shape);
-                hipLaunchKernelGGL((rn::resnorm_bwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, st,
+                hipLaunchKernelGGL((rn::resnorm_bwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT, S::GAINS>), dim3((unsigned)blocks), dim3(S::BLOCK), 0, st,
                                    a);
             });
         });

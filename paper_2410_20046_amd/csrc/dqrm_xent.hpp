@@ -114,7 +114,7 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_fwd_kernel(FwdAr
     const int64_t m0 = (int64_t)at.tm * S::BM, n0 = (int64_t)at.tn * S::BN;
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
     v16f acc[S::TM][S::TN];
-    multiply_tile<T, S, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), acc);
+    multiply_tile<T, S, false, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), at.tn, acc);
     logits<S>(a.c, acc, n0 + wn * S::TN * 32);
     const int64_t row0 = m0 + wm * S::TM * 32 + (lane & 31);
     int target[S::TM];
@@ -159,8 +159,8 @@ struct GradArgs {
     const uint64_t *live;  // rows that have a gradient, a bit each
     const float *most;     // the largest |grad|: d is held in units of it, times `by`
     float by;
-    char *d;               // [planes][rows][pitch]
-    int64_t plane, pitch;  // bytes
+    char *d;               // [planes] in blocks: rows and classes up to multiples of 64, what is past the last ones zeros
+    int64_t plane, rows, cols; // bytes; values
     int planes;
     float *sums; // [tiles of rows][classes of the piece]: d's column sums, or null
 };
@@ -192,7 +192,7 @@ __device__ __forceinline__ float sum_over_rows(const float (&v)[16])
 template <typename T, typename S>
 __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(GradArgs a)
 {
-    constexpr int out_bytes = S::waves * TileOut<T, S, false>::wave_bytes, sum_bytes = S::WM * S::BN * (int)sizeof(float);
+    constexpr int out_bytes = S::waves * TileOut<T, S, To::blocks>::wave_bytes, sum_bytes = S::WM * S::BN * (int)sizeof(float);
     static_assert(out_bytes <= S::lds_bytes && sum_bytes <= S::lds_bytes);
     __shared__ __align__(1024) char lds[S::lds_bytes];
     const Products &g = a.c.g;
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(Grad
     const int64_t m0 = (int64_t)at.tm * S::BM, n0 = (int64_t)at.tn * S::BN;
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN, half = lane >> 5;
     v16f acc[S::TM][S::TN];
-    multiply_tile<T, S, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), acc);
+    multiply_tile<T, S, false, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), at.tn, acc);
     logits<S>(a.c, acc, n0 + wn * S::TN * 32);
     const int64_t row0 = m0 + wm * S::TM * 32 + (lane & 31);
     const float most = *a.most;
@@ -259,10 +259,10 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(Grad
         }
         __syncthreads();
     }
-    const int64_t cols = a.pitch / (int64_t)sizeof(T); // (the padding is zeros)
     for (int plane = 0; plane < a.planes; ++plane) {
-        TileOut<T, S, false>::run(reinterpret_cast<T *>(a.d + plane * a.plane), cols, acc, lds + wave * TileOut<T, S, false>::wave_bytes, m0 + wm * S::TM * 32,
-                                  n0 + wn * S::TN * 32, g.m, cols, a.by);
+        using Out = TileOut<T, S, To::blocks>;
+        Out::run(reinterpret_cast<T *>(a.d + plane * a.plane), a.cols, acc, lds + wave * Out::wave_bytes, m0 + wm * S::TM * 32, n0 + wn * S::TN * 32, a.rows,
+                 a.cols, a.by);
         if (plane + 1 == a.planes) break;
 #pragma unroll
         for (int t = 0; t < S::TM; ++t)
@@ -285,7 +285,7 @@ struct OutArgs {
 template <typename T, typename TO, typename S, bool A_BY_K, bool ADD>
 __global__ __launch_bounds__(S::threads, S::per_simd) void xent_out_kernel(OutArgs a)
 {
-    using Out = TileOut<TO, S, ADD>;
+    using Out = TileOut<TO, S, ADD ? To::sums : To::rows>;
     static_assert(S::waves * Out::wave_bytes <= S::lds_bytes);
     __shared__ __align__(1024) char lds[S::lds_bytes];
     const Products &g = a.g;
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_out_kernel(OutAr
     const int wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
     const int all = (int)(g.stages * g.pairs), first = (int)(at.slice * g.stages_per_slice), last = min(all, first + (int)g.stages_per_slice);
     v16f acc[S::TM][S::TN];
-    multiply_tile<T, S, A_BY_K, true>(g, lds, m0, n0, first, last, acc);
+    multiply_tile<T, S, A_BY_K, true, true>(g, lds, m0, n0, first, last, at.tm + at.tn + at.slice, acc);
     const float by = a.by ? a.scale * *a.by : a.scale;
     Out::run(static_cast<TO *>(a.c) + (int64_t)at.slice * g.m * g.n, a.ldc, acc, lds + wave * Out::wave_bytes, m0 + wm * S::TM * 32, n0 + wn * S::TN * 32, g.m, g.n,
              by);

@@ -20,18 +20,33 @@ constexpr int64_t kSliceTiles = 512; // tiles times slices
 
 using TileBig = Tile<4, 4, 2, 2, 2>; // 256 by 256, one to a CU
 using TileMid = Tile<2, 2, 2, 2, 2>; // 128 by 128, two to a CU
-using TileFew = Tile<2, 2, 1, 4, 2>; // 64 by 256: few rows
+using TileFew = Tile<2, 2, 1, 4, 2, true>; // 64 by 256: few rows
+using TileThin = Tile<2, 2, 4, 1, 2>; // 256 by 64: few columns
 
-enum class Shape { big, mid, few };
+enum class Shape { big, mid, few, thin };
 
 int64_t up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 int planes_of(int32_t dtype) { return dtype == DQRM_F32 ? 3 : 1; }
-int pairs_of(int32_t dtype) { return dtype == DQRM_F32 ? 6 : 1; }
-int rows_of(Shape s) { return s == Shape::big ? 256 : s == Shape::mid ? 128 : 64; }
-int cols_of(Shape s) { return s == Shape::mid ? 128 : 256; }
+int pairs_of(int32_t dtype) { return dtype == DQRM_F32 ? (int)kPlanePairs : 1; }
+int rows_of(Shape s) { return s == Shape::mid ? 128 : s == Shape::few ? 64 : 256; }
+int cols_of(Shape s) { return s == Shape::mid ? 128 : s == Shape::thin ? 64 : 256; }
+int per_cu(Shape s) { return s == Shape::big ? 1 : 2; }
 
 template <typename F>
 void with_shape(Shape s, F f)
+{
+    if (s == Shape::big)
+        f(TileBig{});
+    else if (s == Shape::mid)
+        f(TileMid{});
+    else if (s == Shape::few)
+        f(TileFew{});
+    else
+        f(TileThin{});
+}
+// (the logits' products have no thin ones)
+template <typename F>
+void with_logits_shape(Shape s, F f)
 {
     if (s == Shape::big)
         f(TileBig{});
@@ -51,16 +66,23 @@ void with_operands(int32_t dtype, F f)
         f((__bf16)0.0f);
 }
 
-Shape logits_shape(int64_t m, int64_t n)
+// Sums of few stages: two smaller tiles to a CU, of which one's exponentials and stores go beside the other's products (8192 rows, 200003 classes,
+// width 64 in fp32: forward and backward 12.5 ms with tiles of 256, 11.3 so; from 16 stages on no difference).
+constexpr int64_t kShortSum = 8;
+
+Shape logits_shape(int64_t m, int64_t n, int64_t stages)
 {
     if (m <= 64) return Shape::few;
+    if (stages <= kShortSum) return Shape::mid;
     return ceil_div(m, 256) * ceil_div(n, 256) >= num_cus() ? Shape::big : Shape::mid;
 }
 
 // a gradient's product [m][n]
-Shape out_shape(int64_t m, int64_t n)
+Shape out_shape(int64_t m, int64_t n, int64_t stages)
 {
+    if (n <= 64) return Shape::thin;
     if (m <= 64) return Shape::few;
+    if (stages <= kShortSum) return Shape::mid; // (131072 classes, width 2048, 64 rows, bf16: forward and backward 563 us, with tiles of 256 580)
     return m > 128 && n > 128 ? Shape::big : Shape::mid;
 }
 
@@ -72,10 +94,11 @@ struct Sliced {
 // few tiles: the sum in slices, joined afterwards
 Sliced out_plan(int64_t m, int64_t n, int64_t stages)
 {
-    Sliced p{out_shape(m, n), 1, (unsigned)std::max<int64_t>(stages, 1)};
+    Sliced p{out_shape(m, n, stages), 1, (unsigned)std::max<int64_t>(stages, 1)};
     const int64_t tiles = ceil_div(m, rows_of(p.shape)) * ceil_div(n, cols_of(p.shape));
-    if (tiles < 1 || tiles * 2 > num_cus()) return p;
-    const int64_t slices = std::min<int64_t>({num_cus() / tiles, ceil_div(stages, 4), kMostSlices, kSliceTiles / tiles});
+    const int64_t room = (int64_t)num_cus() * per_cu(p.shape);
+    if (tiles < 1 || tiles * 2 > room) return p;
+    const int64_t slices = std::min<int64_t>({room / tiles, ceil_div(stages, 4), kMostSlices, kSliceTiles / tiles});
     if (slices < 2) return p;
     p.stages_per_slice = (unsigned)ceil_div(stages, slices);
     p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
@@ -97,7 +120,7 @@ int64_t most_classes(int64_t classes, int64_t width, int planes)
 int64_t piece_classes(int64_t rows, int64_t classes, int64_t width, int planes, bool with_d)
 {
     int64_t most = most_classes(classes, width, planes);
-    if (with_d) most = std::min(most, std::max<int64_t>(256, kPieceBytes / (std::max<int64_t>(rows, 1) * 2 * planes) / 256 * 256));
+    if (with_d) most = std::min(most, std::max<int64_t>(256, kPieceBytes / (std::max<int64_t>(up(rows, kBlock), 1) * 2 * planes) / 256 * 256));
     return up(ceil_div(classes, ceil_div(classes, most)), 256);
 }
 
@@ -120,13 +143,11 @@ struct FwdSpace {
     size_t total() const { return parts + at + x + w; }
 };
 
-FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype, bool room)
+FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
 {
     const int pl = planes_of(dtype);
-    const int64_t wide = ceil_div(v, 256) * m;
     FwdSpace s{};
-    // (tiles of 128 are fewer than 2^17 times rows, by the rule that chooses them)
-    s.parts = bytes((room ? std::max(wide, std::min<int64_t>(ceil_div(v, 128) * m, 1 << 17)) : logits_shape(m, v) == Shape::mid ? ceil_div(v, 128) * m : wide) * 8);
+    s.parts = bytes(ceil_div(v, 128) * m * 8); // (of the narrowest tiles)
     s.at = bytes(m * 4);
     s.x = bytes(m * up(k, kDepth) * 2 * pl);
     s.w = bytes(most_classes(v, k, pl) * up(k, kDepth) * 2 * pl);
@@ -143,7 +164,7 @@ BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     const int pl = planes_of(dtype), pairs = pairs_of(dtype);
     const int64_t most = most_classes(v, k, pl);
     // (a piece has at most `most` classes, and at most 256 or those whose d fits)
-    const int64_t d = std::max(m * 256, std::min(m * most, kPieceBytes / (2 * pl)));
+    const int64_t rows = up(m, kBlock), d = std::max(rows * 256, std::min(rows * most, kPieceBytes / (2 * pl)));
     BwdSpace s{};
     s.live = bytes(ceil_div(m, 64) * 8), s.classes = bytes(ceil_div(v, 64) * 8), s.most = 1024, s.unit = 256;
     s.x = bytes(m * up(k, kDepth) * 2 * pl), s.w = bytes(most * up(k, kDepth) * 2 * pl);
@@ -214,7 +235,6 @@ Products products(const Operand &a, const Operand &b, int64_t m, int64_t n, int6
 {
     Products g{};
     g.a = a, g.b = b, g.m = m, g.n = n, g.stages = (unsigned)ceil_div(k, kDepth), g.pairs = (unsigned)pairs;
-    g.by_stages = dqrm::FastDiv::make(std::max(g.stages, 1u));
     g.tiles_m = (unsigned)ceil_div(m, rows_of(shape)), g.tiles_n = (unsigned)ceil_div(n, cols_of(shape)), g.slices = 1;
     g.stages_per_slice = g.stages * g.pairs;
     return g;
@@ -234,20 +254,20 @@ Classifier classifier(const Call &c, const Products &g, int64_t first)
 void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStream_t st)
 {
     const int pairs = pairs_of(c.dtype);
-    const FwdSpace need = fwd_space(c.m, c.v, c.k, c.dtype, false);
+    const FwdSpace need = fwd_space(c.m, c.v, c.k, c.dtype);
     Space ws{static_cast<char *>(workspace)};
     FwdArgs a{};
     a.parts = static_cast<float2 *>(ws.take(need.parts)), a.at = static_cast<float *>(ws.take(need.at));
     void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
-    const Shape shape = logits_shape(c.m, c.v);
+    const Shape shape = logits_shape(c.m, c.v, ceil_div(c.k, kDepth) * pairs);
     const int64_t step = as_it_is(c.w, c.ldw, c.dtype, c.v, c.k) ? c.v : piece_classes(c.m, c.v, c.k, planes_of(c.dtype), false);
     for (int64_t first = 0; first < c.v; first += step) {
         const int64_t n = std::min(step, c.v - first);
         const Products g = products(x, classes_of(c, first, n, w_space, st), c.m, n, c.k, pairs, shape);
         a.c = classifier(c, g, first), a.first_tile = (unsigned)(first / cols_of(shape));
         with_operands(c.dtype, [&](auto zero) {
-            with_shape(shape, [&](auto tile) {
+            with_logits_shape(shape, [&](auto tile) {
                 using S = decltype(tile);
                 hipLaunchKernelGGL((xent_fwd_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
             });
@@ -314,21 +334,21 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
     for (int64_t first = 0; first < c.v; first += step) {
         const int64_t n = std::min(step, c.v - first);
         const Operand w = classes_of(c, first, n, w_space, st);
-        const Shape shape = logits_shape(c.m, n);
+        const Shape shape = logits_shape(c.m, n, ceil_div(c.k, kDepth) * pairs);
         GradArgs a{};
         const Products g = products(x, w, c.m, n, c.k, pairs, shape);
         a.c = classifier(c, g, first), a.lse = lse, a.grad = grad, a.live = live, a.most = unit, a.by = by;
-        a.pitch = up(n, kDepth) * 2, a.plane = c.m * a.pitch, a.planes = planes, a.d = d, a.sums = dbias ? sums : nullptr;
+        a.rows = up(c.m, kBlock), a.cols = up(n, kBlock), a.plane = a.rows * a.cols * 2, a.planes = planes, a.d = d, a.sums = dbias ? sums : nullptr;
         if (g.tiles_m > 0)
             with_operands(c.dtype, [&](auto zero) {
-                with_shape(shape, [&](auto tile) {
+                with_logits_shape(shape, [&](auto tile) {
                     using S = decltype(tile);
                     hipLaunchKernelGGL((xent_grad_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
                 });
             });
         if (dbias) hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, st, sums, n, (int)g.tiles_m, n, n, dbias + first, nullptr);
         if (c.k == 0) continue;
-        const Operand dm{d, a.plane, a.pitch, c.m, a.pitch / 2, nullptr};
+        const Operand dm{d, a.plane, a.cols * 2, a.rows, a.cols, nullptr};
         if (dx && c.m > 0) {
             Operand by = w;
             by.live = c.bias ? live_classes + first / 64 : nullptr;
@@ -360,7 +380,7 @@ extern "C" {
 
 size_t dqrm_softmax_xent_fwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype)
 {
-    return sizes_are_known(rows, classes, width, dtype) ? fwd_space(rows, classes, width, dtype, true).total() : 0;
+    return sizes_are_known(rows, classes, width, dtype) ? fwd_space(rows, classes, width, dtype).total() : 0;
 }
 
 int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
@@ -371,7 +391,7 @@ int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int6
     DQRM_CHECK(check_call(c));
     if (rows > 0 && (!loss || !lse || !aligned(loss, 4) || !aligned(lse, 4))) return DQRM_ERR_INVALID_ARG;
     if (rows == 0) return DQRM_OK;
-    DQRM_CHECK(check_workspace(workspace, workspace_bytes, fwd_space(rows, classes, width, dtype, false).total()));
+    DQRM_CHECK(check_workspace(workspace, workspace_bytes, fwd_space(rows, classes, width, dtype).total()));
     launch_fwd(c, loss, lse, workspace, static_cast<hipStream_t>(stream));
     DQRM_HIP_CHECK(hipGetLastError());
     return DQRM_OK;

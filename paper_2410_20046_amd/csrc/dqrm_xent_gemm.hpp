@@ -3,7 +3,7 @@
 // v_mfma_f32_32x32x16 takes 8 values of k from each lane: lane l holds row l % 32, values 8 (l / 32) .. + 7 of 16.  An operand lies in memory with
 // its k along the rows, whose 16-byte vectors are what a lane needs, or with k as the rows (a gradient's products sum over samples or
 // classes): then it is read from LDS by the transposing read, which gives a lane 4 values of a column.  fp32 operands are three bfloat16
-// planes, whose sum they are exactly; the six largest of the planes' nine products follow each other as more stages of one sum, the smallest first.
+// planes, whose sum they are exactly; the six largest of the planes' nine products are six stages of the sum, the smallest first.
 #pragma once
 
 #include "dqrm_mx_gemm.hpp"
@@ -31,7 +31,9 @@ __device__ __forceinline__ v16f mfma_32x32x16(uint4 a, uint4 b, v16f c)
 }
 
 // An operand in memory: [rows][cols] of 16-bit values, 16-byte aligned, cols and the pitch (in bytes) multiples of 8 values; three planes of it
-// for fp32, `plane` bytes apart.
+// for fp32, `plane` bytes apart.  Or in blocks of 64 by 64 values, 8 KB each, a row of blocks behind the other (cols and rows multiples of 64; the
+// pitch is a row's of blocks over 64): what a tile's stage takes of it then are whole blocks, whichever way it is read, where rows of a large
+// pitch give 128 or 512 bytes here and there.
 struct Operand {
     const char *p;
     int64_t plane, pitch, rows, cols;
@@ -42,13 +44,14 @@ struct Products {
     Operand a, b;
     int64_t m, n;                         // of the result
     unsigned stages;                      // of k, of one pair of planes
-    unsigned pairs;                       // of planes: 1 or 6
-    dqrm::FastDiv by_stages;
+    unsigned pairs;                       // of planes: 1 or kPlanePairs
     unsigned tiles_m, tiles_n, slices, stages_per_slice;
 };
 
 constexpr int kDepth = 64;              // values of k in a stage: 128 bytes of each row
+constexpr int kBlock = 64, kBlockBytes = kBlock * kBlock * 2;
 constexpr int kStageRow = kDepth * 2;
+constexpr unsigned kPlanePairs = 6;
 constexpr unsigned kNowhere = 0xFFFFFFF0u; // an offset past every buffer: reads as zeros
 
 // planes of A and B of a pair, two bits each, the smallest products first
@@ -61,8 +64,10 @@ __device__ __forceinline__ rsrc_t memory_at(const char *p, int64_t bytes)
 }
 
 // WM by WN waves, each with TM by TN accumulators of 32 by 32; LDS for `ring` stages.
-template <int TM_, int TN_, int WM_, int WN_, int RING_>
+// ROTATE: a tile begins its sum somewhere else than its neighbours (see multiply_tile).
+template <int TM_, int TN_, int WM_, int WN_, int RING_, bool ROTATE_ = false>
 struct Tile {
+    static constexpr bool rotate = ROTATE_;
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, ring = RING_, waves = WM * WN, threads = waves * kWaveSize, BM = TM * WM * 32, BN = TN * WN * 32;
     static constexpr int stage_bytes = (BM + BN) * kStageRow, lds_bytes = ring * stage_bytes;
     static constexpr int per_simd = TM * TN > 8 ? 1 : 2; // waves that the accumulators leave room for
@@ -108,8 +113,9 @@ __device__ __forceinline__ Place place_of(const Products &g)
 //                  different banks.
 //   BY_K:          [64 of k][W / 8 vectors], the groups of 4 vectors (32 values) of row r exchanged by r: the 4 rows that half a wave
 //                  reads together do.
-template <int W, int WAVES, bool BY_K>
+template <int W, int WAVES, bool BY_K, bool BLOCKS>
 struct Carrier {
+    static_assert(!BLOCKS || W % kBlock == 0);
     static constexpr int vectors = W / 8, groups = vectors / 4, turns = groups < 8 ? groups : 8;
     static constexpr int rows_per_load = BY_K ? 64 / vectors : 8; // that a wave's load of 1024 bytes covers
 
@@ -125,13 +131,19 @@ struct Carrier {
             row = (unsigned)lane >> 3;
             vector = ((unsigned)lane & 7u) ^ (((unsigned)lane >> 4) + 4u * ((unsigned)wave & 1u));
         }
-        at = row * (unsigned)o.pitch + vector * 16u;
+        if constexpr (BLOCKS)
+            at = (vector / 8u) * (BY_K ? kBlockBytes : 0) + row * (kBlock * 2) + vector % 8u * 16u;
+        else
+            at = row * (unsigned)o.pitch + vector * 16u;
     }
     // the wave's part of the stage at k0 (values), of the rows or columns from `first` on
     __device__ __forceinline__ static rsrc_t memory(const Operand &o, unsigned plane, int64_t first, int64_t k0)
     {
         const char *p = o.p + plane * o.plane;
-        if constexpr (BY_K)
+        if constexpr (BLOCKS) {
+            const int64_t from = BY_K ? k0 * o.pitch + first / kBlock * kBlockBytes : first * o.pitch + k0 / kBlock * kBlockBytes;
+            return memory_at(p + from, o.rows * o.pitch - from);
+        } else if constexpr (BY_K)
             return memory_at(p + k0 * o.pitch + first * 2, (o.rows - k0 - 1) * o.pitch + (o.cols - first) * 2);
         else
             return memory_at(p + first * o.pitch, (o.rows - first - 1) * o.pitch + o.cols * 2);
@@ -140,7 +152,11 @@ struct Carrier {
     __device__ __forceinline__ unsigned offset(const Operand &o, unsigned j, unsigned k0, uint64_t live) const
     {
         const unsigned r = j * rows_per_load;
-        if constexpr (BY_K)
+        if constexpr (BLOCKS && BY_K)
+            return at + r * (kBlock * 2);
+        else if constexpr (BLOCKS) // (a load's 8 rows are of one block)
+            return at + r / kBlock * (kBlock * (unsigned)o.pitch) + r % kBlock * (kBlock * 2);
+        else if constexpr (BY_K)
             return (live >> (r + row)) & 1 ? at + r * (unsigned)o.pitch : kNowhere;
         else
             return k0 * 2 + vector * 16 < (unsigned)o.cols * 2 ? at + k0 * 2 + r * (unsigned)o.pitch : kNowhere;
@@ -168,11 +184,13 @@ struct Carrier {
 
 // The sums of stages [first, last) for the tile at (m0, n0): accumulator [t][j] of a lane has row lane % 32 of block t, and columns
 // 8 (i / 4) + 4 (lane / 32) + i % 4 of block j.  Ends with a barrier: LDS is free.
-template <typename T, typename S, bool A_BY_K, bool B_BY_K>
-__device__ __forceinline__ void multiply_tile(const Products &g, char *lds, int64_t m0, int64_t n0, int first, int last, v16f (&acc)[S::TM][S::TN])
+// S::rotate: the stages are taken in turn from one on that depends on the tile.  Rows whose pitch is a power of two lie in the same few of the
+// memory's channels at any one k; tiles that stream different rows at the same pace would all be there at once.
+template <typename T, typename S, bool A_BY_K, bool B_BY_K, bool A_BLOCKS>
+__device__ __forceinline__ void multiply_tile(const Products &g, char *lds, int64_t m0, int64_t n0, int first, int last, unsigned turn, v16f (&acc)[S::TM][S::TN])
 {
-    using CA = Carrier<S::BM, S::waves, A_BY_K>;
-    using CB = Carrier<S::BN, S::waves, B_BY_K>;
+    using CA = Carrier<S::BM, S::waves, A_BY_K, A_BLOCKS>;
+    using CB = Carrier<S::BN, S::waves, B_BY_K, false>;
     const int lane = threadIdx.x & 63;
     const int wave = (int)uniform(threadIdx.x >> 6);
     const unsigned lds0 = uniform(lds_address(lds));
@@ -182,15 +200,20 @@ __device__ __forceinline__ void multiply_tile(const Products &g, char *lds, int6
     rsrc_t ra, rb;
     unsigned k0 = 0, into = 0;
     uint64_t live_a = ~0ull, live_b = ~0ull;
-    auto aim = [&](int s) {
-        const unsigned pair = g.pairs == 1 ? 0u : uniform(g.by_stages.div((unsigned)s)), stage = uniform((unsigned)s - pair * g.stages);
+    const int shift = S::rotate && last > first ? (int)uniform(turn * 5u % (unsigned)(last - first)) : 0;
+    auto aim = [&](int at) {
+        const bool there = at < last;
+        int s = at + shift;
+        if (S::rotate && s >= last) s -= last - first;
+        // (the planes' products of the same values of k follow each other: a plane that is needed again is still in a cache)
+        const unsigned stage = g.pairs == 1 ? (unsigned)s : uniform((unsigned)s / kPlanePairs), pair = g.pairs == 1 ? 0u : (unsigned)s - stage * kPlanePairs;
         k0 = stage * kDepth;
         ra = CA::memory(g.a, plane_a(g.pairs, pair), m0, k0), rb = CB::memory(g.b, plane_b(g.pairs, pair), n0, k0);
         // (what is past `last` is requested from a buffer without bytes, so that every stage is as many loads)
-        if (s >= last) ra.z = 0u, rb.z = 0u;
-        if (A_BY_K && g.a.live && s < last) live_a = g.a.live[stage];
-        if (B_BY_K && g.b.live && s < last) live_b = g.b.live[stage];
-        into = lds0 + (unsigned)((s - first) & (S::ring - 1)) * S::stage_bytes;
+        if (!there) ra.z = 0u, rb.z = 0u;
+        if (A_BY_K && g.a.live && there) live_a = g.a.live[stage];
+        if (B_BY_K && g.b.live && there) live_b = g.b.live[stage];
+        into = lds0 + (unsigned)((at - first) & (S::ring - 1)) * S::stage_bytes;
     };
     auto request = [&](int q) {
         const bool of_a = q < S::a_loads;
@@ -263,9 +286,15 @@ __device__ __forceinline__ void multiply_tile(const Products &g, char *lds, int6
     lds_barrier(); // the last stage is read
 }
 
-// A wave's accumulators through LDS to memory, 16 bytes of a row beside its neighbours'.  ADD (float): to what is there.
-template <typename T, typename S, bool ADD>
+// A wave's accumulators through LDS to memory, 16 bytes of a row beside its neighbours'.
+enum class To {
+    rows,   // of the result
+    sums,   // the same (float), added to what is there
+    blocks, // 16-bit values in blocks of 64 by 64: ldc is a row's of blocks over 64, n a multiple of 64, m of 64
+};
+template <typename T, typename S, To TO>
 struct TileOut {
+    static constexpr bool ADD = TO == To::sums;
     static constexpr int per = 16 / sizeof(T);
     static constexpr int cols = S::TN * 32, pitch = cols * sizeof(T) + 16;
     static constexpr int vectors = cols / per, rows_each = kWaveSize / vectors; // of a row; rows that a wave stores at a time
@@ -284,6 +313,16 @@ struct TileOut {
         const char *read = lds + r * pitch + v * 16;
         const int64_t row = m0 + r, col = n0 + v * per;
         T *to = c + row * ldc + col;
+        // (blocks: a wave's blocks of 32 rows begin at the first or the 33rd row of one, and a row's vectors lie in 1 or 2 of them)
+        if constexpr (TO == To::blocks) to = c + row / kBlock * kBlock * ldc + col / kBlock * (kBlock * kBlock) + row % kBlock * kBlock + col % kBlock;
+        auto row_at = [&](int i) -> T * { // i rows on, i a multiple of rows_each
+            if constexpr (TO == To::blocks) {
+                const int64_t at = row + i;
+                return to + (at / kBlock - row / kBlock) * kBlock * ldc + (at % kBlock - row % kBlock) * kBlock;
+            } else {
+                return to + (int64_t)i * ldc;
+            }
+        };
         const bool inside = m0 + S::TM * 32 <= m && n0 + cols <= n; // of the whole wave
         struct alignas(16) Many { T v[per]; };
 #pragma unroll
@@ -304,7 +343,7 @@ struct TileOut {
 #pragma unroll 4
                 for (int i = 0; i < together * 32 / rows_each; ++i) {
                     Many x = *reinterpret_cast<const Many *>(read + i * rows_each * pitch);
-                    T *at = to + (int64_t)(first * 32 + i * rows_each) * ldc;
+                    T *at = row_at(first * 32 + i * rows_each);
                     if constexpr (ADD) {
                         Many old;
                         __builtin_memcpy(&old, at, 16);
@@ -317,7 +356,7 @@ struct TileOut {
                 for (int i = 0; i < together * 32 / rows_each; ++i) {
                     const Many x = *reinterpret_cast<const Many *>(read + i * rows_each * pitch);
                     if (row + first * 32 + i * rows_each >= m) break;
-                    T *at = to + (int64_t)(first * 32 + i * rows_each) * ldc;
+                    T *at = row_at(first * 32 + i * rows_each);
                     for (int e = 0; e < per; ++e)
                         if (col + e < n) at[e] = ADD ? (T)(at[e] + x.v[e]) : x.v[e];
                 }

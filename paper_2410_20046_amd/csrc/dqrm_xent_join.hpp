@@ -12,30 +12,35 @@ __device__ __forceinline__ float2 xent_join_parts(float2 a, float2 b)
     return make_float2(most, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
 }
 
-// 16 rows to a workgroup, 16 lanes to a row with every 16th tile each, eight loads at a time on their way; then their results in turn.  A
-// sum is at least 1 (its largest power) and at most the classes, so log2 of it is exact to the last bits.
+// ROWS rows to a workgroup (16; 1 where there are few rows: 782 tiles of 16 rows 9.5 and 3.3 us), 256 / ROWS lanes to a row with the tiles in
+// turn, eight loads at a time on their way; then their results in pairs.  A sum is at least 1 (its largest power) and at most the classes.
+template <int ROWS>
 __global__ __launch_bounds__(256) void xent_join_kernel(const float2 *parts, int64_t tiles, int64_t rows, const float *at, const int64_t *targets,
                                                         int64_t classes, float *loss, float *lse)
 {
-    __shared__ float2 s[16][17];
-    const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
-    const int slice = threadIdx.x >> 4;
+    constexpr int slices = 256 / ROWS;
+    __shared__ float2 s[slices][ROWS == 1 ? 1 : ROWS + 1];
+    const int in = threadIdx.x % ROWS, slice = threadIdx.x / ROWS;
+    const int64_t r = (int64_t)blockIdx.x * ROWS + in;
     float2 v = make_float2(-__builtin_inff(), 0.0f);
     if (r < rows) {
         constexpr int ahead = 8;
-        for (int64_t k = slice; k < tiles; k += 16 * ahead) {
+        for (int64_t k = slice; k < tiles; k += slices * ahead) {
             float2 x[ahead];
 #pragma unroll
-            for (int i = 0; i < ahead; ++i) x[i] = parts[min(k + 16 * i, tiles - 1) * rows + r];
+            for (int i = 0; i < ahead; ++i) x[i] = parts[min(k + slices * i, tiles - 1) * rows + r];
 #pragma unroll
             for (int i = 0; i < ahead; ++i)
-                if (k + 16 * i < tiles) v = xent_join_parts(v, x[i]);
+                if (k + slices * i < tiles) v = xent_join_parts(v, x[i]);
         }
     }
-    s[slice][threadIdx.x & 15] = v;
-    __syncthreads();
+    s[slice][in] = v;
+#pragma unroll
+    for (int h = slices / 2; h >= 1; h /= 2) {
+        __syncthreads();
+        if (slice < h) s[slice][in] = v = xent_join_parts(v, s[slice + h][in]);
+    }
     if (slice != 0 || r >= rows) return;
-    for (int i = 1; i < 16; ++i) v = xent_join_parts(v, s[i][threadIdx.x]);
     constexpr float kLn2 = 0.693147180559945309f;
     const float lse2 = v.x == -__builtin_inff() && v.y == 0.0f ? v.x : v.x + log2f(v.y); // (no classes left; a NaN stays)
     lse[r] = lse2 * kLn2;
