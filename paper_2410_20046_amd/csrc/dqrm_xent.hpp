@@ -153,6 +153,110 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_fwd_kernel(FwdAr
     }
 }
 
+// ---- a few rows -----------------------------------------------------------------------------------------------------------
+// A few requests: w is read once, as it is (fp32 without planes, rows at any alignment), and multiplied with the rows of x, which are in LDS, in
+// 32-bit fused products.  `lanes` of a wave take a class, 8 values each at a time, and then add up; a group of lanes keeps the maximum and
+// sum of its classes.
+struct FewArgs {
+    const void *x, *w;
+    int64_t ldx, ldw, rows, classes, width;
+    const float *bias;
+    float scale2;
+    const int64_t *targets;
+    int64_t per_block; // classes
+    int lanes, padded; // of a class; width up to a multiple of 8 lanes
+    float2 *parts;     // [workgroups][part_rows], from the first of these rows on
+    float *at;
+    int64_t part_rows;
+};
+
+// Bound by w's bytes, with more rows by the products and their sums over lanes: 200003 classes of width 1024 in fp32 (819 MB) one row 152 us, 5.4 TB/s,
+// 4 rows 161, 8 rows 202 (tiles of fp32 planes: 730); 1000 classes of width 16, with the join, 7.3 from a graph (15.2).  Of aligned 16-bit
+// values the tiles are faster (width 1024 in bfloat16: 82 and 116 us).
+template <int DT, int M>
+__global__ __launch_bounds__(256) void xent_rows_fwd_kernel(FewArgs a)
+{
+    using T = elem_t<DT>;
+    constexpr int together = M <= 2 ? 4 : 2; // classes of a group, whose loads are on their way together
+    extern __shared__ __align__(16) float s_x[]; // [M][padded]
+    __shared__ float2 s_part[4][M];
+    const int width = (int)a.width;
+    for (int i = threadIdx.x; i < M * a.padded; i += 256) {
+        const int r = i / a.padded, c = i - r * a.padded;
+        s_x[i] = r < a.rows && c < width ? (float)static_cast<const T *>(a.x)[r * a.ldx + c] : 0.0f;
+    }
+    __syncthreads();
+    const int groups = 256 / a.lanes, group = threadIdx.x / a.lanes, lane = threadIdx.x - group * a.lanes;
+    const int64_t first = (int64_t)blockIdx.x * a.per_block, last = min(first + a.per_block, a.classes);
+    int64_t target[M];
+    float most[M], sum[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) target[m] = m < a.rows ? a.targets[m] : -1, most[m] = -__builtin_inff(), sum[m] = 0.0f;
+    for (int64_t j = first; j < last; j += groups * together) {
+        float acc[together][M] = {};
+        const T *row[together];
+        int64_t cls[together];
+#pragma unroll
+        for (int k = 0; k < together; ++k) {
+            cls[k] = j + k * groups + group;
+            row[k] = static_cast<const T *>(a.w) + min(cls[k], a.classes - 1) * a.ldw;
+        }
+        for (int c = lane * kChunk; c < width; c += a.lanes * kChunk) {
+            Vec8<T> w[together];
+#pragma unroll
+            for (int k = 0; k < together; ++k) w[k] = load_vec(row[k], c, width, false);
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                float x[kChunk];
+                __builtin_memcpy(x, __builtin_assume_aligned(&s_x[m * a.padded + c], 16), sizeof(x));
+#pragma unroll
+                for (int k = 0; k < together; ++k)
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i) acc[k][m] = __builtin_fmaf((float)w[k].v[i], x[i], acc[k][m]);
+            }
+        }
+        for (int d = 1; d < a.lanes; d *= 2) {
+#pragma unroll
+            for (int k = 0; k < together; ++k)
+#pragma unroll
+                for (int m = 0; m < M; ++m) acc[k][m] += __shfl_xor(acc[k][m], d, kWaveSize);
+        }
+#pragma unroll
+        for (int k = 0; k < together; ++k) {
+            const float b = cls[k] >= last ? -__builtin_inff() : a.bias ? a.bias[cls[k]] * kLog2e : 0.0f;
+#pragma unroll
+            for (int m = 0; m < M; ++m) acc[k][m] = b == -__builtin_inff() ? b : __builtin_fmaf(acc[k][m], a.scale2, b);
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            float top = most[m];
+#pragma unroll
+            for (int k = 0; k < together; ++k) {
+                top = fmaxf(top, acc[k][m]);
+                if (cls[k] == target[m] && cls[k] < last && lane == 0) a.at[m] = acc[k][m];
+            }
+            const float base = top == -__builtin_inff() ? 0.0f : top;
+            sum[m] *= power2(most[m] - base);
+#pragma unroll
+            for (int k = 0; k < together; ++k) sum[m] += power2(acc[k][m] - base);
+            most[m] = top;
+        }
+    }
+    // the wave's groups, then the waves
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        float2 p = make_float2(most[m], sum[m]);
+        for (int d = a.lanes; d < kWaveSize; d *= 2) p = join_parts(p, make_float2(__shfl_xor(p.x, d, kWaveSize), __shfl_xor(p.y, d, kWaveSize)));
+        if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6][m] = p;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < a.rows) {
+        float2 p = s_part[0][threadIdx.x];
+        for (int w = 1; w < 4; ++w) p = join_parts(p, s_part[w][threadIdx.x]);
+        a.parts[blockIdx.x * a.part_rows + threadIdx.x] = p;
+    }
+}
+
 struct GradArgs {
     Classifier c;
     const float *lse, *grad;

@@ -15,6 +15,7 @@ constexpr int64_t kMostClasses = 1 << 22; // of a piece, for the same reason
 // chip's last-level cache, which d is read from twice.
 constexpr int64_t kPieceBytes = 256LL << 20;
 constexpr int kMostSlices = 64;
+constexpr int64_t kFewBlocks = 1024;  // workgroups that share the classes where there are a few rows
 constexpr int64_t kRowsAlone = 16384; // rows that one workgroup looks through for the gradients' unit
 constexpr int64_t kSliceTiles = 512; // tiles times slices
 
@@ -147,7 +148,7 @@ FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
 {
     const int pl = planes_of(dtype);
     FwdSpace s{};
-    s.parts = bytes(ceil_div(v, 128) * m * 8); // (of the narrowest tiles)
+    s.parts = bytes(std::max(ceil_div(v, 128), std::min(v, kFewBlocks)) * m * 8); // (of the narrowest tiles, and of few rows' workgroups)
     s.at = bytes(m * 4);
     s.x = bytes(m * up(k, kDepth) * 2 * pl);
     s.w = bytes(most_classes(v, k, pl) * up(k, kDepth) * 2 * pl);
@@ -251,6 +252,59 @@ Classifier classifier(const Call &c, const Products &g, int64_t first)
     return Classifier{g, c.bias ? c.bias + first : nullptr, c.scale * kLog2e, c.targets, first, c.v};
 }
 
+// A few rows of fp32, and of what the matrix instructions' tiles can't read where it is, by the kernel that reads w as it is: up to 8 rows at a
+// time, as many as fit its LDS.  (Laying w out anew costs as much as reading it 3 times in 16 bits and 5 times in fp32.)
+constexpr int64_t kFewLds = 64 << 10;
+
+int few_lanes(int64_t k)
+{
+    int lanes = 1;
+    while (lanes < kWaveSize && lanes * kChunk < k) lanes *= 2;
+    return lanes;
+}
+
+int64_t few_padded(int64_t k) { return up(std::max<int64_t>(k, 1), few_lanes(k) * kChunk); }
+
+int few_at_a_time(int64_t m, int64_t k)
+{
+    int rows = 1;
+    while (rows < 8 && rows < m && rows * 2 * few_padded(k) * 4 <= kFewLds) rows *= 2;
+    return rows;
+}
+
+bool is_few(const Call &c)
+{
+    if (c.m > (c.dtype == DQRM_F32 ? 16 : 8) || few_padded(c.k) * 4 > kFewLds) return false;
+    return !as_it_is(c.w, c.ldw, c.dtype, c.v, c.k);
+}
+
+void launch_few(const Call &c, float2 *parts, float *at, float *loss, float *lse, hipStream_t st)
+{
+    const int lanes = few_lanes(c.k), m = few_at_a_time(c.m, c.k), at_once = 256 / lanes * (m <= 2 ? 4 : 2);
+    // (four workgroups to a CU, and no fewer classes than a group takes at a time)
+    const int64_t per_block = up(ceil_div(c.v, std::min<int64_t>(ceil_div(c.v, at_once), kFewBlocks)), at_once), blocks = ceil_div(c.v, per_block);
+    for (int64_t r = 0; r < c.m; r += m) {
+        const FewArgs a{static_cast<const char *>(c.x) + r * c.ldx * (int64_t)size_of(c.dtype), c.w, c.ldx, c.ldw, std::min<int64_t>(m, c.m - r), c.v, c.k, c.bias,
+                        c.scale * kLog2e, c.targets + r, per_block, lanes, (int)few_padded(c.k), parts + r, at + r, c.m};
+        with_type(c.dtype, [&](auto t) {
+            constexpr int DT = decltype(t)::value;
+            const auto go = [&](auto rows) {
+                constexpr int M = decltype(rows)::value;
+                hipLaunchKernelGGL((xent_rows_fwd_kernel<DT, M>), dim3((unsigned)blocks), dim3(256), (size_t)M * a.padded * sizeof(float), st, a);
+            };
+            if (m == 1)
+                go(std::integral_constant<int, 1>{});
+            else if (m == 2)
+                go(std::integral_constant<int, 2>{});
+            else if (m == 4)
+                go(std::integral_constant<int, 4>{});
+            else
+                go(std::integral_constant<int, 8>{});
+        });
+    }
+    launch_xent_join(parts, blocks, c.m, at, c.targets, c.v, loss, lse, st);
+}
+
 void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStream_t st)
 {
     const int pairs = pairs_of(c.dtype);
@@ -259,6 +313,7 @@ void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStre
     FwdArgs a{};
     a.parts = static_cast<float2 *>(ws.take(need.parts)), a.at = static_cast<float *>(ws.take(need.at));
     void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
+    if (is_few(c)) return launch_few(c, a.parts, a.at, loss, lse, st);
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
     const Shape shape = logits_shape(c.m, c.v, ceil_div(c.k, kDepth) * pairs);
     const int64_t step = as_it_is(c.w, c.ldw, c.dtype, c.v, c.k) ? c.v : piece_classes(c.m, c.v, c.k, planes_of(c.dtype), false);

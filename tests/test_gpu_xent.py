@@ -67,6 +67,21 @@ def test_loss_and_gradients(m, v, k, dtype):
     check(x, w, targets, bias, 0.75, grad)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 5, 8, 9, 16])
+def test_a_few_rows(m, dtype):
+    """Each number of rows of the kernel for a few of them, several times that many, one lane to a class and a whole wave, and more classes than
+    its workgroups take at once."""
+    for v, k in ((5, 8), (3000, 3), (3001, 61), (9, 515), (70001, 17), (40, 9001)):
+        x, w, targets, bias, grad = make(m, v, k, TYPES[dtype], seed=m + v)
+        bias[v // 2] = -math.inf
+        targets[0] = -1
+        loss, lse = forward(x, w, targets, bias, 1.25)
+        r = loss_and_bounds(x, w, targets, bias, 1.25)
+        near(lse, r["lse"], r["lse_off"], "lse")
+        near(loss, r["loss"], r["loss_off"], "loss")
+
+
 @pytest.mark.parametrize("dtype, m, v, k", [("bf16", 4001, 40000, 32), ("f16", 4001, 40000, 32), ("f32", 1501, 40000, 24), ("bf16", 30, 70000, 4104)])
 def test_classes_in_several_pieces(dtype, m, v, k):
     """d, or the rows of w that have to be laid out anew, take more than a piece's room."""
