@@ -37,8 +37,12 @@ void dqrm_host::launch_xent_join(const void *parts, int64_t tiles, int64_t rows,
                                  float *lse, hipStream_t st)
 {
     const auto go = [&](auto kernel, int64_t rows_each) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + rows_each - 1) / rows_each)), dim3(256), 0, st, static_cast<const float2 *>(parts), tiles, rows, at,
-                           targets, classes, loss, lse);
+        const int64_t step = rows_each << 23; // (a launch has fewer than 2^32 threads)
+        for (int64_t first = 0; first < rows; first += step) {
+            const int64_t some = rows - first < step ? rows - first : step;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((some + rows_each - 1) / rows_each)), dim3(256), 0, st, static_cast<const float2 *>(parts) + first, tiles, rows,
+                               some, at + first, targets + first, classes, loss + first, lse + first);
+        }
     };
     if (rows <= 1024)
         go(dqrm::xent_join_kernel<1>, 1);

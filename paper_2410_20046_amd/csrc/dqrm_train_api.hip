@@ -193,18 +193,20 @@ void with_first_that_holds(int64_t cols, F f)
 // Many rows without codes: several chunks to a thread, and the columns' vectors in LDS, where that is faster (bf16: 16384 x 8192 283 us instead of
 // 300 with 1024 threads to a row, 32768 x 4096 235 and 248, 65536 x 1024 104 and 112; fp32: 8192 x 8192 224 and 248, 16384 x 2048 100 and 111,
 // 32768 x 1024 105 and 113; fp32 16384 x 4096 in LDS 210, in registers 203).  Else a chunk to a thread: a row's latency counts.
-template <int DT, typename F>
-void with_resnorm_fwd_shape(int64_t rows, int64_t cols, bool codes, F f)
+template <int DT, bool CODES, typename F>
+void with_resnorm_fwd_shape(int64_t rows, int64_t cols, F f)
 {
     using rn::Gains;
     if (cols < kChunk) return f(RowShape<16, 1, 256, Gains::registers, true>{});
-    if (rows >= (int64_t)num_cus() * 16 && !codes) {
-        if constexpr (DT == DQRM_F32)
-            return with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<64, 2, 256>, RowShape<128, 2, 512, Gains::lds>,
-                                         RowShape<512, 1, 512>, RowShape<512, 2, 1024, Gains::lds>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
-        else
-            return with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<64, 2, 256>, RowShape<256, 1, 256>,
-                                         RowShape<128, 4, 256, Gains::lds>, RowShape<512, 2, 1024, Gains::lds>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
+    if constexpr (!CODES) {
+        if (rows >= (int64_t)num_cus() * 16) {
+            if constexpr (DT == DQRM_F32)
+                return with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<64, 2, 256>, RowShape<128, 2, 512, Gains::lds>,
+                                             RowShape<512, 1, 512>, RowShape<512, 2, 1024, Gains::lds>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
+            else
+                return with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<64, 2, 256>, RowShape<256, 1, 256>,
+                                             RowShape<128, 4, 256, Gains::lds>, RowShape<512, 2, 1024, Gains::lds>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
+        }
     }
     with_first_that_holds<RowShape<16, 1, 256>, RowShape<64, 1, 256>, RowShape<128, 1, 256>, RowShape<256, 1, 256>, RowShape<512, 1, 512>,
                           RowShape<1024, 1, 1024>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
@@ -217,10 +219,9 @@ void with_resnorm_bwd_shape(int64_t cols, F f)
 {
     using rn::Gains;
     if (cols < kChunk) return f(RowShape<16, 1, 512, Gains::registers, true>{});
-    if constexpr (DT == DQRM_F32)
-        if (cols > 4096 && cols <= 8192) return f(RowShape<1024, 1, 1024, Gains::lds>{});
-    with_first_that_holds<RowShape<16, 1, 512>, RowShape<64, 1, 512>, RowShape<128, 1, 512>, RowShape<256, 1, 512>, RowShape<512, 1, 512>,
-                          RowShape<512, 2, 512>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
+    using Wide = std::conditional_t<DT == DQRM_F32, RowShape<1024, 1, 1024, Gains::lds>, RowShape<512, 2, 512>>;
+    with_first_that_holds<RowShape<16, 1, 512>, RowShape<64, 1, 512>, RowShape<128, 1, 512>, RowShape<256, 1, 512>, RowShape<512, 1, 512>, Wide,
+                          RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
 }
 
 int resnorm_bwd_blocks(int64_t rows, int64_t cols)
@@ -313,6 +314,7 @@ int32_t dqrm_residual_norm_fwd(int32_t dtype, int64_t rows, int64_t cols, const 
     if (y) DQRM_CHECK(check_matrix(y, ldy, dtype, rows, cols));
     if (q) DQRM_CHECK(check_mx(q, rows, cols));
     if (stats && !aligned(stats, 4)) return DQRM_ERR_INVALID_ARG;
+    if (rows == 0) return DQRM_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const size_t es = size_of(dtype);
     for (int64_t r0 = 0; r0 < rows; r0 += kMaxBlocks) {
@@ -324,15 +326,20 @@ int32_t dqrm_residual_norm_fwd(int32_t dtype, int64_t rows, int64_t cols, const 
         if (stats) a.stats = stats + r0;
         if (q) a.codes = q->codes + r0 * dqrm_mx::codes_pitch(cols), a.scales = q->scales + r0 * dqrm_mx::scales_pitch(cols);
         with_type(dtype, [&](auto t) {
-            with_resnorm_fwd_shape<decltype(t)::value>(rows, cols, q != nullptr, [&](auto shape) {
-                using S = decltype(shape);
-                // as many workgroups as the chip holds: each keeps the columns' vectors for all of its rows
-                const int64_t most = (int64_t)num_cus() * (S::GAINS == rn::Gains::lds && S::cols > 4096 ? 1 : std::max(1, 1024 / S::BLOCK));
-                const dim3 grid((unsigned)std::min(ceil_div(a.rows, S::rows), most));
-                if constexpr (S::GAINS != rn::Gains::lds)
-                    if (q) hipLaunchKernelGGL((rn::resnorm_fwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT, S::GAINS, true>), grid, dim3(S::BLOCK), 0, st, a);
-                if (!q) hipLaunchKernelGGL((rn::resnorm_fwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT, S::GAINS, false>), grid, dim3(S::BLOCK), 0, st, a);
-            });
+            const auto go = [&](auto codes) {
+                constexpr bool CODES = decltype(codes)::value;
+                with_resnorm_fwd_shape<decltype(t)::value, CODES>(rows, cols, [&](auto shape) {
+                    using S = decltype(shape);
+                    // as many workgroups as the chip holds: each keeps the columns' vectors for all of its rows
+                    const int64_t most = (int64_t)num_cus() * std::max(1, 1024 / S::BLOCK);
+                    hipLaunchKernelGGL((rn::resnorm_fwd_kernel<decltype(t)::value, S::TPR, S::CH, S::BLOCK, S::SHORT, S::GAINS, CODES>),
+                                       dim3((unsigned)std::min(ceil_div(a.rows, S::rows), most)), dim3(S::BLOCK), 0, st, a);
+                });
+            };
+            if (q)
+                go(std::true_type{});
+            else
+                go(std::false_type{});
         });
     }
     DQRM_HIP_CHECK(hipGetLastError());

@@ -15,8 +15,8 @@ __device__ __forceinline__ float2 xent_join_parts(float2 a, float2 b)
 // ROWS rows to a workgroup (16; 1 where there are few rows: 782 tiles of 16 rows 9.5 and 3.3 us), 256 / ROWS lanes to a row with the tiles in
 // turn, eight loads at a time on their way; then their results in pairs.  A sum is at least 1 (its largest power) and at most the classes.
 template <int ROWS>
-__global__ __launch_bounds__(256) void xent_join_kernel(const float2 *parts, int64_t tiles, int64_t rows, const float *at, const int64_t *targets,
-                                                        int64_t classes, float *loss, float *lse)
+__global__ __launch_bounds__(256) void xent_join_kernel(const float2 *parts, int64_t tiles, int64_t stride, int64_t rows, const float *at,
+                                                        const int64_t *targets, int64_t classes, float *loss, float *lse)
 {
     constexpr int slices = 256 / ROWS;
     __shared__ float2 s[slices][ROWS == 1 ? 1 : ROWS + 1];
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2 *parts, int
         for (int64_t k = slice; k < tiles; k += slices * ahead) {
             float2 x[ahead];
 #pragma unroll
-            for (int i = 0; i < ahead; ++i) x[i] = parts[min(k + slices * i, tiles - 1) * rows + r];
+            for (int i = 0; i < ahead; ++i) x[i] = parts[min(k + slices * i, tiles - 1) * stride + r];
 #pragma unroll
             for (int i = 0; i < ahead; ++i)
                 if (k + slices * i < tiles) v = xent_join_parts(v, x[i]);

@@ -15,6 +15,7 @@ EPS = 1e-5
 # every way a row is laid over threads, both sides of each limit, and more rows than workgroups
 SHAPES = [(1, 1), (5, 2), (130, 7), (3, 8), (37, 9), (600, 128), (16, 129), (33, 512), (9, 513), (6, 1024), (7, 1025), (700, 2048), (5, 2049), (300, 4096), (3, 4097),
           (530, 8191), (2, 8192), (3, 8193), (280, 16384)]
+MANY = [(4100, 100), (4097, 500), (4100, 1024), (4096, 2000), (4099, 4096), (4100, 8001), (4096, 9000)]
 BOTH = [("none", "layer"), ("none", "rms"), ("layer", "none"), ("rms", "none"), ("layer", "layer"), ("rms", "rms"), ("layer", "rms"), ("rms", "layer"), ("none", "none")]
 
 
@@ -88,9 +89,13 @@ def both_ways(R, C, dtype, post, pre, vectors, seed=0, gap=0, shift=0):
             same = dq.MxMatrix(R, C, "cuda")
             dq.dqrm_mxfp4_quant(y, same)
             assert torch.equal(q.codes, same.codes) and torch.equal(q.scales, same.scales)
+        # without codes: many rows may lie over threads in another way then, and add up in another order
+        out2, y2, stats2 = matrix(none, gap + 1, shift), matrix(none, gap, shift), torch.full((4, R), math.nan, device="cuda")
+        dq.dqrm_residual_norm_fwd(block, u, r, out2, y=y2, stats=stats2)
+        check_forward(block, p, u, r, out2, y2, stats2)
         again = torch.empty_like(out)
         dq.dqrm_residual_norm_fwd(block, u, r, again)
-        assert torch.equal(again, out)
+        assert torch.equal(again, out2)
     kept = torch.where(torch.isnan(stats), torch.tensor([0.0, 1.0, 0.0, 1.0], device="cuda")[:, None], stats)
     dparams = torch.full((5, C), math.nan, device="cuda")
     dq.dqrm_residual_norm_bwd(block, dout, dy, u, out, stats, du, dr, dparams, space(R, C))
@@ -110,6 +115,14 @@ def test_shapes(shape, dtype):
     kinds = BOTH[(shape[0] + shape[1]) % 8]
     both_ways(*shape, dtype, "layer", "layer", True, seed=sum(shape))
     both_ways(*shape, dtype, *kinds, False, seed=sum(shape), gap=3, shift=1)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", MANY)
+def test_many_rows(shape, dtype):
+    """Rows over threads as many of them are; the columns' vectors in registers, in LDS and in memory."""
+    both_ways(*shape, dtype, "layer", "rms", True, seed=sum(shape), gap=shape[1] % 3, shift=shape[1] % 2)
+    both_ways(*shape, dtype, "rms", "layer", True, seed=sum(shape))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
