@@ -170,9 +170,8 @@ struct FewArgs {
     int64_t part_rows;
 };
 
-// Bound by w's bytes, with more rows by the products and their sums over lanes: 200003 classes of width 1024 in fp32 (819 MB) one row 152 us, 5.4 TB/s,
-// 4 rows 161, 8 rows 202 (tiles of fp32 planes: 730); 1000 classes of width 16, with the join, 7.3 from a graph (15.2).  Of aligned 16-bit
-// values the tiles are faster (width 1024 in bfloat16: 82 and 116 us).
+// Bound by w's bytes: 457731 classes of width 1172 in fp32 (2.15 GB), 2 rows 401 us, 5.4 TB/s, 4 rows 424; 1000 classes of width 16, with the join, 7.3
+// from a graph.  Of aligned 16-bit values the tiles are faster (200003 of width 1024 in bfloat16: 82 and 116 us).
 template <int DT, int M>
 __global__ __launch_bounds__(256) void xent_rows_fwd_kernel(FewArgs a)
 {

@@ -2,6 +2,7 @@
 // Every entry point validates on the host first and enqueues nothing on error.
 #include "dqrm_checks.hpp"
 #include "dqrm_xent.hpp"
+#include "dqrm_xent_strips.hpp"
 
 namespace {
 
@@ -140,6 +141,12 @@ struct Space {
     }
 };
 
+// rows of x laid out anew: as an operand of the tiles, or up to 64 of them by the steps of the strips' products (32 or 64 rows then)
+size_t x_space(int64_t m, int64_t k, int32_t dtype)
+{
+    return bytes(std::max<int64_t>(m, m <= 32 ? 32 : 64) * up(std::max<int64_t>(k, 1), kDepth) * 2 * planes_of(dtype));
+}
+
 struct FwdSpace {
     size_t parts, at, x, w;
     size_t total() const { return parts + at + x + w; }
@@ -151,14 +158,14 @@ FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     FwdSpace s{};
     s.parts = bytes(std::max(ceil_div(v, 128), std::min(v, kFewBlocks)) * m * 8); // (of the narrowest tiles, and of few rows' workgroups)
     s.at = bytes(m * 4);
-    s.x = bytes(m * up(k, kDepth) * 2 * pl);
+    s.x = x_space(m, k, dtype);
     s.w = bytes(most_classes(v, k, pl) * up(k, kDepth) * 2 * pl);
     return s;
 }
 
 struct BwdSpace {
-    size_t live, classes, most, unit, x, w, d, sums, dx, dw;
-    size_t total() const { return live + classes + most + unit + x + w + d + sums + dx + dw; }
+    size_t live, classes, most, unit, x, strip, w, d, sums, dx, dw;
+    size_t total() const { return live + classes + most + unit + x + strip + w + d + sums + dx + dw; }
 };
 
 BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
@@ -169,7 +176,7 @@ BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     const int64_t rows = up(m, kBlock), d = std::max(rows * 256, std::min(rows * most, kPieceBytes / (2 * pl)));
     BwdSpace s{};
     s.live = bytes(ceil_div(m, 64) * 8), s.classes = bytes(ceil_div(v, 64) * 8), s.most = 1024, s.unit = 256;
-    s.x = bytes(m * up(k, kDepth) * 2 * pl), s.w = bytes(most * up(k, kDepth) * 2 * pl);
+    s.x = x_space(m, k, dtype), s.strip = m <= 64 ? s.x : x_space(64, k, dtype), s.w = bytes(most * up(k, kDepth) * 2 * pl);
     s.d = bytes(d * 2 * pl);
     s.sums = bytes((d / 64 + most) * 4);
     s.dx = bytes(std::max(m * k * 4, slices_room(m, k, most / kDepth * pairs)));
@@ -253,8 +260,10 @@ Classifier classifier(const Call &c, const Products &g, int64_t first)
     return Classifier{g, c.bias ? c.bias + first : nullptr, c.scale * kLog2e, c.targets, first, c.v};
 }
 
-// A few rows of fp32, and of what the matrix instructions' tiles can't read where it is, by the kernel that reads w as it is: up to 8 rows at a
-// time, as many as fit its LDS.  (Laying w out anew costs as much as reading it 3 times in 16 bits and 5 times in fp32.)
+// Up to 4 rows of fp32, and of what the tiles can't read where it is, by the kernel that reads w as it is, as long as its LDS holds them.  (More rows
+// by strips: 200003 classes of width 1021 in fp32, 2, 4, 8 and 16 rows 161, 176, 231 and 457 us, by strips 254 for each; bf16 143, 165, 222 and
+// 434, by strips 170.)
+constexpr int64_t kFewRows = 4;
 constexpr int64_t kFewLds = 64 << 10;
 
 int few_lanes(int64_t k)
@@ -266,44 +275,85 @@ int few_lanes(int64_t k)
 
 int64_t few_padded(int64_t k) { return up(std::max<int64_t>(k, 1), few_lanes(k) * kChunk); }
 
-int few_at_a_time(int64_t m, int64_t k)
-{
-    int rows = 1;
-    while (rows < 8 && rows < m && rows * 2 * few_padded(k) * 4 <= kFewLds) rows *= 2;
-    return rows;
-}
+int few_held(int64_t m) { return m <= 2 ? (int)m : 4; }
 
 bool is_few(const Call &c)
 {
-    if (c.m > (c.dtype == DQRM_F32 ? 16 : 8) || few_padded(c.k) * 4 > kFewLds) return false;
-    return !as_it_is(c.w, c.ldw, c.dtype, c.v, c.k);
+    return c.m <= kFewRows && few_held(c.m) * few_padded(c.k) * 4 <= kFewLds && !as_it_is(c.w, c.ldw, c.dtype, c.v, c.k);
 }
 
 void launch_few(const Call &c, float2 *parts, float *at, float *loss, float *lse, hipStream_t st)
 {
-    const int lanes = few_lanes(c.k), m = few_at_a_time(c.m, c.k), at_once = 256 / lanes * (m <= 2 ? 4 : 2);
+    const int lanes = few_lanes(c.k), at_once = 256 / lanes * (c.m <= 2 ? 4 : 2);
     // (four workgroups to a CU, and no fewer classes than a group takes at a time)
     const int64_t per_block = up(ceil_div(c.v, std::min<int64_t>(ceil_div(c.v, at_once), kFewBlocks)), at_once), blocks = ceil_div(c.v, per_block);
-    for (int64_t r = 0; r < c.m; r += m) {
-        const FewArgs a{static_cast<const char *>(c.x) + r * c.ldx * (int64_t)size_of(c.dtype), c.w, c.ldx, c.ldw, std::min<int64_t>(m, c.m - r), c.v, c.k, c.bias,
-                        c.scale * kLog2e, c.targets + r, per_block, lanes, (int)few_padded(c.k), parts + r, at + r, c.m};
-        with_type(c.dtype, [&](auto t) {
-            constexpr int DT = decltype(t)::value;
-            const auto go = [&](auto rows) {
-                constexpr int M = decltype(rows)::value;
-                hipLaunchKernelGGL((xent_rows_fwd_kernel<DT, M>), dim3((unsigned)blocks), dim3(256), (size_t)M * a.padded * sizeof(float), st, a);
-            };
-            if (m == 1)
-                go(std::integral_constant<int, 1>{});
-            else if (m == 2)
-                go(std::integral_constant<int, 2>{});
-            else if (m == 4)
-                go(std::integral_constant<int, 4>{});
-            else
-                go(std::integral_constant<int, 8>{});
-        });
-    }
+    const FewArgs a{static_cast<const char *>(c.x), c.w, c.ldx, c.ldw, c.m, c.v, c.k, c.bias, c.scale * kLog2e, c.targets, per_block, lanes,
+                    (int)few_padded(c.k), parts, at, c.m};
+    with_type(c.dtype, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        const auto go = [&](auto rows) {
+            constexpr int M = decltype(rows)::value;
+            hipLaunchKernelGGL((xent_rows_fwd_kernel<DT, M>), dim3((unsigned)blocks), dim3(256), (size_t)M * a.padded * sizeof(float), st, a);
+        };
+        if (c.m == 1)
+            go(std::integral_constant<int, 1>{});
+        else if (c.m == 2)
+            go(std::integral_constant<int, 2>{});
+        else
+            go(std::integral_constant<int, 4>{});
+    });
     launch_xent_join(parts, blocks, c.m, at, c.targets, c.v, loss, lse, st);
+}
+
+// Up to 64 rows, by strips of the classes.
+int64_t strips_of(int64_t n) { return up(n, kBlock) / 32; }
+int strip_blocks(int64_t rows) { return rows <= 32 ? 1 : 2; }
+int64_t strip_chunks(int64_t k) { return std::max<int64_t>(1, ceil_div(k, kDepth)); }
+size_t strip_space(int64_t rows, int64_t k, int32_t dtype) { return (size_t)(strip_chunks(k) * 4 * planes_of(dtype) * strip_blocks(rows)) * 1024; }
+int strip_grid(int64_t strips) { return (int)std::min<int64_t>(ceil_div(strips, 4), kFewBlocks); }
+
+bool is_strips(const Call &c) { return c.m <= 64 && !as_it_is(c.w, c.ldw, c.dtype, c.v, c.k); }
+
+StripArgs strip_args(const Call &c, int64_t first, int64_t n, const void *x)
+{
+    StripArgs a{};
+    a.w = static_cast<const char *>(c.w) + first * c.ldw * (int64_t)size_of(c.dtype), a.ldw = c.ldw, a.classes = n, a.first = first, a.all = c.v;
+    a.width = (int)c.k, a.rows = (int)c.m, a.chunks = (int)ceil_div(c.k, kDepth), a.strips = (int)strips_of(n);
+    a.x = static_cast<const uint4 *>(x), a.bias = c.bias ? c.bias + first : nullptr, a.scale2 = c.scale * kLog2e, a.targets = c.targets;
+    return a;
+}
+
+void launch_strip_pack(const Call &c, void *out, hipStream_t st)
+{
+    const int blocks = strip_blocks(c.m), vectors = (int)strip_chunks(c.k) * 4 * blocks * 64;
+    with_type(c.dtype, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        hipLaunchKernelGGL(xent_strip_pack_kernel<DT>, dim3((unsigned)ceil_div(vectors, 256)), dim3(256), 0, st, static_cast<const elem_t<DT> *>(c.x), c.ldx, (int)c.m,
+                           (int)c.k, blocks, vectors, static_cast<uint4 *>(out));
+    });
+}
+
+template <bool GRAD>
+void launch_strips(const Call &c, const StripArgs &a, hipStream_t st)
+{
+    with_type(c.dtype, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        if (strip_blocks(c.m) == 1)
+            hipLaunchKernelGGL((xent_strip_kernel<DT, 1, GRAD>), dim3((unsigned)strip_grid(a.strips)), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((xent_strip_kernel<DT, 2, GRAD>), dim3((unsigned)strip_grid(a.strips)), dim3(256), 0, st, a);
+    });
+}
+
+void launch_strip_dx(const Call &c, const StripDxArgs &a, int slices, hipStream_t st)
+{
+    with_type(c.dtype, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        if (strip_blocks(c.m) == 1)
+            hipLaunchKernelGGL((xent_strip_dx_kernel<DT, 1>), dim3((unsigned)(slices * a.columns)), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((xent_strip_dx_kernel<DT, 2>), dim3((unsigned)(slices * a.columns)), dim3(256), 0, st, a);
+    });
 }
 
 void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStream_t st)
@@ -315,6 +365,13 @@ void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStre
     a.parts = static_cast<float2 *>(ws.take(need.parts)), a.at = static_cast<float *>(ws.take(need.at));
     void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
     if (is_few(c)) return launch_few(c, a.parts, a.at, loss, lse, st);
+    if (is_strips(c)) {
+        launch_strip_pack(c, x_space, st);
+        StripArgs strips = strip_args(c, 0, c.v, x_space);
+        strips.parts = a.parts, strips.at = a.at;
+        launch_strips<false>(c, strips, st);
+        return launch_xent_join(a.parts, strip_grid(strips.strips), c.m, a.at, c.targets, c.v, loss, lse, st);
+    }
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
     const Shape shape = logits_shape(c.m, c.v, ceil_div(c.k, kDepth) * pairs);
     const int64_t step = as_it_is(c.w, c.ldw, c.dtype, c.v, c.k) ? c.v : piece_classes(c.m, c.v, c.k, planes_of(c.dtype), false);
@@ -372,7 +429,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
     uint64_t *live = static_cast<uint64_t *>(ws.take(need.live)), *live_classes = static_cast<uint64_t *>(ws.take(need.classes));
     unsigned *most = static_cast<unsigned *>(ws.take(need.most));
     float *unit = static_cast<float *>(ws.take(need.unit));
-    void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
+    void *x_space = ws.take(need.x), *strip_space = ws.take(need.strip), *w_space = ws.take(need.w);
     char *d = static_cast<char *>(ws.take(need.d));
     float *sums = static_cast<float *>(ws.take(need.sums)), *dx_sums = static_cast<float *>(ws.take(need.dx)), *dw_sums = static_cast<float *>(ws.take(need.dw));
 
@@ -386,26 +443,43 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
     const int64_t step = piece_classes(c.m, c.v, c.k, planes, true);
     const bool one = step >= c.v;
-    const Sliced dx_plan = out_plan(c.m, c.k, ceil_div(std::min(step, c.v), kDepth) * pairs);
+    const bool strips = is_strips(c);
+    if (strips) launch_strip_pack(c, strip_space, st);
+    const int64_t columns = ceil_div(c.k, kBlock), blocks = ceil_div(std::min(step, c.v), kBlock);
+    Sliced dx_plan = out_plan(c.m, c.k, blocks * pairs);
+    if (strips) { // (of blocks of classes; four waves to a workgroup, six workgroups to a CU)
+        const int64_t slices = std::min<int64_t>({std::max<int64_t>(1, num_cus() * 6 / std::max<int64_t>(columns, 1)), ceil_div(blocks, 4), kMostSlices});
+        dx_plan.stages_per_slice = (unsigned)ceil_div(blocks, slices), dx_plan.slices = (unsigned)ceil_div(blocks, dx_plan.stages_per_slice);
+    }
     for (int64_t first = 0; first < c.v; first += step) {
         const int64_t n = std::min(step, c.v - first);
-        const Operand w = classes_of(c, first, n, w_space, st);
+        const Operand w = strips ? Operand{} : classes_of(c, first, n, w_space, st);
         const Shape shape = logits_shape(c.m, n, ceil_div(c.k, kDepth) * pairs);
         GradArgs a{};
         const Products g = products(x, w, c.m, n, c.k, pairs, shape);
         a.c = classifier(c, g, first), a.lse = lse, a.grad = grad, a.live = live, a.most = unit, a.by = by;
         a.rows = up(c.m, kBlock), a.cols = up(n, kBlock), a.plane = a.rows * a.cols * 2, a.planes = planes, a.d = d, a.sums = dbias ? sums : nullptr;
-        if (g.tiles_m > 0)
+        if (strips && c.m > 0) {
+            StripArgs b = strip_args(c, first, n, strip_space);
+            b.lse = lse, b.grad = grad, b.most = unit, b.live = live, b.by = by, b.d = d, b.plane = a.plane, b.dbias = dbias ? dbias + first : nullptr;
+            launch_strips<true>(c, b, st);
+        } else if (g.tiles_m > 0)
             with_operands(c.dtype, [&](auto zero) {
                 with_logits_shape(shape, [&](auto tile) {
                     using S = decltype(tile);
                     hipLaunchKernelGGL((xent_grad_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
                 });
             });
-        if (dbias) hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, st, sums, n, (int)g.tiles_m, n, n, dbias + first, nullptr);
+        if (dbias && !(strips && c.m > 0)) hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, st, sums, n, (int)g.tiles_m, n, n, dbias + first, nullptr);
         if (c.k == 0) continue;
         const Operand dm{d, a.plane, a.cols * 2, a.rows, a.cols, nullptr};
-        if (dx && c.m > 0) {
+        if (dx && c.m > 0 && strips) {
+            StripDxArgs b{};
+            b.w = static_cast<const char *>(c.w) + first * c.ldw * (int64_t)size_of(c.dtype), b.ldw = c.ldw, b.classes = n, b.width = (int)c.k, b.rows = (int)c.m;
+            b.columns = (int)columns, b.d = d, b.plane = a.plane, b.live = c.bias ? live_classes + first / 64 : nullptr, b.blocks = (int)ceil_div(n, kBlock);
+            b.per_slice = (int)dx_plan.stages_per_slice, b.sums = dx_sums, b.add = first > 0;
+            launch_strip_dx(c, b, (int)dx_plan.slices, st);
+        } else if (dx && c.m > 0) {
             Operand by = w;
             by.live = c.bias ? live_classes + first / 64 : nullptr;
             OutArgs o{products(dm, by, c.m, c.k, n, pairs, dx_plan.shape), dx, lddx, scale, unit};
@@ -426,7 +500,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
             if (p.slices > 1) launch_out_join(c.dtype, dw_sums, p.slices, n, c.k, to, lddw, scale, unit, st);
         }
     }
-    if (dx && c.m > 0 && c.k > 0 && (!one || dx_plan.slices > 1))
+    if (dx && c.m > 0 && c.k > 0 && (!one || dx_plan.slices > 1 || strips))
         launch_out_join(c.dtype, dx_sums, dx_plan.slices, c.m, c.k, dx, lddx, scale, unit, st);
 }
 
