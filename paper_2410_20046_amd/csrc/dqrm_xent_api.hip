@@ -310,7 +310,13 @@ int64_t strips_of(int64_t n) { return up(n, kBlock) / 32; }
 int strip_blocks(int64_t rows) { return rows <= 32 ? 1 : 2; }
 int64_t strip_chunks(int64_t k) { return std::max<int64_t>(1, ceil_div(k, kDepth)); }
 size_t strip_space(int64_t rows, int64_t k, int32_t dtype) { return (size_t)(strip_chunks(k) * 4 * planes_of(dtype) * strip_blocks(rows)) * 1024; }
-int strip_grid(int64_t strips) { return (int)std::min<int64_t>(ceil_div(strips, 4), kFewBlocks); }
+
+// as many workgroups as the registers let run at once
+int strip_grid(const Call &c, int64_t strips)
+{
+    const int64_t per_cu = strip_blocks(c.m) == 2 ? 2 : c.dtype == DQRM_F32 ? 3 : 4;
+    return (int)std::min<int64_t>({ceil_div(strips, 4), num_cus() * per_cu, kFewBlocks});
+}
 
 bool is_strips(const Call &c) { return c.m <= 64 && !as_it_is(c.w, c.ldw, c.dtype, c.v, c.k); }
 
@@ -339,9 +345,9 @@ void launch_strips(const Call &c, const StripArgs &a, hipStream_t st)
     with_type(c.dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
         if (strip_blocks(c.m) == 1)
-            hipLaunchKernelGGL((xent_strip_kernel<DT, 1, GRAD>), dim3((unsigned)strip_grid(a.strips)), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((xent_strip_kernel<DT, 1, GRAD>), dim3((unsigned)strip_grid(c, a.strips)), dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL((xent_strip_kernel<DT, 2, GRAD>), dim3((unsigned)strip_grid(a.strips)), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((xent_strip_kernel<DT, 2, GRAD>), dim3((unsigned)strip_grid(c, a.strips)), dim3(256), 0, st, a);
     });
 }
 
@@ -370,7 +376,7 @@ void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStre
         StripArgs strips = strip_args(c, 0, c.v, x_space);
         strips.parts = a.parts, strips.at = a.at;
         launch_strips<false>(c, strips, st);
-        return launch_xent_join(a.parts, strip_grid(strips.strips), c.m, a.at, c.targets, c.v, loss, lse, st);
+        return launch_xent_join(a.parts, strip_grid(c, strips.strips), c.m, a.at, c.targets, c.v, loss, lse, st);
     }
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
     const Shape shape = logits_shape(c.m, c.v, ceil_div(c.k, kDepth) * pairs);

@@ -10,6 +10,8 @@
 
 namespace dqrm_xent {
 
+using v4u = unsigned __attribute__((ext_vector_type(4)));
+
 template <int DT> struct Planes {
     using T = std::conditional_t<DT == DQRM_F16, _Float16, __bf16>; // of the products
     static constexpr int n = DT == DQRM_F32 ? 3 : 1, pairs = DT == DQRM_F32 ? (int)kPlanePairs : 1;
@@ -52,7 +54,7 @@ __global__ __launch_bounds__(256) void xent_strip_pack_kernel(const elem_t<DT> *
     const int at = blockIdx.x * 256 + threadIdx.x; // of [chunk][step][block][lane]
     if (at >= vectors) return;
     const int lane = at & 63, block = (at >> 6) % blocks, step = ((at >> 6) / blocks) & 3, chunk = (at >> 6) / blocks >> 2;
-    const int r = block * 32 + (lane & 31), c = chunk * 64 + (lane >> 5) * 32 + step * kChunk;
+    const int r = block * 32 + (lane & 31), c = chunk * 64 + step * 16 + (lane >> 5) * kChunk;
     Vec8<elem_t<DT>> v{};
     if (r < rows) v = load_vec(x + r * ldx, c, width, false);
     uint4 p[planes];
@@ -98,6 +100,9 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
     using Q = typename Planes<DT>::T;
     constexpr int planes = Planes<DT>::n;
     using S = StripTile<MB>;
+    constexpr int vectors = 4 * planes * MB * 64; // of x to 64 values
+    constexpr int mine = vectors / 256;
+    __shared__ __align__(16) uint4 s_x[2][vectors];
     __shared__ float2 s_part[4][MB * 32];
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = (int)uniform(threadIdx.x >> 6);
     const int stride = (int)gridDim.x * 4;
@@ -120,18 +125,31 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
     auto ask = [&](int strip, int chunk) {
         const int64_t r = min((int64_t)strip * 32 + (lane & 31), a.classes - 1);
         const T *row = static_cast<const T *>(a.w) + r * a.ldw;
-        const int c = chunk * 64 + half * 32;
+        const int c = chunk * 64 + half * kChunk;
         if (chunk * 64 + 64 <= a.width) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) __builtin_memcpy(&next[s], row + c + s * kChunk, sizeof(next[s]));
+            for (int s = 0; s < 4; ++s) __builtin_memcpy(&next[s], row + c + s * 16, sizeof(next[s]));
         } else {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) next[s] = load_vec(row, c + s * kChunk, a.width, false);
+            for (int s = 0; s < 4; ++s) next[s] = load_vec(row, c + s * 16, a.width, false);
         }
     };
-    int strip = (int)blockIdx.x * 4 + wave;
-    if (strip < a.strips) ask(strip, 0);
-    for (; strip < a.strips; strip += stride) {
+    v4u x_next[mine];
+    auto ask_x = [&](int chunk) {
+#pragma unroll
+        for (int i = 0; i < mine; ++i) x_next[i] = reinterpret_cast<const v4u *>(a.x)[(int64_t)chunk * vectors + i * 256 + (int)threadIdx.x];
+    };
+    auto put_x = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < mine; ++i) reinterpret_cast<v4u *>(s_x[buffer])[i * 256 + (int)threadIdx.x] = x_next[i];
+    };
+    int buffer = 0;
+    ask_x(0);
+    put_x(0);
+    ask((int)blockIdx.x * 4 + wave, 0);
+    __syncthreads();
+    for (int four = (int)blockIdx.x * 4; four < a.strips; four += stride) { // (past the last strip, the last class is read)
+        const int strip = four + wave;
         v16f acc[MB][1];
 #pragma unroll
         for (int b = 0; b < MB; ++b) acc[b][0] = v16f{};
@@ -139,10 +157,9 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
             Vec8<T> w[4];
 #pragma unroll
             for (int s = 0; s < 4; ++s) w[s] = next[s];
-            if (chunk + 1 < a.chunks)
-                ask(strip, chunk + 1);
-            else if (strip + stride < a.strips)
-                ask(strip + stride, 0);
+            const bool more = chunk + 1 < a.chunks;
+            ask_x(more ? chunk + 1 : 0); // (before w, whose arrival it need not await)
+            ask(more ? strip : strip + stride, more ? chunk + 1 : 0);
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 uint4 p[planes];
@@ -151,11 +168,15 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
                 for (int b = 0; b < MB; ++b) {
                     uint4 x[planes];
 #pragma unroll
-                    for (int k = 0; k < planes; ++k) x[k] = a.x[(((chunk * 4 + s) * planes + k) * MB + b) * 64 + lane];
+                    for (int k = 0; k < planes; ++k) x[k] = s_x[buffer][((s * planes + k) * MB + b) * 64 + lane];
                     acc[b][0] = multiply_planes<DT>(p, x, acc[b][0]);
                 }
             }
+            buffer ^= 1;
+            put_x(buffer); // (which the products before the last barrier read)
+            __syncthreads();
         }
+        if (strip >= a.strips) continue;
         const int64_t n0 = (int64_t)strip * 32;
         Classifier c{};
         c.g.n = a.classes, c.bias = a.bias, c.scale2 = a.scale2;
