@@ -261,8 +261,8 @@ Classifier classifier(const Call &c, const Products &g, int64_t first)
 }
 
 // Up to 4 rows of fp32, and of what the tiles can't read where it is, by the kernel that reads w as it is, as long as its LDS holds them.  (More rows
-// by strips: 200003 classes of width 1021 in fp32, 2, 4, 8 and 16 rows 161, 176, 231 and 457 us, by strips 254 for each; bf16 143, 165, 222 and
-// 434, by strips 170.)
+// by strips: 200003 classes of width 1021 in fp32, 2, 4, 8 and 16 rows 161, 176, 231 and 457 us, by strips 220 for each; bf16 143, 165, 222 and
+// 434, by strips 140.)
 constexpr int64_t kFewRows = 4;
 constexpr int64_t kFewLds = 64 << 10;
 
