@@ -15,7 +15,7 @@ UNITS = {
                      "dqrm_dense.hpp", "dqrm_step.hpp", "dqrm_xent_join.hpp"] + _SHARED,
     "dqrm_mx_api.hip": ["dqrm_checks.hpp", "dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_mx_few.hpp", "dqrm_norm.hpp"] + _SHARED,
     "dqrm_train_api.hip": ["dqrm_checks.hpp", "dqrm_mx.hpp", "dqrm_norm.hpp", "dqrm_grad.hpp", "dqrm_resnorm.hpp"] + _SHARED,
-    "dqrm_xent_api.hip": ["dqrm_checks.hpp", "dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_xent_gemm.hpp", "dqrm_xent.hpp", "dqrm_xent_strips.hpp"] + _SHARED,
+    "dqrm_xent_api.hip": ["dqrm_checks.hpp", "dqrm_mx.hpp", "dqrm_mx_gemm.hpp", "dqrm_xent_gemm.hpp", "dqrm_xent.hpp", "dqrm_xent_strips.hpp", "dqrm_xent_narrow.hpp"] + _SHARED,
 }
 SOURCES = [os.path.join(CSRC, f) for f in UNITS]
 HEADERS = sorted({os.path.join(CSRC, f) for headers in UNITS.values() for f in headers})

@@ -2,7 +2,7 @@
 // Every entry point validates on the host first and enqueues nothing on error.
 #include "dqrm_checks.hpp"
 #include "dqrm_xent.hpp"
-#include "dqrm_xent_strips.hpp"
+#include "dqrm_xent_narrow.hpp"
 
 namespace {
 
@@ -24,32 +24,18 @@ constexpr int64_t kSliceTiles = 512; // tiles times slices
 using TileBig = Tile<4, 4, 2, 2, 2>; // 256 by 256, one to a CU
 using TileMid = Tile<2, 2, 2, 2, 2>; // 128 by 128, two to a CU
 using TileFew = Tile<2, 2, 1, 4, 2, true>; // 64 by 256: few rows
-using TileThin = Tile<2, 2, 4, 1, 2>; // 256 by 64: few columns
 
-enum class Shape { big, mid, few, thin };
+enum class Shape { big, mid, few };
 
 int64_t up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 int planes_of(int32_t dtype) { return dtype == DQRM_F32 ? 3 : 1; }
 int pairs_of(int32_t dtype) { return dtype == DQRM_F32 ? (int)kPlanePairs : 1; }
 int rows_of(Shape s) { return s == Shape::mid ? 128 : s == Shape::few ? 64 : 256; }
-int cols_of(Shape s) { return s == Shape::mid ? 128 : s == Shape::thin ? 64 : 256; }
+int cols_of(Shape s) { return s == Shape::mid ? 128 : 256; }
 int per_cu(Shape s) { return s == Shape::big ? 1 : 2; }
 
 template <typename F>
 void with_shape(Shape s, F f)
-{
-    if (s == Shape::big)
-        f(TileBig{});
-    else if (s == Shape::mid)
-        f(TileMid{});
-    else if (s == Shape::few)
-        f(TileFew{});
-    else
-        f(TileThin{});
-}
-// (the logits' products have no thin ones)
-template <typename F>
-void with_logits_shape(Shape s, F f)
 {
     if (s == Shape::big)
         f(TileBig{});
@@ -83,7 +69,6 @@ Shape logits_shape(int64_t m, int64_t n, int64_t stages)
 // a gradient's product [m][n]
 Shape out_shape(int64_t m, int64_t n, int64_t stages)
 {
-    if (n <= 64) return Shape::thin;
     if (m <= 64) return Shape::few;
     if (stages <= kShortSum) return Shape::mid; // (131072 classes, width 2048, 64 rows, bf16: forward and backward 563 us, with tiles of 256 580)
     return m > 128 && n > 128 ? Shape::big : Shape::mid;
@@ -128,6 +113,27 @@ int64_t piece_classes(int64_t rows, int64_t classes, int64_t width, int planes, 
 }
 
 size_t bytes(int64_t n) { return align_up((size_t)n, 256); }
+
+// Gradients of widths up to 64: without d.  Workgroups of 128 rows of x or w, slices of the others.
+constexpr int64_t kNarrowSums = 256LL << 20; // bytes of their sums, if a slice is less
+constexpr int64_t kNarrowSlices = 256;
+bool is_narrow(int64_t m, int64_t k) { return m > 64 && k > 0 && k <= kDepth; }
+int64_t most_narrow_slices(int64_t rows, int64_t k) { return std::max<int64_t>(1, std::min<int64_t>(kNarrowSlices, kNarrowSums / (rows * k * 4))); }
+// (values; enough for fewer rows too)
+int64_t narrow_sums(int64_t rows, int64_t k) { return std::max(rows * k, std::min<int64_t>(kNarrowSums / 4, kNarrowSlices * rows * k)); }
+
+// the slices with which the last workgroup ends first, each with some stages' time before and after its own (three workgroups to a CU)
+Sliced narrow_plan(int64_t rows, int64_t others, int64_t k)
+{
+    const int64_t tiles = ceil_div(rows, 128), stages = ceil_div(others, 64), room = num_cus() * 3;
+    Sliced p{Shape::mid, 1, (unsigned)stages};
+    int64_t least = std::numeric_limits<int64_t>::max();
+    for (int64_t n = 1; n <= std::min(most_narrow_slices(rows, k), ceil_div(stages, 2)); ++n) {
+        const int64_t each = ceil_div(stages, n), time = ceil_div(tiles * n, room) * (each + 4) + n / 32;
+        if (time < least) least = time, p.stages_per_slice = (unsigned)each, p.slices = (unsigned)ceil_div(stages, each);
+    }
+    return p;
+}
 
 // the regions of the workspace
 struct Space {
@@ -177,6 +183,10 @@ BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     BwdSpace s{};
     s.live = bytes(ceil_div(m, 64) * 8), s.classes = bytes(ceil_div(v, 64) * 8), s.most = 1024, s.unit = 256;
     s.x = x_space(m, k, dtype), s.strip = m <= 64 ? s.x : x_space(64, k, dtype), s.w = bytes(most * up(k, kDepth) * 2 * pl);
+    if (is_narrow(m, k)) {
+        s.dx = bytes(narrow_sums(m, k) * 4), s.dw = bytes(narrow_sums(most, k) * 4), s.sums = bytes(narrow_sums(most, k) / k * 4 + 4);
+        return s;
+    }
     s.d = bytes(d * 2 * pl);
     s.sums = bytes((d / 64 + most) * 4);
     s.dx = bytes(std::max(m * k * 4, slices_room(m, k, most / kDepth * pairs)));
@@ -362,6 +372,21 @@ void launch_strip_dx(const Call &c, const StripDxArgs &a, int slices, hipStream_
     });
 }
 
+template <Narrow WHAT>
+void launch_narrow(const Call &c, const NarrowArgs &a, unsigned slices, hipStream_t st)
+{
+    with_type(c.dtype, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        const dim3 grid(a.tiles * slices);
+        if (c.k <= 16)
+            hipLaunchKernelGGL((xent_narrow_kernel<DT, 1, WHAT>), grid, dim3(256), 0, st, a);
+        else if (c.k <= 32)
+            hipLaunchKernelGGL((xent_narrow_kernel<DT, 2, WHAT>), grid, dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((xent_narrow_kernel<DT, 4, WHAT>), grid, dim3(256), 0, st, a);
+    });
+}
+
 void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStream_t st)
 {
     const int pairs = pairs_of(c.dtype);
@@ -379,6 +404,22 @@ void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStre
         return launch_xent_join(a.parts, strip_grid(c, strips.strips), c.m, a.at, c.targets, c.v, loss, lse, st);
     }
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
+    if (is_narrow(c.m, c.k)) {
+        const int64_t step = piece_classes(c.m, c.v, c.k, planes_of(c.dtype), false);
+        int64_t slices = 0;
+        for (int64_t first = 0; first < c.v; first += step) {
+            const int64_t n = std::min(step, c.v - first);
+            const Sliced p = narrow_plan(c.m, n, c.k);
+            NarrowArgs b{};
+            b.x = x, b.w = classes_of(c, first, n, w_space, st), b.rows = c.m, b.classes = n, b.width = (int)c.k;
+            b.bias = c.bias ? c.bias + first : nullptr, b.scale2 = c.scale * kLog2e, b.targets = c.targets, b.first = first;
+            b.tiles = (unsigned)ceil_div(c.m, 128), b.stages = (unsigned)ceil_div(n, 64), b.per_slice = p.stages_per_slice;
+            b.parts = a.parts + slices * c.m, b.at = a.at;
+            launch_narrow<Narrow::loss>(c, b, p.slices, st);
+            slices += p.slices;
+        }
+        return launch_xent_join(a.parts, slices, c.m, a.at, c.targets, c.v, loss, lse, st);
+    }
     const Shape shape = logits_shape(c.m, c.v, ceil_div(c.k, kDepth) * pairs);
     const int64_t step = as_it_is(c.w, c.ldw, c.dtype, c.v, c.k) ? c.v : piece_classes(c.m, c.v, c.k, planes_of(c.dtype), false);
     for (int64_t first = 0; first < c.v; first += step) {
@@ -386,7 +427,7 @@ void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStre
         const Products g = products(x, classes_of(c, first, n, w_space, st), c.m, n, c.k, pairs, shape);
         a.c = classifier(c, g, first), a.first_tile = (unsigned)(first / cols_of(shape));
         with_operands(c.dtype, [&](auto zero) {
-            with_logits_shape(shape, [&](auto tile) {
+            with_shape(shape, [&](auto tile) {
                 using S = decltype(tile);
                 hipLaunchKernelGGL((xent_fwd_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
             });
@@ -447,7 +488,8 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
     if (c.bias && dx) hipLaunchKernelGGL(xent_classes_kernel, dim3((unsigned)ceil_div(c.v, 256)), dim3(256), 0, st, c.bias, c.v, live_classes);
 
     const Operand x = operand(c.dtype, c.x, c.ldx, c.m, c.k, x_space, st);
-    const int64_t step = piece_classes(c.m, c.v, c.k, planes, true);
+    const bool narrow = is_narrow(c.m, c.k);
+    const int64_t step = piece_classes(c.m, c.v, c.k, planes, !narrow);
     const bool one = step >= c.v;
     const bool strips = is_strips(c);
     if (strips) launch_strip_pack(c, strip_space, st);
@@ -457,8 +499,30 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
         const int64_t slices = std::min<int64_t>({std::max<int64_t>(1, num_cus() * 6 / std::max<int64_t>(columns, 1)), ceil_div(blocks, 4), kMostSlices});
         dx_plan.stages_per_slice = (unsigned)ceil_div(blocks, slices), dx_plan.slices = (unsigned)ceil_div(blocks, dx_plan.stages_per_slice);
     }
+    if (narrow) dx_plan = narrow_plan(c.m, std::min(step, c.v), c.k);
     for (int64_t first = 0; first < c.v; first += step) {
         const int64_t n = std::min(step, c.v - first);
+        if (narrow) {
+            NarrowArgs a{};
+            a.x = x, a.w = classes_of(c, first, n, w_space, st), a.rows = c.m, a.classes = n, a.width = (int)c.k;
+            a.x.live = live, a.w.live = c.bias && dx ? live_classes + first / 64 : nullptr;
+            a.bias = c.bias ? c.bias + first : nullptr, a.scale2 = c.scale * kLog2e, a.targets = c.targets, a.first = first;
+            a.lse = lse, a.grad = grad, a.most = unit, a.by = by;
+            if (dx) {
+                a.tiles = (unsigned)ceil_div(c.m, 128), a.stages = (unsigned)ceil_div(n, 64), a.per_slice = dx_plan.stages_per_slice, a.sums = dx_sums, a.add = first > 0;
+                launch_narrow<Narrow::dx>(c, a, dx_plan.slices, st);
+            }
+            if (dw || dbias) {
+                const Sliced p = narrow_plan(n, c.m, c.k);
+                a.tiles = (unsigned)ceil_div(n, 128), a.stages = (unsigned)ceil_div(c.m, 64), a.per_slice = p.stages_per_slice, a.sums = dw_sums, a.add = false;
+                a.dbias = dbias ? sums : nullptr;
+                launch_narrow<Narrow::dw>(c, a, p.slices, st);
+                if (dw)
+                    launch_out_join(c.dtype, dw_sums, p.slices, n, c.k, static_cast<char *>(dw) + first * lddw * (int64_t)size_of(c.dtype), lddw, scale, unit, st);
+                if (dbias) hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, st, sums, n, (int)p.slices, n, n, dbias + first, nullptr);
+            }
+            continue;
+        }
         const Operand w = strips ? Operand{} : classes_of(c, first, n, w_space, st);
         const Shape shape = logits_shape(c.m, n, ceil_div(c.k, kDepth) * pairs);
         GradArgs a{};
@@ -471,7 +535,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
             launch_strips<true>(c, b, st);
         } else if (g.tiles_m > 0)
             with_operands(c.dtype, [&](auto zero) {
-                with_logits_shape(shape, [&](auto tile) {
+                with_shape(shape, [&](auto tile) {
                     using S = decltype(tile);
                     hipLaunchKernelGGL((xent_grad_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
                 });
@@ -506,7 +570,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
             if (p.slices > 1) launch_out_join(c.dtype, dw_sums, p.slices, n, c.k, to, lddw, scale, unit, st);
         }
     }
-    if (dx && c.m > 0 && c.k > 0 && (!one || dx_plan.slices > 1 || strips))
+    if (dx && c.m > 0 && c.k > 0 && (!one || dx_plan.slices > 1 || strips || narrow))
         launch_out_join(c.dtype, dx_sums, dx_plan.slices, c.m, c.k, dx, lddx, scale, unit, st);
 }
 

@@ -59,7 +59,8 @@ def check(x, w, targets, bias, scale, grad):
 SHAPES = [(1, 1, 1), (1, 1000, 16), (3, 7, 5), (17, 257, 64), (64, 300, 200), (65, 300, 64), (130, 513, 72), (300, 1000, 40), (257, 700, 1021), (2, 35, 1059),
           (64, 20000, 40), (1000, 12, 22), (5000, 40, 300), (600, 33000, 96), (129, 100, 2048), (520, 33000, 600), (8300, 700, 1100), (40, 100, 100),
           (30, 50, 100), (20, 200, 50), (17000, 40, 24), (100, 200, 100), (100, 500, 100), (300, 5000, 200), (5000, 300, 200),
-          (30, 200, 96), (40, 300, 61), (33, 9000, 130), (64, 70001, 41), (7, 4500, 1021)]
+          (30, 200, 96), (40, 300, 61), (33, 9000, 130), (64, 70001, 41), (7, 4500, 1021), (30, 200, 40),
+          (100, 300, 16), (200, 5000, 32), (70, 500, 9), (65, 64, 33), (1025, 129, 1), (128, 20000, 64), (129, 130, 48)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -86,7 +87,7 @@ def test_a_few_rows(m, dtype):
 
 # more classes than a piece takes, of d or of rows of w that have to be laid out anew
 PIECES = [(t, 8001, 40000, k) for t in ("bf16", "f16") for k in (32, 72, 160)] + [("f32", 3001, 40000, 24), ("bf16", 30, 70000, 4104), ("f16", 30, 70000, 4104),
-                                                                                                  ("f32", 30, 30000, 4104), ("f32", 50, 30000, 4104)]
+                                                                                                  ("f32", 30, 30000, 4104), ("f32", 50, 30000, 4104), ("f32", 70, 1500000, 8)]
 
 
 @pytest.mark.parametrize("dtype, m, v, k", PIECES)
