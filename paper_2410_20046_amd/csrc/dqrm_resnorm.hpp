@@ -189,7 +189,7 @@ __device__ __forceinline__ void statistics(int kind, float eps, int cols, const 
 enum class Gains { registers, lds, memory };
 
 // TPR threads to a row, CH chunks of 8 values to a thread, the next rows of u and r requested before this one's sums.  Bound by its bytes, two
-// reads and two writes, where a copy has 5.0 TB/s: 65536 x 1024 bfloat16 104 us, 5.2 TB/s, 32768 x 4096 235 us, 4.6; wide rows by the two
+// reads and two writes, where a copy has 5.0 TB/s: with two layer norms, all five vectors and the statistics 65536 x 1024 bfloat16 104 us, 5.2 TB/s, 32768 x 4096 235 us, 4.6; wide rows by the two
 // reductions' latency as well, for as many rows as are in a CU's registers: 16384 x 8192 283 us, 3.8.
 template <int DT, int TPR, int CH, int BLOCK, bool SHORT, Gains GAINS, bool CODES>
 __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
 }
 
 // The workgroups' sums in turn, 16 lanes with every 16th each, and the five vectors' gradients [5][cols] from them: post gamma and beta,
-// gate, pre gamma and beta; those of a norm that is not there are 0.
+// gate, pre gamma and beta; those of a norm that is not there are 0.  Latency: 256 sums of 4096 columns 7 us, of 512 5.
 static __global__ __launch_bounds__(256) void resnorm_join_kernel(const float *partial, int n, int cols, Params p, float *dparams)
 {
     __shared__ float s[4][16][17];

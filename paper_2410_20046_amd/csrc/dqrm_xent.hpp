@@ -104,6 +104,8 @@ struct FwdArgs {
     unsigned first_tile;
 };
 
+// The tile of 256 by 256 is bound by the matrix instructions, 8192 rows, 131072 classes, width 4096 in bf16 6.7-6.9 ms, 1.3 PFLOP/s; its exponentials, in
+// nobody's shadow, are a twentieth of it.  Tiles of few rows by the classes' bytes: 16 rows, 200003 classes, width 1024 in bf16 78-83 us, 5.1 TB/s.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::threads, S::per_simd) void xent_fwd_kernel(FwdArgs a)
 {
@@ -292,6 +294,7 @@ __device__ __forceinline__ float sum_over_rows(const float (&v)[16])
     return d + __shfl_xor(d, 1, kWaveSize);
 }
 
+// As the forward, then d's bytes: 8192 rows, 32768 classes, width 4096 in bf16 1.81-1.83 ms, 1.2 PFLOP/s, with 0.5 GB of d.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(GradArgs a)
 {
@@ -384,7 +387,9 @@ struct OutArgs {
     const float *by; // and times this, or null
 };
 
-// A gradient's product, B with k as the rows.  ADD: to the sums of the pieces before.
+// A gradient's product, B with k as the rows.  ADD: to the sums of the pieces before.  Bound by the matrix instructions, whose operands take two
+// transposing reads each: 8192 rows, 32768 classes, width 4096 in bf16, dx 1.97-2.09 ms, 1.1 PFLOP/s, dw 1.92-1.96, 1.1 (torch's products of
+// these sizes: 1.13 and 1.01).
 template <typename T, typename TO, typename S, bool A_BY_K, bool ADD>
 __global__ __launch_bounds__(S::threads, S::per_simd) void xent_out_kernel(OutArgs a)
 {

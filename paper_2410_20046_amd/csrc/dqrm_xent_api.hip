@@ -13,8 +13,9 @@ constexpr int64_t kMostTiles = 1 << 22;  // of 256 by 256, of any of the product
 constexpr int64_t kMostStride = 1 << 22; // values: a tile's offsets stay below 2^32 bytes
 constexpr int64_t kMostClasses = 1 << 22; // of a piece, for the same reason
 // What a piece of the classes may take of the workspace: its gradients d, and its rows of w where they are laid out anew.  Smaller pieces stay in the
-// chip's last-level cache, larger ones are fewer sums to add up (256, 512, 1024 and 4096 MB, forward and backward: 8192 rows, 131072 classes,
-// width 4096, bf16 30.0, 29.5, 29.3 and 29.1 ms; 200003 classes, width 64, fp32 10.9, 10.6, 10.2 and 11.0).
+// chip's last-level cache, larger ones are fewer sums to add up, but all of it is the caller's memory (64, 256, 512 and 1024 MB, forward and backward:
+// 8192 rows, 131072 classes, width 4096, bf16 32.1, 30.4, 29.8 and 29.3 ms; 200003 classes, width 256, 256, 512 and 1024 MB: fp32 24.0, 22.2 and
+// 20.9, bf16 6.5, 6.1 and 5.9).
 constexpr int64_t kPieceBytes = 512LL << 20;
 constexpr int kMostSlices = 64;
 constexpr int64_t kFewBlocks = 1024;  // workgroups that share the classes where there are a few rows
@@ -55,8 +56,8 @@ void with_operands(int32_t dtype, F f)
         f((__bf16)0.0f);
 }
 
-// Sums of few stages: two smaller tiles to a CU, of which one's exponentials and stores go beside the other's products (8192 rows, 200003 classes,
-// width 64 in fp32: forward and backward 12.5 ms with tiles of 256, 11.3 so; from 16 stages on no difference).
+// Sums of few stages: two smaller tiles to a CU, of which one's exponentials and stores go beside the other's products (8192 rows, 200003 classes
+// in bf16: forward and backward, width 128 4.9 ms with tiles of 256, 4.5 so, width 256 6.4 and 6.1; from 16 stages on no difference).
 constexpr int64_t kShortSum = 8;
 
 Shape logits_shape(int64_t m, int64_t n, int64_t stages)
@@ -114,7 +115,9 @@ int64_t piece_classes(int64_t rows, int64_t classes, int64_t width, int planes, 
 
 size_t bytes(int64_t n) { return align_up((size_t)n, 256); }
 
-// Gradients of widths up to 64: without d.  Workgroups of 128 rows of x or w, slices of the others.
+// Widths up to 64, more than 64 rows: without d.  Workgroups of 128 rows of x or w, slices of the others.  (Forward and backward, with the tiles of
+// the other widths and so: 8192 rows, 200003 classes, width 64 in fp32 10.3 and 5.7 ms, in bf16 4.0 and 2.1; 8192 x 1000 x 64 in fp32 110 and
+// 101 us; 100 x 1000000 x 16 in fp32 1976 and 709.  In bf16 64 rows of 200003 classes take 102 and 128 us: up to 64 rows the other kernels are used.)
 constexpr int64_t kNarrowSums = 256LL << 20; // bytes of their sums, if a slice is less
 constexpr int64_t kNarrowSlices = 256;
 bool is_narrow(int64_t m, int64_t k) { return m > 64 && k > 0 && k <= kDepth; }

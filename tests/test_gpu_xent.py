@@ -124,7 +124,7 @@ def test_strides_and_alignment(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m, v, k", [(70, 900, 48), (3, 130, 17)])
+@pytest.mark.parametrize("m, v, k", [(70, 900, 48), (3, 130, 17), (70, 900, 120), (40, 900, 75), (200, 600, 200), (30, 500, 40)])
 def test_rows_without_target_and_classes_taken_out(m, v, k, dtype):
     """Rows without a target, with a gradient of zero, classes with a bias of -infinity: whatever x and w hold there."""
     t = TYPES[dtype]
@@ -156,14 +156,15 @@ def test_rows_without_target_and_classes_taken_out(m, v, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_rows_with_no_class_left(dtype):
-    x, w, targets, _, grad = make(5, 300, 24, TYPES[dtype], seed=6)
+@pytest.mark.parametrize("m, k", [(5, 24), (100, 24), (100, 136), (40, 75)])
+def test_rows_with_no_class_left(m, k, dtype):
+    x, w, targets, _, grad = make(m, 300, k, TYPES[dtype], seed=6)
     bias = torch.full((300,), -math.inf, device="cuda")
     loss, lse = forward(x, w, targets, bias)
     assert bool((lse == -math.inf).all()) and bool((loss == math.inf).all())
     for out in backward(x, w, targets, lse, grad, bias):
         assert bool((out == 0).all())
-    # the target alone is taken out
+    # the targets alone are taken out
     bias = torch.zeros(300, device="cuda")
     bias[targets] = -math.inf
     r = gradients_and_bounds(x, w, targets, bias, 1.0, grad)
@@ -176,31 +177,34 @@ def test_rows_with_no_class_left(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_infinities_and_nans_stay_in_their_rows(dtype):
-    x, w, targets, bias, grad = make(140, 300, 24, TYPES[dtype], seed=7)
+@pytest.mark.parametrize("m, k", [(140, 24), (140, 136), (60, 75), (60, 24)])
+def test_infinities_and_nans_stay_in_their_rows(m, k, dtype):
+    x, w, targets, bias, grad = make(m, 300, k, TYPES[dtype], seed=7)
     loss0, _ = forward(x, w, targets, bias)
-    x[77, 3] = math.nan
+    x[m // 2 + 7, 3] = math.nan
     x[12, 5] = math.inf
     loss, lse = forward(x, w, targets, bias)
-    bad = torch.zeros(140, dtype=torch.bool, device="cuda")
-    bad[[12, 77]] = True
+    bad = torch.zeros(m, dtype=torch.bool, device="cuda")
+    bad[[12, m // 2 + 7]] = True
     assert bool(torch.isnan(loss[bad]).all()) and bool(torch.isnan(lse[bad]).all()) and torch.equal(loss[~bad], loss0[~bad])
     dx, dw, dbias = backward(x, w, targets, lse, grad, bias)
     assert bool(torch.isnan(dx[bad]).all()) and not bool(torch.isnan(dx[~bad]).any()) and bool(torch.isnan(dbias).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_large_logits(dtype):
+@pytest.mark.parametrize("m, k", [(33, 64), (133, 64), (133, 200)])
+def test_large_logits(m, k, dtype):
     """Far beyond where exponentials overflow; a row whose one class has all the weight; a loss near zero."""
-    x, w, targets, bias, grad = make(33, 400, 64, TYPES[dtype], seed=8, spread=300.0)
+    x, w, targets, bias, grad = make(m, 400, k, TYPES[dtype], seed=8, spread=300.0)
     check(x, w, targets, bias, 1.0, grad)
     l = x.double() @ w.double().t() + bias.double()
     check(x, w, l.argmax(1), bias, 1.0, grad)
 
 
-def test_gradients_of_very_different_sizes_in_half():
+@pytest.mark.parametrize("k", [40, 104])
+def test_gradients_of_very_different_sizes_in_half(k):
     """fp16 keeps d times a power of two: the smallest rows' gradients are there, down to 2^-40 of the largest."""
-    x, w, targets, bias, _ = make(200, 300, 40, torch.float16, seed=10)
+    x, w, targets, bias, _ = make(200, 300, k, torch.float16, seed=10)
     grad = torch.exp2(-torch.arange(200, device="cuda").float() / 12) * 1e-5
     check(x, w, targets, bias, 1.0, grad)
     grad = torch.full((200,), 2.0 ** -130, device="cuda")
@@ -209,8 +213,9 @@ def test_gradients_of_very_different_sizes_in_half():
     check(x, w, targets, bias, 1.0, grad)
 
 
-def test_a_target_past_the_last_class_is_recorded():
-    x, w, targets, bias, grad = make(40, 300, 24, torch.bfloat16, seed=11)
+@pytest.mark.parametrize("m, k", [(40, 24), (40, 75), (140, 24), (140, 136)])
+def test_a_target_past_the_last_class_is_recorded(m, k):
+    x, w, targets, bias, grad = make(m, 300, k, torch.bfloat16, seed=11)
     dq.dqrm_check_status()
     good = targets.clone()
     good[17] = -1
@@ -225,12 +230,13 @@ def test_a_target_past_the_last_class_is_recorded():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_outputs_one_by_one_and_empty_calls(dtype):
+@pytest.mark.parametrize("k", [24, 136])
+def test_outputs_one_by_one_and_empty_calls(k, dtype):
     t = TYPES[dtype]
-    x, w, targets, bias, grad = make(70, 300, 24, t, seed=12)
+    x, w, targets, bias, grad = make(70, 300, k, t, seed=12)
     _, lse = forward(x, w, targets, bias)
     dx, dw, dbias = backward(x, w, targets, lse, grad, bias)
-    ws = space(dq.dqrm_softmax_xent_bwd_workspace_bytes(70, 300, 24, t))
+    ws = space(dq.dqrm_softmax_xent_bwd_workspace_bytes(70, 300, k, t))
     for name, want in (("dx", dx), ("dw", dw), ("dbias", dbias)):
         got = torch.full_like(want, math.nan)
         dq.dqrm_softmax_xent_bwd(x, w, targets, lse, grad, bias=bias, workspace=ws, **{name: got})
@@ -239,7 +245,7 @@ def test_outputs_one_by_one_and_empty_calls(dtype):
     none = x[:0], w, targets[:0]
     forward(*none, bias)
     ex, ew, eb = backward(*none, lse[:0], grad[:0], bias)
-    assert ex.shape == (0, 24) and bool((ew == 0).all()) and bool((eb == 0).all())
+    assert ex.shape == (0, k) and bool((ew == 0).all()) and bool((eb == 0).all())
     # no width: the bias alone
     loss, lse = forward(x[:, :0], w[:, :0], targets, bias)
     want = torch.logsumexp(bias.double(), 0)
@@ -247,9 +253,9 @@ def test_outputs_one_by_one_and_empty_calls(dtype):
     near(loss, want - bias.double()[targets], torch.full((70,), 2.0 ** -24 * 300, device="cuda"), "loss")
 
 
-def test_equal_on_another_stream_and_replayed():
-    x, w, targets, bias, grad = make(300, 5000, 64, torch.bfloat16, seed=13)
-    m, v, k = 300, 5000, 64
+@pytest.mark.parametrize("m, v, k", [(300, 5000, 64), (300, 5000, 136), (20, 5000, 75)])
+def test_equal_on_another_stream_and_replayed(m, v, k):
+    x, w, targets, bias, grad = make(m, v, k, torch.bfloat16, seed=13)
     loss, lse = forward(x, w, targets, bias)
     want = [loss, lse, *backward(x, w, targets, lse, grad, bias)]
     side = torch.cuda.Stream()
