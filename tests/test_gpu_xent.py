@@ -16,11 +16,19 @@ def space(n):
     return torch.empty(max(n, 1), dtype=torch.uint8, device="cuda").fill_(0xFF)  # (NaNs, wherever something is read that nobody wrote)
 
 
+BEHIND = 4096
+
+
+def untouched(room):
+    assert bool((room[-BEHIND:] == 0xFF).all()), "written behind the workspace"
+
+
 def forward(x, w, targets, bias=None, scale=1.0, stream=None):
     m, v, k = x.shape[0], w.shape[0], x.shape[1]
     loss, lse = (torch.full((m,), math.nan, device="cuda") for _ in range(2))
-    dq.dqrm_softmax_xent_fwd(x, w, targets, loss, lse, bias=bias, scale=scale, workspace=space(dq.dqrm_softmax_xent_fwd_workspace_bytes(m, v, k, x.dtype)),
-                             stream=stream)
+    room = space(dq.dqrm_softmax_xent_fwd_workspace_bytes(m, v, k, x.dtype) + BEHIND)
+    dq.dqrm_softmax_xent_fwd(x, w, targets, loss, lse, bias=bias, scale=scale, workspace=room[:-BEHIND], stream=stream)
+    untouched(room)
     return loss, lse
 
 
@@ -28,8 +36,9 @@ def backward(x, w, targets, lse, grad, bias=None, scale=1.0):
     m, v, k = x.shape[0], w.shape[0], x.shape[1]
     dx, dw = torch.full_like(x, math.nan).contiguous(), torch.full((v, k), math.nan, dtype=x.dtype, device="cuda")
     dbias = torch.full((v,), math.nan, device="cuda")
-    dq.dqrm_softmax_xent_bwd(x, w, targets, lse, grad, dx=dx, dw=dw, dbias=dbias, bias=bias, scale=scale,
-                             workspace=space(dq.dqrm_softmax_xent_bwd_workspace_bytes(m, v, k, x.dtype)))
+    room = space(dq.dqrm_softmax_xent_bwd_workspace_bytes(m, v, k, x.dtype) + BEHIND)
+    dq.dqrm_softmax_xent_bwd(x, w, targets, lse, grad, dx=dx, dw=dw, dbias=dbias, bias=bias, scale=scale, workspace=room[:-BEHIND])
+    untouched(room)
     return dx, dw, dbias
 
 

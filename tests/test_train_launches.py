@@ -29,6 +29,11 @@ def clip(*items):
     return ("dqrm_grad_clip", grads(*items), len(items), 0, 1.0, FAKE, None, FAKE, ROOM, None)
 
 
+def loss(t, m, v, k):
+    return [("dqrm_softmax_xent_fwd", t, m, v, k, FAKE, k, FAKE, k, FAKE, 1.0, FAKE, FAKE, FAKE, FAKE, ROOM, None),
+            ("dqrm_softmax_xent_bwd", t, m, v, k, FAKE, k, FAKE, k, FAKE, 1.0, FAKE, FAKE, FAKE, FAKE, k, FAKE, k, FAKE, FAKE, ROOM, None)]
+
+
 def tensor(k, rows, cols, t=0):
     return (FAKE + (k << 44), rows, cols, cols, None, 0, None, t)
 
@@ -62,6 +67,14 @@ def test_very_large_tensors():
     assert rc == OK and launches and all(map(fits, launches))
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("m, v, k", [(1, 1 << 30, 64), (64, 1 << 22, 4097), (64, 3, 1 << 22), (65, 1 << 30, 1), (100, (1 << 22) + 5, 33), (1 << 29, 256, 1), (1 << 22, 64, 64),
+                                     (129, 1 << 23, 64), (65, 3, 1 << 22), (300, 1 << 20, 100)])
+def test_the_loss_of_extreme_shapes(m, v, k, t):
+    for rc, launches in would_launch(loss(t, m, v, k)):
+        assert rc == OK and launches and all(map(fits, launches))
+
+
 def of_the_library(name):
     found = {k for k in library_kernels() if name in k}
     assert found
@@ -89,9 +102,8 @@ def test_the_losses_kernels_are_tested():
     calls = []
     shapes = [(t, *s) for t in TYPES for s in losses.SHAPES + [(m, 70001, 17) for m in (1, 2, 3, 4, 5, 8, 9, 16)]] + [
         ({"f32": 0, "bf16": 1, "f16": 2}[t], *s) for t, *s in losses.PIECES]
-    for t, m, v, k in shapes:
-        calls += [("dqrm_softmax_xent_fwd", t, m, v, k, FAKE, k, FAKE, k, FAKE, 1.0, FAKE, FAKE, FAKE, FAKE, ROOM, None),
-                  ("dqrm_softmax_xent_bwd", t, m, v, k, FAKE, k, FAKE, k, FAKE, 1.0, FAKE, FAKE, FAKE, FAKE, k, FAKE, k, FAKE, FAKE, ROOM, None)]
+    for shape in shapes:
+        calls += loss(*shape)
     missing = (of_the_library("xent")) - launched(calls)
     assert not missing, missing
 
