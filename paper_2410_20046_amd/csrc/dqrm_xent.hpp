@@ -437,11 +437,12 @@ struct PackArgs {
     int64_t plane, pitch; // bytes
 };
 
-// a float as three bfloat16, whose sum it is exactly (of 2^-110 and more); one that would round to infinity is cut instead
+// a float as three bfloat16, whose sum it is exactly (of 2^-110 and more); ANY: one that would round to infinity is cut instead
+template <bool ANY = true>
 __device__ __forceinline__ void split(float v, __bf16 (&p)[3])
 {
     p[0] = (__bf16)v;
-    if (__builtin_isinf((float)p[0])) {
+    if (ANY && __builtin_isinf((float)p[0])) {
         const unsigned cut = __float_as_uint(v) & 0xFFFF0000u;
         p[0] = (__bf16)__uint_as_float(cut);
     }

@@ -58,12 +58,13 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
     const bool inside = row < held_rows;
     const float most = LOSS ? 1.0f : *a.most;
 
+    const bool there = inside && !(DW && a.bias && a.bias[row] == -__builtin_inff());
     uint4 mine[KS][planes];
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int k = 0; k < planes; ++k)
-            mine[s][k] = inside && s * 16 + half * 8 < held.cols ? *reinterpret_cast<const uint4 *>(held.p + k * held.plane + row * held.pitch + s * 32 + half * 16)
+            mine[s][k] = there && s * 16 + half * 8 < held.cols ? *reinterpret_cast<const uint4 *>(held.p + k * held.plane + row * held.pitch + s * 32 + half * 16)
                                                                  : make_uint4(0, 0, 0, 0);
     // of the lane's row: loss: target; dx: lse, gradient and target; dw: bias
     float lse2 = 0.0f, grad = 0.0f, bias2 = -__builtin_inff();
@@ -141,32 +142,33 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
                 for (int k = 0; k < planes; ++k) o[k] = C::read(now + k * plane_bytes, block, t, lane);
                 acc = multiply_planes<DT>(o, mine[t], acc);
             }
+            // what is rare is looked for once: a target among the block's logits, a class that is taken out.  (Gradients need not look for those: their
+            // operands are zeros.)
             const int64_t at = target - ((int64_t)s * 64 + block * 32);
-            const int place_of = at >= 0 && at < 32 ? (int)at : -1;
+            int place_of = at >= 0 && at < 32 ? (int)at : -1;
+            bool taken_out = false;
+            if constexpr (LOSS) taken_out = __any(s_a[buffer][block * 32 + (lane & 31)] == -__builtin_inff());
+            if constexpr (DW) place_of = s_target[buffer][block * 32 + (lane & 31)] - (int)(row - (lane & 31)); // (of a row among the wave's classes)
+            const bool hit = __any(place_of >= 0 && place_of < 32);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int from = block * 32 + q * 8 + half * 4;
-                const float4 va = *reinterpret_cast<const float4 *>(&s_a[buffer][from]), vb = DW ? *reinterpret_cast<const float4 *>(&s_b[buffer][from]) : float4{};
-                const int4 vt = DW ? *reinterpret_cast<const int4 *>(&s_target[buffer][from]) : int4{};
-                const float la[4] = {va.x, va.y, va.z, va.w}, lb[4] = {vb.x, vb.y, vb.z, vb.w};
-                const int lt[4] = {vt.x, vt.y, vt.z, vt.w};
+                const float4 v = *reinterpret_cast<const float4 *>(&s_a[buffer][block * 32 + q * 8 + half * 4]);
+                const float side[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float b = DW ? bias2 : la[i], g = DW ? lb[i] : grad;
-                    const float l = b == -__builtin_inff() ? b : __builtin_fmaf(acc[q * 4 + i], a.scale2, b);
-                    if constexpr (LOSS) {
-                        acc[q * 4 + i] = l;
-                        continue;
-                    }
-                    float v = power2(l - (DW ? la[i] : lse2));
-                    v = (DW ? lt[i] == (int)row : place_of == q * 8 + half * 4 + i) ? v - 1.0f : v;
-                    v = g == 0.0f ? 0.0f : v * g; // (a row without a gradient, whatever its logits are)
-                    if constexpr (DW) column += v;
-                    acc[q * 4 + i] = v;
+                    const float l = __builtin_fmaf(acc[q * 4 + i], a.scale2, DW ? bias2 : side[i]);
+                    acc[q * 4 + i] = LOSS ? l : power2(l - (DW ? side[i] : lse2));
+                }
+            }
+            if (LOSS && taken_out) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float b = s_a[buffer][block * 32 + (i >> 2) * 8 + half * 4 + (i & 3)];
+                    acc[i] = b == -__builtin_inff() ? b : acc[i];
                 }
             }
             if constexpr (LOSS) {
-                if (__any(place_of >= 0)) {
+                if (hit) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (place_of == (i >> 2) * 8 + half * 4 + (i & 3)) a.at[row] = acc[i];
@@ -181,6 +183,29 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
                 sum = sum * power2(best - base) + part, best = top;
                 continue;
             }
+            if (hit) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int from = (i >> 2) * 8 + half * 4 + (i & 3);
+                    if (DW ? s_target[buffer][block * 32 + from] == (int)row : place_of == from) acc[i] -= 1.0f;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float4 v{};
+                if constexpr (DW) v = *reinterpret_cast<const float4 *>(&s_b[buffer][block * 32 + q * 8 + half * 4]);
+                const float side[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // (a row without a gradient, whatever its logits are: dx of such a row is not what the sums are)
+                    if constexpr (DW) {
+                        acc[q * 4 + i] = side[i] == 0.0f ? 0.0f : acc[q * 4 + i] * side[i];
+                        column += acc[q * 4 + i];
+                    } else {
+                        acc[q * 4 + i] *= grad;
+                    }
+                }
+            }
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 uint4 d[planes];
@@ -188,7 +213,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
                     float v[kChunk];
 #pragma unroll
                     for (int i = 0; i < kChunk; ++i) v[i] = acc[8 * t + i];
-                    planes_of<DT>(v, d);
+                    planes_of<DT, false>(v, d);
                 } else {
                     Q v[kChunk];
 #pragma unroll
@@ -227,7 +252,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
                 const int col = c * 32 + q * 8 + half * 4;
                 float v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = out[c][q * 4 + i];
+                for (int i = 0; i < 4; ++i) v[i] = !DW && grad == 0.0f ? 0.0f : out[c][q * 4 + i];
                 if (!a.add && col + 4 <= a.width) {
                     __builtin_memcpy(to + col, v, sizeof(v));
                 } else {

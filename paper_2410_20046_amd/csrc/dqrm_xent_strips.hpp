@@ -17,8 +17,8 @@ template <int DT> struct Planes {
     static constexpr int n = DT == DQRM_F32 ? 3 : 1, pairs = DT == DQRM_F32 ? (int)kPlanePairs : 1;
 };
 
-// eight values as operands of the products
-template <int DT>
+// eight values as operands of the products; ANY: also such as would round to infinity
+template <int DT, bool ANY = true>
 __device__ __forceinline__ void planes_of(const elem_t<DT> (&v)[kChunk], uint4 (&p)[Planes<DT>::n])
 {
     if constexpr (DT == DQRM_F32) {
@@ -26,7 +26,7 @@ __device__ __forceinline__ void planes_of(const elem_t<DT> (&v)[kChunk], uint4 (
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) {
             __bf16 s[3];
-            split(v[i], s);
+            split<ANY>(v[i], s);
             e[0].v[i] = s[0], e[1].v[i] = s[1], e[2].v[i] = s[2];
         }
 #pragma unroll
