@@ -379,6 +379,124 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(Grad
     }
 }
 
+// ---- few logits of long sums ------------------------------------------------------------------------------------------------
+// Where a few tiles are all the logits, their sums are cut into slices (xent_sums_kernel: [slices][rows][classes] in 32 bits) and what follows
+// reads them.  Bound by the launches' and the stages' latency: 233 rows, 27 classes, width 5541 in fp32, forward 28 us, 234 without slices.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::threads, S::per_simd) void xent_sums_kernel(Products g, float *sums)
+{
+    using Out = TileOut<float, S, To::rows>;
+    static_assert(S::waves * Out::wave_bytes <= S::lds_bytes);
+    __shared__ __align__(1024) char lds[S::lds_bytes];
+    const Place at = place_of(g);
+    const int64_t m0 = (int64_t)at.tm * S::BM, n0 = (int64_t)at.tn * S::BN;
+    const int wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+    const int all = (int)(g.stages * g.pairs), first = (int)(at.slice * g.stages_per_slice), last = min(all, first + (int)g.stages_per_slice);
+    v16f acc[S::TM][S::TN];
+    multiply_tile<T, S, false, false, false>(g, lds, m0, n0, first, last, at.tm + at.tn + at.slice, acc);
+    Out::run(sums + (int64_t)at.slice * g.m * g.n, g.n, acc, lds + wave * Out::wave_bytes, m0 + wm * S::TM * 32, n0 + wn * S::TN * 32, g.m, g.n, 1.0f);
+}
+
+struct SumsArgs {
+    const float *sums;
+    int slices, classes;
+    int64_t rows;
+    const float *bias;
+    float scale2;
+    const int64_t *targets;
+    // loss
+    float2 *parts; // [1024s of classes][rows]
+    float *at;
+    // gradient
+    const float *lse, *grad, *most;
+    const uint64_t *live;
+    float by;
+    char *d; // in blocks of 64 by 64
+    int64_t plane, pitch;
+    float *dbias; // [64s of rows][classes], or null
+};
+
+// a logit, in powers of two
+__device__ __forceinline__ float logit_of(const SumsArgs &a, int64_t r, int c)
+{
+    const float b = a.bias ? a.bias[c] * kLog2e : 0.0f;
+    if (b == -__builtin_inff()) return b;
+    const float *from = a.sums + r * a.classes + c;
+    const int64_t slice = a.rows * a.classes;
+    float v = 0.0f;
+    constexpr int ahead = 8; // loads in flight
+    int s = 0;
+    for (; s + ahead <= a.slices; s += ahead) {
+        float x[ahead];
+#pragma unroll
+        for (int i = 0; i < ahead; ++i) x[i] = from[(s + i) * slice];
+#pragma unroll
+        for (int i = 0; i < ahead; ++i) v += x[i];
+    }
+    for (; s < a.slices; ++s) v += from[s * slice];
+    return __builtin_fmaf(v, a.scale2, b);
+}
+
+// 1024 classes of a row to a workgroup.
+constexpr int kSumsClasses = 1024;
+static __global__ __launch_bounds__(256) void xent_sums_loss_kernel(SumsArgs a)
+{
+    __shared__ float2 s_part[4];
+    const int64_t r = blockIdx.x, target = a.targets[r];
+    const int first = blockIdx.y * kSumsClasses, last = min(first + kSumsClasses, a.classes);
+    float2 v = make_float2(-__builtin_inff(), 0.0f);
+    for (int c = first + (int)threadIdx.x; c < last; c += 256) {
+        const float l = logit_of(a, r, c);
+        if (c == target) a.at[r] = l;
+        v = join_parts(v, make_float2(l, l == -__builtin_inff() ? 0.0f : 1.0f));
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v = join_parts(v, make_float2(__shfl_xor(v.x, d, kWaveSize), __shfl_xor(v.y, d, kWaveSize)));
+    if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) a.parts[blockIdx.y * a.rows + r] = join_parts(join_parts(s_part[0], s_part[1]), join_parts(s_part[2], s_part[3]));
+}
+
+// A block of 64 rows by 64 classes of d to a workgroup, 16 classes of a row to a thread.
+template <int DT>
+__global__ __launch_bounds__(256) void xent_sums_grad_kernel(SumsArgs a)
+{
+    using Q = std::conditional_t<DT == DQRM_F16, _Float16, __bf16>;
+    constexpr int planes = DT == DQRM_F32 ? 3 : 1;
+    __shared__ float s_d[64][65];
+    const int row = threadIdx.x >> 2, from = (threadIdx.x & 3) * 16, c0 = blockIdx.x * kBlock;
+    const int64_t r = (int64_t)blockIdx.y * kBlock + row;
+    const bool live = r < a.rows && (a.live[blockIdx.y] >> row) & 1;
+    const float most = *a.most, lse2 = live ? a.lse[r] * kLog2e : 0.0f, grad = live ? a.grad[r] / most : 0.0f;
+    const int64_t target = live ? a.targets[r] : -1;
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int c = c0 + from + i;
+        v[i] = 0.0f;
+        if (live && c < a.classes) v[i] = (power2(logit_of(a, r, c) - lse2) - (c == target ? 1.0f : 0.0f)) * grad;
+        s_d[row][from + i] = v[i];
+    }
+    char *to = a.d + ((int64_t)blockIdx.y * (a.pitch / (kBlock * 2)) + blockIdx.x) * kBlockBytes + row * (kBlock * 2) + from * 2;
+#pragma unroll
+    for (int k = 0; k < planes; ++k) {
+        struct alignas(16) Many { Q v[16]; } f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            f.v[i] = (Q)(v[i] * a.by);
+            v[i] -= (float)f.v[i]; // (more than one plane: by is 1)
+        }
+        *reinterpret_cast<Many *>(to + k * a.plane) = f;
+    }
+    if (!a.dbias) return;
+    __syncthreads();
+    const int c = c0 + (int)threadIdx.x;
+    if (threadIdx.x >= 64 || c >= a.classes) return;
+    float sum = 0.0f;
+    for (int i = 0; i < 64; ++i) sum += s_d[i][threadIdx.x];
+    a.dbias[(int64_t)blockIdx.y * a.classes + c] = sum * most;
+}
+
 struct OutArgs {
     Products g;
     void *c; // the result, or [slices][m][n] of 32-bit sums

@@ -116,8 +116,8 @@ int64_t piece_classes(int64_t rows, int64_t classes, int64_t width, int planes, 
 size_t bytes(int64_t n) { return align_up((size_t)n, 256); }
 
 // Widths up to 64, more than 64 rows: without d.  Workgroups of 128 rows of x or w, slices of the others.  (Forward and backward, with the tiles of
-// the other widths and so: 8192 rows, 200003 classes, width 64 in fp32 10.3 and 5.7 ms, in bf16 4.0 and 2.1; 8192 x 1000 x 64 in fp32 110 and
-// 101 us; 100 x 1000000 x 16 in fp32 1976 and 709.  In bf16 64 rows of 200003 classes take 102 and 128 us: up to 64 rows the other kernels are used.)
+// the other widths and so: 8192 rows, 200003 classes, width 64 in fp32 10.3 and 5.1 ms, in bf16 4.0 and 1.7; 8192 x 1000 x 64 in fp32 110 and
+// 94 us; 100 x 1000000 x 16 in fp32 1976 and 632.  In bf16 64 rows of 200003 classes took 102 and 128 us: up to 64 rows the other kernels are used.)
 constexpr int64_t kNarrowSums = 256LL << 20; // bytes of their sums, if a slice is less
 constexpr int64_t kNarrowSlices = 256;
 bool is_narrow(int64_t m, int64_t k) { return m > 64 && k > 0 && k <= kDepth; }
@@ -136,6 +136,26 @@ Sliced narrow_plan(int64_t rows, int64_t others, int64_t k)
         if (time < least) least = time, p.stages_per_slice = (unsigned)each, p.slices = (unsigned)ceil_div(stages, each);
     }
     return p;
+}
+
+// Few tiles of long sums: in slices, joined by what follows.  (Forward and backward, in one piece by tiles or strips and so: 233 rows, 27 classes, width
+// 5541 in fp32 504 and 96 us, bf16 128 and 65; 1024 x 1024 x 8192 945 and 521, 235 and 185; 300 x 300 x 384 in fp32 109 and 94; but 64 x 16000 x
+// 2048 in fp32, 63 tiles of few rows, 326 and 376.)
+constexpr int64_t kSumsTiles = 64, kSumsTilesOfFew = 32, kSumsStages = 32;
+Sliced sums_plan(int64_t m, int64_t v, int64_t k, int32_t dtype)
+{
+    const int64_t stages = ceil_div(k, kDepth) * pairs_of(dtype);
+    Sliced p{m <= 64 ? Shape::few : Shape::mid, 1, (unsigned)std::max<int64_t>(stages, 1)};
+    const int64_t tiles = ceil_div(m, rows_of(p.shape)) * ceil_div(v, cols_of(p.shape));
+    if (tiles < 1 || tiles > (p.shape == Shape::few ? kSumsTilesOfFew : kSumsTiles) || stages < kSumsStages || piece_classes(m, v, k, planes_of(dtype), true) < v) return p;
+    const int64_t slices = std::min<int64_t>({kSliceTiles / tiles, ceil_div(stages, 4), kMostSlices});
+    p.stages_per_slice = (unsigned)ceil_div(stages, slices), p.slices = (unsigned)ceil_div(stages, p.stages_per_slice);
+    return p;
+}
+size_t sums_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
+{
+    const Sliced p = sums_plan(m, v, k, dtype);
+    return p.slices > 1 ? bytes(p.slices * m * v * 4) : 0;
 }
 
 // the regions of the workspace
@@ -157,8 +177,8 @@ size_t x_space(int64_t m, int64_t k, int32_t dtype)
 }
 
 struct FwdSpace {
-    size_t parts, at, x, w;
-    size_t total() const { return parts + at + x + w; }
+    size_t parts, at, x, w, logits;
+    size_t total() const { return parts + at + x + w + logits; }
 };
 
 FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
@@ -169,12 +189,13 @@ FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     s.at = bytes(m * 4);
     s.x = x_space(m, k, dtype);
     s.w = bytes(most_classes(v, k, pl) * up(k, kDepth) * 2 * pl);
+    s.logits = sums_space(m, v, k, dtype);
     return s;
 }
 
 struct BwdSpace {
-    size_t live, classes, most, unit, x, strip, w, d, sums, dx, dw;
-    size_t total() const { return live + classes + most + unit + x + strip + w + d + sums + dx + dw; }
+    size_t live, classes, most, unit, x, strip, w, logits, d, sums, dx, dw;
+    size_t total() const { return live + classes + most + unit + x + strip + w + logits + d + sums + dx + dw; }
 };
 
 BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
@@ -186,6 +207,7 @@ BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     BwdSpace s{};
     s.live = bytes(ceil_div(m, 64) * 8), s.classes = bytes(ceil_div(v, 64) * 8), s.most = 1024, s.unit = 256;
     s.x = x_space(m, k, dtype), s.strip = m <= 64 ? s.x : x_space(64, k, dtype), s.w = bytes(most * up(k, kDepth) * 2 * pl);
+    s.logits = sums_space(m, v, k, dtype);
     if (is_narrow(m, k)) {
         s.dx = bytes(narrow_sums(m, k) * 4), s.dw = bytes(narrow_sums(most, k) * 4), s.sums = bytes(narrow_sums(most, k) / k * 4 + 4);
         return s;
@@ -331,7 +353,10 @@ int strip_grid(const Call &c, int64_t strips)
     return (int)std::min<int64_t>({ceil_div(strips, 4), num_cus() * per_cu, kFewBlocks});
 }
 
-bool is_strips(const Call &c) { return c.m <= 64 && !as_it_is(c.w, c.ldw, c.dtype, c.v, c.k); }
+bool is_strips(const Call &c)
+{
+    return c.m <= 64 && !as_it_is(c.w, c.ldw, c.dtype, c.v, c.k) && sums_plan(c.m, c.v, c.k, c.dtype).slices == 1;
+}
 
 StripArgs strip_args(const Call &c, int64_t first, int64_t n, const void *x)
 {
@@ -390,6 +415,24 @@ void launch_narrow(const Call &c, const NarrowArgs &a, unsigned slices, hipStrea
     });
 }
 
+// the logits' sums in slices, and what of the arguments of those that read them is the same
+SumsArgs launch_sums(const Call &c, const Operand &x, const Operand &w, const Sliced &p, float *sums, hipStream_t st)
+{
+    Products g = products(x, w, c.m, c.v, c.k, pairs_of(c.dtype), p.shape);
+    g.slices = p.slices, g.stages_per_slice = p.stages_per_slice;
+    with_operands(c.dtype, [&](auto zero) {
+        using T = decltype(zero);
+        const dim3 grid(g.tiles_m * g.tiles_n * g.slices);
+        if (p.shape == Shape::few)
+            hipLaunchKernelGGL((xent_sums_kernel<T, TileFew>), grid, dim3(TileFew::threads), 0, st, g, sums);
+        else
+            hipLaunchKernelGGL((xent_sums_kernel<T, TileMid>), grid, dim3(TileMid::threads), 0, st, g, sums);
+    });
+    SumsArgs a{};
+    a.sums = sums, a.slices = (int)p.slices, a.classes = (int)c.v, a.rows = c.m, a.bias = c.bias, a.scale2 = c.scale * kLog2e, a.targets = c.targets;
+    return a;
+}
+
 void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStream_t st)
 {
     const int pairs = pairs_of(c.dtype);
@@ -398,6 +441,7 @@ void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStre
     FwdArgs a{};
     a.parts = static_cast<float2 *>(ws.take(need.parts)), a.at = static_cast<float *>(ws.take(need.at));
     void *x_space = ws.take(need.x), *w_space = ws.take(need.w);
+    float *logits_space = static_cast<float *>(ws.take(need.logits));
     if (is_few(c)) return launch_few(c, a.parts, a.at, loss, lse, st);
     if (is_strips(c)) {
         launch_strip_pack(c, x_space, st);
@@ -422,6 +466,13 @@ void launch_fwd(const Call &c, float *loss, float *lse, void *workspace, hipStre
             slices += p.slices;
         }
         return launch_xent_join(a.parts, slices, c.m, a.at, c.targets, c.v, loss, lse, st);
+    }
+    if (const Sliced p = sums_plan(c.m, c.v, c.k, c.dtype); p.slices > 1) {
+        SumsArgs s = launch_sums(c, x, classes_of(c, 0, c.v, w_space, st), p, logits_space, st);
+        s.parts = a.parts, s.at = a.at;
+        const int64_t parts = ceil_div(c.v, kSumsClasses);
+        hipLaunchKernelGGL(xent_sums_loss_kernel, dim3((unsigned)c.m, (unsigned)parts), dim3(256), 0, st, s);
+        return launch_xent_join(a.parts, parts, c.m, a.at, c.targets, c.v, loss, lse, st);
     }
     const Shape shape = logits_shape(c.m, c.v, ceil_div(c.k, kDepth) * pairs);
     const int64_t step = as_it_is(c.w, c.ldw, c.dtype, c.v, c.k) ? c.v : piece_classes(c.m, c.v, c.k, planes_of(c.dtype), false);
@@ -480,6 +531,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
     unsigned *most = static_cast<unsigned *>(ws.take(need.most));
     float *unit = static_cast<float *>(ws.take(need.unit));
     void *x_space = ws.take(need.x), *strip_space = ws.take(need.strip), *w_space = ws.take(need.w);
+    float *logits_space = static_cast<float *>(ws.take(need.logits));
     char *d = static_cast<char *>(ws.take(need.d));
     float *sums = static_cast<float *>(ws.take(need.sums)), *dx_sums = static_cast<float *>(ws.take(need.dx)), *dw_sums = static_cast<float *>(ws.take(need.dw));
 
@@ -495,6 +547,7 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
     const int64_t step = piece_classes(c.m, c.v, c.k, planes, !narrow);
     const bool one = step >= c.v;
     const bool strips = is_strips(c);
+    const Sliced in_slices = sums_plan(c.m, c.v, c.k, c.dtype);
     if (strips) launch_strip_pack(c, strip_space, st);
     const int64_t columns = ceil_div(c.k, kBlock), blocks = ceil_div(std::min(step, c.v), kBlock);
     Sliced dx_plan = out_plan(c.m, c.k, blocks * pairs);
@@ -536,6 +589,14 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
             StripArgs b = strip_args(c, first, n, strip_space);
             b.lse = lse, b.grad = grad, b.most = unit, b.live = live, b.by = by, b.d = d, b.plane = a.plane, b.dbias = dbias ? dbias + first : nullptr;
             launch_strips<true>(c, b, st);
+        } else if (in_slices.slices > 1) {
+            SumsArgs b = launch_sums(c, x, w, in_slices, logits_space, st);
+            // (added up where the first one is, a value to a thread: a block of d has few threads)
+            launch_out_join(DQRM_F32, logits_space, in_slices.slices, c.m, n, logits_space, n, 1.0f, nullptr, st);
+            b.slices = 1;
+            b.lse = lse, b.grad = grad, b.most = unit, b.live = live, b.by = by, b.d = d, b.plane = a.plane, b.pitch = a.cols * 2, b.dbias = a.sums;
+            const dim3 grid((unsigned)(a.cols / kBlock), (unsigned)(a.rows / kBlock));
+            with_type(c.dtype, [&](auto t) { hipLaunchKernelGGL(xent_sums_grad_kernel<decltype(t)::value>, grid, dim3(256), 0, st, b); });
         } else if (g.tiles_m > 0)
             with_operands(c.dtype, [&](auto zero) {
                 with_shape(shape, [&](auto tile) {
@@ -543,7 +604,8 @@ void launch_bwd(const Call &c, const float *lse, const float *grad, void *dx, in
                     hipLaunchKernelGGL((xent_grad_kernel<decltype(zero), S>), dim3(g.tiles_m * g.tiles_n), dim3(S::threads), 0, st, a);
                 });
             });
-        if (dbias && !(strips && c.m > 0)) hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, st, sums, n, (int)g.tiles_m, n, n, dbias + first, nullptr);
+        if (dbias && !(strips && c.m > 0)) hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, st, sums, n,
+                               in_slices.slices > 1 ? (int)(a.rows / kBlock) : (int)g.tiles_m, n, n, dbias + first, nullptr);
         if (c.k == 0) continue;
         const Operand dm{d, a.plane, a.cols * 2, a.rows, a.cols, nullptr};
         if (dx && c.m > 0 && strips) {

@@ -31,8 +31,9 @@ struct NarrowArgs {
     float *dbias; // dw: [slices][classes], or null
 };
 
-// Bound by the matrix instructions and the vector ones beside them: 8192 rows, 200003 classes, width 64 in fp32 (six products), loss 1.1 ms, 1.1
-// PFLOP/s, dx and dw 2.3 each, 1.1 PFLOP/s with the logits.  d in memory would be 29 GB of traffic. Three workgroups to a CU, as LDS has it for three planes;
+// Bound by the matrix instructions and the vector ones beside them: 8192 rows, 200003 classes, width 64 in fp32 (six products), loss 1.04 ms, 1.2
+// PFLOP/s, dx and dw 1.9-2.0 each, 1.3 PFLOP/s with the logits, where a large library product has 1.46.  d in memory would be 29 GB of traffic. In bf16
+// vector instructions bound it (an exponential takes as long as four others): 0.43, 0.6 and 0.6 ms.  Three workgroups to a CU, as LDS has it for three planes;
 // the loop over the two blocks is not unrolled: its operands' addresses and reads would take the registers of a wave.
 enum class Narrow { loss, dx, dw };
 

@@ -69,7 +69,8 @@ SHAPES = [(1, 1, 1), (1, 1000, 16), (3, 7, 5), (17, 257, 64), (64, 300, 200), (6
           (64, 20000, 40), (1000, 12, 22), (5000, 40, 300), (600, 33000, 96), (129, 100, 2048), (520, 33000, 600), (8300, 700, 1100), (40, 100, 100),
           (30, 50, 100), (20, 200, 50), (17000, 40, 24), (100, 200, 100), (100, 500, 100), (300, 5000, 200), (5000, 300, 200),
           (30, 200, 96), (40, 300, 61), (33, 9000, 130), (64, 70001, 41), (7, 4500, 1021), (30, 200, 40),
-          (100, 300, 16), (200, 5000, 32), (70, 500, 9), (65, 64, 33), (1025, 129, 1), (128, 20000, 64), (129, 130, 48)]
+          (100, 300, 16), (200, 5000, 32), (70, 500, 9), (65, 64, 33), (1025, 129, 1), (128, 20000, 64), (129, 130, 48),
+          (233, 27, 5541), (8, 1118, 6953), (64, 5, 2080), (65, 1000, 4096), (1000, 700, 2056), (1, 1, 9000), (40, 3000, 2100)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -133,7 +134,7 @@ def test_strides_and_alignment(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m, v, k", [(70, 900, 48), (3, 130, 17), (70, 900, 120), (40, 900, 75), (200, 600, 200), (30, 500, 40)])
+@pytest.mark.parametrize("m, v, k", [(70, 900, 48), (3, 130, 17), (70, 900, 120), (40, 900, 75), (200, 600, 200), (30, 500, 40), (70, 900, 2052), (20, 500, 2056)])
 def test_rows_without_target_and_classes_taken_out(m, v, k, dtype):
     """Rows without a target, with a gradient of zero, classes with a bias of -infinity: whatever x and w hold there."""
     t = TYPES[dtype]
@@ -165,7 +166,7 @@ def test_rows_without_target_and_classes_taken_out(m, v, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m, k", [(5, 24), (100, 24), (100, 136), (40, 75)])
+@pytest.mark.parametrize("m, k", [(5, 24), (100, 24), (100, 136), (40, 75), (100, 2052)])
 def test_rows_with_no_class_left(m, k, dtype):
     x, w, targets, _, grad = make(m, 300, k, TYPES[dtype], seed=6)
     bias = torch.full((300,), -math.inf, device="cuda")
@@ -186,7 +187,7 @@ def test_rows_with_no_class_left(m, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m, k", [(140, 24), (140, 136), (60, 75), (60, 24)])
+@pytest.mark.parametrize("m, k", [(140, 24), (140, 136), (60, 75), (60, 24), (140, 2052)])
 def test_infinities_and_nans_stay_in_their_rows(m, k, dtype):
     x, w, targets, bias, grad = make(m, 300, k, TYPES[dtype], seed=7)
     loss0, _ = forward(x, w, targets, bias)
@@ -262,7 +263,7 @@ def test_outputs_one_by_one_and_empty_calls(k, dtype):
     near(loss, want - bias.double()[targets], torch.full((70,), 2.0 ** -24 * 300, device="cuda"), "loss")
 
 
-@pytest.mark.parametrize("m, v, k", [(300, 5000, 64), (300, 5000, 136), (20, 5000, 75)])
+@pytest.mark.parametrize("m, v, k", [(300, 5000, 64), (300, 5000, 136), (20, 5000, 75), (30, 300, 2056)])
 def test_equal_on_another_stream_and_replayed(m, v, k):
     x, w, targets, bias, grad = make(m, v, k, torch.bfloat16, seed=13)
     loss, lse = forward(x, w, targets, bias)
