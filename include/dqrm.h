@@ -552,10 +552,11 @@ int32_t dqrm_residual_norm_bwd(int32_t dtype, int64_t rows, int64_t cols, const 
  * A row with all its classes taken out has lse = -infinity, loss = +infinity and no gradient; a row with a target that alone is taken out
  * has loss = +infinity and the gradient of lse, less that of the target's logit.  An infinity in x or w counts as a NaN, and one in a logit
  * other than by bias = -infinity gives NaN.
- * Products are of 16-bit values as they are and of fp32 values as sums of three bfloat16 (six of the nine products, as in the dense step);
+ * Products are of 16-bit values as they are and of fp32 values as sums of three bfloat16 (six of the nine products, as in the dense step), for
+ * up to 4 rows of fp32 or of unaligned values as fused products in fp32;
  * sums, maxima and exponentials are fp32.  classes >= 1 unless rows = 0; rows, classes and width up to 2147482623, the tiles of 256 by 256
  * of any two of them up to 4194304, width and row strides up to 4194304; more are DQRM_ERR_UNSUPPORTED.  The order of all sums depends on shape,
- * strides and type alone. */
+ * strides, alignment and type alone. */
 size_t dqrm_softmax_xent_fwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);
 int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
                               const float *bias, float scale, const int64_t *targets, float *loss, float *lse, void *workspace, size_t workspace_bytes,
@@ -563,7 +564,7 @@ int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int6
 
 /* Its backward, for the gradients grad [rows] fp32 of the rows' losses: with d[i][j] = grad_i (exp(l[i][j] - lse_i) - (1 if j = targets[i])),
  *   dx = scale d w, dw = scale d^T x (of x's type), dbias[j] = sum over i of d[i][j] (fp32)     each may be NULL, but not all
- * The logits are computed again, some classes at a time.  For the products d is held in units of the largest finite |grad|,
+ * The logits are computed again.  For the products d is held in units of the largest finite |grad|,
  * rounded to the type (fp16: times 2^14; fp32: as three bfloat16); dbias is of d in 32 bits. */
 size_t dqrm_softmax_xent_bwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);
 int32_t dqrm_softmax_xent_bwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
