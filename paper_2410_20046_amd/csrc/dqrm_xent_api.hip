@@ -60,10 +60,16 @@ void with_operands(int32_t dtype, F f)
 // in bf16: forward and backward, width 128 4.9 ms with tiles of 256, 4.5 so, width 256 6.4 and 6.1; from 16 stages on no difference).
 constexpr int64_t kShortSum = 8;
 
+// (a launch has fewer than 2^32 threads, 256 to a tile: of the largest products' tiles of 256 there are up to kMostTiles, of 128 four times as many)
+bool is_short(int64_t m, int64_t n, int64_t stages)
+{
+    return stages <= kShortSum && ceil_div(m, rows_of(Shape::mid)) * ceil_div(n, cols_of(Shape::mid)) < (int64_t)1 << 24;
+}
+
 Shape logits_shape(int64_t m, int64_t n, int64_t stages)
 {
     if (m <= 64) return Shape::few;
-    if (stages <= kShortSum) return Shape::mid;
+    if (is_short(m, n, stages)) return Shape::mid;
     return ceil_div(m, 256) * ceil_div(n, 256) >= num_cus() ? Shape::big : Shape::mid;
 }
 
@@ -71,7 +77,7 @@ Shape logits_shape(int64_t m, int64_t n, int64_t stages)
 Shape out_shape(int64_t m, int64_t n, int64_t stages)
 {
     if (m <= 64) return Shape::few;
-    if (stages <= kShortSum) return Shape::mid; // (131072 classes, width 2048, 64 rows, bf16: forward and backward 563 us, with tiles of 256 580)
+    if (is_short(m, n, stages)) return Shape::mid; // (131072 classes, width 2048, 64 rows, bf16: forward and backward 563 us, with tiles of 256 580)
     return m > 128 && n > 128 ? Shape::big : Shape::mid;
 }
 
