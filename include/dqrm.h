@@ -556,7 +556,7 @@ int32_t dqrm_residual_norm_bwd(int32_t dtype, int64_t rows, int64_t cols, const 
  * up to 4 rows of fp32 or of unaligned values as fused products in fp32;
  * sums, maxima and exponentials are fp32.  classes >= 1 unless rows = 0; rows, classes and width up to 2147482623, the tiles of 256 by 256
  * of any two of them up to 4194304, width and row strides up to 4194304; more are DQRM_ERR_UNSUPPORTED.  The order of all sums depends on shape,
- * strides, alignment and type alone. */
+ * strides, alignment and type alone.  A workspace for some rows is enough for fewer of the same classes, width and type. */
 size_t dqrm_softmax_xent_fwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);
 int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
                               const float *bias, float scale, const int64_t *targets, float *loss, float *lse, void *workspace, size_t workspace_bytes,

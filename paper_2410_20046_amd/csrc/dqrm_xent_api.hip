@@ -163,6 +163,16 @@ size_t sums_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     const Sliced p = sums_plan(m, v, k, dtype);
     return p.slices > 1 ? bytes(p.slices * m * v * 4) : 0;
 }
+// ... the most that any number of rows up to m takes: there are fewer slices the more tiles there are, so it is one that fills its tiles
+size_t most_sums_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
+{
+    if (ceil_div(k, kDepth) * pairs_of(dtype) < kSumsStages) return 0;
+    size_t most = 0;
+    for (int64_t rows = std::min<int64_t>(m, 64);; rows = std::min(m, up(rows + 1, 128))) {
+        most = std::max(most, sums_space(rows, v, k, dtype));
+        if (rows == m || rows > kSumsTiles * 128) return most;
+    }
+}
 
 // the regions of the workspace
 struct Space {
@@ -651,7 +661,10 @@ extern "C" {
 
 size_t dqrm_softmax_xent_fwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype)
 {
-    return sizes_are_known(rows, classes, width, dtype) ? fwd_space(rows, classes, width, dtype).total() : 0;
+    if (!sizes_are_known(rows, classes, width, dtype)) return 0;
+    FwdSpace s = fwd_space(rows, classes, width, dtype);
+    s.logits = most_sums_space(rows, classes, width, dtype); // (for fewer rows too)
+    return s.total();
 }
 
 int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
@@ -670,7 +683,10 @@ int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int6
 
 size_t dqrm_softmax_xent_bwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype)
 {
-    return sizes_are_known(rows, classes, width, dtype) ? bwd_space(rows, classes, width, dtype).total() : 0;
+    if (!sizes_are_known(rows, classes, width, dtype)) return 0;
+    BwdSpace s = bwd_space(rows, classes, width, dtype);
+    s.logits = most_sums_space(rows, classes, width, dtype); // (for fewer rows too)
+    return s.total();
 }
 
 int32_t dqrm_softmax_xent_bwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,

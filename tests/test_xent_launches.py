@@ -15,3 +15,21 @@ def test_short_sums_of_many_tiles(m, v, k, t):
     """Sums of few stages take small tiles, and the largest sizes are counted in large ones: no launch has 2^32 threads."""
     for rc, launches in would_launch(loss(t, m, v, k)):
         assert rc == OK and launches and all(map(fits, launches))
+
+
+def queries(m, v, k, t):
+    """What the forward and the backward ask for."""
+    (forward, _), (backward, _) = would_launch([("dqrm_softmax_xent_fwd_workspace_bytes", m, v, k, t), ("dqrm_softmax_xent_bwd_workspace_bytes", m, v, k, t)])
+    return forward, backward
+
+
+# long sums in slices: as many rows as a number of tiles has, and one more and less
+@pytest.mark.parametrize("t, most, v, k", [(1, 2048, 1024, 2056), (0, 2048, 1000, 1000), (1, 8192, 1024, 2056), (1, 1400, 1024, 8192), (2, 20000, 1024, 8192), (0, 9000, 27, 5541), (0, 3000, 8000, 513),
+                                           (1, 130, 1118, 6953), (2, 70, 1000, 4100), (0, 1 << 20, 5, 2080)])
+def test_the_workspace_is_enough_for_fewer_rows_whose_sums_go_in_slices(t, most, v, k):
+    forward, backward = queries(most, v, k, t)
+    rows = {1, 31, 63, 64, 65, 1000, most - 1, most} | {128 * n + e for n in range(1, 66) for e in (-1, 0, 1)}
+    rows = sorted(r for r in rows if 1 <= r <= most)
+    calls = [(*call[:-2], room, None) for r in rows for call, room in zip(loss(t, r, v, k), (forward, backward))]
+    codes = [rc for rc, _ in would_launch(calls)]
+    assert set(codes) == {OK}, [(rows[i // 2], "backward" if i % 2 else "forward") for i, rc in enumerate(codes) if rc != OK]
