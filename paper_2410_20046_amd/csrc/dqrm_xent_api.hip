@@ -127,22 +127,25 @@ size_t bytes(int64_t n) { return align_up((size_t)n, 256); }
 constexpr int64_t kNarrowSums = 256LL << 20; // bytes of their sums, if a slice is less
 constexpr int64_t kNarrowSlices = 256;
 bool is_narrow(int64_t m, int64_t k) { return m > 64 && k > 0 && k <= kDepth; }
-int64_t most_narrow_slices(int64_t rows, int64_t k) { return std::max<int64_t>(1, std::min<int64_t>(kNarrowSlices, kNarrowSums / (rows * k * 4))); }
-// (values; enough for fewer rows too)
-int64_t narrow_sums(int64_t rows, int64_t k) { return std::max(rows * k, std::min<int64_t>(kNarrowSums / 4, kNarrowSlices * rows * k)); }
+int64_t most_narrow_slices(int64_t rows, int64_t k) { return std::max<int64_t>(1, std::min<int64_t>(kNarrowSlices, kNarrowSums / (up(rows, 128) * k * 4))); }
 
 // the slices with which the last workgroup ends first, each with some stages' time before and after its own (three workgroups to a CU)
 Sliced narrow_plan(int64_t rows, int64_t others, int64_t k)
 {
     const int64_t tiles = ceil_div(rows, 128), stages = ceil_div(others, 64), room = num_cus() * 3;
     Sliced p{Shape::mid, 1, (unsigned)stages};
+    const int64_t most = std::min(most_narrow_slices(rows, k), ceil_div(stages, 2));
     int64_t least = std::numeric_limits<int64_t>::max();
-    for (int64_t n = 1; n <= std::min(most_narrow_slices(rows, k), ceil_div(stages, 2)); ++n) {
-        const int64_t each = ceil_div(stages, n), time = ceil_div(tiles * n, room) * (each + 4) + n / 32;
+    for (int64_t n = 1, each; n <= most; n = each > 1 ? ceil_div(stages, each - 1) : most + 1) { // (the fewest slices of each length)
+        each = ceil_div(stages, n);
+        const int64_t time = ceil_div(tiles * n, room) * (each + 4) + n / 32;
         if (time < least) least = time, p.stages_per_slice = (unsigned)each, p.slices = (unsigned)ceil_div(stages, each);
     }
     return p;
 }
+size_t narrow_sums(int64_t rows, int64_t others, int64_t k) { return (size_t)narrow_plan(rows, others, k).slices * (size_t)(rows * k * 4); }
+// ... and the most that any plan for so many rows or fewer takes, without a look at them
+size_t most_narrow_sums(int64_t rows, int64_t k) { return std::max(rows * k * 4, std::min(kNarrowSums, kNarrowSlices * rows * k * 4)); }
 
 // Few tiles of long sums: in slices, joined by what follows.  (Forward and backward, in one piece by tiles or strips and so: 233 rows, 27 classes, width
 // 5541 in fp32 504 and 96 us, bf16 128 and 65; 1024 x 1024 x 8192 945 and 521, 235 and 185; 300 x 300 x 384 in fp32 109 and 94; but 64 x 16000 x
@@ -209,6 +212,16 @@ FwdSpace fwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     return s;
 }
 
+// widths up to 64: classes of the pieces
+struct NarrowPieces {
+    int64_t whole, last;
+};
+NarrowPieces narrow_pieces(int64_t m, int64_t v, int64_t k, int planes)
+{
+    const int64_t step = v > 0 ? piece_classes(m, v, k, planes, false) : 1;
+    return {std::min(step, v), v > 0 ? v - (v - 1) / step * step : 0};
+}
+
 struct BwdSpace {
     size_t live, classes, most, unit, x, strip, w, logits, d, sums, dx, dw;
     size_t total() const { return live + classes + most + unit + x + strip + w + logits + d + sums + dx + dw; }
@@ -225,7 +238,9 @@ BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     s.x = x_space(m, k, dtype), s.strip = m <= 64 ? s.x : x_space(64, k, dtype), s.w = bytes(most * up(k, kDepth) * 2 * pl);
     s.logits = sums_space(m, v, k, dtype);
     if (is_narrow(m, k)) {
-        s.dx = bytes(narrow_sums(m, k) * 4), s.dw = bytes(narrow_sums(most, k) * 4), s.sums = bytes(narrow_sums(most, k) / k * 4 + 4);
+        const NarrowPieces p = narrow_pieces(m, v, k, pl);
+        const size_t dw = std::max(narrow_sums(p.whole, m, k), narrow_sums(p.last, m, k));
+        s.dx = bytes(narrow_sums(m, p.whole, k)), s.dw = bytes(dw), s.sums = bytes(dw / k);
         return s;
     }
     s.d = bytes(d * 2 * pl);
@@ -233,6 +248,24 @@ BwdSpace bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
     s.dx = bytes(std::max(m * k * 4, slices_room(m, k, most / kDepth * pairs)));
     s.dw = bytes(slices_room(most, k, ceil_div(m, kDepth) * pairs));
     return s;
+}
+
+// what is enough for any number of rows up to m
+size_t most_bwd_space(int64_t m, int64_t v, int64_t k, int32_t dtype)
+{
+    BwdSpace s = bwd_space(m, v, k, dtype);
+    s.logits = most_sums_space(m, v, k, dtype);
+    if (!is_narrow(m, k)) return s.total();
+    // Fewer rows may have more slices of dx's sums, or dw's: by the tiles or stages that the rows are, up to so many of them
+    constexpr int64_t kTried = 256;
+    const NarrowPieces p = narrow_pieces(m, v, k, planes_of(dtype));
+    for (int64_t tiles = 1; tiles <= std::min(ceil_div(m, 128), kTried); ++tiles) s.dx = std::max(s.dx, bytes(narrow_sums(std::min(m, tiles * 128), p.whole, k)));
+    size_t dw = 0;
+    for (int64_t stages = 2; stages <= std::min(ceil_div(m, 64), kTried * 2); ++stages)
+        dw = std::max({dw, narrow_sums(p.whole, stages * 64, k), narrow_sums(p.last, stages * 64, k)});
+    if (m > kTried * 128) s.dx = std::max(s.dx, bytes(most_narrow_sums(m, k))), dw = std::max(dw, most_narrow_sums(p.whole, k));
+    s.dw = std::max(s.dw, bytes(dw)), s.sums = std::max(s.sums, bytes(dw / k));
+    return std::max(s.total(), bwd_space(64, v, k, dtype).total()); // (up to 64 rows other kernels are used)
 }
 
 struct Call {
@@ -683,10 +716,7 @@ int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int6
 
 size_t dqrm_softmax_xent_bwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype)
 {
-    if (!sizes_are_known(rows, classes, width, dtype)) return 0;
-    BwdSpace s = bwd_space(rows, classes, width, dtype);
-    s.logits = most_sums_space(rows, classes, width, dtype); // (for fewer rows too)
-    return s.total();
+    return sizes_are_known(rows, classes, width, dtype) ? most_bwd_space(rows, classes, width, dtype) : 0;
 }
 
 int32_t dqrm_softmax_xent_bwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,

@@ -33,3 +33,22 @@ def test_the_workspace_is_enough_for_fewer_rows_whose_sums_go_in_slices(t, most,
     calls = [(*call[:-2], room, None) for r in rows for call, room in zip(loss(t, r, v, k), (forward, backward))]
     codes = [rc for rc, _ in would_launch(calls)]
     assert set(codes) == {OK}, [(rows[i // 2], "backward" if i % 2 else "forward") for i, rc in enumerate(codes) if rc != OK]
+
+
+@pytest.mark.parametrize("most, v, k", [(128, 10000, 64), (8192, 200003, 64), (1000, 1_500_000, 8), (5000, 1000, 16), (3000, 130, 64), (40000, 3000, 33), (100, 64, 1)])
+def test_the_workspace_is_enough_for_fewer_rows_of_few_columns(most, v, k):
+    rows = {1, 2, 33, 64, 65, 127, 128, 129, 191, 192, 193, most // 2, most - 129, most - 128, most - 64, most - 1, most} | {most * n // 40 for n in range(1, 40)}
+    rows = sorted(r for r in rows if 1 <= r <= most)
+    for t in (0, 1):
+        forward, backward = queries(most, v, k, t)
+        calls = [(*call[:-2], room, None) for r in rows for call, room in zip(loss(t, r, v, k), (forward, backward))]
+        assert {rc for rc, _ in would_launch(calls)} == {OK}, t
+
+
+def test_the_workspace_of_few_columns_is_what_their_slices_take():
+    """dx's and dw's sums are [slices][rows or classes][width] in 32 bits, of as many slices as any plan for so many rows or fewer has."""
+    MB = 1 << 20
+    # two stages of rows are one slice of dw's sums, 10000 x 64 (2.5 MB); the 157 stages of classes are up to 79 of dx's, 128 x 64 (2.5 MB)
+    assert queries(128, 10000, 64, 1)[1] < 8 * MB
+    # w's planes 73 MB; 64 tiles of rows, three workgroups to each of 256 CUs: tens of slices of 2 MB of dx's sums, a few of 49 MB of dw's
+    assert queries(8192, 200003, 64, 0)[1] < 500 * MB
