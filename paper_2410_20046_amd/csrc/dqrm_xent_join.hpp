@@ -41,13 +41,16 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2 *parts, int
         if (slice < h) s[slice][in] = v = xent_join_parts(v, s[slice + h][in]);
     }
     if (slice != 0 || r >= rows) return;
-    constexpr float kLn2 = 0.693147180559945309f;
-    const float lse2 = v.x == -__builtin_inff() && v.y == 0.0f ? v.x : v.x + log2f(v.y); // (no classes left; a NaN stays)
-    lse[r] = lse2 * kLn2;
+    // The maximum less the target's logit before the sum's logarithm is added: a loss far below the logits keeps its bits.  In 64 bits up to the one
+    // rounding of each; of a sum of 1 and little more the logarithm too.
+    constexpr double kLn2 = 0.693147180559945309;
+    const bool none = v.x == -__builtin_inff() && v.y == 0.0f; // (no classes left; a NaN stays)
+    const double rest = log2((double)v.y);
+    lse[r] = none ? v.x : (float)(((double)v.x + rest) * kLn2);
     const int64_t t = targets[r];
     float l = 0.0f;
     if (t >= classes) report(DQRM_ERR_INDEX_OUT_OF_RANGE, -1, t);
-    if (t >= 0 && t < classes) l = lse2 == -__builtin_inff() ? __builtin_inff() : (lse2 - at[r]) * kLn2;
+    if (t >= 0 && t < classes) l = none ? __builtin_inff() : (float)(((double)v.x - (double)at[r] + rest) * kLn2);
     loss[r] = l;
 }
 
