@@ -90,6 +90,19 @@ __device__ __forceinline__ int place_of_target(int64_t target, int64_t n0)
 
 __device__ __forceinline__ float power2(float v) { return __builtin_amdgcn_exp2f(v); }
 
+// exp(l - lse) of logits in powers of two: power2(l2 - lse2) factor.  lse times log2 e is not a number of 32 bits: what is left of it is in
+// the factor, which a row's gradient takes with it (and 1, a target's place, its inverse).  Where lse's own rounding is a power and more, nothing is.
+struct RowLse {
+    float lse2, factor, inverse;
+};
+__device__ __forceinline__ RowLse lse_of(float lse)
+{
+    constexpr float kLow = 1.92596303e-8f; // log2 e less kLog2e
+    const float lse2 = lse * kLog2e;
+    const float rest = fminf(fmaxf(__builtin_fmaf(lse, kLow, __builtin_fmaf(lse, kLog2e, -lse2)), -1.0f), 1.0f);
+    return {lse2, power2(-rest), power2(rest)};
+}
+
 // maximum and sum of two parts of a row; a part without classes is (-infinity, 0)
 __device__ __forceinline__ float2 join_parts(float2 a, float2 b)
 {
@@ -315,19 +328,20 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(Grad
     for (int t = 0; t < S::TM; ++t) {
         const int64_t row = row0 + t * 32;
         const bool live = row < g.m && (a.live[row >> 6] >> (row & 63)) & 1;
-        const float lse2 = live ? a.lse[row] * kLog2e : 0.0f, grad = live ? a.grad[row] / most : 0.0f;
+        const RowLse lse = lse_of(live ? a.lse[row] : 0.0f);
+        const float grad = live ? a.grad[row] / most * lse.factor : 0.0f;
         target[t] = place_of_target<S>(live ? a.c.targets[row] : -1, a.c.first + n0 + wn * S::TN * 32);
 #pragma unroll
         for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[t][j][i] = power2(acc[t][j][i] - lse2);
+            for (int i = 0; i < 16; ++i) acc[t][j][i] = power2(acc[t][j][i] - lse.lse2);
         // (the target's place before the gradient's factor)
         if (__any(target[t] >= 0)) {
 #pragma unroll
             for (int j = 0; j < S::TN; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (target[t] == j * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) acc[t][j][i] -= 1.0f;
+                    if (target[t] == j * 32 + (i >> 2) * 8 + half * 4 + (i & 3)) acc[t][j][i] -= lse.inverse;
         }
 #pragma unroll
         for (int j = 0; j < S::TN; ++j)
@@ -467,14 +481,15 @@ __global__ __launch_bounds__(256) void xent_sums_grad_kernel(SumsArgs a)
     const int row = threadIdx.x >> 2, from = (threadIdx.x & 3) * 16, c0 = blockIdx.x * kBlock;
     const int64_t r = (int64_t)blockIdx.y * kBlock + row;
     const bool live = r < a.rows && (a.live[blockIdx.y] >> row) & 1;
-    const float most = *a.most, lse2 = live ? a.lse[r] * kLog2e : 0.0f, grad = live ? a.grad[r] / most : 0.0f;
+    const RowLse lse = lse_of(live ? a.lse[r] : 0.0f);
+    const float most = *a.most, grad = live ? a.grad[r] / most * lse.factor : 0.0f;
     const int64_t target = live ? a.targets[r] : -1;
     float v[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int c = c0 + from + i;
         v[i] = 0.0f;
-        if (live && c < a.classes) v[i] = (power2(logit_of(a, r, c) - lse2) - (c == target ? 1.0f : 0.0f)) * grad;
+        if (live && c < a.classes) v[i] = (power2(logit_of(a, r, c) - lse.lse2) - (c == target ? lse.inverse : 0.0f)) * grad;
         s_d[row][from + i] = v[i];
     }
     char *to = a.d + ((int64_t)blockIdx.y * (a.pitch / (kBlock * 2)) + blockIdx.x) * kBlockBytes + row * (kBlock * 2) + from * 2;

@@ -46,6 +46,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
     constexpr int planes = Planes<DT>::n, CB = (KS + 1) / 2, plane_bytes = 64 * kStageRow, stage_bytes = planes * plane_bytes;
     __shared__ __align__(1024) char lds[2 * stage_bytes];
     __shared__ __align__(16) float s_a[2][64], s_b[2][64]; // of the 64 others: bias; lse and gradient
+    __shared__ float s_one[2][64];                         // ... and what a target's place is less
     __shared__ __align__(16) int s_target[2][64];
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), half = lane >> 5;
     const Operand &held = DW ? a.w : a.x, &others = DW ? a.x : a.w;
@@ -68,14 +69,15 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
             mine[s][k] = there && s * 16 + half * 8 < held.cols ? *reinterpret_cast<const uint4 *>(held.p + k * held.plane + row * held.pitch + s * 32 + half * 16)
                                                                  : make_uint4(0, 0, 0, 0);
     // of the lane's row: loss: target; dx: lse, gradient and target; dw: bias
-    float lse2 = 0.0f, grad = 0.0f, bias2 = -__builtin_inff();
+    float lse2 = 0.0f, one = 1.0f, grad = 0.0f, bias2 = -__builtin_inff();
     int64_t target = -1;
     if constexpr (DW) {
         if (inside) bias2 = a.bias ? a.bias[row] * kLog2e : 0.0f;
     } else if constexpr (LOSS) {
         if (inside) target = a.targets[row] - a.first;
     } else if (inside && (a.x.live[row >> 6] >> (row & 63)) & 1) {
-        lse2 = a.lse[row] * kLog2e, grad = a.grad[row] / most, target = a.targets[row] - a.first;
+        const RowLse lse = lse_of(a.lse[row]);
+        lse2 = lse.lse2, one = lse.inverse, grad = a.grad[row] / most * lse.factor, target = a.targets[row] - a.first;
     }
     const C carrier(others, lane, wave);
     const unsigned lds0 = uniform(lds_address(lds));
@@ -93,7 +95,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
         }
     };
     // what goes with the others, by the first wave
-    float side_a = 0.0f, side_b = 0.0f;
+    float side_a = 0.0f, side_b = 0.0f, side_one = 1.0f;
     int side_target = -1;
     auto ask_side = [&](unsigned stage) {
         if (threadIdx.x >= 64) return;
@@ -101,7 +103,8 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
         if constexpr (DW) {
             const bool live = r < a.rows && (a.x.live[stage] >> lane) & 1;
             const int64_t t = live ? a.targets[r] - a.first : -1;
-            side_a = live ? a.lse[r] * kLog2e : 0.0f, side_b = live ? a.grad[r] / most : 0.0f, side_target = t >= 0 && t < a.classes ? (int)t : -1;
+            const RowLse lse = lse_of(live ? a.lse[r] : 0.0f);
+            side_a = lse.lse2, side_one = lse.inverse, side_b = live ? a.grad[r] / most * lse.factor : 0.0f, side_target = t >= 0 && t < a.classes ? (int)t : -1;
         } else {
             side_a = r >= a.classes ? -__builtin_inff() : a.bias ? a.bias[r] * kLog2e : 0.0f;
         }
@@ -109,7 +112,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
     auto put_side = [&](int buffer) {
         if (threadIdx.x >= 64) return;
         s_a[buffer][lane] = side_a;
-        if constexpr (DW) s_b[buffer][lane] = side_b, s_target[buffer][lane] = side_target;
+        if constexpr (DW) s_b[buffer][lane] = side_b, s_one[buffer][lane] = side_one, s_target[buffer][lane] = side_target;
     };
     // the lane's place in a transposing read of 8 rows by 32 columns c and half i of a step: row 4 half + j / 4 (j: lane % 16) of them, the vector of its 4
     // columns where the row's number exchanges it (i exchanges the halves of the row)
@@ -188,7 +191,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int from = (i >> 2) * 8 + half * 4 + (i & 3);
-                    if (DW ? s_target[buffer][block * 32 + from] == (int)row : place_of == from) acc[i] -= 1.0f;
+                    if (DW ? s_target[buffer][block * 32 + from] == (int)row : place_of == from) acc[i] -= DW ? s_one[buffer][block * 32 + from] : one;
                 }
             }
 #pragma unroll

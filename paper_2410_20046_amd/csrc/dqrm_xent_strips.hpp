@@ -107,7 +107,8 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = (int)uniform(threadIdx.x >> 6);
     const int stride = (int)gridDim.x * 4;
     int64_t target[MB];
-    float lse2[MB], grad[MB], best[MB], sum[MB];
+    RowLse lse[MB];
+    float grad[MB], best[MB], sum[MB];
     bool live[MB];
     const float most = GRAD ? *a.most : 1.0f;
 #pragma unroll
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
         best[b] = -__builtin_inff(), sum[b] = 0.0f;
         if constexpr (GRAD) {
             live[b] = r < a.rows && (a.live[0] >> r) & 1;
-            lse2[b] = live[b] ? a.lse[r] * kLog2e : 0.0f, grad[b] = live[b] ? a.grad[r] / most : 0.0f;
+            lse[b] = lse_of(live[b] ? a.lse[r] : 0.0f), grad[b] = live[b] ? a.grad[r] / most * lse[b].factor : 0.0f;
             if (!live[b]) target[b] = -1;
         }
     }
@@ -203,8 +204,8 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
             for (int b = 0; b < MB; ++b) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    float v = power2(acc[b][0][i] - lse2[b]);
-                    v = (at[b] == (i >> 2) * 8 + half * 4 + (i & 3) ? v - 1.0f : v) * grad[b];
+                    float v = power2(acc[b][0][i] - lse[b].lse2);
+                    v = (at[b] == (i >> 2) * 8 + half * 4 + (i & 3) ? v - lse[b].inverse : v) * grad[b];
                     acc[b][0][i] = live[b] ? v : 0.0f;
                     total[i] += acc[b][0][i];
                 }

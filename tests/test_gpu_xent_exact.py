@@ -6,12 +6,13 @@ few terms, in runs) by its rounding.  The loss is (maximum - target's logit) + l
 import pytest
 import torch
 
-from test_gpu_xent import forward
+from test_gpu_xent import backward, forward
 
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {t: torch.finfo(t).eps / 2 for t in TYPES.values()}
 
 # of each kernel: a few rows, strips, tiles of few rows, widths up to 64, tiles, the largest tiles, sums in slices
 KERNELS = [("f32", 1, 300, 40), ("f32", 4, 300, 40), ("f32", 60, 300, 40), ("f32", 130, 300, 40), ("f32", 130, 300, 72), ("f32", 130, 300, 1100), ("f32", 1030, 33000, 104)] + [
@@ -47,3 +48,20 @@ def test_a_loss_near_zero_of_large_logits(dtype, m, v, k):
         # the maximum's rounding, the constant's, that of lse
         off = beside * least + 8 * U + 2.4 * U * a.abs()
         assert bool(((lse.double() - want).abs() <= off).all()), float(((lse.double() - want).abs() / off).max())
+
+
+@pytest.mark.parametrize("dtype, m, v, k", KERNELS)
+def test_gradients_are_off_by_no_more_than_lse_is_rounded(dtype, m, v, k):
+    """exp(l - lse) has lse's rounding to 32 bits, half a step of it, and beside it a few roundings of numbers around 1; dx of the columns that are one class's
+    alone is that class's d, rounded to the type twice."""
+    x, w, a, g = known(m, v, k, dtype)
+    targets = torch.zeros(m, dtype=torch.int64, device="cuda")
+    _, lse = forward(x, w, targets)
+    dx, _, _ = backward(x, w, targets, lse, torch.ones(m, device="cuda"))
+    total = 1 + torch.exp(-g) + (v - 2) * torch.exp(-8 * g)
+    half = torch.exp2(torch.floor(torch.log2(lse.double().abs().clamp(min=2.0 ** -20))) - 24)
+    step = HALF[TYPES[dtype]] * (0 if dtype == "f32" else 2.1)
+    for column, want, more in ((5, 1 / total - 1, 0.0), (k - 5, torch.exp(-g) / total, 2.1 * U * a.abs())):
+        off = (1 if column == 5 else want) * (1.02 * half + more + 10 * U) + step * want.abs() + (2.0 ** -24 if dtype == "f16" else 0.0)
+        got = dx[:, column].double()
+        assert bool(((got - want).abs() <= off).all()), (column, float(((got - want).abs() / off).max()))
