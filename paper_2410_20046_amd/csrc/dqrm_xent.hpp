@@ -23,8 +23,12 @@ struct Classifier {
     int64_t classes;
 };
 
+// a logit that is -infinity of itself, not by its class's bias
+__device__ __forceinline__ float no_infinity(float l) { return l == -__builtin_inff() ? __builtin_nanf("") : l; }
+
 // The tile's logits, in powers of two, in place of its sums; classes past the last one -infinity, and those that are taken out whatever their sums are.
-template <typename S>
+// CHECKED: other infinities are NaNs, whose rows' lse is one then (+infinity comes to that by itself; a gradient's have their lse's).
+template <typename S, bool CHECKED>
 __device__ __forceinline__ void logits(const Classifier &c, v16f (&acc)[S::TM][S::TN], int64_t n0)
 {
     const int half = (threadIdx.x & 63) >> 5;
@@ -55,11 +59,19 @@ __device__ __forceinline__ void logits(const Classifier &c, v16f (&acc)[S::TM][S
         for (int t = 0; t < S::TM; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[t][j][i] = __builtin_fmaf(acc[t][j][i], c.scale2, b[i]);
+        if constexpr (CHECKED) {
+            float least = 0.0f;
+#pragma unroll
+            for (int t = 0; t < S::TM; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) least = fminf(least, acc[t][j][i]);
+            out |= least == -__builtin_inff();
+        }
         if (__any(out)) {
 #pragma unroll
             for (int t = 0; t < S::TM; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[t][j][i] = b[i] == -__builtin_inff() ? b[i] : acc[t][j][i];
+                for (int i = 0; i < 16; ++i) acc[t][j][i] = b[i] == -__builtin_inff() ? b[i] : CHECKED ? no_infinity(acc[t][j][i]) : acc[t][j][i];
         }
     }
 }
@@ -130,7 +142,7 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_fwd_kernel(FwdAr
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
     v16f acc[S::TM][S::TN];
     multiply_tile<T, S, false, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), at.tn, acc);
-    logits<S>(a.c, acc, n0 + wn * S::TN * 32);
+    logits<S, true>(a.c, acc, n0 + wn * S::TN * 32);
     const int64_t row0 = m0 + wm * S::TM * 32 + (lane & 31);
     int target[S::TM];
 #pragma unroll
@@ -239,7 +251,7 @@ __global__ __launch_bounds__(256) void xent_rows_fwd_kernel(FewArgs a)
         for (int k = 0; k < together; ++k) {
             const float b = cls[k] >= last ? -__builtin_inff() : a.bias ? a.bias[cls[k]] * kLog2e : 0.0f;
 #pragma unroll
-            for (int m = 0; m < M; ++m) acc[k][m] = b == -__builtin_inff() ? b : __builtin_fmaf(acc[k][m], a.scale2, b);
+            for (int m = 0; m < M; ++m) acc[k][m] = b == -__builtin_inff() ? b : no_infinity(__builtin_fmaf(acc[k][m], a.scale2, b));
         }
 #pragma unroll
         for (int m = 0; m < M; ++m) {
@@ -320,7 +332,7 @@ __global__ __launch_bounds__(S::threads, S::per_simd) void xent_grad_kernel(Grad
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN, half = lane >> 5;
     v16f acc[S::TM][S::TN];
     multiply_tile<T, S, false, false, false>(g, lds, m0, n0, 0, (int)(g.stages * g.pairs), at.tn, acc);
-    logits<S>(a.c, acc, n0 + wn * S::TN * 32);
+    logits<S, false>(a.c, acc, n0 + wn * S::TN * 32);
     const int64_t row0 = m0 + wm * S::TM * 32 + (lane & 31);
     const float most = *a.most;
     int target[S::TM];
@@ -448,7 +460,7 @@ __device__ __forceinline__ float logit_of(const SumsArgs &a, int64_t r, int c)
         for (int i = 0; i < ahead; ++i) v += x[i];
     }
     for (; s < a.slices; ++s) v += from[s * slice];
-    return __builtin_fmaf(v, a.scale2, b);
+    return no_infinity(__builtin_fmaf(v, a.scale2, b));
 }
 
 // 1024 classes of a row to a workgroup.

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
                 for (int k = 0; k < planes; ++k) o[k] = C::read(now + k * plane_bytes, block, t, lane);
                 acc = multiply_planes<DT>(o, mine[t], acc);
             }
-            // what is rare is looked for once: a target among the block's logits, a class that is taken out.  (Gradients need not look for those: their
+            // what is rare is looked for once: a target among the block's logits, a class that is taken out, an infinity.  (Gradients need not look for those: their
             // operands are zeros.)
             const int64_t at = target - ((int64_t)s * 64 + block * 32);
             int place_of = at >= 0 && at < 32 ? (int)at : -1;
@@ -164,11 +164,16 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
                     acc[q * 4 + i] = LOSS ? l : power2(l - (DW ? side[i] : lse2));
                 }
             }
-            if (LOSS && taken_out) {
+            if constexpr (LOSS) {
+                float least = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float b = s_a[buffer][block * 32 + (i >> 2) * 8 + half * 4 + (i & 3)];
-                    acc[i] = b == -__builtin_inff() ? b : acc[i];
+                for (int i = 0; i < 16; ++i) least = fminf(least, acc[i]);
+                if (taken_out || __any(least == -__builtin_inff())) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float b = s_a[buffer][block * 32 + (i >> 2) * 8 + half * 4 + (i & 3)];
+                        acc[i] = b == -__builtin_inff() ? b : no_infinity(acc[i]);
+                    }
                 }
             }
             if constexpr (LOSS) {

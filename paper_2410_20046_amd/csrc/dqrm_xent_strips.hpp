@@ -181,7 +181,7 @@ __global__ __launch_bounds__(256) void xent_strip_kernel(StripArgs a)
         const int64_t n0 = (int64_t)strip * 32;
         Classifier c{};
         c.g.n = a.classes, c.bias = a.bias, c.scale2 = a.scale2;
-        logits<S>(c, acc, n0);
+        logits<S, !GRAD>(c, acc, n0);
         int at[MB];
 #pragma unroll
         for (int b = 0; b < MB; ++b) at[b] = place_of_target<S>(target[b], a.first + n0);
