@@ -549,9 +549,8 @@ int32_t dqrm_residual_norm_bwd(int32_t dtype, int64_t rows, int64_t cols, const 
  * x [rows][width], w [classes][width] of one type; bias [classes] fp32 or NULL (0; -infinity takes a class out); scale finite;
  * targets [rows] int64.  A negative target: the row has none, its loss is 0 and it has no gradient.  A target >= classes is recorded as
  * DQRM_ERR_INDEX_OUT_OF_RANGE (table -1, the target) by the forward and counts as none.  lse [rows] fp32 is what the backward needs.
- * A row with all its classes taken out has lse = -infinity, loss = +infinity and no gradient; a row with a target that alone is taken out
- * has loss = +infinity and the gradient of lse, less that of the target's logit.  An infinity in x or w counts as a NaN, and one in a logit
- * other than by bias = -infinity gives NaN.
+ * A row with all its classes taken out has lse = -infinity, loss = +infinity and no gradient; a row whose target is taken out and other classes
+ * are not has loss = +infinity.  An infinity in x or w counts as a NaN, and one in a logit other than by bias = -infinity gives NaN.
  * Products are of 16-bit values as they are and of fp32 values as sums of three bfloat16 (six of the nine products, as in the dense step), for
  * up to 4 rows of fp32 or of unaligned values as fused products in fp32;
  * sums, maxima and exponentials are fp32.  classes >= 1 unless rows = 0; rows, classes and width up to 2147482623, the tiles of 256 by 256
@@ -564,7 +563,8 @@ int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int6
 
 /* Its backward, for the gradients grad [rows] fp32 of the rows' losses: with d[i][j] = grad_i (exp(l[i][j] - lse_i) - (1 if j = targets[i])),
  *   dx = scale d w, dw = scale d^T x (of x's type), dbias[j] = sum over i of d[i][j] (fp32)     each may be NULL, but not all
- * The logits are computed again.  For the products d is held in units of the largest finite |grad|,
+ * A class that is taken out counts as zeros in dx's w, whatever it holds: where it is a row's target, d = -grad there is in dw and dbias, and dx is the
+ * gradient of lse alone.  The logits are computed again.  For the products d is held in units of the largest finite |grad|,
  * rounded to the type (fp16: times 2^14; fp32: as three bfloat16); dbias is of d in 32 bits.  A probability is as good as lse, whose rounding to
  * 32 bits is up to 2^-24 |lse|: it is off by as much of itself, and a target's d, however little is left of it, by as much of grad. */
 size_t dqrm_softmax_xent_bwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);

@@ -6,6 +6,7 @@ import torch
 
 from test_gpu_xent import TYPES, backward, forward, make
 from test_gpu_xent_exact import KERNELS
+from xent_reference import gradients_and_bounds, near
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +57,27 @@ def test_a_logit_that_overflows(dtype, m, v, k):
         w[v // 2, 7] = value
         loss, lse = forward(x, w, targets)
         assert bool(lse.isnan().all()) and bool(loss.isnan().all()), value
+
+
+@pytest.mark.parametrize("dtype, m, v, k", KERNELS)
+def test_a_target_that_is_taken_out(dtype, m, v, k):
+    """The loss is infinite.  d is -grad at the target, in dw and dbias too; dx leaves aside what w holds there: it is the gradient of lse."""
+    x, w, targets, b, grad = make(m, v, k, TYPES[dtype], seed=24)
+    targets = targets % 5 + torch.arange(m, device="cuda") % 2 * (v // 2)  # (some rows' alone)
+    out = torch.zeros(v, dtype=torch.bool, device="cuda")
+    out[targets[::2]] = True
+    b[out] = -math.inf
+    r = gradients_and_bounds(x, w, targets, b, 1.0, grad)
+    bad = w.clone()
+    bad[out] = math.nan
+    loss, lse = forward(x, bad, targets, b)
+    near(loss, r["loss"], r["loss_off"], "loss")
+    near(lse, r["lse"], r["lse_off"], "lse")
+    assert bool((loss.isinf() == out[targets]).all())
+    dx, dw, dbias = backward(x, bad, targets, lse, grad, b)
+    near(dx, *r["dx"], "dx")
+    near(dw, *r["dw"], "dw")
+    near(dbias, *r["dbias"], "dbias")
+    # of such a class there is nothing but its targets' part
+    of = torch.zeros(v, dtype=torch.float64, device="cuda").index_add_(0, targets, grad.double())
+    assert bool((of[out] > 0).any()) and bool(((dbias.double() + of)[out].abs() <= (m + 8) * 2.0 ** -24 * of[out]).all())
