@@ -564,9 +564,10 @@ int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int6
 /* Its backward, for the gradients grad [rows] fp32 of the rows' losses: with d[i][j] = grad_i (exp(l[i][j] - lse_i) - (1 if j = targets[i])),
  *   dx = scale d w, dw = scale d^T x (of x's type), dbias[j] = sum over i of d[i][j] (fp32)     each may be NULL, but not all
  * A class that is taken out counts as zeros in dx's w, whatever it holds: where it is a row's target, d = -grad there is in dw and dbias, and dx is the
- * gradient of lse alone.  The logits are computed again.  For the products d is held in units of the largest finite |grad|,
- * rounded to the type (fp16: times 2^14; fp32: as three bfloat16); dbias is of d in 32 bits.  A probability is as good as lse, whose rounding to
- * 32 bits is up to 2^-24 |lse|: it is off by as much of itself, and a target's d, however little is left of it, by as much of grad. */
+ * gradient of lse alone.  The logits are computed again.  For the products d is held in units of the largest finite |grad|, rounded to the
+ * type (fp16: times 2^14, so that all bits are there down to 2^-28 of it and none below 2^-39; fp32: as three bfloat16); dbias is of d in 32 bits.
+ * A probability is as good as lse, whose rounding to 32 bits is up to 2^-24 |lse|: it is off by as much of itself, and a target's d, however little
+ * is left of it, by as much of grad. */
 size_t dqrm_softmax_xent_bwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);
 int32_t dqrm_softmax_xent_bwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
                               const float *bias, float scale, const int64_t *targets, const float *lse, const float *grad, void *dx, int64_t lddx, void *dw,

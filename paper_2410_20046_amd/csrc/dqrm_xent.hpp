@@ -20,7 +20,6 @@ struct Classifier {
     float scale2;      // scale times log2 e
     const int64_t *targets;
     int64_t first; // the products' first class
-    int64_t classes;
 };
 
 // a logit that is -infinity of itself, not by its class's bias
@@ -634,7 +633,8 @@ __device__ __forceinline__ unsigned largest(unsigned v)
 }
 
 // The gradients' unit: the largest of them (of the finite ones; 1 if there is none).  d in units of it: where all rows weigh the same, as in a
-// mean, the targets' places are close to -1 and lose nothing by their rounding; and fp16, times 2^14, has all its bits down to 2^-28 of the unit.
+// mean, the targets' places are close to -1 and lose nothing by their rounding; and fp16, times 2^14, has all its bits down to 2^-28 of the unit
+// and none below 2^-39.
 __device__ __forceinline__ float unit_of(unsigned bits) { return bits ? __uint_as_float(bits) : 1.0f; }
 
 // Which rows have a gradient, a bit each, and the bits of the largest |grad| of a workgroup's rows; of all rows, by a single workgroup, as the unit.

@@ -341,7 +341,7 @@ Operand classes_of(const Call &c, int64_t first, int64_t n, void *space, hipStre
 
 Classifier classifier(const Call &c, const Products &g, int64_t first)
 {
-    return Classifier{g, c.bias ? c.bias + first : nullptr, c.scale * kLog2e, c.targets, first, c.v};
+    return Classifier{g, c.bias ? c.bias + first : nullptr, c.scale * kLog2e, c.targets, first};
 }
 
 // Up to 4 rows of fp32, and of what the tiles can't read where it is, by the kernel that reads w as it is, as long as its LDS holds them.  (More rows
@@ -410,7 +410,7 @@ bool is_strips(const Call &c)
 StripArgs strip_args(const Call &c, int64_t first, int64_t n, const void *x)
 {
     StripArgs a{};
-    a.w = static_cast<const char *>(c.w) + first * c.ldw * (int64_t)size_of(c.dtype), a.ldw = c.ldw, a.classes = n, a.first = first, a.all = c.v;
+    a.w = static_cast<const char *>(c.w) + first * c.ldw * (int64_t)size_of(c.dtype), a.ldw = c.ldw, a.classes = n, a.first = first;
     a.width = (int)c.k, a.rows = (int)c.m, a.chunks = (int)ceil_div(c.k, kDepth), a.strips = (int)strips_of(n);
     a.x = static_cast<const uint4 *>(x), a.bias = c.bias ? c.bias + first : nullptr, a.scale2 = c.scale * kLog2e, a.targets = c.targets;
     return a;

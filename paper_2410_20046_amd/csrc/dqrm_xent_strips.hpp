@@ -70,7 +70,7 @@ template <int MB> struct StripTile {
 
 struct StripArgs {
     const void *w;
-    int64_t ldw, classes, first, all; // of this piece, its first one, of all
+    int64_t ldw, classes, first; // of this piece, its first one
     int width, rows, chunks, strips;
     const uint4 *x; // as xent_strip_pack_kernel lays it out
     const float *bias;

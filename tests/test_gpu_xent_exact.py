@@ -65,3 +65,20 @@ def test_gradients_are_off_by_no_more_than_lse_is_rounded(dtype, m, v, k):
         off = (1 if column == 5 else want) * (1.02 * half + more + 10 * U) + step * want.abs() + (2.0 ** -24 if dtype == "f16" else 0.0)
         got = dx[:, column].double()
         assert bool(((got - want).abs() <= off).all()), (column, float(((got - want).abs() / off).max()))
+
+
+@pytest.mark.parametrize("dtype, m, v, k", [s for s in KERNELS if s[0] == "f16"])
+def test_the_range_of_gradients_in_half(dtype, m, v, k):
+    """d is held in units of the largest |grad| times 2^14: a d of that size has fp16's bits down to 2^-28 of it, half a step of the subnormals is 2^-39 of it, and
+    what is below that is zero.  Class 0 has all the weight and class 1 is the target: d of class 0, which is dx's column of its own, is grad."""
+    x, w, a, g = known(m, v, k, dtype)
+    below = torch.arange(m, device="cuda", dtype=torch.float64) % 46
+    grad = torch.exp2(15 - below)
+    targets = torch.ones(m, dtype=torch.int64, device="cuda")
+    _, lse = forward(x, w, targets)
+    dx, _, _ = backward(x, w, targets, lse, grad.float())
+    want, got = grad / (1 + torch.exp(-g) + (v - 2) * torch.exp(-8 * g)), dx[:, 5].double()
+    step = want * (2.1 * HALF[torch.float16] + 2.0 ** -24 * (a.abs() + 10)) + 2.0 ** -25  # d's rounding and the result's, lse's; the result's subnormals
+    assert bool(((got - want).abs() <= step)[below <= 28].all()) and bool((want[below <= 28] >= 2.0 ** -14).all())
+    assert bool(((got - want).abs() <= step + 2.0 ** (15 - 39)).all())
+    assert bool((dx[below >= 40] == 0).all()) and bool((got[below < 38] > 0).all())
