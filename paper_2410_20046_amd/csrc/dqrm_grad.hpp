@@ -106,6 +106,22 @@ __device__ __forceinline__ void take_values(const Raw<T> &raw, int64_t c, int64_
     }
 }
 
+// a vector to where it is copied to, bit for bit (a float that is a signalling NaN would not stay one)
+template <typename T, bool SHORT>
+__device__ __forceinline__ void copy_values(const Raw<T> &raw, int64_t c, int64_t cols, T *row)
+{
+    struct Bits { std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> v[kChunk]; } t;
+    __builtin_memcpy(&t, &raw, sizeof(t));
+    if constexpr (!SHORT) drop_before(t.v, c, cols);
+    if (c + kChunk <= cols) {
+        __builtin_memcpy(row + c, &t, sizeof(t));
+    } else {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+            if (c + i < cols) __builtin_memcpy(row + c + i, &t.v[i], sizeof(T));
+    }
+}
+
 // the tensor's type, and whether its rows are shorter than a vector
 template <typename F>
 __device__ __forceinline__ void with_item(const Item &t, F f)
@@ -250,7 +266,7 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Batch b, const dou
         total = *given;
     }
     const bool scaled = total > max_norm && total < __builtin_inff(); // (not with a NaN)
-    const float by = scaled ? max_norm / total : 1.0f;
+    const float by = max_norm / total;
     if (!scaled && t.out == t.data) return;
     const int64_t per_row = (t.cols + kChunk - 1) / kChunk, v0 = (int64_t)(piece - t.first) * b.per_piece;
     const int64_t v1 = min(v0 + b.per_piece, rows_of(t) * per_row);
@@ -265,6 +281,10 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Batch b, const dou
             for (int i = 0; i < kAhead; ++i) load_values<T, SHORT>(data + r[i] * t.ld, c[i], t.cols, raw[i]);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
+                if (!scaled) {
+                    if (i < n) copy_values<T, SHORT>(raw[i], c[i], t.cols, out + r[i] * t.ld_out);
+                    continue;
+                }
                 float v[kChunk];
                 take_values<T, SHORT>(raw[i], c[i], t.cols, v);
                 if (i >= n) break;
