@@ -575,7 +575,8 @@ int32_t dqrm_softmax_xent_bwd(int32_t dtype, int64_t rows, int64_t classes, int6
 
 /* ---- the norm of all gradients, and the clip ------------------------------------------------------------------------
  * A gradient tensor: [rows][cols] of `dtype` with a row stride (ld >= cols; any value if there is one row; a flat buffer is one row).
- *   out    where the scaled values go, [rows][cols] of the same type with stride ld_out; NULL: in place.  Not to overlap other tensors' memory.
+ *   out    where the scaled values go, [rows][cols] of the same type with stride ld_out; NULL: in place.  Not to overlap other tensors' memory, nor
+ *          the tensor's own but for being the same, with the same stride.
  *   count  device int32, or NULL: only the first `count` rows are there (clamped to 0 .. rows), what lies behind them is neither read
  *          nor written: the `values` of a table's sparse gradient with their num_unique
  * The array of these is HOST memory, read during the call; up to 65536 tensors of 2^44 values in all. */
@@ -598,7 +599,7 @@ int32_t dqrm_grad_norm(const dqrm_grad_t *grads, int32_t n, int32_t kind, float 
 
 /* Each value times max_norm / norm (a 32-bit quotient, product rounded once to the type) where norm > max_norm >= 0.  Where it is not, and where
  * norm is infinite or NaN (the caller sees it and drops the step), values keep their bits; `out` then is a copy.  `norm`: device memory, from
- * dqrm_grad_norm, or joined over several GPUs.  Tensors that are written must not overlap: the same memory twice is
+ * dqrm_grad_norm, or joined over several GPUs.  Memory that is written and overlaps other memory that is written or read is
  * DQRM_ERR_INVALID_ARG; rows may lie in the gaps between another tensor's rows. */
 int32_t dqrm_grad_scale(const dqrm_grad_t *grads, int32_t n, const float *norm, float max_norm, void *stream);
 

@@ -54,30 +54,71 @@ int32_t check_grads(const dqrm_grad_t *g, int32_t n)
     return DQRM_OK;
 }
 
-// Tensors that are written must not lie on top of each other: the same one twice, and contiguous ones that overlap, are refused.  (Rows
-// with gaps may lie in each other's gaps.)
+// Memory of a tensor: rows of `width` bytes every `pitch`, or one block.
+struct Region {
+    uintptr_t from, to;
+    int64_t rows, width, pitch;
+    bool written;
+};
+
+Region region_of(const void *p, const dqrm_grad_t &g, int64_t ld, bool written)
+{
+    const int64_t size = (int64_t)size_of(g.dtype);
+    Region r{reinterpret_cast<uintptr_t>(p), 0, g.rows, g.cols * size, ld * size, written};
+    if (g.rows == 1 || ld == g.cols) r.width *= g.rows, r.rows = 1, r.pitch = r.width;
+    r.to = r.from + (uintptr_t)((r.rows - 1) * r.pitch + r.width);
+    return r;
+}
+
+// does [from, to) meet a row? (it begins in or behind the first one)
+bool meets(const Region &r, uintptr_t from, uintptr_t to)
+{
+    if (from >= r.to) return false;
+    const int64_t at = (int64_t)(from - r.from), row = at < r.pitch ? 0 : at / r.pitch, in = at - row * r.pitch;
+    return in < r.width || (row + 1 < r.rows && (int64_t)(to - from) > r.pitch - in);
+}
+
+// b begins in or behind a.  Rows of one pitch lie to each other as the first ones do; of others each is looked at, of the shorter tensor.
+bool overlap(const Region &a, const Region &b)
+{
+    if (a.pitch == b.pitch || b.rows == 1) return meets(a, b.from, b.from + (uintptr_t)b.width);
+    for (int64_t r = 0; r < a.rows && a.rows <= b.rows; ++r) {
+        const uintptr_t from = a.from + (uintptr_t)(r * a.pitch), to = from + (uintptr_t)a.width;
+        if (to > b.from && meets(b, std::max(from, b.from), to)) return true;
+    }
+    for (int64_t r = 0; r < b.rows && a.rows > b.rows; ++r) {
+        const uintptr_t from = b.from + (uintptr_t)(r * b.pitch);
+        if (meets(a, from, from + (uintptr_t)b.width)) return true;
+    }
+    return false;
+}
+
+// What is written must be nothing else's memory: no other tensor's, nor the tensor's own input with another stride or shifted.  (Rows may lie in
+// another's gaps.)  Regions in the order of their first bytes, each against those before it that have not ended.
 int32_t check_apart(const dqrm_grad_t *g, int32_t n)
 {
-    struct Span {
-        uintptr_t from, to;
-        bool gaps;
-    };
-    if (n < 2) return DQRM_OK;
-    Span *s = static_cast<Span *>(std::malloc(sizeof(Span) * (size_t)n));
+    if (n < 1) return DQRM_OK;
+    Region *s = static_cast<Region *>(std::malloc((sizeof(Region) * 2 + sizeof(int32_t) * 2) * (size_t)n));
     if (!s) return DQRM_ERR_UNSUPPORTED;
-    int32_t some = 0;
+    int32_t *open = reinterpret_cast<int32_t *>(s + 2 * (size_t)n);
+    int32_t some = 0, opened = 0;
     for (int32_t i = 0; i < n; ++i) {
         if (empty(g[i])) continue;
-        const int64_t ld = g[i].out ? g[i].ld_out : g[i].ld;
-        const uintptr_t from = reinterpret_cast<uintptr_t>(g[i].out ? g[i].out : g[i].data);
-        s[some++] = Span{from, from + (uintptr_t)(((g[i].rows - 1) * ld + g[i].cols) * (int64_t)size_of(g[i].dtype)), g[i].rows > 1 && ld > g[i].cols};
+        const bool in_place = !g[i].out || (g[i].out == g[i].data && (g[i].ld_out == g[i].ld || g[i].rows == 1));
+        s[some++] = in_place ? region_of(g[i].data, g[i], g[i].ld, true) : region_of(g[i].out, g[i], g[i].ld_out, true);
+        if (!in_place) s[some++] = region_of(g[i].data, g[i], g[i].ld, false);
     }
-    std::sort(s, s + some, [](const Span &a, const Span &b) { return a.from < b.from; });
+    std::sort(s, s + some, [](const Region &a, const Region &b) { return a.from < b.from; });
     bool bad = false;
-    uintptr_t whole = 0; // where the contiguous ones so far end
-    for (int32_t i = 0; i < some; ++i) {
-        bad |= (i > 0 && s[i].from == s[i - 1].from) || (!s[i].gaps && s[i].from < whole);
-        if (!s[i].gaps) whole = std::max(whole, s[i].to);
+    for (int32_t i = 0; i < some && !bad; ++i) {
+        int32_t left = 0;
+        for (int32_t k = 0; k < opened; ++k) {
+            const Region &a = s[open[k]];
+            if (a.to <= s[i].from) continue;
+            bad |= (a.written || s[i].written) && overlap(a, s[i]);
+            open[left++] = open[k];
+        }
+        open[left++] = i, opened = left;
     }
     std::free(s);
     return bad ? DQRM_ERR_INVALID_ARG : DQRM_OK;

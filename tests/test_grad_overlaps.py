@@ -1,0 +1,97 @@
+"""CPU-only: which gradient tensors may be written together.  Nothing is launched where a call is refused, and what is accepted is only written down."""
+import itertools
+import random
+
+import pytest
+
+import paper_2410_20046_amd as dq
+from train_launches import FAKE, grads, would_launch
+
+INVALID, OK = dq.ERR_INVALID_ARG, dq.OK
+ROOM = 1 << 60
+
+
+def tensor(at, rows, cols, ld, out=None, ld_out=0, t=0):
+    """Of places in values from a common start"""
+    size = 4 if t == 0 else 2
+    return (FAKE + at * size, rows, cols, ld, None if out is None else FAKE + out * size, ld_out, None, t)
+
+
+def codes(cases):
+    calls = [call for items in cases for call in (("dqrm_grad_scale", grads(*items), len(items), 1 << 40, 1.0, None),
+                                                  ("dqrm_grad_clip", grads(*items), len(items), 0, 1.0, 1 << 40, None, 1 << 41, ROOM, None))]
+    found = [rc for rc, _ in would_launch(calls)]
+    assert all(a == b for a, b in zip(found[::2], found[1::2]))
+    return found[::2]
+
+
+APART = [
+    [tensor(0, 8, 10, 30), tensor(10, 8, 10, 30), tensor(20, 8, 10, 30)],  # the columns of a matrix in parts
+    [tensor(20, 8, 10, 30), tensor(0, 8, 20, 30)],
+    [tensor(0, 4, 10, 30), tensor(10, 1, 20, 20)],  # a flat one in a gap
+    [tensor(0, 4, 10, 30), tensor(10, 2, 5, 60), tensor(15, 3, 15, 30)],
+    [tensor(0, 4, 10, 30), tensor(100, 3, 7, 9)],  # one right behind another's last row
+    [tensor(0, 8, 10, 10), tensor(80, 8, 10, 10, out=200, ld_out=10)],
+    [tensor(0, 8, 10, 10, out=0, ld_out=10)],  # in place, said twice
+    [tensor(0, 1, 10, 10, out=0, ld_out=99)],
+    [tensor(0, 8, 10, 10, out=100, ld_out=12), tensor(0, 8, 10, 10, out=200, ld_out=12)],  # one input, two outputs
+    [tensor(0, 8, 10, 20, out=10, ld_out=20)],  # beside itself
+    [tensor(0, 0, 10, 10), tensor(0, 8, 0, 10), tensor(0, 8, 10, 10)],  # nothing overlaps
+]
+OVERLAPPING = [
+    [tensor(0, 8, 10, 30), tensor(9, 8, 10, 30)],  # columns of a matrix, one of them twice
+    [tensor(0, 8, 10, 30), tensor(20, 8, 10, 30), tensor(10, 8, 11, 30)],
+    [tensor(20, 8, 15, 30), tensor(0, 8, 10, 30)],  # round the row's end
+    [tensor(0, 1, 100, 100), tensor(50, 8, 10, 30)],  # rows that begin inside a flat one
+    [tensor(0, 4, 10, 30), tensor(15, 1, 16, 16)],  # a flat one over a gap's end
+    [tensor(0, 4, 10, 30), tensor(10, 3, 5, 25)],  # another pitch, its second row
+    [tensor(0, 8, 10, 10, out=0, ld_out=12)],  # itself, with another stride
+    [tensor(0, 8, 10, 10, out=5, ld_out=10)],
+    [tensor(0, 1, 10, 10, out=5, ld_out=10)],
+    [tensor(0, 8, 10, 10, out=200, ld_out=10), tensor(400, 8, 10, 10, out=79, ld_out=10)],  # an output on another's input
+    [tensor(400, 8, 10, 10, out=70, ld_out=20), tensor(0, 8, 10, 10, out=500, ld_out=10)],
+    [tensor(0, 8, 10, 10, out=100, ld_out=12), tensor(200, 8, 10, 10, out=105, ld_out=12)],
+    [tensor(0, 8, 10, 10), tensor(2 * 79, 8, 10, 10, t=1)],  # of another type
+]
+
+
+def test_tensors_that_are_apart():
+    assert codes(APART) == [OK] * len(APART)
+    assert codes([list(reversed(c)) for c in APART]) == [OK] * len(APART)
+
+
+def test_tensors_that_overlap():
+    assert codes(OVERLAPPING) == [INVALID] * len(OVERLAPPING)
+    assert codes([list(reversed(c)) for c in OVERLAPPING]) == [INVALID] * len(OVERLAPPING)
+
+
+def places(at, rows, cols, ld):
+    return {at + r * ld + c for r in range(rows) for c in range(cols)}
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_as_a_look_at_every_value_says(seed):
+    rng = random.Random(seed)
+    cases, want = [], []
+    for _ in range(150):
+        items, written, read = [], [], []
+        for _ in range(rng.choice((1, 2, 2, 3))):
+            rows, cols = rng.randint(1, 5), rng.randint(1, 8)
+            ld, at = cols + rng.choice((0, 0, 3, 8, 13)), rng.randint(0, 60)
+            out = rng.choice((None, None, at, rng.randint(0, 120)))
+            ld_out = cols + rng.choice((0, 3, 8)) if out is not None else 0
+            items.append(tensor(at, rows, cols, ld, out, ld_out))
+            same = out is None or (out == at and (ld_out == ld or rows == 1))
+            written.append(places(at, rows, cols, ld) if same else places(out, rows, cols, ld_out))
+            if not same:
+                read.append(places(at, rows, cols, ld))
+        bad = any(a & b for a, b in itertools.combinations(written, 2)) or any(a & b for a in written for b in read)
+        cases.append(items)
+        want.append(INVALID if bad else OK)
+    assert 20 < want.count(OK) < 130
+    assert codes(cases) == want
+
+
+def test_many_columns_of_one_matrix():
+    assert codes([[tensor(7 * k, 50, 7, 7 * 500) for k in range(500)]]) == [OK]
+    assert codes([[tensor(7 * k, 50, 7 + (k == 250), 7 * 500) for k in range(500)]]) == [INVALID]
