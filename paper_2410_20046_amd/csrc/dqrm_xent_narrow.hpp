@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
     constexpr int planes = Planes<DT>::n, CB = (KS + 1) / 2, plane_bytes = 64 * kStageRow, stage_bytes = planes * plane_bytes;
     __shared__ __align__(1024) char lds[2 * stage_bytes];
     __shared__ __align__(16) float s_a[2][64], s_b[2][64]; // of the 64 others: bias; lse and gradient
-    __shared__ float s_one[2][64];                         // ... and what a target's place is less
+    __shared__ __align__(16) float s_one[2][64];           // ... and what a target's place is less
     __shared__ __align__(16) int s_target[2][64];
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), half = lane >> 5;
     const Operand &held = DW ? a.w : a.x, &others = DW ? a.x : a.w;
@@ -94,8 +94,8 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
             }
         }
     };
-    // what goes with the others, by the first wave
-    float side_a = 0.0f, side_b = 0.0f, side_one = 1.0f;
+    // what goes with the others, by the first wave: asked for with their stage, made of it when that is computed
+    float side_a = 0.0f, side_b = 0.0f;
     int side_target = -1;
     auto ask_side = [&](unsigned stage) {
         if (threadIdx.x >= 64) return;
@@ -103,16 +103,19 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
         if constexpr (DW) {
             const bool live = r < a.rows && (a.x.live[stage] >> lane) & 1;
             const int64_t t = live ? a.targets[r] - a.first : -1;
-            const RowLse lse = lse_of(live ? a.lse[r] : 0.0f);
-            side_a = lse.lse2, side_one = lse.inverse, side_b = live ? a.grad[r] / most * lse.factor : 0.0f, side_target = t >= 0 && t < a.classes ? (int)t : -1;
+            side_a = live ? a.lse[r] : 0.0f, side_b = live ? a.grad[r] : 0.0f, side_target = t >= 0 && t < a.classes ? (int)t : -1;
         } else {
-            side_a = r >= a.classes ? -__builtin_inff() : a.bias ? a.bias[r] * kLog2e : 0.0f;
+            side_a = r >= a.classes ? -__builtin_inff() : a.bias ? a.bias[r] : 0.0f;
         }
     };
     auto put_side = [&](int buffer) {
         if (threadIdx.x >= 64) return;
-        s_a[buffer][lane] = side_a;
-        if constexpr (DW) s_b[buffer][lane] = side_b, s_one[buffer][lane] = side_one, s_target[buffer][lane] = side_target;
+        if constexpr (DW) {
+            const RowLse lse = lse_of(side_a);
+            s_a[buffer][lane] = lse.lse2, s_b[buffer][lane] = side_b / most * lse.factor, s_one[buffer][lane] = lse.inverse, s_target[buffer][lane] = side_target;
+        } else {
+            s_a[buffer][lane] = side_a * kLog2e;
+        }
     };
     // the lane's place in a transposing read of 8 rows by 32 columns c and half i of a step: row 4 half + j / 4 (j: lane % 16) of them, the vector of its 4
     // columns where the row's number exchanges it (i exchanges the halves of the row)
@@ -194,9 +197,18 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
             }
             if (hit) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int from = (i >> 2) * 8 + half * 4 + (i & 3);
-                    if (DW ? s_target[buffer][block * 32 + from] == (int)row : place_of == from) acc[i] -= DW ? s_one[buffer][block * 32 + from] : one;
+                for (int q = 0; q < 4; ++q) {
+                    const int from = q * 8 + half * 4;
+                    int4 t{};
+                    float4 o = make_float4(one, one, one, one);
+                    if constexpr (DW) {
+                        t = *reinterpret_cast<const int4 *>(&s_target[buffer][block * 32 + from]);
+                        o = *reinterpret_cast<const float4 *>(&s_one[buffer][block * 32 + from]);
+                    }
+                    const int targets[4] = {t.x, t.y, t.z, t.w};
+                    const float ones[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[q * 4 + i] -= (DW ? targets[i] == (int)row : place_of == from + i) ? ones[i] : 0.0f;
                 }
             }
 #pragma unroll
