@@ -189,8 +189,9 @@ __device__ __forceinline__ void statistics(int kind, float eps, int cols, const 
 enum class Gains { registers, lds, memory };
 
 // TPR threads to a row, CH chunks of 8 values to a thread, the next rows of u and r requested before this one's sums.  Bound by its bytes, two
-// reads and two writes, where a copy has 5.0 TB/s: with two layer norms, all five vectors and the statistics 65536 x 1024 bfloat16 104 us, 5.2 TB/s, 32768 x 4096 235 us, 4.6; wide rows by the two
-// reductions' latency as well, for as many rows as are in a CU's registers: 16384 x 8192 283 us, 3.8.
+// reads and two writes, where a copy has 5.0 TB/s: with two layer norms, all five vectors and the statistics 65536 x 1024 bfloat16 106 us, 5.1 TB/s, 32768 x 4096 224-238 us, 4.5-4.8; wide rows by the two
+// reductions' latency as well, for as many rows as are in a CU's registers: 16384 x 8192 233-257 us as the matrices lie, 4.2-4.6.  With MXFP4 codes by
+// their conversion and stores of four bytes to a lane as well: 16384 x 8192 266 us, 4.3 TB/s, 32768 x 4096 324, 3.5, 65536 x 1024 141, 4.1.
 template <int DT, int TPR, int CH, int BLOCK, bool SHORT, Gains GAINS, bool CODES>
 __global__ __launch_bounds__(BLOCK) void resnorm_fwd_kernel(FwdArgs a)
 {
@@ -335,8 +336,10 @@ struct BwdArgs {
 };
 
 // The rows of dout, dy, u and out in registers, the next ones on their way; a thread has the same columns in every row of its workgroup's
-// slice and keeps their sums, so that all is read once.  Bound by its bytes, four reads and two writes: 32768 x 4096 bfloat16 281 us, 5.7 TB/s,
-// 16384 x 8192 286 us, 5.6, 32768 x 512 float 64 us, 6.2.
+// slice and keeps their sums, so that all is read once.  Bound by its bytes, four reads and two writes: 32768 x 4096 bfloat16 285 us, 5.7 TB/s,
+// 16384 x 8192 296 us, 5.4, 32768 x 512 float 71 us, 5.7; 8192 x 8192 float, a few of whose registers are in memory, 361, 4.5.  Of rows beyond 8192 values a
+// thread of 1024 has two chunks, 64 values of sums and as many of the row beside the next row's, where there are 128 registers: the rest is in memory,
+// read and written for every row, and that is what bounds it: 10000 x 16384 bfloat16 1490 us, 1.3 TB/s.
 template <int DT, int TPR, int CH, int BLOCK, bool SHORT, Gains GAINS>
 __global__ __launch_bounds__(BLOCK) void resnorm_bwd_kernel(BwdArgs a)
 {

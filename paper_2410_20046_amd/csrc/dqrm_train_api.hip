@@ -231,9 +231,10 @@ void with_first_that_holds(int64_t cols, F f)
     (void)((cols <= S::cols ? (f(S{}), true) : false) || ...);
 }
 
-// Many rows without codes: several chunks to a thread, and the columns' vectors in LDS, where that is faster (bf16: 16384 x 8192 283 us instead of
-// 300 with 1024 threads to a row, 32768 x 4096 235 and 248, 65536 x 1024 104 and 112; fp32: 8192 x 8192 224 and 248, 16384 x 2048 100 and 111,
-// 32768 x 1024 105 and 113; fp32 16384 x 4096 in LDS 210, in registers 203).  Else a chunk to a thread: a row's latency counts.
+// Many rows without codes: several chunks to a thread, and the columns' vectors in LDS; else a chunk to a thread: a row's latency counts.  Both ways, us,
+// the second one what is taken of few rows: bf16 65536 x 1024 105 and 111, 32768 x 3000 221 and 232, 16384 x 6000 230 and 244, of 4096 and 8192 columns
+// 229 and 221, 246 and 244; fp32 16384 x 2048 101 and 109, 32768 x 1024 106 and 107, 8192 x 6000 175 and 203, 8192 x 8192 226 and 247.  With codes bf16
+// 65536 x 1024 164 and 141, 32768 x 4096 388 and 324, 16384 x 8192 336 and 266, fp32 16384 x 2048 103 either way, 8192 x 8192 263 and 271.
 template <int DT, bool CODES, typename F>
 void with_resnorm_fwd_shape(int64_t rows, int64_t cols, F f)
 {
@@ -253,8 +254,8 @@ void with_resnorm_fwd_shape(int64_t rows, int64_t cols, F f)
                           RowShape<1024, 1, 1024>, RowShape<1024, 2, 1024, Gains::memory>>(cols, f);
 }
 
-// (fp32, 8192 x 8192: 1024 threads and the columns' vectors in LDS 297 us, 512 threads with two chunks 390; bf16, 16384 x 8192: 296 and 286.
-// Rows beyond 8192 values keep some of the sums in memory: 10000 x 16384 bf16 1517 us.)
+// (1024 threads and the columns' vectors in LDS, and 512 threads with two chunks, us: fp32 8192 x 8192 371 and 422, 8192 x 6000 265 and 364; bf16 4000 x
+// 8192 88 and 86, 16384 x 8192 307 and 310, but 16384 x 6000 234 and 257.  Rows beyond 8192 values: 10000 x 16384 bf16 1510 us, of fp32 2210.)
 template <int DT, typename F>
 void with_resnorm_bwd_shape(int64_t cols, F f)
 {

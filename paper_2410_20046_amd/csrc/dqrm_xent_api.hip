@@ -122,8 +122,8 @@ int64_t piece_classes(int64_t rows, int64_t classes, int64_t width, int planes, 
 size_t bytes(int64_t n) { return align_up((size_t)n, 256); }
 
 // Widths up to 64, more than 64 rows: without d.  Workgroups of 128 rows of x or w, slices of the others.  (Forward and backward, with the tiles of
-// the other widths and so: 8192 rows, 200003 classes, width 64 in fp32 10.3 and 5.1 ms, in bf16 4.0 and 1.7; 8192 x 1000 x 64 in fp32 110 and
-// 94 us; 100 x 1000000 x 16 in fp32 1976 and 632.  In bf16 64 rows of 200003 classes took 102 and 128 us: up to 64 rows the other kernels are used.)
+// the other widths and so: 8192 rows, 200003 classes, width 64 in fp32 10.3 and 5.1 ms, in bf16 4.0 and 1.75; 8192 x 1000 x 64 in fp32 110 and
+// 89 us; 100 x 1000000 x 16 in fp32 1976 and 666.  In bf16 64 rows of 200003 classes took 102 and 128 us: up to 64 rows the other kernels are used.)
 constexpr int64_t kNarrowSums = 256LL << 20; // bytes of their sums, if a slice is less
 constexpr int64_t kNarrowSlices = 256;
 bool is_narrow(int64_t m, int64_t k) { return m > 64 && k > 0 && k <= kDepth; }
