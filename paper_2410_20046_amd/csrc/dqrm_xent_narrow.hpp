@@ -31,7 +31,7 @@ struct NarrowArgs {
     float *dbias; // dw: [slices][classes], or null
 };
 
-// Bound by the matrix instructions and the vector ones beside them: 8192 rows, 200003 classes, width 64 in fp32 (six products), loss 1.06 ms, 1.2
+// Bound by the matrix instructions and the vector ones beside them: 8192 rows, 200003 classes, width 64 in fp32 (six products), loss 1.06-1.13 ms, 1.1-1.2
 // PFLOP/s, dx and dw 1.9-2.0 each, 1.3 PFLOP/s with the logits, where a large library product has 1.46.  d in memory would be 29 GB of traffic.  In bf16
 // vector instructions bound it (an exponential takes as long as four others): 0.47-0.49, 0.59 and 0.67 ms, 3-6 % of the loss for the look for
 // infinities.  Three workgroups to a CU, as LDS has it for three planes; the loop over the two blocks is not unrolled: its operands' addresses and
