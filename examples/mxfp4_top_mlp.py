@@ -114,7 +114,8 @@ class ClickModel:
         grad_out = g[:, self.dense:].float().reshape(self.B, self.T, self.D).contiguous()
         dq.dqrm_embbag_bwd(self.tables, idx, self.offsets, self.B, grad_out, b.sorted_pos, b.uniq_rows, b.seg_offsets, b.table_uniq_offsets, b.num_unique,
                            b.values, b.g_absmax, b.workspace)
-        dq.dqrm_quant_update(self.tables, b.cap, idx.numel(), b.values, b.uniq_rows, b.table_uniq_offsets, b.g_absmax, b.gq, b.g_scale, lr, b.workspace)
+        dq.dqrm_grad_quant_int8(self.T, self.D, b.cap, b.values, b.table_uniq_offsets, b.g_absmax, b.gq, b.g_scale)
+        dq.dqrm_sparse_update(self.tables, b.cap, b.uniq_rows, b.table_uniq_offsets, b.gq, b.g_scale, lr)
         return loss
 
     def serve(self, dense: torch.Tensor, idx: torch.Tensor) -> torch.Tensor:
