@@ -528,7 +528,7 @@ typedef struct {
 
 /* u, r, out, y: [rows][cols] of one type; out may be r's or u's own memory, with the same stride.  y and q (y in MXFP4, quantised from its
  * 32-bit values) may be NULL.  stats: [4][rows] fp32 or NULL: mean and rstd of N1, mean and rstd of N2 (what the backward needs); those of
- * a norm that is not there are not written. */
+ * a norm that is not there are not written.  Outputs overlap nothing else but as said. */
 int32_t dqrm_residual_norm_fwd(int32_t dtype, int64_t rows, int64_t cols, const dqrm_residual_norm_t *norm, const void *u, int64_t ldu, const void *r,
                                int64_t ldr, void *out, int64_t ldo, void *y, int64_t ldy, float *stats, const dqrm_mxfp4_t *q, void *stream);
 
@@ -555,7 +555,8 @@ int32_t dqrm_residual_norm_bwd(int32_t dtype, int64_t rows, int64_t cols, const 
  * up to 4 rows of fp32 or of unaligned values as fused products in fp32;
  * sums, maxima and exponentials are fp32.  classes >= 1 unless rows = 0; rows, classes and width up to 2147482623, the tiles of 256 by 256
  * of any two of them up to 4194304, width and row strides up to 4194304; more are DQRM_ERR_UNSUPPORTED.  The order of all sums depends on shape,
- * strides, alignment and type alone.  A workspace for some rows is enough for fewer of the same classes, width and type. */
+ * strides, alignment and type alone.  A workspace for some rows is enough for fewer of the same classes, width and type.  What these two calls write is
+ * not to overlap what they read, nor other outputs. */
 size_t dqrm_softmax_xent_fwd_workspace_bytes(int64_t rows, int64_t classes, int64_t width, int32_t dtype);
 int32_t dqrm_softmax_xent_fwd(int32_t dtype, int64_t rows, int64_t classes, int64_t width, const void *x, int64_t ldx, const void *w, int64_t ldw,
                               const float *bias, float scale, const int64_t *targets, float *loss, float *lse, void *workspace, size_t workspace_bytes,

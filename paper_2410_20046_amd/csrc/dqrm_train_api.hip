@@ -64,8 +64,9 @@ struct Region {
 Region region_of(const void *p, const dqrm_grad_t &g, int64_t ld, bool written)
 {
     const int64_t size = (int64_t)size_of(g.dtype);
-    Region r{reinterpret_cast<uintptr_t>(p), 0, g.rows, g.cols * size, ld * size, written};
-    if (g.rows == 1 || ld == g.cols) r.width *= g.rows, r.rows = 1, r.pitch = r.width;
+    const bool block = g.rows == 1 || ld == g.cols; // (a single row's stride may be anything)
+    Region r{reinterpret_cast<uintptr_t>(p), 0, block ? 1 : g.rows, (block ? g.rows : 1) * g.cols * size, 0, written};
+    r.pitch = block ? r.width : ld * size;
     r.to = r.from + (uintptr_t)((r.rows - 1) * r.pitch + r.width);
     return r;
 }

@@ -34,6 +34,7 @@ APART = [
     [tensor(0, 8, 10, 10), tensor(80, 8, 10, 10, out=200, ld_out=10)],
     [tensor(0, 8, 10, 10, out=0, ld_out=10)],  # in place, said twice
     [tensor(0, 1, 10, 10, out=0, ld_out=99)],
+    [tensor(0, 1, 10, 1 << 62), tensor(10, 1, 10, -5), tensor(20, 1, 10, 10, out=30, ld_out=1 << 62)],  # (the stride of one row)
     [tensor(0, 8, 10, 10, out=100, ld_out=12), tensor(0, 8, 10, 10, out=200, ld_out=12)],  # one input, two outputs
     [tensor(0, 8, 10, 20, out=10, ld_out=20)],  # beside itself
     [tensor(0, 0, 10, 10), tensor(0, 8, 0, 10), tensor(0, 8, 10, 10)],  # nothing overlaps
