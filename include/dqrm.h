@@ -546,7 +546,8 @@ int32_t dqrm_residual_norm_bwd(int32_t dtype, int64_t rows, int64_t cols, const 
 /* ---- softmax cross entropy over many classes ------------------------------------------------------------------------
  * The loss of a linear classifier whose classes are the rows of w (the items of a table, say), without the logits in memory:
  *   l[i][j] = scale (x_i . w_j) + bias[j], lse_i = log sum over j of exp(l[i][j]), loss_i = lse_i - l[i][targets[i]]
- * x [rows][width], w [classes][width] of one type; bias [classes] fp32 or NULL (0; -infinity takes a class out); scale finite;
+ * x [rows][width], w [classes][width] of one type; bias [classes] fp32 or NULL (0; -infinity takes a class out, and so
+ * does what is it when multiplied by log2 e, below -2.358e38, such as float's lowest value); scale finite;
  * targets [rows] int64.  A negative target: the row has none, its loss is 0 and it has no gradient.  A target >= classes is recorded as
  * DQRM_ERR_INDEX_OUT_OF_RANGE (table -1, the target) by the forward and counts as none.  lse [rows] fp32 is what the backward needs.
  * A row with all its classes taken out has lse = -infinity, loss = +infinity and no gradient; a row whose target is taken out and other classes

@@ -14,6 +14,9 @@ namespace dqrm_xent {
 
 constexpr float kLog2e = 1.44269504088896341f;
 
+// by its bias in powers of two (that of float's lowest value is -infinity too)
+__device__ __forceinline__ bool taken_out(float bias) { return bias * kLog2e == -__builtin_inff(); }
+
 struct Classifier {
     Products g;
     const float *bias; // [n] or null
@@ -668,7 +671,7 @@ static __global__ __launch_bounds__(1024) void xent_unit_kernel(const unsigned *
 static __global__ __launch_bounds__(256) void xent_classes_kernel(const float *bias, int64_t classes, uint64_t *live)
 {
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint64_t word = __ballot(j < classes && bias[min(j, classes - 1)] != -__builtin_inff());
+    const uint64_t word = __ballot(j < classes && !taken_out(bias[min(j, classes - 1)]));
     if ((threadIdx.x & 63) == 0 && j < classes) live[j >> 6] = word;
 }
 

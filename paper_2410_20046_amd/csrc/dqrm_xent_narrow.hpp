@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
     const bool inside = row < held_rows;
     const float most = LOSS ? 1.0f : *a.most;
 
-    const bool there = inside && !(DW && a.bias && a.bias[row] == -__builtin_inff());
+    const bool there = inside && !(DW && a.bias && taken_out(a.bias[row]));
     uint4 mine[KS][planes];
 #pragma unroll
     for (int s = 0; s < KS; ++s)
@@ -154,8 +154,8 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
             // operands are zeros.)
             const int64_t at = target - ((int64_t)s * 64 + block * 32);
             int place_of = at >= 0 && at < 32 ? (int)at : -1;
-            bool taken_out = false;
-            if constexpr (LOSS) taken_out = __any(s_a[buffer][block * 32 + (lane & 31)] == -__builtin_inff());
+            bool some_out = false;
+            if constexpr (LOSS) some_out = __any(s_a[buffer][block * 32 + (lane & 31)] == -__builtin_inff());
             if constexpr (DW) place_of = s_target[buffer][block * 32 + (lane & 31)] - (int)(row - (lane & 31)); // (of a row among the wave's classes)
             const bool hit = __any(place_of >= 0 && place_of < 32);
 #pragma unroll
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(256, 3) void xent_narrow_kernel(NarrowArgs a)
                 float least = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) least = fminf(least, acc[i]);
-                if (taken_out || __any(least == -__builtin_inff())) {
+                if (some_out || __any(least == -__builtin_inff())) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float b = s_a[buffer][block * 32 + (i >> 2) * 8 + half * 4 + (i & 3)];

@@ -81,3 +81,23 @@ def test_a_target_that_is_taken_out(dtype, m, v, k):
     # of such a class there is nothing but its targets' part
     of = torch.zeros(v, dtype=torch.float64, device="cuda").index_add_(0, targets, grad.double())
     assert bool((of[out] > 0).any()) and bool(((dbias.double() + of)[out].abs() <= (m + 8) * 2.0 ** -24 * of[out]).all())
+
+
+@pytest.mark.parametrize("dtype, m, v, k", KERNELS)
+def test_a_bias_of_the_lowest_value(dtype, m, v, k):
+    """A class whose bias is float's lowest value is taken out as one with -infinity: its logit in powers of two is -infinity, whatever w holds."""
+    x, w, targets, b, grad = make(m, v, k, TYPES[dtype], seed=25)
+    out = torch.arange(v, device="cuda") % 3 == 1
+    w[out] = math.nan
+    targets = torch.where(torch.arange(m, device="cuda") % 4 == 0, targets // 3 * 3 + 1, targets).clamp(max=v - 2)  # (some rows' among them)
+    got = []
+    for value in (-math.inf, torch.finfo(torch.float32).min):
+        b[out] = value
+        loss, lse = forward(x, w, targets, b)
+        got.append((loss, lse, *backward(x, w, targets, lse, grad, b)))
+    assert all(torch.equal(p, q) for p, q in zip(*got)) and bool(lse.isfinite().all()) and not any(bool(t.isnan().any()) for t in got[0])
+    b[:] = torch.finfo(torch.float32).min  # no class left
+    loss, lse = forward(x, w, targets, b)
+    assert bool((lse == -math.inf).all()) and bool((loss == math.inf).all())
+    for t in backward(x, w, targets, lse, grad, b):
+        assert bool((t == 0).all())
